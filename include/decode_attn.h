@@ -315,6 +315,132 @@ da_status da_decode_attn_noalloc(const float *q, const float *K,
 
 /*
  * ---------------------------------------------------------------------------
+ * Paged cache: rows in 32, 16 or 4 bits, appended with the position rotation
+ * on the way, and attention over the pages.
+ *
+ * The cache is a pool of pages of page_rows positions each.  pages[b][i] names
+ * the page that holds positions page_rows*i .. page_rows*(i+1)-1 of sequence b;
+ * one table serves the K and V pools of every layer.  An entry outside
+ * [0, n_pages) is a page that is not there: rows for it are dropped, queries do
+ * not see its positions, and reading it back gives 0.  Sequences may share
+ * pages that no call appends to.
+ *
+ * A step submits rows (tokens): row r of sequence b stands at position
+ * past[b] + r, past[b] being the positions that the sequence held before.  No
+ * call changes past: every layer of a step is called with the same one, and the
+ * program advances it once a step.  Rows lie one after the other, token-major
+ * ([rows][heads][d], heads of one token contiguous, any stride between
+ * tokens): T rows of every sequence (row_start NULL, rows = B*T), or
+ * rows row_start[b] .. row_start[b+1]-1 of sequence b, at most T of them (a
+ * longer sequence's further rows are not its rows).  Arrays may hold rows
+ * behind the last sequence's: neither they nor their results are touched.
+ * Sequences with past[b] < 0 hold nothing and take nothing; their rows attend
+ * to nothing.  Positions at or beyond page_rows*max_pages do not exist: such
+ * rows are dropped.
+ *
+ * Types.  dtype is that of every row given and returned (q, k_new, v_new, out,
+ * ...).  format DA_KV_DENSE: the pools hold the same type,
+ *     K, V  [n_pages][h_kv][page_rows][d].
+ * format DA_KV_MX4 (4.25 bits a value): blocks of 32 consecutive dimensions of
+ * a row share a power of two 2^X, X = max(floor(log2 max|v|) - 2, -126), held
+ * as the byte X + 127; each value is a sign and the nearest of 0, 0.5, 1, 1.5,
+ * 2, 3, 4, 6 times 2^X (ties to the even code; above 6: 6), the code's low
+ * three bits counting these levels and its bit 3 the sign (the OCP microscaling
+ * format MXFP4).  A block with an infinity or a NaN has the byte 255 and reads
+ * as NaN.  A page of one head is page_rows*(d/2 + d/32) bytes:
+ *     K: code bytes [page_rows][d/2] (dimension 2j in the low half of byte j),
+ *        then scale bytes [page_rows][d/32];
+ *     V: code bytes [page_rows/8][d/8][8][4]: for 8 rows, 8 dimensions of each
+ *        row in turn, then scale bytes [page_rows/8][d/32][8].
+ * Rotated rows are quantised from their values in 64 bits, so the codes are
+ * those of the exact product with the table.
+ *
+ * Supported: d in {64, 128, 256}; page_rows a power of two from 16 to 32768;
+ * page_rows*max_pages <= 2^30; T <= 32768; h_kv dividing h_q.  Pools, rows and
+ * tables are 16-byte aligned, strides between tokens multiples of 16 bytes and
+ * at least a token's own size.
+ * Errors are checked in the order of the enumeration (workspace last).
+ * ---------------------------------------------------------------------------
+ */
+typedef enum da_dtype { DA_F32 = 0, DA_BF16 = 1, DA_F16 = 2 } da_dtype;
+typedef enum da_kv_format { DA_KV_DENSE = 0, DA_KV_MX4 = 1 } da_kv_format;
+
+/* The cache of one layer and the step's rows (host struct; K, V, pages, past
+ * and row_start are device pointers). */
+typedef struct da_paged_kv {
+    void *K, *V;
+    const int32_t *pages;     /* [B][max_pages]                        */
+    const int32_t *past;      /* [B]                                   */
+    const int32_t *row_start; /* [B+1], or NULL: T rows each           */
+    int B, h_kv, d;
+    int n_pages, page_rows, max_pages;
+    int rows, T;              /* rows of the arrays; most rows of a sequence */
+    int dtype, format;        /* da_dtype, da_kv_format                */
+} da_paged_kv;
+
+/* Bytes of one head's page in the K pool (and in the V pool): the pools are
+ * n_pages*h_kv of these.  0 if an argument is invalid. */
+size_t da_paged_page_bytes(int page_rows, int d, int dtype, int format);
+
+/*
+ * Appends k_new and v_new [rows][h_kv][d] (token strides in elements), and
+ * rotates q [rows][h_q][d] into q_out [rows][h_q][d] (contiguous; q_out may be q
+ * where q is contiguous; q NULL: no queries, h_q and q_out unused).  Rotation by
+ * the table rotary [n_rotary][rot_dim] float, cosines then sines, of the row's
+ * position: with half = rot_dim/2, dimensions (i, i + half), or (2i, 2i+1) if
+ * interleaved, become
+ *     x1*cos[i] - x2*sin[i],  x2*cos[i] + x1*sin[i];
+ * dimensions from rot_dim on, and V, are copied.  Products and sums in 32 bits
+ * (a DA_KV_MX4 cache's in 64), one rounding to the type.  rot_dim: 0 (no
+ * rotation, rotary unused) or a multiple of 16 up to d; n_rotary at least
+ * page_rows*max_pages.  A row that is dropped writes neither cache nor q_out,
+ * except that a row on a missing page still has its q.
+ * One launch.  Two rows must not have the same place (pages shared by
+ * sequences are not appended to).
+ */
+da_status da_paged_append(const da_paged_kv *kv, const void *k_new,
+                          const void *v_new, int64_t k_stride,
+                          int64_t v_stride, const void *q, int64_t q_stride,
+                          int h_q, void *q_out, const float *rotary,
+                          int n_rotary, int rot_dim, int interleaved,
+                          void *stream);
+
+/*
+ * The rows' places read back: k_out and v_out [rows][h_kv][d], contiguous; a
+ * 4-bit cache's values rounded to dtype (float16 only can round them).  A row
+ * that would be dropped reads 0.  One launch.
+ */
+da_status da_paged_gather(const da_paged_kv *kv, void *k_out, void *v_out,
+                          void *stream);
+
+/*
+ * Attention of every row over its sequence's pages, head map as above:
+ *     out[n,h,:] = softmax_l(scale * q[n,h,:].K[l,:]) V[l,:]
+ * over the positions l that row r sees: 0 .. past[b] + r if causal (the rows of
+ * the step are in the cache already: append first), else 0 .. past[b] - 1 (cross
+ * attention to past[b] states of an encoder, of any number per sequence).  A
+ * row that sees nothing, or whose scores are all -infinity, gives 0.  What a
+ * row does not see stays out of it, infinities and NaN included.
+ * q [rows][h_q][d] with a token stride in elements, out [rows][h_q][d]
+ * contiguous.  Two launches: the work, counted from past and row_start on the
+ * device, is divided evenly over a resident grid whatever the lengths, and
+ * the parts of a row are then combined in a fixed order: equal calls give equal
+ * bits.  Scores, softmax and sums in 32 bits; 16-bit types multiply in
+ * their own type (weights rounded to it, once), float32 in float32.
+ * workspace: da_paged_workspace_bytes(...) bytes, 16-byte aligned, of any
+ * content; one call at a time.
+ */
+da_status da_paged_attn(const da_paged_kv *kv, const void *q, int64_t q_stride,
+                        int h_q, float scale, int causal, void *out,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/* Workspace of da_paged_attn for these sizes, on any device and for any
+ * lengths, page table and format; no smaller for a larger B.  0 if invalid. */
+size_t da_paged_workspace_bytes(int B, int h_q, int h_kv, int d, int T,
+                                int dtype);
+
+/*
+ * ---------------------------------------------------------------------------
  * Tuning and testing only.  The entry points above choose their own segment
  * size (the most rows a workgroup reads from its static range in one go,
  * and for caches scheduled without a static share also the unit handed out

@@ -15,6 +15,8 @@ _BINDING_NAMES = {
     "decode_multi", "decode_multi_step", "kv_append_rows", "alloc_multi_workspace",
     "chunk_rows", "workspace_bytes", "workspace_counter_bytes", "workspace_reset",
     "alloc_workspace", "DecodeAttnError",
+    "paged_alloc", "paged_append", "paged_attn", "paged_gather", "paged_workspace",
+    "paged_workspace_bytes", "rotary_table",
     "LIBRARY_PATH",
 }
 

@@ -7,6 +7,8 @@ returns an error status, a Python exception is raised.
 
 Tensors must be contiguous, on the current HIP device, float32 (int32 for
 ``len``).  Calls are asynchronous on torch's current stream (or ``stream``).
+The ``paged_*`` calls also take bfloat16 and float16, and rows with a stride
+between tokens (views into a fused projection's output).
 """
 from __future__ import annotations
 
@@ -25,6 +27,7 @@ STATUS = {
 
 # Every symbol the header declares, with its ctypes signature.
 _vp, _ci, _cf, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
+_i64 = ctypes.c_int64
 SIGNATURES = {
     "da_status_string": (ctypes.c_char_p, [_ci]),
     "da_decode_workspace_bytes": (_sz, [_ci] * 6),
@@ -39,6 +42,12 @@ SIGNATURES = {
     "da_kv_append": (_ci, [_vp] * 5 + [_ci] * 5 + [_vp]),
     "da_kv_append_rows": (_ci, [_vp] * 5 + [_ci] * 6 + [_vp]),
     "da_decode_attn_noalloc": (_ci, [_vp, _vp, _vp, _vp, _cf, _vp] + [_ci] * 6 + [_vp]),
+    "da_paged_page_bytes": (_sz, [_ci] * 4),
+    "da_paged_append": (_ci, [_vp, _vp, _vp, _i64, _i64, _vp, _i64, _ci, _vp, _vp]
+                        + [_ci] * 3 + [_vp]),
+    "da_paged_gather": (_ci, [_vp] * 4),
+    "da_paged_attn": (_ci, [_vp, _vp, _i64, _ci, _cf, _ci, _vp, _vp, _sz, _vp]),
+    "da_paged_workspace_bytes": (_sz, [_ci] * 6),
     # tuning and testing only (explicit segment size)
     "da_decode_chunk_rows": (_ci, [_ci] * 6),
     "da_decode_workspace_bytes_ex": (_sz, [_ci] * 7),
@@ -370,3 +379,196 @@ def kv_append_rows(K, V, k_new, v_new, lens, stream=None) -> None:
         _dev(K, "K", torch.float32), _dev(V, "V", torch.float32),
         _dev(k_new, "k_new", torch.float32), _dev(v_new, "v_new", torch.float32),
         _dev(lens, "len", torch.int32), B, h_kv, n_max, d_k, d_v, T, _stream(stream)))
+
+
+# --- paged cache ----------------------------------------------------------------
+
+class _PagedKV(ctypes.Structure):
+    """da_paged_kv"""
+    _fields_ = ([(n, _vp) for n in ("K", "V", "pages", "past", "row_start")]
+                + [(n, _ci) for n in ("B", "h_kv", "d", "n_pages", "page_rows", "max_pages",
+                                      "rows", "T", "dtype", "format")])
+
+
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_DENSE, _MX4 = 0, 1
+
+
+def paged_alloc(n_pages: int, page_rows: int, h_kv: int, d: int, dtype=torch.bfloat16,
+                format: str = "dense", device="cuda"):
+    """Zeroed K and V pools: [n_pages,h_kv,page_rows,d] of ``dtype``, or of 4 bits a
+    value (format "mx4"): uint8 [n_pages,h_kv,page_rows,d/2 + d/32], where the last
+    two dimensions are one run of bytes, in the layout of the C header."""
+    if format not in ("dense", "mx4"):
+        raise ValueError("format must be 'dense' or 'mx4'")
+    if dtype not in _DTYPES:
+        raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
+    if _lib.da_paged_page_bytes(page_rows, d, _DTYPES[dtype], int(format == "mx4")) == 0:
+        raise ValueError("page_rows must be a power of two from 16 to 32768 and d 64, 128 or 256")
+    if format == "mx4":
+        shape, dtype = (n_pages, h_kv, page_rows, d // 2 + d // 32), torch.uint8
+    else:
+        shape = (n_pages, h_kv, page_rows, d)
+    return (torch.zeros(shape, dtype=dtype, device=device),
+            torch.zeros(shape, dtype=dtype, device=device))
+
+
+def rotary_table(n: int, rot_dim: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """cos and sin of position * base^(-2i/rot_dim), i < rot_dim/2, for positions 0
+    to n-1: float32 [n, rot_dim], the angles computed in 64 bits."""
+    i = torch.arange(rot_dim // 2, dtype=torch.float64)
+    a = torch.arange(n, dtype=torch.float64)[:, None] * base ** (-2.0 * i / rot_dim)
+    return torch.cat((a.cos(), a.sin()), 1).to(device=device, dtype=torch.float32)
+
+
+def _here(t, name, dtype) -> int:
+    """_dev, and on the current device (whose stream the kernels run on)."""
+    p = _dev(t, name, dtype)
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current device")
+    return p
+
+
+def _tokens(t, name, dtype):
+    """Address and token stride (elements) of rows [rows, heads, d]."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be on the GPU")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current device")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [rows, heads, d]")
+    rows, heads, d = t.shape
+    stride, head_stride, one = t.stride()
+    if (one != 1 and d != 1) or (head_stride != d and heads != 1):
+        raise ValueError(f"{name}: a token's heads must be contiguous")
+    return t.data_ptr(), stride if rows > 1 else max(stride, heads * d)
+
+
+def _paged(K, V, pages, past, rows, d, dtype, row_start, T) -> _PagedKV:
+    if not (isinstance(K, torch.Tensor) and isinstance(V, torch.Tensor)):
+        raise TypeError("K and V must be torch.Tensors")
+    if K.dim() != 4 or K.shape != V.shape:
+        raise ValueError("K and V must be pools of one shape, [n_pages,h_kv,page_rows,..]")
+    if dtype not in _DTYPES:
+        raise TypeError(f"rows must be float32, bfloat16 or float16, got {dtype}")
+    n_pages, h_kv, page_rows, width = K.shape
+    mx4 = K.dtype == torch.uint8
+    if width != (d // 2 + d // 32 if mx4 else d):
+        raise ValueError(f"pools of width {width} do not hold rows of d={d}")
+    pool = torch.uint8 if mx4 else dtype
+    kp, vp = _here(K, "K", pool), _here(V, "V", pool)
+    pp, np_ = _here(pages, "pages", torch.int32), _here(past, "past", torch.int32)
+    if pages.dim() != 2 or past.dim() != 1 or pages.shape[0] != past.shape[0]:
+        raise ValueError("pages must be [B,max_pages] and past [B]")
+    B, max_pages = pages.shape
+    rp = None
+    if row_start is not None:
+        rp = _here(row_start, "row_start", torch.int32)
+        if tuple(row_start.shape) != (B + 1,):
+            raise ValueError("row_start must be [B+1]")
+        if T < 1:
+            raise ValueError("with row_start, T is the most rows of a sequence")
+    elif T == 0 and B and rows % B == 0:
+        T = rows // B
+    if row_start is None and rows != B * T:
+        raise ValueError("without row_start every sequence has T rows: rows must be B*T")
+    return _PagedKV(kp, vp, pp, np_, rp, B, h_kv, d, n_pages, page_rows, max_pages, rows, T,
+                    _DTYPES[dtype], _MX4 if mx4 else _DENSE)
+
+
+def paged_append(K, V, pages, past, k_new, v_new, q=None, rotary=None, interleaved: bool = False,
+                 row_start=None, T: int = 0, q_out=None, stream=None):
+    """Rows k_new, v_new [rows,h_kv,d] into the pages of positions past[b] + r, k_new
+    turned by ``rotary`` [positions, rot_dim] on the way, and q [rows,h_q,d] turned
+    into q_out (returned).  ``row_start`` [B+1]: each sequence's rows, at most ``T``;
+    else T rows each.  past is not changed."""
+    if not isinstance(k_new, torch.Tensor) or k_new.dim() != 3:
+        raise ValueError("k_new must be [rows,h_kv,d]")
+    rows, h_kv, d = k_new.shape
+    dtype = k_new.dtype
+    p = _paged(K, V, pages, past, rows, d, dtype, row_start, T)
+    if h_kv != p.h_kv or v_new.shape != k_new.shape:
+        raise ValueError("k_new and v_new must be [rows,h_kv,d]")
+    kp, ks = _tokens(k_new, "k_new", dtype)
+    vp, vs = _tokens(v_new, "v_new", dtype)
+    qp = qo = rp = None
+    qs = h_q = n_rot = rot_dim = 0
+    if q is not None:
+        qp, qs = _tokens(q, "q", dtype)
+        h_q = q.shape[1]
+        if q.shape[0] != rows or q.shape[2] != d:
+            raise ValueError("q must be [rows,h_q,d]")
+        if q_out is None:
+            q_out = torch.empty((rows, h_q, d), dtype=dtype, device=q.device)
+        elif q_out.shape != q.shape:
+            raise ValueError("q_out must have q's shape")
+        qo = _here(q_out, "q_out", dtype)
+    if rotary is not None:
+        rp = _here(rotary, "rotary", torch.float32)
+        if rotary.dim() != 2:
+            raise ValueError("rotary must be [positions, rot_dim]")
+        n_rot, rot_dim = rotary.shape
+    _check("da_paged_append", _lib.da_paged_append(
+        ctypes.byref(p), kp, vp, ks, vs, qp, qs, h_q, qo, rp, n_rot, rot_dim,
+        int(bool(interleaved)), _stream(stream)))
+    return q_out
+
+
+def paged_gather(K, V, pages, past, k_out, v_out, row_start=None, T: int = 0, stream=None):
+    """The rows at positions past[b] + r into k_out and v_out [rows,h_kv,d] (zeros
+    where there is no page): the places that paged_append with the same
+    ``past``, ``row_start`` and ``T`` writes."""
+    if not isinstance(k_out, torch.Tensor) or k_out.dim() != 3:
+        raise ValueError("k_out must be [rows,h_kv,d]")
+    rows, h_kv, d = k_out.shape
+    p = _paged(K, V, pages, past, rows, d, k_out.dtype, row_start, T)
+    if h_kv != p.h_kv or v_out.shape != k_out.shape:
+        raise ValueError("k_out and v_out must be [rows,h_kv,d]")
+    _check("da_paged_gather", _lib.da_paged_gather(
+        ctypes.byref(p), _here(k_out, "k_out", k_out.dtype), _here(v_out, "v_out", k_out.dtype),
+        _stream(stream)))
+    return k_out, v_out
+
+
+def paged_workspace_bytes(B, h_q, h_kv, d, T: int = 1, dtype=torch.bfloat16) -> int:
+    """Workspace bytes of paged_attn for these sizes (0: invalid)."""
+    return int(_lib.da_paged_workspace_bytes(B, h_q, h_kv, d, T, _DTYPES[dtype]))
+
+
+def paged_workspace(q, K, pages, T: int = 0) -> torch.Tensor:
+    """A workspace for paged_attn with q [rows,h_q,d] and these pools and sequences
+    (T: most rows of a sequence; 0: rows / B)."""
+    B = pages.shape[0]
+    n = paged_workspace_bytes(B, q.shape[1], K.shape[1], q.shape[2], T or q.shape[0] // B,
+                              q.dtype)
+    if n == 0:
+        _check("da_paged_workspace_bytes", 2)
+    return torch.empty(n, dtype=torch.uint8, device=q.device)
+
+
+def paged_attn(q, K, V, pages, past, scale: float, causal: bool = True, row_start=None,
+               T: int = 0, out=None, workspace=None, stream=None) -> torch.Tensor:
+    """out[n,h,:] = softmax(scale * q[n,h].K) V over the sequence's positions up to
+    the row's own, past[b] + r (causal; append first), or over all past[b] of
+    them.  q [rows,h_q,d], any stride between tokens."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be [rows,h_q,d]")
+    rows, h_q, d = q.shape
+    dtype = q.dtype
+    p = _paged(K, V, pages, past, rows, d, dtype, row_start, T)
+    if out is None:
+        out = torch.empty((rows, h_q, d), dtype=dtype, device=q.device)
+    elif out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    if workspace is None:
+        workspace = paged_workspace(q, K, pages, p.T)
+    qp, qs = _tokens(q, "q", dtype)
+    wp, wn = _ws(workspace)
+    _check("da_paged_attn", _lib.da_paged_attn(
+        ctypes.byref(p), qp, qs, h_q, float(scale), int(bool(causal)), _here(out, "out", dtype),
+        wp, wn, _stream(stream)))
+    return out

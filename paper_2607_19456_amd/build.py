@@ -1,4 +1,5 @@
-"""Build the gfx950 HIP library ``libdecode_attn.so`` in-tree with hipcc.
+"""Build the gfx950 HIP library ``libdecode_attn.so`` in-tree with hipcc: one
+object for each of its sources, side by side, then one link.
 
 Used by ``__graft_entry__.build()``; also runnable as
 ``python -m paper_2607_19456_amd.build``.
@@ -12,6 +13,7 @@ import sys
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "decode_attn.hip")
+PAGED_SRC = os.path.join(PKG, "csrc", "paged_kv.hip")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libdecode_attn.so")
 # The read-ceiling probe the benchmark reports beside the decode (not part of
@@ -39,21 +41,37 @@ FLAGS = [
 ]
 
 
-def _compile(src: str, lib: str, verbose: bool) -> str:
-    tmp = lib + ".tmp%d" % os.getpid()
-    cmd = [HIPCC, *FLAGS, "-o", tmp, src]
+def _start(cmd: list, verbose: bool) -> subprocess.Popen:
     if verbose:
         print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
-    os.replace(tmp, lib)
-    return lib
+    return subprocess.Popen(cmd)
+
+
+def _finish(jobs: list) -> None:
+    failed = [p.args for p in jobs if p.wait() != 0]
+    if failed:
+        raise subprocess.CalledProcessError(1, failed[0])
 
 
 def build(verbose: bool = False) -> str:
     """Compile the decode library and the read-ceiling probe (always; a stale
     build must never be used).  Returns the decode library's path."""
-    _compile(PROBE_SRC, PROBE_LIB, verbose)
-    return _compile(SRC, LIB, verbose)
+    tag = ".tmp%d" % os.getpid()
+    objects = [LIB + tag + ".%d.o" % i for i in range(2)]
+    compile_flags = [f for f in FLAGS if f != "-shared"]
+    try:
+        _finish([_start([HIPCC, *compile_flags, "-c", "-o", obj, src], verbose)
+                 for obj, src in zip(objects, (SRC, PAGED_SRC))]
+                + [_start([HIPCC, *FLAGS, "-o", PROBE_LIB + tag, PROBE_SRC], verbose)])
+        _finish([_start([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", LIB + tag,
+                         *objects], verbose)])
+        os.replace(PROBE_LIB + tag, PROBE_LIB)
+        os.replace(LIB + tag, LIB)
+    finally:
+        for path in (*objects, LIB + tag, PROBE_LIB + tag):
+            if os.path.exists(path):
+                os.unlink(path)
+    return LIB
 
 
 if __name__ == "__main__":

@@ -1,0 +1,1421 @@
+// paged_kv.hip -- gfx950 kernels and C ABI of the paged KV cache: rows appended
+// with the position rotation on the way, read back, and attended to, the cache
+// in 32 or 16 bits or in 4 (blocks of 32 values that share a power of two).
+//
+// Kernels
+//   paged_append_kernel   q, K and V rows of a step: q and K turned by the
+//                         position's angles, K and V written to their pages.
+//   paged_gather_kernel   the same places read back as dense rows.
+//   paged_attn_kernel     softmax(scale q.K) V over the pages of each (sequence,
+//                         KV head, tile of query rows), split evenly over a
+//                         resident grid, as partial states.
+//   paged_merge_kernel    combines the parts of each query row.
+//
+// Register layouts of the matrix instructions used below (lane = 0..63,
+// i = lane % 16, k = lane / 16), 16 x 16 results:
+//   A operand: lane holds A[i][..], k's share of the summed index
+//   B operand: lane holds B[..][i], k's share of the summed index
+//   result:    lane holds D[4k + r][i] in component r = 0..3
+// The summed index is shared out 8 to a lane (16-bit types, 32 in all) or 1
+// (float32, 4 in all); any assignment of it to (k, element) serves as long as
+// both operands use the same.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cmath>
+#include <cstdint>
+
+#include "decode_attn.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kMaxCus = 256;
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+template <class T>
+constexpr bool is_f32 = std::is_same<T, float>::value;
+
+// ---------------------------------------------------------------------------
+// The batch, as the kernels see it.
+// ---------------------------------------------------------------------------
+struct Batch {
+  char* K;
+  char* V;
+  const int32_t* pages;
+  const int32_t* past;
+  const int32_t* row_start;
+  int B, h_kv, n_pages, page_log2, max_pages, rows, T;
+};
+
+__device__ __forceinline__ int capacity(const Batch& bt) { return bt.max_pages << bt.page_log2; }
+
+// First row and number of rows of sequence b, within the arrays whatever
+// row_start holds.
+struct SeqRows {
+  int start, n;
+};
+__device__ __forceinline__ SeqRows seq_rows(const Batch& bt, int b) {
+  if (!bt.row_start) return {b * bt.T, bt.T};
+  const int s = min(max(bt.row_start[b], 0), bt.rows);
+  const int e = min(max(bt.row_start[b + 1], s), bt.rows);
+  return {s, min(e - s, bt.T)};
+}
+
+// Bytes of the codes (or values) of one row, and of one head's page.
+template <class T, bool MX, int D>
+constexpr int kRowBytes = MX ? D / 2 : D * (int)sizeof(T);
+template <class T, bool MX, int D>
+__device__ __forceinline__ int64_t block_bytes(int page_log2) {
+  return (int64_t)(kRowBytes<T, MX, D> + (MX ? D / 32 : 0)) << page_log2;
+}
+
+// ---------------------------------------------------------------------------
+// Append: one thread turns and writes 8 dimensions of one head of one row.
+// Memory-bound: 6 operations for each pair of values that it reads and writes.
+// ---------------------------------------------------------------------------
+template <class T>
+__device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
+  if constexpr (is_f32<T>) {
+    const f32x4 a = *reinterpret_cast<const f32x4*>(p);
+    const f32x4 b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = a[e], x[4 + e] = b[e];
+  } else {
+    typedef T t8 __attribute__((ext_vector_type(8)));
+    const t8 a = *reinterpret_cast<const t8*>(p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)a[e];
+  }
+}
+
+template <class T>
+__device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
+  if constexpr (is_f32<T>) {
+    *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<f32x4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+  } else {
+    typedef T t8 __attribute__((ext_vector_type(8)));
+    t8 a;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a[e] = (T)x[e];
+    *reinterpret_cast<t8*>(p) = a;
+  }
+}
+
+struct AppendArgs {
+  const void *q, *k, *v;
+  void* q_out;
+  int64_t q_stride, k_stride, v_stride;
+  const float* rotary;
+  int h_q, rot_dim, interleaved;
+};
+
+// Dimensions 8*piece .. +7 of a row after the rotation, in W (the type of the
+// products and sums).
+template <class T, class W>
+__device__ __forceinline__ void turned8(const T* row, int piece, const AppendArgs& a,
+                                        const float* angles, W (&y)[8]) {
+  float x[8];
+  load8(row + 8 * piece, x);
+  const int half = a.rot_dim / 2;
+  if (8 * piece >= a.rot_dim) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = (W)x[e];
+    return;
+  }
+  if (a.interleaved) {
+    const f32x4 c = *reinterpret_cast<const f32x4*>(angles + 4 * piece);
+    const f32x4 s = *reinterpret_cast<const f32x4*>(angles + half + 4 * piece);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const W x1 = x[2 * e], x2 = x[2 * e + 1], cc = c[e], ss = s[e];
+      y[2 * e] = x1 * cc - x2 * ss;
+      y[2 * e + 1] = x2 * cc + x1 * ss;
+    }
+    return;
+  }
+  const bool upper = 8 * piece >= half;
+  const int at = 8 * piece - (upper ? half : 0);
+  float o[8], c[8], s[8];
+  load8(row + at + (upper ? 0 : half), o);
+  load8(angles + at, c);
+  load8(angles + half + at, s);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const W cc = c[e], ss = upper ? s[e] : -s[e];
+    y[e] = (W)x[e] * cc + (W)o[e] * ss;
+  }
+}
+
+// The float32 value of y rounded to odd: toward zero, with the last bit set
+// where that was inexact, so that a rounding to fewer bits is that of y itself.
+__device__ __forceinline__ float to_odd(double y) {
+  const float f = (float)y;
+  const double back = f;
+  uint32_t u = __float_as_uint(f);
+  if (back != y && y == y) {
+    if (fabs(back) > fabs(y)) --u;
+    u |= 1u;
+  }
+  return __uint_as_float(u);
+}
+__device__ __forceinline__ float to_odd(float y) { return y; }
+
+// 2^(byte - 127), bytes 1 to 254.
+__device__ __forceinline__ float power_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Codes and scale byte of 8 values whose block of 32 lies in four lanes in
+// turn.  The block's largest exponent is found on the bits; the codes count
+// the levels' midpoints that a value has passed, ties to the even code.
+template <class W>
+__device__ __forceinline__ uint32_t quantise8(const W (&y)[8], uint32_t* scale_byte) {
+  float f[8];
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    f[e] = to_odd(y[e]);
+    top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);
+  }
+  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+  if (top >= 0x7f800000u) {            // an infinity or a NaN in the block
+    *scale_byte = 255;
+    return 0x77777777u;
+  }
+  const int byte = max((int)(top >> 23) - 2, 1);
+  *scale_byte = (uint32_t)byte;
+  // 2^-(byte - 127) in two factors, either of them a normal number
+  const float down = power_of((uint32_t)(254 - max(byte, 127)));
+  const float up = power_of((uint32_t)(254 - min(byte, 127)));
+  uint32_t codes = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float z = fabsf(f[e]) * down * up;
+    uint32_t c = z > 0.25f;
+    c += z >= 0.75f;
+    c += z > 1.25f;
+    c += z >= 1.75f;
+    c += z > 2.5f;
+    c += z >= 3.5f;
+    c += z > 5.f;
+    codes |= (c | (__float_as_uint(f[e]) >> 31) << 3) << (4 * e);
+  }
+  return codes;
+}
+
+// Offsets of a 4-bit row's codes and scale bytes in its page.
+template <int D>
+__device__ __forceinline__ int64_t mx_code_at(bool value, int slot, int piece) {
+  return value ? (int64_t)(slot >> 3) * (4 * D) + piece * 32 + (slot & 7) * 4
+               : (int64_t)slot * (D / 2) + piece * 4;
+}
+template <int D>
+__device__ __forceinline__ int64_t mx_scale_at(bool value, int page_log2, int slot, int block) {
+  return ((int64_t)(D / 2) << page_log2) +
+         (value ? (int64_t)(slot >> 3) * (D / 4) + block * 8 + (slot & 7)
+                : (int64_t)slot * (D / 32) + block);
+}
+
+template <class T, bool MX, int D>
+__global__ __launch_bounds__(kThreads) void paged_append_kernel(Batch bt, AppendArgs a,
+                                                                unsigned seq_groups) {
+  constexpr int kPieces = D / 8;
+  const int b = blockIdx.x / seq_groups;
+  const SeqRows sr = seq_rows(bt, b);
+  const int per_row = (a.h_q + 2 * bt.h_kv) * kPieces;
+  const int64_t unit = (int64_t)(blockIdx.x % seq_groups) * kThreads + threadIdx.x;
+  const int r = (int)(unit / per_row);
+  if (r >= sr.n) return;
+  const int past = bt.past[b];
+  if (past < 0 || past >= capacity(bt) - r) return;
+  const int pos = past + r;
+  const int u = (int)(unit - (int64_t)r * per_row);
+  const int piece = u % kPieces;
+  int head = u / kPieces;
+  const int64_t row = sr.start + r;
+  const float* angles = a.rotary + (int64_t)pos * a.rot_dim;
+  if (head < a.h_q) {
+    float y[8];
+    turned8<T, float>(static_cast<const T*>(a.q) + row * a.q_stride + (int64_t)head * D, piece, a,
+                      angles, y);
+    // Where q_out is q, another lane of this wave may still read what is
+    // written here: all lanes of a head are in one wave, and have loaded.
+    store8(static_cast<T*>(a.q_out) + (row * a.h_q + head) * D + 8 * piece, y);
+    return;
+  }
+  head -= a.h_q;
+  const bool value = head >= bt.h_kv;
+  if (value) head -= bt.h_kv;
+  const int page = bt.pages[(int64_t)b * bt.max_pages + (pos >> bt.page_log2)];
+  if ((unsigned)page >= (unsigned)bt.n_pages) return;
+  const int slot = pos & ((1 << bt.page_log2) - 1);
+  char* block = (value ? bt.V : bt.K) +
+                ((int64_t)page * bt.h_kv + head) * block_bytes<T, MX, D>(bt.page_log2);
+  const T* src = value ? static_cast<const T*>(a.v) + row * a.v_stride + (int64_t)head * D
+                       : static_cast<const T*>(a.k) + row * a.k_stride + (int64_t)head * D;
+  if constexpr (MX) {
+    // Rotated in 64 bits: the products of 32-bit numbers are exact, so a
+    // value next to the border of two codes falls on the right side of it.
+    uint32_t scale, codes;
+    if (value) {
+      float y[8];
+      load8(src + 8 * piece, y);
+      codes = quantise8(y, &scale);
+    } else {
+      double y[8];
+      turned8<T, double>(src, piece, a, angles, y);
+      codes = quantise8(y, &scale);
+    }
+    *reinterpret_cast<uint32_t*>(block + mx_code_at<D>(value, slot, piece)) = codes;
+    if (piece % 4 == 0)
+      block[mx_scale_at<D>(value, bt.page_log2, slot, piece / 4)] = (char)scale;
+  } else {
+    T* dst = reinterpret_cast<T*>(block) + (int64_t)slot * D + 8 * piece;
+    float y[8];
+    if (value)
+      load8(src + 8 * piece, y);
+    else
+      turned8<T, float>(src, piece, a, angles, y);
+    store8(dst, y);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Gather: one thread reads 8 dimensions of one head of one row's place.
+// ---------------------------------------------------------------------------
+template <class T, bool MX, int D>
+__global__ __launch_bounds__(kThreads) void paged_gather_kernel(Batch bt, void* k_out,
+                                                                void* v_out,
+                                                                unsigned seq_groups) {
+  constexpr int kPieces = D / 8;
+  const int b = blockIdx.x / seq_groups;
+  const SeqRows sr = seq_rows(bt, b);
+  const int per_row = 2 * bt.h_kv * kPieces;
+  const int64_t unit = (int64_t)(blockIdx.x % seq_groups) * kThreads + threadIdx.x;
+  const int r = (int)(unit / per_row);
+  if (r >= sr.n) return;
+  const int u = (int)(unit - (int64_t)r * per_row);
+  const int piece = u % kPieces;
+  int head = u / kPieces;
+  const bool value = head >= bt.h_kv;
+  if (value) head -= bt.h_kv;
+  T* dst = static_cast<T*>(value ? v_out : k_out) +
+           ((int64_t)(sr.start + r) * bt.h_kv + head) * D + 8 * piece;
+  float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  const int past = bt.past[b];
+  if (past >= 0 && past < capacity(bt) - r) {
+    const int pos = past + r;
+    const int page = bt.pages[(int64_t)b * bt.max_pages + (pos >> bt.page_log2)];
+    if ((unsigned)page < (unsigned)bt.n_pages) {
+      const int slot = pos & ((1 << bt.page_log2) - 1);
+      const char* block = (value ? bt.V : bt.K) +
+                          ((int64_t)page * bt.h_kv + head) * block_bytes<T, MX, D>(bt.page_log2);
+      if constexpr (MX) {
+        const uint32_t codes =
+            *reinterpret_cast<const uint32_t*>(block + mx_code_at<D>(value, slot, piece));
+        const uint32_t byte =
+            (uint8_t)block[mx_scale_at<D>(value, bt.page_log2, slot, piece / 4)];
+        // the byte 255 as a scale is not a number, and so is what it scales
+        const float scale = byte == 255 ? __uint_as_float(0x7fc00000u) : power_of(byte);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t c = codes >> (4 * e) & 15u;
+          const uint32_t ex = c >> 1 & 3u;
+          const float m = ex ? (float)(2 + (c & 1u)) * (float)(1u << ex) * 0.25f
+                             : (float)(c & 1u) * 0.5f;
+          y[e] = (c & 8u ? -m : m) * scale;
+        }
+      } else {
+        load8(reinterpret_cast<const T*>(block) + (int64_t)slot * D + 8 * piece, y);
+      }
+    }
+  }
+  store8(dst, y);
+}
+
+// ---------------------------------------------------------------------------
+// Attention.
+//
+// Items.  An item is (sequence, KV head, tile of up to R = 16*NB query rows);
+// row x of a KV head's rows is (token x / G, query head x % G of the group), so
+// a tile's rows see nearly the same keys.  An item's keys are cut into tiles of
+// KT = 4*TK, and all items' tiles, laid end to end (sequences, heads, row
+// tiles), are divided evenly over the resident workgroups: of W tiles, workgroup
+// w of NW (at most W) takes floor(w W / NW) .. floor((w+1) W / NW) - 1, which it
+// counts itself from past and row_start.  A workgroup begins and ends inside at most
+// one item each; those parts go to its two slots of the workspace, the rest
+// straight to out.  The parts of an item are then those of consecutive
+// workgroups, and the merge finds them from the same counts: no atomics, and
+// equal calls sum in equal order.
+//
+// Tile of a wave: TK keys (32; 16 of float32), all from registers:
+//   S^T [TK keys x 16 rows] = K . Q^T  and  O^T [D x 16 rows] += V^T . P^T.
+// Rows of the score product are assigned to keys so that lane (i, k) holds, for
+// query row i, the scores of keys KPL*k .. KPL*k + KPL-1, KPL = TK/4: that is
+// the share of the summed index that the second product wants of it, so the
+// weights go from one product to the other without leaving the lane.  V comes
+// in by rows (lane (i, k): its keys, D/16 dimensions of each), which float32
+// products take as they are; 16-bit ones want a dimension's keys side by side
+// in a register, two byte permutes for four values.
+// ---------------------------------------------------------------------------
+template <class T, bool MX, int D>
+struct Tile {
+  static constexpr int TK = is_f32<T> && !MX ? 16 : 32;  // keys
+  static constexpr int NH = TK / 16;                     // score products
+  static constexpr int KPL = TK / 4;                     // keys of a lane group
+  static constexpr int NC = D / 16;                      // output products (tiles of 16 dims)
+  // Dimensions that a lane holds side by side of a V row: dimension
+  // VCH*i + 16*VCH*(c/VCH) + c%VCH is row i of output tile c.
+  static constexpr int VCH = D == 64 ? 4 : (is_f32<T> && !MX) ? 4 : 8;
+  static constexpr int NP = NC / VCH;                    // pieces of a V row
+  // 32-bit words of a lane's share of a K row, and of a V row.
+  static constexpr int KW = MX ? D / 32 : is_f32<T> ? D / 4 : D / 8;
+  static constexpr int VW = MX ? NP : is_f32<T> ? D / 16 : D / 32;
+  // values of q that a lane holds: D/4, as words
+  static constexpr int QW = is_f32<T> ? D / 4 : D / 8;
+};
+
+template <class T>
+struct Vec8;
+template <>
+struct Vec8<__bf16> {
+  using type = bf16x8;
+};
+template <>
+struct Vec8<_Float16> {
+  using type = f16x8;
+};
+
+__device__ __forceinline__ f32x4 mma16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma16(f16x8 a, f16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+template <class T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  typedef T t2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), t2));
+}
+
+// Two values of byte `sel` of `codes`, times the scale, as two T.
+template <class T, int sel>
+__device__ __forceinline__ uint32_t widen2(uint32_t codes, float scale) {
+  if constexpr (std::is_same<T, __bf16>::value)
+    return __builtin_bit_cast(uint32_t,
+                              __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, sel));
+  else
+    return __builtin_bit_cast(uint32_t,
+                              __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, sel));
+}
+
+// A scale byte as the factor that the conversions take: they read its exponent
+// alone, 255 as not a number and 0 as 2^-127.
+__device__ __forceinline__ float mx_scale(uint32_t byte) { return power_of(byte); }
+
+template <class T>
+__device__ __forceinline__ bool not_finite(uint32_t w) {
+  if constexpr (is_f32<T>)
+    return (w & 0x7f800000u) == 0x7f800000u;
+  else if constexpr (std::is_same<T, __bf16>::value)
+    return (w & 0x7f800000u) == 0x7f800000u || (w & 0x7f80u) == 0x7f80u;
+  else
+    return (w & 0x7c000000u) == 0x7c000000u || (w & 0x7c00u) == 0x7c00u;
+}
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+struct AttnArgs {
+  const void* q;
+  void* out;
+  int64_t q_stride;
+  float scale;          // times log2(e)
+  int h_q, G, causal;
+  int64_t* offsets;     // [B + 1]: tiles before each sequence
+  float* parts;         // [2 * grid][R][D], then [2 * grid][R][2]
+  int grid;             // workgroups of the attention kernel
+};
+
+// Keys that token t of a sequence sees.
+__device__ __forceinline__ int seen_by(const Batch& bt, const AttnArgs& a, int past, int t) {
+  const int cap = capacity(bt);
+  if (past < 0) return 0;
+  if (!a.causal) return min(past, cap);
+  return past >= cap - t - 1 ? cap : past + t + 1;
+}
+
+// Row tiles of a sequence (each of R rows), tiles of keys of one of them, and
+// of all of them (for one KV head).
+template <int R>
+__device__ __forceinline__ int row_tiles(const AttnArgs& a, int n) {
+  return (int)(((int64_t)n * a.G + R - 1) / R);
+}
+template <int R, int KT>
+__device__ __forceinline__ int key_tiles(const Batch& bt, const AttnArgs& a, int past, int n,
+                                         int rt) {
+  const int64_t last = min((int64_t)n * a.G, (int64_t)(rt + 1) * R) - 1;
+  const int seen = seen_by(bt, a, past, (int)(last / a.G));
+  return (seen + KT - 1) / KT;
+}
+template <int R, int KT>
+__device__ __forceinline__ int64_t head_tiles(const Batch& bt, const AttnArgs& a, int past, int n) {
+  const int nr = row_tiles<R>(a, n);
+  if (nr == 0) return 0;
+  if (!a.causal) return (int64_t)nr * key_tiles<R, KT>(bt, a, past, n, 0);
+  int64_t sum = 0;
+  for (int rt = 0; rt < nr; ++rt) sum += key_tiles<R, KT>(bt, a, past, n, rt);
+  return sum;
+}
+
+template <class T, bool MX, int D, int NB>
+__global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs a) {
+  using L = Tile<T, MX, D>;
+  constexpr int TK = L::TK, NH = L::NH, KPL = L::KPL, NC = L::NC, VCH = L::VCH, NP = L::NP;
+  constexpr int KT = kWaves * TK, R = 16 * NB;
+  constexpr int RB = kRowBytes<T, MX, D>;
+  constexpr int SB = D / 32;                // scale bytes of a 4-bit row
+  constexpr int kLdsRow = D + 4;            // floats: 16-byte accesses of 16 rows spread evenly
+
+  __shared__ float s_acc[kWaves][16][kLdsRow];
+  __shared__ float s_ref[kWaves][16], s_sum[kWaves][16];
+  __shared__ int64_t s_scan[kWaves], s_first;
+  __shared__ int s_seq;
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63, wave = uniform(tid >> 6);
+  const int i = lane & 15, k = lane >> 4;
+
+  // --- the schedule: a prefix over the sequences, a run of them per thread ---
+  const int per = (bt.B + kThreads - 1) / kThreads;
+  const int b_lo = min(tid * per, bt.B), b_hi = min(b_lo + per, bt.B);
+  int64_t mine = 0;
+  for (int b = b_lo; b < b_hi; ++b)
+    mine += bt.h_kv * head_tiles<R, KT>(bt, a, bt.past[b], seq_rows(bt, b).n);
+  int64_t scan = mine;
+#pragma unroll
+  for (int step = 1; step < 64; step <<= 1) {
+    const int64_t other = __shfl_up(scan, step);
+    if (lane >= step) scan += other;
+  }
+  if (lane == 63) s_scan[wave] = scan;
+  __syncthreads();
+  int64_t total = 0;
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) scan += s_scan[w];
+    total += s_scan[w];
+  }
+  const int64_t before = scan - mine;
+  if (blockIdx.x == 0) {
+    int64_t at = before;
+    for (int b = b_lo; b < b_hi; ++b) {
+      a.offsets[b] = at;
+      at += bt.h_kv * head_tiles<R, KT>(bt, a, bt.past[b], seq_rows(bt, b).n);
+    }
+    if (tid == 0) a.offsets[bt.B] = total;
+  }
+  const int64_t share = min(total, (int64_t)a.grid);      // workgroups that have work
+  if (blockIdx.x >= share) return;
+  const int64_t lo = total * blockIdx.x / share, hi = total * (blockIdx.x + 1) / share;
+  if (before <= lo && lo < scan) {
+    int64_t at = before;
+    int b = b_lo;
+    for (; b < b_hi - 1; ++b) {
+      const int64_t n = bt.h_kv * head_tiles<R, KT>(bt, a, bt.past[b], seq_rows(bt, b).n);
+      if (lo < at + n) break;
+      at += n;
+    }
+    s_seq = b;
+    s_first = at;
+  }
+  __syncthreads();
+
+  int b = uniform(s_seq);
+  int64_t cur = lo;
+  SeqRows sr = seq_rows(bt, b);
+  int past = bt.past[b];
+  int64_t rem = lo - s_first;
+  int64_t per_head = head_tiles<R, KT>(bt, a, past, sr.n);
+  int head = (int)(rem / per_head);
+  rem -= head * per_head;
+  int rt = 0;
+  int tiles = key_tiles<R, KT>(bt, a, past, sr.n, 0);
+  while (rem >= tiles) {
+    rem -= tiles;
+    tiles = key_tiles<R, KT>(bt, a, past, sr.n, ++rt);
+  }
+  int t0 = (int)rem;
+
+  const int64_t blk = block_bytes<T, MX, D>(bt.page_log2);
+  const int page_mask = (1 << bt.page_log2) - 1;
+
+  // Lane offsets within a half tile (16 keys) of the K rows and the V rows.
+  const int k_half = TK == 32 ? i >> 3 : 0, v_half = TK == 32 ? k >> 1 : 0;
+  const int k_key = TK == 32 ? 8 * ((i >> 2) & 1) + (i & 3) : i;
+  const int v_key = TK == 32 ? 8 * (k & 1) : 4 * k;
+
+  while (true) {
+    const int t1 = (int)min((int64_t)tiles, t0 + (hi - cur));
+    // --- one part of one item: key tiles t0 .. t1-1 ---
+    const int64_t n_rows = (int64_t)sr.n * a.G;
+    const int64_t row0 = (int64_t)rt * R;
+    const int in_tile = (int)min(n_rows - row0, (int64_t)R);
+    const int min_seen = seen_by(bt, a, past, (int)(row0 / a.G));
+    const int max_seen = seen_by(bt, a, past, (int)((row0 + in_tile - 1) / a.G));
+    const int32_t* table = bt.pages + (int64_t)b * bt.max_pages;
+
+    // q: lane (i, k) holds row i's share of the score products' summed index.
+    uint32_t q[NB][L::QW];
+    int seen[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int x = nb * 16 + i;
+      seen[nb] = 0;
+#pragma unroll
+      for (int w = 0; w < L::QW; ++w) q[nb][w] = 0u;
+      if (x < in_tile) {
+        const int t = (int)((row0 + x) / a.G), g = (int)((row0 + x) % a.G);
+        seen[nb] = seen_by(bt, a, past, t);
+        const T* src = static_cast<const T*>(a.q) + (int64_t)(sr.start + t) * a.q_stride +
+                       (int64_t)(head * a.G + g) * D;
+        constexpr int per16 = 16 / (int)sizeof(T);   // values of a 16-byte load
+#pragma unroll
+        for (int w = 0; w < L::QW / 4; ++w) {
+          const int dim = MX ? D / 4 * k + per16 * w : 4 * per16 * w + per16 * k;
+          const u32x4 v = *reinterpret_cast<const u32x4*>(src + dim);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) q[nb][4 * w + e] = v[e];
+        }
+      }
+    }
+
+    f32x4 acc[NB][NC], sums[NB];
+    float limit[NB], ref[NB];   // raise the reference above limit; scores are taken less ref
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      limit[nb] = -INFINITY;
+      ref[nb] = 0.f;
+      sums[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < NC; ++c) acc[nb][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    uint32_t kw[NH][L::KW], vw[KPL][L::VW];
+    uint32_t ks[NH], vs[NP][2];
+    bool there_a = false, there_b = false;
+
+    // Page of positions p .. p+15 of the sequence: -1 past the table's end.
+    auto page_at = [&](int p) -> int {
+      const int at = p >> bt.page_log2;
+      const int id = at < bt.max_pages ? table[at] : -1;
+      return uniform((unsigned)id < (unsigned)bt.n_pages ? id : -1);
+    };
+    auto base_of = [&](int page, int slot, const char* pool) -> const char* {
+      return pool + ((int64_t)max(page, 0) * bt.h_kv + head) * blk + slot * RB;
+    };
+    auto load_k = [&](int key0, int pa, int pb) {
+      const int sa = key0 & page_mask, sb = (key0 + 16) & page_mask;
+      const char* base = base_of(pa, sa, bt.K);
+      const char* scales = nullptr;
+      if (MX) scales = base + (((int64_t)RB << bt.page_log2) - (int64_t)sa * (RB - SB));
+      if (TK == 32) {
+        const char* other = base_of(pb, sb, bt.K);
+        if (MX && k_half)
+          scales = other + (((int64_t)RB << bt.page_log2) - (int64_t)sb * (RB - SB));
+        if (k_half) base = other;
+      }
+#pragma unroll
+      for (int h = 0; h < NH; ++h) {
+        const char* row = base + (k_key + 4 * h) * RB;
+        if constexpr (MX) {
+          row += k * (D / 8);
+          if constexpr (D == 64) {
+            const u32x2 v = *reinterpret_cast<const u32x2*>(row);
+            kw[h][0] = v[0], kw[h][1] = v[1];
+          } else {
+#pragma unroll
+            for (int w = 0; w < L::KW / 4; ++w) {
+              const u32x4 v = *reinterpret_cast<const u32x4*>(row + 16 * w);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) kw[h][4 * w + e] = v[e];
+            }
+          }
+          const char* s = scales + (k_key + 4 * h) * SB;
+          if constexpr (D == 256)
+            ks[h] = *reinterpret_cast<const uint16_t*>(s + 2 * k);
+          else
+            ks[h] = *reinterpret_cast<const uint8_t*>(s + (D == 64 ? k >> 1 : k));
+        } else {
+#pragma unroll
+          for (int w = 0; w < L::KW / 4; ++w) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(row + 64 * w + 16 * k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) kw[h][4 * w + e] = v[e];
+          }
+        }
+      }
+    };
+    auto load_v = [&](int key0, int pa, int pb) {
+      const int sa = key0 & page_mask, sb = (key0 + 16) & page_mask;
+      const char* base = base_of(pa, sa, bt.V);
+      const char* scales = nullptr;
+      if (MX) scales = base + (((int64_t)RB << bt.page_log2) - (int64_t)sa * (RB - SB));
+      if (TK == 32) {
+        const char* other = base_of(pb, sb, bt.V);
+        if (MX && v_half)
+          scales = other + (((int64_t)RB << bt.page_log2) - (int64_t)sb * (RB - SB));
+        if (v_half) base = other;
+      }
+      base += v_key * RB;
+      if constexpr (MX) {
+        scales += v_key * SB;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+          const int chunk = D == 64 ? i >> 1 : 16 * p + i;      // of 8 dimensions
+          const u32x4 lo4 = *reinterpret_cast<const u32x4*>(base + 32 * chunk);
+          const u32x4 hi4 = *reinterpret_cast<const u32x4*>(base + 32 * chunk + 16);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) vw[e][p] = lo4[e], vw[4 + e][p] = hi4[e];
+          const u32x2 s = *reinterpret_cast<const u32x2*>(scales + 8 * (chunk / 4));
+          vs[p][0] = s[0], vs[p][1] = s[1];
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < KPL; ++j)
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            const char* at = base + j * RB + (VCH * i + 16 * VCH * p) * (int)sizeof(T);
+            if constexpr (VCH * sizeof(T) == 8) {
+              const u32x2 v = *reinterpret_cast<const u32x2*>(at);
+              vw[j][2 * p] = v[0], vw[j][2 * p + 1] = v[1];
+            } else {
+              const u32x4 v = *reinterpret_cast<const u32x4*>(at);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) vw[j][4 * p + e] = v[e];
+            }
+          }
+      }
+    };
+
+    // The V rows' words of piece p as values of T (16-bit types): word w of key
+    // j holds dimensions 2w and 2w+1 of the piece.
+    auto v_words = [&](int p, uint32_t (&x)[KPL][VCH / 2]) {
+      if constexpr (!is_f32<T>) {
+#pragma unroll
+        for (int j = 0; j < KPL; ++j) {
+          if constexpr (MX) {
+            const float scale = mx_scale(vs[p][j / 4] >> (8 * (j % 4)) & 255u);
+            const uint32_t codes = D == 64 ? vw[j][p] >> (16 * (i & 1)) : vw[j][p];
+            x[j][0] = widen2<T, 0>(codes, scale);
+            x[j][1] = widen2<T, 1>(codes, scale);
+            if constexpr (VCH == 8) {
+              x[j][2] = widen2<T, 2>(codes, scale);
+              x[j][3] = widen2<T, 3>(codes, scale);
+            }
+          } else {
+#pragma unroll
+            for (int w = 0; w < VCH / 2; ++w) x[j][w] = vw[j][VCH / 2 * p + w];
+          }
+        }
+      }
+    };
+    // float32: the VCH values of key j in piece p.
+    auto v_floats = [&](int p, int j, float (&x)[VCH]) {
+      if constexpr (MX) {
+        const float scale = mx_scale(vs[p][j / 4] >> (8 * (j % 4)) & 255u);
+        const uint32_t codes = D == 64 ? vw[j][p] >> (16 * (i & 1)) : vw[j][p];
+        const f32x2 a0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0);
+        const f32x2 a1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1);
+        x[0] = a0[0], x[1] = a0[1], x[2] = a1[0], x[3] = a1[1];
+        if constexpr (VCH == 8) {
+          const f32x2 a2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 2);
+          const f32x2 a3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 3);
+          x[4] = a2[0], x[5] = a2[1], x[6] = a3[0], x[7] = a3[1];
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < VCH; ++e) x[e] = __uint_as_float(vw[j][VCH * p + e]);
+      }
+    };
+
+    // Wave w takes 16-key-aligned wave tiles w, w + 4, ...
+    const int wt_end = min(t1 * kWaves, (max_seen + TK - 1) / TK);
+    int wt = t0 * kWaves + wave;
+    int pa = -1, pb = -1;
+    if (wt < wt_end) {
+      pa = page_at(wt * TK);
+      pb = TK == 32 ? page_at(wt * TK + 16) : pa;
+      load_k(wt * TK, pa, pb);
+      load_v(wt * TK, pa, pb);
+      there_a = pa >= 0, there_b = pb >= 0;
+    }
+    for (; wt < wt_end; wt += kWaves) {
+      const int key0 = wt * TK;
+      const int next = key0 + KT;
+      const bool more = wt + kWaves < wt_end;
+      int na = -1, nb_ = -1;
+      if (more) {
+        na = page_at(next);
+        nb_ = TK == 32 ? page_at(next + 16) : na;
+      }
+      // --- scores ---
+      f32x4 s[NB][NH];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int h = 0; h < NH; ++h) s[nb][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int h = 0; h < NH; ++h) {
+        if constexpr (is_f32<T>) {
+          if constexpr (MX) {
+#pragma unroll
+            for (int w = 0; w < L::KW; ++w) {
+              const float scale = mx_scale(D == 256 ? ks[h] >> (8 * (w / 4)) & 255u : ks[h]);
+              const f32x2 a0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(kw[h][w], scale, 0);
+              const f32x2 a1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(kw[h][w], scale, 1);
+              const f32x2 a2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(kw[h][w], scale, 2);
+              const f32x2 a3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(kw[h][w], scale, 3);
+              const float x[8] = {a0[0], a0[1], a1[0], a1[1], a2[0], a2[1], a3[0], a3[1]};
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                  s[nb][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                      x[e], __uint_as_float(q[nb][8 * w + e]), s[nb][h], 0, 0, 0);
+            }
+          } else {
+#pragma unroll
+            for (int w = 0; w < L::KW; ++w)
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb)
+                s[nb][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                    __uint_as_float(kw[h][w]), __uint_as_float(q[nb][w]), s[nb][h], 0, 0, 0);
+          }
+        } else {
+          using V8 = typename Vec8<T>::type;
+#pragma unroll
+          for (int w = 0; w < D / 32; ++w) {
+            u32x4 x;
+            if constexpr (MX) {
+              const float scale = mx_scale(D == 256 ? ks[h] >> (8 * (w / 4)) & 255u : ks[h]);
+              x = u32x4{widen2<T, 0>(kw[h][w], scale), widen2<T, 1>(kw[h][w], scale),
+                        widen2<T, 2>(kw[h][w], scale), widen2<T, 3>(kw[h][w], scale)};
+            } else {
+              x = u32x4{kw[h][4 * w], kw[h][4 * w + 1], kw[h][4 * w + 2], kw[h][4 * w + 3]};
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+              const u32x4 y = {q[nb][4 * w], q[nb][4 * w + 1], q[nb][4 * w + 2],
+                               q[nb][4 * w + 3]};
+              s[nb][h] = mma16(__builtin_bit_cast(V8, x), __builtin_bit_cast(V8, y), s[nb][h]);
+            }
+          }
+        }
+      }
+      if (more) load_k(next, na, nb_);
+
+      // --- masks: only where a row does not see every key of the tile ---
+      const bool edge = key0 + TK > min_seen || !there_a || !there_b;
+      bool spoilt = false;      // V rows that some rows must not see, not finite
+      const bool here = v_half ? there_b : there_a;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s[nb][h][r] *= a.scale;
+      if (edge) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int h = 0; h < NH; ++h)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (!(here && key0 + KPL * k + 4 * h + r < seen[nb])) s[nb][h][r] = -INFINITY;
+        // V rows that no row sees are left out ...
+#pragma unroll
+        for (int j = 0; j < KPL; ++j)
+          if (!(here && key0 + KPL * k + j < max_seen)) {
+#pragma unroll
+            for (int w = 0; w < L::VW; ++w) vw[j][w] = 0u;
+            if constexpr (MX)
+#pragma unroll
+              for (int p = 0; p < NP; ++p) {
+                vs[p][j / 4] &= ~(255u << (8 * (j % 4)));
+                vs[p][j / 4] |= 127u << (8 * (j % 4));
+              }
+          }
+        // ... and those that only some rows see are added one by one if a
+        // weight of 0 would not take them out (0 * infinity).
+        if (min_seen < max_seen) {
+          bool bad = false;
+          if constexpr (MX) {
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+              for (int j = 0; j < KPL; ++j) bad |= (vs[p][j / 4] >> (8 * (j % 4)) & 255u) == 255u;
+          } else {
+#pragma unroll
+            for (int j = 0; j < KPL; ++j)
+#pragma unroll
+              for (int w = 0; w < L::VW; ++w) bad |= not_finite<T>(vw[j][w]);
+          }
+          spoilt = __any(bad);
+        }
+      }
+
+      // --- softmax against a reference that is raised only by a score more
+      // than 8 above it (in base-2 units): the weights stay below 2^8, and
+      // most tiles need neither the maximum over the lanes nor a rescaling ---
+      uint32_t pw[NB][NH * 2];                   // weights, two to a word (16-bit types)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        float top = s[nb][0][0];
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) top = fmaxf(top, s[nb][h][r]);
+        // (a NaN among only NaN becomes the reference, and spoils the row)
+        if (__any(!(top <= limit[nb]))) {
+          top = fmaxf(top, __shfl_xor(top, 16));
+          top = fmaxf(top, __shfl_xor(top, 32));
+          if (!(top <= limit[nb])) {
+            const float f = limit[nb] == -INFINITY ? 0.f : exp2f(ref[nb] - top);
+            ref[nb] = top;
+            limit[nb] = top + 8.f;
+            sums[nb] *= f;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) acc[nb][c] *= f;
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            s[nb][h][r] = __builtin_amdgcn_exp2f(s[nb][h][r] - ref[nb]);
+          if constexpr (is_f32<T>) {
+            sums[nb] += s[nb][h];
+          } else {
+            pw[nb][2 * h] = pack2<T>(s[nb][h][0], s[nb][h][1]);
+            pw[nb][2 * h + 1] = pack2<T>(s[nb][h][2], s[nb][h][3]);
+          }
+        }
+      }
+
+      // --- O^T += V^T P^T ---
+      if constexpr (is_f32<T>) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+          for (int j = 0; j < KPL; ++j) {
+            float x[VCH];
+            v_floats(p, j, x);
+            if (!spoilt) {
+#pragma unroll
+              for (int c = 0; c < VCH; ++c)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+                  acc[nb][VCH * p + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                      x[c], s[nb][j / 4][j % 4], acc[nb][VCH * p + c], 0, 0, 0);
+            } else {
+              for (int g = 0; g < 4; ++g) {      // key KPL*g + j alone
+                const int key = key0 + KPL * g + j;
+#pragma unroll
+                for (int c = 0; c < VCH; ++c)
+#pragma unroll
+                  for (int nb = 0; nb < NB; ++nb) {
+                    const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                        k == g ? x[c] : 0.f, s[nb][j / 4][j % 4], acc[nb][VCH * p + c], 0, 0, 0);
+                    if (key < seen[nb]) acc[nb][VCH * p + c] = y;
+                  }
+              }
+            }
+          }
+      } else {
+        using V8 = typename Vec8<T>::type;
+        V8 weights[NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+          weights[nb] =
+              __builtin_bit_cast(V8, (u32x4{pw[nb][0], pw[nb][1], pw[nb][2], pw[nb][3]}));
+        V8 ones;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ones[e] = (T)1.f;
+        // the sum of the weights as they are multiplied, in every lane
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) sums[nb] = mma16(ones, weights[nb], sums[nb]);
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+          uint32_t x[KPL][VCH / 2];
+          v_words(p, x);
+          if (!spoilt) {
+#pragma unroll
+            for (int c = 0; c < VCH; ++c) {
+              const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
+              const u32x4 col = {__builtin_amdgcn_perm(x[1][c / 2], x[0][c / 2], sel),
+                                 __builtin_amdgcn_perm(x[3][c / 2], x[2][c / 2], sel),
+                                 __builtin_amdgcn_perm(x[5][c / 2], x[4][c / 2], sel),
+                                 __builtin_amdgcn_perm(x[7][c / 2], x[6][c / 2], sel)};
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb)
+                acc[nb][VCH * p + c] = mma16(__builtin_bit_cast(V8, col), weights[nb],
+                                             acc[nb][VCH * p + c]);
+            }
+          } else {
+            for (int key = 0; key < TK; ++key) {  // each key alone
+              const bool my_k = k == key / KPL;
+              const int j = key % KPL;
+#pragma unroll
+              for (int c = 0; c < VCH; ++c) {
+                const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
+                u32x4 col;
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                  col[y] = __builtin_amdgcn_perm(my_k && j == 2 * y + 1 ? x[2 * y + 1][c / 2] : 0u,
+                                                 my_k && j == 2 * y ? x[2 * y][c / 2] : 0u, sel);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                  const f32x4 y = mma16(__builtin_bit_cast(V8, col), weights[nb],
+                                        acc[nb][VCH * p + c]);
+                  if (key0 + key < seen[nb]) acc[nb][VCH * p + c] = y;
+                }
+              }
+            }
+          }
+        }
+      }
+      if (more) load_v(next, na, nb_);
+      there_a = na >= 0, there_b = nb_ >= 0;
+    }
+
+    // --- the four waves' states, one column block at a time ---
+    const bool whole = t0 == 0 && t1 == tiles;
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (t0 == 0 ? 1 : 0);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      float sum = sums[nb][0];
+      if constexpr (is_f32<T>) {
+        sum = (sums[nb][0] + sums[nb][1]) + (sums[nb][2] + sums[nb][3]);
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+      }
+      const float my_ref = limit[nb] == -INFINITY ? -INFINITY : ref[nb];
+      __syncthreads();
+      if (k == 0) {
+        s_ref[wave][i] = my_ref;
+        s_sum[wave][i] = sum;
+      }
+      __syncthreads();
+      float top = s_ref[0][i];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_ref[w][i]);
+      const float f = my_ref == -INFINITY ? 0.f : exp2f(my_ref - top);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < NC; c += 4) {
+          const int dim = VCH * (4 * k + r) + 16 * VCH * (c / VCH) + c % VCH;
+          // a state that saw nothing holds zeros, and its factor is 0
+          *reinterpret_cast<f32x4*>(&s_acc[wave][i][dim]) =
+              f32x4{acc[nb][c][r], acc[nb][c + 1][r], acc[nb][c + 2][r], acc[nb][c + 3][r]} * f;
+        }
+      __syncthreads();
+#pragma unroll
+      for (int e = tid; e < 16 * D / 4; e += kThreads) {
+        const int x = e / (D / 4), dim = e % (D / 4) * 4;
+        const int in = nb * 16 + x;
+        if (in >= in_tile) continue;
+        float m = s_ref[0][x];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_ref[w][x]);
+        float l = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          const float rw = s_ref[w][x];
+          l += rw == -INFINITY ? 0.f : s_sum[w][x] * exp2f(rw - m);
+          o += *reinterpret_cast<const f32x4*>(&s_acc[w][x][dim]);
+        }
+        if (whole) {
+          o = l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o / l;
+          const int t = (int)((row0 + in) / a.G), g = (int)((row0 + in) % a.G);
+          T* dst = static_cast<T*>(a.out) +
+                   ((int64_t)(sr.start + t) * a.h_q + head * a.G + g) * D + dim;
+          if constexpr (is_f32<T>)
+            *reinterpret_cast<f32x4*>(dst) = o;
+          else
+            *reinterpret_cast<u32x2*>(dst) = u32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
+        } else {
+          *reinterpret_cast<f32x4*>(a.parts + (slot * R + in) * D + dim) = o;
+          if (dim == 0)
+            *reinterpret_cast<f32x2*>(a.parts + (int64_t)2 * a.grid * R * D +
+                                      (slot * R + in) * 2) = f32x2{m, l};
+        }
+      }
+    }
+
+    // --- the next item ---
+    cur += t1 - t0;
+    if (cur >= hi) break;
+    t0 = 0;
+    tiles = 0;
+    while (tiles == 0) {
+      if (++rt >= row_tiles<R>(a, sr.n)) {
+        rt = 0;
+        if (++head >= bt.h_kv) {
+          head = 0;
+          sr = seq_rows(bt, ++b);
+          past = bt.past[b];
+          if (sr.n == 0) {                        // (a later sequence has tiles: cur < hi)
+            head = bt.h_kv - 1;
+            continue;
+          }
+        }
+      }
+      tiles = key_tiles<R, KT>(bt, a, past, sr.n, rt);
+    }
+  }
+}
+
+// Combines the parts of an item's rows: blockIdx.x names the item (sequence, KV
+// head, row tile), the rows are shared out over blockIdx.y; four waves share a
+// row's parts.  Rows that see nothing are written here.
+template <class T, int D, int R, int KT>
+__global__ __launch_bounds__(kThreads) void paged_merge_kernel(Batch bt, AttnArgs a,
+                                                               int max_row_tiles) {
+  constexpr int kVec = D / 64;
+  __shared__ float s_part[kWaves][D], s_m[kWaves], s_l[kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int rt = blockIdx.x % max_row_tiles;
+  const int bh = blockIdx.x / max_row_tiles;
+  const int head = bh % bt.h_kv, b = bh / bt.h_kv;
+  const SeqRows sr = seq_rows(bt, b);
+  if (rt >= row_tiles<R>(a, sr.n)) return;
+  const int past = bt.past[b];
+  const int count = key_tiles<R, KT>(bt, a, past, sr.n, rt);
+  const int64_t row0 = (int64_t)rt * R;
+  const int in_tile = (int)min((int64_t)sr.n * a.G - row0, (int64_t)R);
+  int64_t w0 = 0, w1 = -1;
+  if (count > 0) {
+    const int64_t total = a.offsets[bt.B], first = a.offsets[b];
+    int64_t at = first + head * ((a.offsets[b + 1] - first) / bt.h_kv);
+    if (!a.causal)
+      at += (int64_t)rt * count;
+    else
+      for (int x = 0; x < rt; ++x) at += key_tiles<R, KT>(bt, a, past, sr.n, x);
+    const int64_t share = min(total, (int64_t)a.grid);
+    w0 = ((at + 1) * share - 1) / total;
+    w1 = ((at + count) * share - 1) / total;
+    if (w0 == w1) return;                          // one workgroup had it all
+  }
+  const float* ml = a.parts + (int64_t)2 * a.grid * R * D;
+  for (int in = blockIdx.y; in < in_tile; in += gridDim.y) {
+    float m = -INFINITY, l = 0.f, o[kVec];
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) o[e] = 0.f;
+    for (int64_t w = w0 + wave; w <= w1; w += kWaves) {
+      const int64_t slot = 2 * w + (w == w0 ? 1 : 0);
+      const f32x2 s = *reinterpret_cast<const f32x2*>(ml + (slot * R + in) * 2);
+      const float* p = a.parts + (slot * R + in) * D + lane * kVec;
+      float v[kVec];
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) v[e] = p[e];
+      if (s[0] == -INFINITY) continue;             // saw nothing
+      const float mn = s[0] <= m ? m : s[0];       // (a NaN stays)
+      const float fo = m == -INFINITY ? 0.f : exp2f(m - mn), fn = exp2f(s[0] - mn);
+      l = l * fo + s[1] * fn;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) o[e] = o[e] * fo + v[e] * fn;
+      m = mn;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) s_part[wave][lane * kVec + e] = o[e];
+    if (lane == 0) s_m[wave] = m, s_l[wave] = l;
+    __syncthreads();
+    if (tid < D) {
+      float top = s_m[0];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_m[w]);
+      float sum = 0.f, y = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        if (s_m[w] == -INFINITY) continue;
+        const float f = exp2f(s_m[w] - top);
+        sum += s_l[w] * f;
+        y += s_part[w][tid] * f;
+      }
+      const int t = (int)((row0 + in) / a.G), g = (int)((row0 + in) % a.G);
+      static_cast<T*>(a.out)[((int64_t)(sr.start + t) * a.h_q + head * a.G + g) * D + tid] =
+          (T)(sum == 0.f ? 0.f : y / sum);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+// ---------------------------------------------------------------------------
+bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+size_t pad256(size_t x) { return (x + 255) / 256 * 256; }
+bool dim_ok(int d) { return d == 64 || d == 128 || d == 256; }
+bool type_ok(int dtype) { return dtype >= DA_F32 && dtype <= DA_F16; }
+int type_bytes(int dtype) { return dtype == DA_F32 ? 4 : 2; }
+
+constexpr int kMaxPageRows = 32768;
+constexpr int64_t kMaxPositions = int64_t(1) << 30;
+constexpr int kMaxRowsPerSeq = 32768;
+constexpr int64_t kMaxItems = int64_t(1) << 24;   // sequences x query heads
+constexpr int64_t kMaxGroups = (int64_t(1) << 24) - 1;  // of 256 threads: a grid has < 2^32
+
+// Compute units of the current device, at most kMaxCus, queried once per
+// device.  Without a device (the call can then only fail at launch) kMaxCus.
+constexpr int kMaxDevices = 64;
+std::atomic<int> g_cus[kMaxDevices];
+
+int device_cus() {
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) {
+    (void)hipGetLastError();
+    return kMaxCus;
+  }
+  int c = g_cus[dev].load(std::memory_order_relaxed);
+  if (c == 0) {
+    int n = 0;
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess ||
+        n < 1) {
+      (void)hipGetLastError();
+      return kMaxCus;
+    }
+    c = std::min(n, kMaxCus);
+    g_cus[dev].store(c, std::memory_order_relaxed);
+  }
+  return c;
+}
+
+da_status launch_status() { return hipGetLastError() == hipSuccess ? DA_OK : DA_ERR_HIP; }
+
+// Everything about the batch but NULL pointers of the arrays: shapes, then
+// what is supported.
+da_status check_batch(const da_paged_kv& p) {
+  if (p.B < 1 || p.h_kv < 1 || p.d < 1 || p.n_pages < 1 || p.page_rows < 1 || p.max_pages < 1 ||
+      p.rows < 1 || p.T < 1)
+    return DA_ERR_SHAPE;
+  if ((int64_t)p.page_rows * p.max_pages > kMaxPositions || p.T > kMaxRowsPerSeq ||
+      (int64_t)p.B * p.h_kv > kMaxItems)
+    return DA_ERR_SHAPE;
+  if (!p.row_start && (int64_t)p.B * p.T != p.rows) return DA_ERR_SHAPE;
+  if (!dim_ok(p.d) || !type_ok(p.dtype) ||
+      (p.format != DA_KV_DENSE && p.format != DA_KV_MX4) || p.page_rows < 16 ||
+      p.page_rows > kMaxPageRows || (p.page_rows & (p.page_rows - 1)) != 0)
+    return DA_ERR_UNSUPPORTED;
+  return DA_OK;
+}
+
+bool batch_aligned(const da_paged_kv& p) {
+  return aligned(p.K, 16) && aligned(p.V, 16) && aligned(p.pages, 4) && aligned(p.past, 4) &&
+         aligned(p.row_start, 4);
+}
+
+Batch device_batch(const da_paged_kv& p) {
+  int log2 = 0;
+  while ((1 << log2) < p.page_rows) ++log2;
+  return {static_cast<char*>(p.K), static_cast<char*>(p.V), p.pages, p.past, p.row_start, p.B,
+          p.h_kv, p.n_pages, log2, p.max_pages, p.rows, p.T};
+}
+
+// Calls f(type tag, mx, d) with the batch's as compile-time constants.
+template <class T>
+struct Tag {
+  using type = T;
+};
+template <bool MX, int D, class F>
+void with_type(int dtype, F&& f) {
+  if (dtype == DA_F32)
+    f(Tag<float>{}, std::bool_constant<MX>{}, std::integral_constant<int, D>{});
+  else if (dtype == DA_BF16)
+    f(Tag<__bf16>{}, std::bool_constant<MX>{}, std::integral_constant<int, D>{});
+  else
+    f(Tag<_Float16>{}, std::bool_constant<MX>{}, std::integral_constant<int, D>{});
+}
+template <bool MX, class F>
+void with_dim(int dtype, int d, F&& f) {
+  if (d == 64)
+    with_type<MX, 64>(dtype, f);
+  else if (d == 128)
+    with_type<MX, 128>(dtype, f);
+  else
+    with_type<MX, 256>(dtype, f);
+}
+template <class F>
+void dispatch(const da_paged_kv& p, F&& f) {
+  if (p.format == DA_KV_MX4)
+    with_dim<true>(p.dtype, p.d, f);
+  else
+    with_dim<false>(p.dtype, p.d, f);
+}
+
+// Query rows of a row tile: 16 for one column block, else 32.
+int tile_rows(int64_t rows_per_head) { return rows_per_head <= 16 ? 16 : 32; }
+
+constexpr int kGroupsPerCu = 2;       // workgroups of the attention kernel per CU
+
+struct AttnPlan {
+  int R;
+  size_t offsets_bytes, bytes;
+};
+
+da_status plan_attn(int B, int h_q, int h_kv, int d, int T, int dtype, AttnPlan* plan) {
+  if (B < 1 || h_q < 1 || h_kv < 1 || d < 1 || T < 1 || T > kMaxRowsPerSeq || h_q % h_kv != 0 ||
+      (int64_t)B * h_q > kMaxItems || (int64_t)h_q * T > (int64_t(1) << 30))
+    return DA_ERR_SHAPE;
+  if (!dim_ok(d) || !type_ok(dtype)) return DA_ERR_UNSUPPORTED;
+  const int64_t per_head = (int64_t)(h_q / h_kv) * T;
+  plan->R = tile_rows(per_head);
+  // (the merge's grid is the items)
+  if ((int64_t)B * h_kv * ceil_div(per_head, plan->R) > kMaxGroups) return DA_ERR_SHAPE;
+  plan->offsets_bytes = pad256(((size_t)B + 1) * sizeof(int64_t));
+  plan->bytes = plan->offsets_bytes +
+                (size_t)2 * kMaxCus * kGroupsPerCu * plan->R * ((size_t)d + 2) * sizeof(float);
+  return DA_OK;
+}
+
+template <class T, bool MX, int D, int NB>
+void launch_attn(const Batch& bt, const AttnArgs& a, hipStream_t s) {
+  constexpr int R = 16 * NB, KT = kWaves * Tile<T, MX, D>::TK;
+  hipLaunchKernelGGL((paged_attn_kernel<T, MX, D, NB>), dim3((unsigned)a.grid), dim3(kThreads), 0,
+                     s, bt, a);
+  const int64_t per_head = (int64_t)a.G * bt.T;
+  const int nr = (int)ceil_div(per_head, R);
+  // one row of a small tile each; the many tiles of long chunks share less
+  const unsigned split = nr > 1 ? 4u : (unsigned)per_head;
+  hipLaunchKernelGGL((paged_merge_kernel<T, D, R, KT>),
+                     dim3((unsigned)((int64_t)bt.B * bt.h_kv * nr), split), dim3(kThreads), 0, s,
+                     bt, a, nr);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t da_paged_page_bytes(int page_rows, int d, int dtype, int format) {
+  if (page_rows < 16 || page_rows > kMaxPageRows || (page_rows & (page_rows - 1)) != 0 ||
+      !dim_ok(d) || !type_ok(dtype))
+    return 0;
+  if (format == DA_KV_MX4) return (size_t)page_rows * (d / 2 + d / 32);
+  return format == DA_KV_DENSE ? (size_t)page_rows * d * type_bytes(dtype) : 0;
+}
+
+da_status da_paged_append(const da_paged_kv* kv, const void* k_new, const void* v_new,
+                          int64_t k_stride, int64_t v_stride, const void* q, int64_t q_stride,
+                          int h_q, void* q_out, const float* rotary, int n_rotary, int rot_dim,
+                          int interleaved, void* stream) {
+  if (!kv || !k_new || !v_new || !kv->K || !kv->V || !kv->pages || !kv->past ||
+      (q && !q_out) || (rot_dim != 0 && !rotary))
+    return DA_ERR_NULL;
+  const da_paged_kv& p = *kv;
+  da_status st = check_batch(p);
+  if (st != DA_OK && st != DA_ERR_UNSUPPORTED) return st;
+  if (!q) h_q = 0;
+  if (h_q < 0 || (q && h_q < 1) || (int64_t)h_q * p.d > (1 << 30) || rot_dim < 0 ||
+      rot_dim > p.d || (rot_dim != 0 && n_rotary < (int64_t)p.page_rows * p.max_pages) ||
+      k_stride < (int64_t)p.h_kv * p.d || v_stride < (int64_t)p.h_kv * p.d ||
+      (q && q_stride < (int64_t)h_q * p.d))
+    return DA_ERR_SHAPE;
+  if (st != DA_OK || rot_dim % 16 != 0) return DA_ERR_UNSUPPORTED;
+  const int per16 = 16 / type_bytes(p.dtype);
+  if (!batch_aligned(p) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(q, 16) ||
+      !aligned(q_out, 16) || !aligned(rotary, 16) || k_stride % per16 || v_stride % per16 ||
+      (q && q_stride % per16))
+    return DA_ERR_ALIGN;
+  const AppendArgs a{q,        k_new,    v_new,  q_out, q_stride, k_stride,
+                     v_stride, rotary, h_q, rot_dim, interleaved};
+  const Batch bt = device_batch(p);
+  const int64_t units = (int64_t)p.T * (h_q + 2 * (int64_t)p.h_kv) * (p.d / 8);
+  const int64_t groups = ceil_div(units, kThreads);
+  if (groups > kMaxGroups || groups * p.B > kMaxGroups) return DA_ERR_SHAPE;
+  (void)hipGetLastError();
+  dispatch(p, [&](auto t, auto mx, auto d) {
+    hipLaunchKernelGGL((paged_append_kernel<typename decltype(t)::type, mx.value, d.value>),
+                       dim3((unsigned)(groups * p.B)), dim3(kThreads), 0,
+                       static_cast<hipStream_t>(stream), bt, a, (unsigned)groups);
+  });
+  return launch_status();
+}
+
+da_status da_paged_gather(const da_paged_kv* kv, void* k_out, void* v_out, void* stream) {
+  if (!kv || !k_out || !v_out || !kv->K || !kv->V || !kv->pages || !kv->past) return DA_ERR_NULL;
+  const da_paged_kv& p = *kv;
+  const da_status st = check_batch(p);
+  if (st != DA_OK) return st;
+  if (!batch_aligned(p) || !aligned(k_out, 16) || !aligned(v_out, 16)) return DA_ERR_ALIGN;
+  const Batch bt = device_batch(p);
+  const int64_t groups = ceil_div((int64_t)p.T * 2 * p.h_kv * (p.d / 8), kThreads);
+  if (groups > kMaxGroups || groups * p.B > kMaxGroups) return DA_ERR_SHAPE;
+  (void)hipGetLastError();
+  dispatch(p, [&](auto t, auto mx, auto d) {
+    hipLaunchKernelGGL((paged_gather_kernel<typename decltype(t)::type, mx.value, d.value>),
+                       dim3((unsigned)(groups * p.B)), dim3(kThreads), 0,
+                       static_cast<hipStream_t>(stream), bt, k_out, v_out, (unsigned)groups);
+  });
+  return launch_status();
+}
+
+size_t da_paged_workspace_bytes(int B, int h_q, int h_kv, int d, int T, int dtype) {
+  AttnPlan plan;
+  return plan_attn(B, h_q, h_kv, d, T, dtype, &plan) == DA_OK ? plan.bytes : 0;
+}
+
+da_status da_paged_attn(const da_paged_kv* kv, const void* q, int64_t q_stride, int h_q,
+                        float scale, int causal, void* out, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  if (!kv || !q || !out || !kv->K || !kv->V || !kv->pages || !kv->past) return DA_ERR_NULL;
+  const da_paged_kv& p = *kv;
+  da_status st = check_batch(p);
+  if (st != DA_OK && st != DA_ERR_UNSUPPORTED) return st;
+  AttnPlan plan;
+  const da_status sp = plan_attn(p.B, h_q, p.h_kv, p.d, p.T, p.dtype, &plan);
+  if (sp == DA_ERR_SHAPE || q_stride < (int64_t)h_q * p.d) return DA_ERR_SHAPE;
+  if (st != DA_OK || sp != DA_OK) return DA_ERR_UNSUPPORTED;
+  if (!batch_aligned(p) || !aligned(q, 16) || !aligned(out, 16) ||
+      q_stride % (16 / type_bytes(p.dtype)))
+    return DA_ERR_ALIGN;
+  if (!std::isfinite(scale)) return DA_ERR_SCALE;
+  if (!workspace || workspace_bytes < plan.bytes) return DA_ERR_WORKSPACE;
+  if (!aligned(workspace, 16)) return DA_ERR_ALIGN;
+  const Batch bt = device_batch(p);
+  const AttnArgs a{q,
+                   out,
+                   q_stride,
+                   scale * kLog2e,
+                   h_q,
+                   h_q / p.h_kv,
+                   causal,
+                   static_cast<int64_t*>(workspace),
+                   reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.offsets_bytes),
+                   device_cus() * kGroupsPerCu};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  dispatch(p, [&](auto t, auto mx, auto d) {
+    using T = typename decltype(t)::type;
+    if (plan.R == 16)
+      launch_attn<T, mx.value, d.value, 1>(bt, a, s);
+    else
+      launch_attn<T, mx.value, d.value, 2>(bt, a, s);
+  });
+  return launch_status();
+}
+
+}  // extern "C"
