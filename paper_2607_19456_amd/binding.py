@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -383,15 +384,13 @@ def kv_append_rows(K, V, k_new, v_new, lens, stream=None) -> None:
 
 # --- paged cache ----------------------------------------------------------------
 
-class _PagedKV(ctypes.Structure):
-    """da_paged_kv"""
-    _fields_ = ([(n, _vp) for n in ("K", "V", "pages", "past", "row_start")]
-                + [(n, _ci) for n in ("B", "h_kv", "d", "n_pages", "page_rows", "max_pages",
-                                      "rows", "T", "dtype", "format")])
-
+# da_paged_kv: five pointers, ten ints.  Packed as bytes: filling a
+# ctypes.Structure of 15 fields takes twice as long.
+_pack_kv = struct.Struct("=5Q10i").pack
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _DENSE, _MX4 = 0, 1
+_i32, _u8, _f32 = torch.int32, torch.uint8, torch.float32
 
 
 def paged_alloc(n_pages: int, page_rows: int, h_kv: int, d: int, dtype=torch.bfloat16,
@@ -421,63 +420,93 @@ def rotary_table(n: int, rot_dim: int, base: float = 10000.0, device="cuda") -> 
     return torch.cat((a.cos(), a.sin()), 1).to(device=device, dtype=torch.float32)
 
 
-def _here(t, name, dtype) -> int:
-    """_dev, and on the current device (whose stream the kernels run on)."""
-    p = _dev(t, name, dtype)
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name} must be on the current device")
-    return p
-
-
-def _tokens(t, name, dtype):
-    """Address and token stride (elements) of rows [rows, heads, d]."""
+def _refuse(t, name, dtype, gpu):
+    """The error of a tensor that a paged call cannot take."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_cuda:
         raise TypeError(f"{name} must be on the GPU")
-    if t.get_device() != torch.cuda.current_device():
+    if t.get_device() != gpu:
         raise ValueError(f"{name} must be on the current device")
-    if t.dim() != 3:
-        raise ValueError(f"{name} must be [rows, heads, d]")
-    rows, heads, d = t.shape
+    raise ValueError(f"{name} must be contiguous")
+
+
+def _here(t, name, dtype, gpu) -> int:
+    """Address of a contiguous tensor of this type on the current device, gpu."""
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == gpu
+            and t.is_contiguous()):
+        return t.data_ptr()
+    _refuse(t, name, dtype, gpu)
+
+
+def _stride(t, name, shape) -> int:
+    """Token stride (elements) of rows [rows, heads, d] that are not contiguous."""
+    rows, heads, d = shape
     stride, head_stride, one = t.stride()
-    if (one != 1 and d != 1) or (head_stride != d and heads != 1):
+    if one != 1 or (head_stride != d and heads != 1):
         raise ValueError(f"{name}: a token's heads must be contiguous")
-    return t.data_ptr(), stride if rows > 1 else max(stride, heads * d)
+    return stride if rows > 1 else heads * d
 
 
-def _paged(K, V, pages, past, rows, d, dtype, row_start, T) -> _PagedKV:
-    if not (isinstance(K, torch.Tensor) and isinstance(V, torch.Tensor)):
-        raise TypeError("K and V must be torch.Tensors")
-    if K.dim() != 4 or K.shape != V.shape:
-        raise ValueError("K and V must be pools of one shape, [n_pages,h_kv,page_rows,..]")
-    if dtype not in _DTYPES:
+def _need(condition, message):
+    if not condition:
+        raise ValueError(message)
+
+
+def _paged(K, V, pages, past, rows, d, dtype, row_start, T):
+    """(da_paged_kv as bytes, current device, h_kv, T) of a call.  The checks are
+    written out: a tensor's attributes take 0.1 us each, and so does a call."""
+    if not (isinstance(K, torch.Tensor) and isinstance(V, torch.Tensor)
+            and isinstance(pages, torch.Tensor) and isinstance(past, torch.Tensor)):
+        raise TypeError("K, V, pages and past must be torch.Tensors")
+    code = _DTYPES.get(dtype)
+    if code is None:
         raise TypeError(f"rows must be float32, bfloat16 or float16, got {dtype}")
-    n_pages, h_kv, page_rows, width = K.shape
-    mx4 = K.dtype == torch.uint8
+    shape = K.shape
+    if len(shape) != 4 or V.shape != shape:
+        raise ValueError("K and V must be pools of one shape, [n_pages,h_kv,page_rows,..]")
+    n_pages, h_kv, page_rows, width = shape
+    mx4 = K.dtype is _u8
+    pool = _u8 if mx4 else dtype
     if width != (d // 2 + d // 32 if mx4 else d):
         raise ValueError(f"pools of width {width} do not hold rows of d={d}")
-    pool = torch.uint8 if mx4 else dtype
-    kp, vp = _here(K, "K", pool), _here(V, "V", pool)
-    pp, np_ = _here(pages, "pages", torch.int32), _here(past, "past", torch.int32)
-    if pages.dim() != 2 or past.dim() != 1 or pages.shape[0] != past.shape[0]:
-        raise ValueError("pages must be [B,max_pages] and past [B]")
+    gpu = K.get_device()
+    if not (gpu >= 0 and gpu == torch._C._cuda_getDevice() and K.dtype is pool
+            and V.dtype is pool and pages.dtype is _i32 and past.dtype is _i32
+            and V.get_device() == gpu and pages.get_device() == gpu and past.get_device() == gpu
+            and K.is_contiguous() and V.is_contiguous() and pages.is_contiguous()
+            and past.is_contiguous()):
+        gpu = torch.cuda.current_device() if gpu >= 0 else 0
+        for t, name, kind in ((K, "K", pool), (V, "V", pool), (pages, "pages", _i32),
+                              (past, "past", _i32)):
+            _here(t, name, kind, gpu)
+    _need(pages.dim() == 2, "pages must be [B,max_pages]")
     B, max_pages = pages.shape
-    rp = None
+    _need(past.dim() == 1 and past.numel() == B, "past must be [B], as pages is [B,max_pages]")
+    start = 0
     if row_start is not None:
-        rp = _here(row_start, "row_start", torch.int32)
-        if tuple(row_start.shape) != (B + 1,):
-            raise ValueError("row_start must be [B+1]")
-        if T < 1:
-            raise ValueError("with row_start, T is the most rows of a sequence")
-    elif T == 0 and B and rows % B == 0:
-        T = rows // B
-    if row_start is None and rows != B * T:
-        raise ValueError("without row_start every sequence has T rows: rows must be B*T")
-    return _PagedKV(kp, vp, pp, np_, rp, B, h_kv, d, n_pages, page_rows, max_pages, rows, T,
-                    _DTYPES[dtype], _MX4 if mx4 else _DENSE)
+        start = _here(row_start, "row_start", _i32, gpu)
+        _need(row_start.dim() == 1 and row_start.numel() == B + 1, "row_start must be [B+1]")
+        _need(T >= 1, "with row_start, T is the most rows of a sequence")
+    else:
+        if T == 0 and B:
+            T = rows // B
+        _need(rows == B * T, "without row_start every sequence has T rows: rows must be B*T")
+    return _pack_kv(K.data_ptr(), V.data_ptr(), pages.data_ptr(), past.data_ptr(), start, B,
+                    h_kv, d, n_pages, page_rows, max_pages, rows, T, code,
+                    _MX4 if mx4 else _DENSE), gpu, h_kv, T
+
+
+def _paged_stream(stream, gpu) -> int:
+    return _stream(stream) if stream is not None or _raw_stream is None else _raw_stream(gpu)
+
+
+def _rows(t, name):
+    if not isinstance(t, torch.Tensor) or t.dim() != 3:
+        raise ValueError(f"{name} must be [rows, heads, d]")
+    return t.shape
 
 
 def paged_append(K, V, pages, past, k_new, v_new, q=None, rotary=None, interleaved: bool = False,
@@ -486,35 +515,42 @@ def paged_append(K, V, pages, past, k_new, v_new, q=None, rotary=None, interleav
     turned by ``rotary`` [positions, rot_dim] on the way, and q [rows,h_q,d] turned
     into q_out (returned).  ``row_start`` [B+1]: each sequence's rows, at most ``T``;
     else T rows each.  past is not changed."""
-    if not isinstance(k_new, torch.Tensor) or k_new.dim() != 3:
-        raise ValueError("k_new must be [rows,h_kv,d]")
-    rows, h_kv, d = k_new.shape
+    shape = _rows(k_new, "k_new")
+    rows, heads, d = shape
     dtype = k_new.dtype
-    p = _paged(K, V, pages, past, rows, d, dtype, row_start, T)
-    if h_kv != p.h_kv or v_new.shape != k_new.shape:
+    kv, gpu, h_kv, T = _paged(K, V, pages, past, rows, d, dtype, row_start, T)
+    if heads != h_kv or _rows(v_new, "v_new") != shape:
         raise ValueError("k_new and v_new must be [rows,h_kv,d]")
-    kp, ks = _tokens(k_new, "k_new", dtype)
-    vp, vs = _tokens(v_new, "v_new", dtype)
+    if not (v_new.dtype is dtype and k_new.get_device() == gpu and v_new.get_device() == gpu):
+        _refuse(k_new if k_new.get_device() != gpu else v_new, "k_new and v_new", dtype, gpu)
+    ks = vs = heads * d
+    if not k_new.is_contiguous():
+        ks = _stride(k_new, "k_new", shape)
+    if not v_new.is_contiguous():
+        vs = _stride(v_new, "v_new", shape)
     qp = qo = rp = None
     qs = h_q = n_rot = rot_dim = 0
     if q is not None:
-        qp, qs = _tokens(q, "q", dtype)
-        h_q = q.shape[1]
-        if q.shape[0] != rows or q.shape[2] != d:
-            raise ValueError("q must be [rows,h_q,d]")
+        shape = _rows(q, "q")
+        h_q = shape[1]
+        _need(shape[0] == rows and shape[2] == d, "q must be [rows,h_q,d]")
+        if not (q.dtype is dtype and q.get_device() == gpu):
+            _refuse(q, "q", dtype, gpu)
+        qs = h_q * d if q.is_contiguous() else _stride(q, "q", shape)
+        qp = q.data_ptr()
         if q_out is None:
-            q_out = torch.empty((rows, h_q, d), dtype=dtype, device=q.device)
-        elif q_out.shape != q.shape:
-            raise ValueError("q_out must have q's shape")
-        qo = _here(q_out, "q_out", dtype)
+            q_out = torch.empty(shape, dtype=dtype, device=q.device)
+        qo = _here(q_out, "q_out", dtype, gpu)
+        _need(q_out.shape == shape, "q_out must have q's shape")
     if rotary is not None:
-        rp = _here(rotary, "rotary", torch.float32)
-        if rotary.dim() != 2:
-            raise ValueError("rotary must be [positions, rot_dim]")
+        rp = _here(rotary, "rotary", _f32, gpu)
+        _need(rotary.dim() == 2, "rotary must be [positions, rot_dim]")
         n_rot, rot_dim = rotary.shape
-    _check("da_paged_append", _lib.da_paged_append(
-        ctypes.byref(p), kp, vp, ks, vs, qp, qs, h_q, qo, rp, n_rot, rot_dim,
-        int(bool(interleaved)), _stream(stream)))
+    status = _lib.da_paged_append(kv, k_new.data_ptr(), v_new.data_ptr(), ks, vs, qp, qs, h_q, qo,
+                                  rp, n_rot, rot_dim, 1 if interleaved else 0,
+                                  _paged_stream(stream, gpu))
+    if status:
+        _check("da_paged_append", status)
     return q_out
 
 
@@ -522,15 +558,15 @@ def paged_gather(K, V, pages, past, k_out, v_out, row_start=None, T: int = 0, st
     """The rows at positions past[b] + r into k_out and v_out [rows,h_kv,d] (zeros
     where there is no page): the places that paged_append with the same
     ``past``, ``row_start`` and ``T`` writes."""
-    if not isinstance(k_out, torch.Tensor) or k_out.dim() != 3:
-        raise ValueError("k_out must be [rows,h_kv,d]")
-    rows, h_kv, d = k_out.shape
-    p = _paged(K, V, pages, past, rows, d, k_out.dtype, row_start, T)
-    if h_kv != p.h_kv or v_out.shape != k_out.shape:
+    rows, heads, d = _rows(k_out, "k_out")
+    dtype = k_out.dtype
+    kv, gpu, h_kv, T = _paged(K, V, pages, past, rows, d, dtype, row_start, T)
+    if heads != h_kv or _rows(v_out, "v_out") != k_out.shape:
         raise ValueError("k_out and v_out must be [rows,h_kv,d]")
-    _check("da_paged_gather", _lib.da_paged_gather(
-        ctypes.byref(p), _here(k_out, "k_out", k_out.dtype), _here(v_out, "v_out", k_out.dtype),
-        _stream(stream)))
+    status = _lib.da_paged_gather(kv, _here(k_out, "k_out", dtype, gpu),
+                                  _here(v_out, "v_out", dtype, gpu), _paged_stream(stream, gpu))
+    if status:
+        _check("da_paged_gather", status)
     return k_out, v_out
 
 
@@ -555,20 +591,22 @@ def paged_attn(q, K, V, pages, past, scale: float, causal: bool = True, row_star
     """out[n,h,:] = softmax(scale * q[n,h].K) V over the sequence's positions up to
     the row's own, past[b] + r (causal; append first), or over all past[b] of
     them.  q [rows,h_q,d], any stride between tokens."""
-    if not isinstance(q, torch.Tensor) or q.dim() != 3:
-        raise ValueError("q must be [rows,h_q,d]")
-    rows, h_q, d = q.shape
+    shape = _rows(q, "q")
+    rows, h_q, d = shape
     dtype = q.dtype
-    p = _paged(K, V, pages, past, rows, d, dtype, row_start, T)
+    kv, gpu, _, T = _paged(K, V, pages, past, rows, d, dtype, row_start, T)
+    if q.get_device() != gpu:
+        _refuse(q, "q", dtype, gpu)
     if out is None:
-        out = torch.empty((rows, h_q, d), dtype=dtype, device=q.device)
-    elif out.shape != q.shape:
-        raise ValueError("out must have q's shape")
+        out = torch.empty(shape, dtype=dtype, device=q.device)
+    op = _here(out, "out", dtype, gpu)
+    _need(out.shape == shape, "out must have q's shape")
     if workspace is None:
-        workspace = paged_workspace(q, K, pages, p.T)
-    qp, qs = _tokens(q, "q", dtype)
-    wp, wn = _ws(workspace)
-    _check("da_paged_attn", _lib.da_paged_attn(
-        ctypes.byref(p), qp, qs, h_q, float(scale), int(bool(causal)), _here(out, "out", dtype),
-        wp, wn, _stream(stream)))
+        workspace = paged_workspace(q, K, pages, T)
+    status = _lib.da_paged_attn(
+        kv, q.data_ptr(), h_q * d if q.is_contiguous() else _stride(q, "q", shape), h_q, scale,
+        1 if causal else 0, op, _here(workspace, "workspace", _u8, gpu), workspace.numel(),
+        _paged_stream(stream, gpu))
+    if status:
+        _check("da_paged_attn", status)
     return out

@@ -25,6 +25,7 @@
 #include <atomic>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "decode_attn.h"
 
@@ -58,6 +59,14 @@ struct Batch {
   const int32_t* row_start;
   int B, h_kv, n_pages, page_log2, max_pages, rows, T;
 };
+
+// A word of an array that no kernel here writes, at an address that is the same
+// for the whole wave: through the scalar cache, so that waiting for it does not
+// wait for the vector loads under way.
+__device__ __forceinline__ int fixed(const int32_t* p) {
+  typedef const int32_t __attribute__((address_space(4))) * constant_ptr;
+  return *(constant_ptr)p;
+}
 
 __device__ __forceinline__ int capacity(const Batch& bt) { return bt.max_pages << bt.page_log2; }
 
@@ -352,9 +361,8 @@ __global__ __launch_bounds__(kThreads) void paged_gather_kernel(Batch bt, void* 
 // row x of a KV head's rows is (token x / G, query head x % G of the group), so
 // a tile's rows see nearly the same keys.  An item's keys are cut into tiles of
 // KT = 4*TK, and all items' tiles, laid end to end (sequences, heads, row
-// tiles), are divided evenly over the resident workgroups: of W tiles, workgroup
-// w of NW (at most W) takes floor(w W / NW) .. floor((w+1) W / NW) - 1, which it
-// counts itself from past and row_start.  A workgroup begins and ends inside at most
+// tiles), are divided evenly over the resident workgroups, which count for
+// themselves, from past and row_start, where each one's share begins.  A workgroup begins and ends inside at most
 // one item each; those parts go to its two slots of the workspace, the rest
 // straight to out.  The parts of an item are then those of consecutive
 // workgroups, and the merge finds them from the same counts: no atomics, and
@@ -436,6 +444,16 @@ __device__ __forceinline__ bool not_finite(uint32_t w) {
     return (w & 0x7c000000u) == 0x7c000000u || (w & 0x7c00u) == 0x7c00u;
 }
 
+// w with its values that are not finite zeroed.
+template <class T>
+__device__ __forceinline__ uint32_t finite_part(uint32_t w) {
+  if constexpr (is_f32<T>) return not_finite<T>(w) ? 0u : w;
+  constexpr uint32_t e = std::is_same<T, __bf16>::value ? 0x7f80u : 0x7c00u;
+  if ((w & e) == e) w &= 0xffff0000u;
+  if ((w & e << 16) == e << 16) w &= 0xffffu;
+  return w;
+}
+
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 struct AttnArgs {
@@ -444,7 +462,6 @@ struct AttnArgs {
   int64_t q_stride;
   float scale;          // times log2(e)
   int h_q, G, causal;
-  int64_t* offsets;     // [B + 1]: tiles before each sequence
   float* parts;         // [2 * grid][R][D], then [2 * grid][R][2]
   int grid;             // workgroups of the attention kernel
 };
@@ -458,27 +475,152 @@ __device__ __forceinline__ int seen_by(const Batch& bt, const AttnArgs& a, int p
 }
 
 // Row tiles of a sequence (each of R rows), tiles of keys of one of them, and
-// of all of them (for one KV head).
+// of row tiles lo, lo + step, ... below hi.
 template <int R>
 __device__ __forceinline__ int row_tiles(const AttnArgs& a, int n) {
-  return (int)(((int64_t)n * a.G + R - 1) / R);
+  return (n * a.G + R - 1) / R;
 }
 template <int R, int KT>
 __device__ __forceinline__ int key_tiles(const Batch& bt, const AttnArgs& a, int past, int n,
                                          int rt) {
-  const int64_t last = min((int64_t)n * a.G, (int64_t)(rt + 1) * R) - 1;
-  const int seen = seen_by(bt, a, past, (int)(last / a.G));
-  return (seen + KT - 1) / KT;
+  // (the last row of most tiles is a token's last: no division)
+  const int last = min(n * a.G, (rt + 1) * R) - 1;
+  return (seen_by(bt, a, past, last == n * a.G - 1 ? n - 1 : last / a.G) + KT - 1) / KT;
+}
+template <int R, int KT>
+__device__ __forceinline__ int64_t sum_tiles(const Batch& bt, const AttnArgs& a, int past, int n,
+                                             int lo, int hi, int step) {
+  int64_t sum = 0;
+  for (int rt = lo; rt < hi; rt += step) sum += key_tiles<R, KT>(bt, a, past, n, rt);
+  return sum;
 }
 template <int R, int KT>
 __device__ __forceinline__ int64_t head_tiles(const Batch& bt, const AttnArgs& a, int past, int n) {
   const int nr = row_tiles<R>(a, n);
-  if (nr == 0) return 0;
+  if (nr <= 1) return nr ? key_tiles<R, KT>(bt, a, past, n, 0) : 0;
   if (!a.causal) return (int64_t)nr * key_tiles<R, KT>(bt, a, past, n, 0);
-  int64_t sum = 0;
-  for (int rt = 0; rt < nr; ++rt) sum += key_tiles<R, KT>(bt, a, past, n, rt);
-  return sum;
+  return sum_tiles<R, KT>(bt, a, past, n, 0, nr, 1);
 }
+
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  if ((a | b) >> 32) return a / b;
+  return (int64_t)((uint32_t)a / (uint32_t)b);
+}
+__device__ __forceinline__ int64_t lane_value(int64_t x, int lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)x, lane);
+  const int hi = __builtin_amdgcn_readlane((int)(x >> 32), lane);
+  return (int64_t)hi << 32 | lo;
+}
+
+// The division of all items' tiles over the workgroups, counted by each wave
+// for itself: a lane counts a run of sequences.
+template <int R, int KT>
+struct Division {
+  int run;                    // sequences of a lane
+  int64_t before, upto;       // tiles before the lane's run and up to its end
+  int64_t total, each;        // all tiles; workgroup w takes each, the first
+  int share, more;            //   `more` ones one more; share of them have work
+
+  __device__ __forceinline__ static int64_t tiles_of(const Batch& bt, const AttnArgs& a, int b) {
+    return bt.h_kv * head_tiles<R, KT>(bt, a, bt.past[b], seq_rows(bt, b).n);
+  }
+  __device__ __forceinline__ void count(const Batch& bt, const AttnArgs& a, int lane) {
+    run = (bt.B + 63) / 64;
+    const int lo = min(lane * run, bt.B), hi = min(lo + run, bt.B);
+    int64_t mine = 0;
+    for (int b = lo; b < hi; ++b) mine += tiles_of(bt, a, b);
+    upto = mine;
+#pragma unroll
+    for (int step = 1; step < 64; step <<= 1) {
+      const int64_t other = __shfl_up(upto, step);
+      if (lane >= step) upto += other;
+    }
+    before = upto - mine;
+    total = lane_value(upto, 63);
+    share = (int)min(total, (int64_t)a.grid);
+    each = share ? quotient(total, share) : 0;
+    more = (int)(total - each * share);
+  }
+  __device__ __forceinline__ int64_t begin_of(int w) const { return w * each + min(w, more); }
+  // The workgroup that takes tile x.
+  __device__ __forceinline__ int owner(int64_t x) const {
+    const int64_t big = more * (each + 1);
+    return (int)(x < big ? quotient(x, each + 1) : more + quotient(x - big, each));
+  }
+  // Tiles before sequence b.
+  __device__ __forceinline__ int64_t before_seq(const Batch& bt, const AttnArgs& a, int b) const {
+    const int at = b / run;
+    int64_t n = lane_value(before, at);
+    for (int x = at * run; x < b; ++x) n += tiles_of(bt, a, x);
+    return n;
+  }
+};
+
+// The parts of items that a workgroup takes, one after the other.
+template <int R, int KT>
+struct Walk {
+  int b, head, rt;            // the item: sequence, KV head, row tile
+  int tiles, t0, t1;          // its key tiles; those taken are t0 .. t1-1
+  int past;
+  SeqRows sr;
+  int64_t left;               // tiles to take, from t0 on
+
+  __device__ __forceinline__ void cut() { t1 = (int)min((int64_t)tiles, t0 + left); }
+  __device__ __forceinline__ bool begin(const Batch& bt, const AttnArgs& a, int lane) {
+    Division<R, KT> d;
+    d.count(bt, a, lane);
+    const int w = blockIdx.x;
+    if (w >= d.share) return false;
+    const int64_t lo = d.begin_of(w);
+    left = d.each + (w < d.more ? 1 : 0);
+    const int at = __ffsll((unsigned long long)__ballot(d.upto > lo)) - 1;
+    int64_t rem = lo - lane_value(d.before, at);
+    b = at * d.run;
+    sr = seq_rows(bt, b);
+    past = fixed(bt.past + b);
+    int64_t per_head = head_tiles<R, KT>(bt, a, past, sr.n);
+    while (rem >= bt.h_kv * per_head) {          // (ends: d.upto > lo)
+      rem -= bt.h_kv * per_head;
+      sr = seq_rows(bt, ++b);
+      past = fixed(bt.past + b);
+      per_head = head_tiles<R, KT>(bt, a, past, sr.n);
+    }
+    head = (int)quotient(rem, per_head);
+    rem -= head * per_head;
+    rt = 0;
+    tiles = key_tiles<R, KT>(bt, a, past, sr.n, 0);
+    while (rem >= tiles) {
+      rem -= tiles;
+      tiles = key_tiles<R, KT>(bt, a, past, sr.n, ++rt);
+    }
+    t0 = (int)rem;
+    cut();
+    return true;
+  }
+  __device__ __forceinline__ bool next(const Batch& bt, const AttnArgs& a) {
+    left -= t1 - t0;
+    if (left <= 0) return false;
+    t0 = 0;
+    tiles = 0;
+    while (tiles == 0) {
+      if (++rt >= row_tiles<R>(a, sr.n)) {
+        rt = 0;
+        if (++head >= bt.h_kv) {
+          head = 0;
+          sr = seq_rows(bt, ++b);
+          past = fixed(bt.past + b);
+          if (sr.n == 0) {                       // (a later sequence has tiles: left > 0)
+            head = bt.h_kv - 1;
+            continue;
+          }
+        }
+      }
+      tiles = key_tiles<R, KT>(bt, a, past, sr.n, rt);
+    }
+    cut();
+    return true;
+  }
+};
 
 template <class T, bool MX, int D, int NB>
 __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs a) {
@@ -491,72 +633,13 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
 
   __shared__ float s_acc[kWaves][16][kLdsRow];
   __shared__ float s_ref[kWaves][16], s_sum[kWaves][16];
-  __shared__ int64_t s_scan[kWaves], s_first;
-  __shared__ int s_seq;
 
   const int tid = threadIdx.x;
   const int lane = tid & 63, wave = uniform(tid >> 6);
   const int i = lane & 15, k = lane >> 4;
 
-  // --- the schedule: a prefix over the sequences, a run of them per thread ---
-  const int per = (bt.B + kThreads - 1) / kThreads;
-  const int b_lo = min(tid * per, bt.B), b_hi = min(b_lo + per, bt.B);
-  int64_t mine = 0;
-  for (int b = b_lo; b < b_hi; ++b)
-    mine += bt.h_kv * head_tiles<R, KT>(bt, a, bt.past[b], seq_rows(bt, b).n);
-  int64_t scan = mine;
-#pragma unroll
-  for (int step = 1; step < 64; step <<= 1) {
-    const int64_t other = __shfl_up(scan, step);
-    if (lane >= step) scan += other;
-  }
-  if (lane == 63) s_scan[wave] = scan;
-  __syncthreads();
-  int64_t total = 0;
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) scan += s_scan[w];
-    total += s_scan[w];
-  }
-  const int64_t before = scan - mine;
-  if (blockIdx.x == 0) {
-    int64_t at = before;
-    for (int b = b_lo; b < b_hi; ++b) {
-      a.offsets[b] = at;
-      at += bt.h_kv * head_tiles<R, KT>(bt, a, bt.past[b], seq_rows(bt, b).n);
-    }
-    if (tid == 0) a.offsets[bt.B] = total;
-  }
-  const int64_t share = min(total, (int64_t)a.grid);      // workgroups that have work
-  if (blockIdx.x >= share) return;
-  const int64_t lo = total * blockIdx.x / share, hi = total * (blockIdx.x + 1) / share;
-  if (before <= lo && lo < scan) {
-    int64_t at = before;
-    int b = b_lo;
-    for (; b < b_hi - 1; ++b) {
-      const int64_t n = bt.h_kv * head_tiles<R, KT>(bt, a, bt.past[b], seq_rows(bt, b).n);
-      if (lo < at + n) break;
-      at += n;
-    }
-    s_seq = b;
-    s_first = at;
-  }
-  __syncthreads();
-
-  int b = uniform(s_seq);
-  int64_t cur = lo;
-  SeqRows sr = seq_rows(bt, b);
-  int past = bt.past[b];
-  int64_t rem = lo - s_first;
-  int64_t per_head = head_tiles<R, KT>(bt, a, past, sr.n);
-  int head = (int)(rem / per_head);
-  rem -= head * per_head;
-  int rt = 0;
-  int tiles = key_tiles<R, KT>(bt, a, past, sr.n, 0);
-  while (rem >= tiles) {
-    rem -= tiles;
-    tiles = key_tiles<R, KT>(bt, a, past, sr.n, ++rt);
-  }
-  int t0 = (int)rem;
+  Walk<R, KT> at;
+  if (!at.begin(bt, a, lane)) return;
 
   const int64_t blk = block_bytes<T, MX, D>(bt.page_log2);
   const int page_mask = (1 << bt.page_log2) - 1;
@@ -566,14 +649,14 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
   const int k_key = TK == 32 ? 8 * ((i >> 2) & 1) + (i & 3) : i;
   const int v_key = TK == 32 ? 8 * (k & 1) : 4 * k;
 
-  while (true) {
-    const int t1 = (int)min((int64_t)tiles, t0 + (hi - cur));
+  do {
     // --- one part of one item: key tiles t0 .. t1-1 ---
-    const int64_t n_rows = (int64_t)sr.n * a.G;
-    const int64_t row0 = (int64_t)rt * R;
-    const int in_tile = (int)min(n_rows - row0, (int64_t)R);
-    const int min_seen = seen_by(bt, a, past, (int)(row0 / a.G));
-    const int max_seen = seen_by(bt, a, past, (int)((row0 + in_tile - 1) / a.G));
+    const int b = at.b, head = at.head, past = at.past, t0 = at.t0, t1 = at.t1;
+    const SeqRows sr = at.sr;
+    const int row0 = at.rt * R;
+    const int in_tile = min(sr.n * a.G - row0, R);
+    const int min_seen = seen_by(bt, a, past, row0 / a.G);
+    const int max_seen = seen_by(bt, a, past, (row0 + in_tile - 1) / a.G);
     const int32_t* table = bt.pages + (int64_t)b * bt.max_pages;
 
     // q: lane (i, k) holds row i's share of the score products' summed index.
@@ -586,7 +669,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
 #pragma unroll
       for (int w = 0; w < L::QW; ++w) q[nb][w] = 0u;
       if (x < in_tile) {
-        const int t = (int)((row0 + x) / a.G), g = (int)((row0 + x) % a.G);
+        const int t = (row0 + x) / a.G, g = (row0 + x) - t * a.G;
         seen[nb] = seen_by(bt, a, past, t);
         const T* src = static_cast<const T*>(a.q) + (int64_t)(sr.start + t) * a.q_stride +
                        (int64_t)(head * a.G + g) * D;
@@ -615,12 +698,15 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
     uint32_t kw[NH][L::KW], vw[KPL][L::VW];
     uint32_t ks[NH], vs[NP][2];
     bool there_a = false, there_b = false;
+    bool spoilt = false;        // V rows that only some rows see held infinities or NaN
 
-    // Page of positions p .. p+15 of the sequence: -1 past the table's end.
-    auto page_at = [&](int p) -> int {
-      const int at = p >> bt.page_log2;
-      const int id = at < bt.max_pages ? table[at] : -1;
-      return uniform((unsigned)id < (unsigned)bt.n_pages ? id : -1);
+    // The table's entry for positions p .. p+15 of the sequence, and the page
+    // that it names: -1 if none, or past the table's end.
+    auto entry_of = [&](int p) -> int {
+      return fixed(table + min(p >> bt.page_log2, bt.max_pages - 1));
+    };
+    auto page_of = [&](int p, int id) -> int {
+      return (p >> bt.page_log2) < bt.max_pages && (unsigned)id < (unsigned)bt.n_pages ? id : -1;
     };
     auto base_of = [&](int page, int slot, const char* pool) -> const char* {
       return pool + ((int64_t)max(page, 0) * bt.h_kv + head) * blk + slot * RB;
@@ -750,26 +836,39 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
       }
     };
 
-    // Wave w takes 16-key-aligned wave tiles w, w + 4, ...
+    // Wave w takes wave tiles w, w + 4, ...  A tile's K is loaded as soon as the
+    // last one's is used up, its V likewise, and its entries of the page table
+    // a tile before that.  The last tile loads itself once more (from the cache):
+    // with a branch around the loads, the products would wait for all of them.
     const int wt_end = min(t1 * kWaves, (max_seen + TK - 1) / TK);
     int wt = t0 * kWaves + wave;
-    int pa = -1, pb = -1;
+    int next = wt * TK, next_a = 0, next_b = 0;    // the next tile and its entries
+    auto advance = [&](int tile) {
+      next = tile * TK;
+      next_a = entry_of(next);
+      next_b = TK == 32 ? entry_of(next + 16) : next_a;
+    };
     if (wt < wt_end) {
-      pa = page_at(wt * TK);
-      pb = TK == 32 ? page_at(wt * TK + 16) : pa;
-      load_k(wt * TK, pa, pb);
-      load_v(wt * TK, pa, pb);
+      const int pa = page_of(next, entry_of(next));
+      const int pb = TK == 32 ? page_of(next + 16, entry_of(next + 16)) : pa;
+      // K before V, here as in the loop: the wait for K is a count of the loads
+      // behind it, and the compiler takes the smaller of the two places'.
+      load_k(next, pa, pb);
+      asm volatile("" ::: "memory");
+      load_v(next, pa, pb);
       there_a = pa >= 0, there_b = pb >= 0;
+      advance(wt + kWaves < wt_end ? wt + kWaves : wt);
     }
+    // (q is waited for here, not by its uses in the loop)
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int w = 0; w < L::QW; ++w) asm volatile("" : "+v"(q[nb][w]));
     for (; wt < wt_end; wt += kWaves) {
       const int key0 = wt * TK;
-      const int next = key0 + KT;
-      const bool more = wt + kWaves < wt_end;
-      int na = -1, nb_ = -1;
-      if (more) {
-        na = page_at(next);
-        nb_ = TK == 32 ? page_at(next + 16) : na;
-      }
+      const int now = next, na = page_of(now, next_a);
+      const int nb_ = TK == 32 ? page_of(now + 16, next_b) : na;
+      advance(wt + 2 * kWaves < wt_end ? wt + 2 * kWaves : wt);
       // --- scores ---
       f32x4 s[NB][NH];
 #pragma unroll
@@ -824,11 +923,10 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
           }
         }
       }
-      if (more) load_k(next, na, nb_);
+      load_k(now, na, nb_);
 
       // --- masks: only where a row does not see every key of the tile ---
       const bool edge = key0 + TK > min_seen || !there_a || !there_b;
-      bool spoilt = false;      // V rows that some rows must not see, not finite
       const bool here = v_half ? there_b : there_a;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
@@ -857,22 +955,30 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
                 vs[p][j / 4] |= 127u << (8 * (j % 4));
               }
           }
-        // ... and those that only some rows see are added one by one if a
-        // weight of 0 would not take them out (0 * infinity).
-        if (min_seen < max_seen) {
+        // ... and where only some rows see a tile's keys, infinities and NaN,
+        // which a weight of 0 does not take out (0 * infinity), are zeroed here
+        // and added at the end to the rows that see them.
+        if (min_seen < max_seen && key0 + TK > min_seen) {
           bool bad = false;
-          if constexpr (MX) {
 #pragma unroll
-            for (int p = 0; p < NP; ++p)
+          for (int j = 0; j < KPL; ++j) {
+            if constexpr (MX) {
 #pragma unroll
-              for (int j = 0; j < KPL; ++j) bad |= (vs[p][j / 4] >> (8 * (j % 4)) & 255u) == 255u;
-          } else {
+              for (int p = 0; p < NP; ++p)
+                if ((vs[p][j / 4] >> (8 * (j % 4)) & 255u) == 255u) {
+                  bad = true;
+                  vw[j][p] = 0u;
+                  vs[p][j / 4] &= ~(128u << (8 * (j % 4)));
+                }
+            } else {
 #pragma unroll
-            for (int j = 0; j < KPL; ++j)
-#pragma unroll
-              for (int w = 0; w < L::VW; ++w) bad |= not_finite<T>(vw[j][w]);
+              for (int w = 0; w < L::VW; ++w) {
+                bad |= not_finite<T>(vw[j][w]);
+                vw[j][w] = finite_part<T>(vw[j][w]);
+              }
+            }
           }
-          spoilt = __any(bad);
+          spoilt |= bad;
         }
       }
 
@@ -922,26 +1028,12 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
           for (int j = 0; j < KPL; ++j) {
             float x[VCH];
             v_floats(p, j, x);
-            if (!spoilt) {
 #pragma unroll
-              for (int c = 0; c < VCH; ++c)
+            for (int c = 0; c < VCH; ++c)
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
-                  acc[nb][VCH * p + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                      x[c], s[nb][j / 4][j % 4], acc[nb][VCH * p + c], 0, 0, 0);
-            } else {
-              for (int g = 0; g < 4; ++g) {      // key KPL*g + j alone
-                const int key = key0 + KPL * g + j;
-#pragma unroll
-                for (int c = 0; c < VCH; ++c)
-#pragma unroll
-                  for (int nb = 0; nb < NB; ++nb) {
-                    const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                        k == g ? x[c] : 0.f, s[nb][j / 4][j % 4], acc[nb][VCH * p + c], 0, 0, 0);
-                    if (key < seen[nb]) acc[nb][VCH * p + c] = y;
-                  }
-              }
-            }
+              for (int nb = 0; nb < NB; ++nb)
+                acc[nb][VCH * p + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                    x[c], s[nb][j / 4][j % 4], acc[nb][VCH * p + c], 0, 0, 0);
           }
       } else {
         using V8 = typename Vec8<T>::type;
@@ -960,49 +1052,31 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
         for (int p = 0; p < NP; ++p) {
           uint32_t x[KPL][VCH / 2];
           v_words(p, x);
-          if (!spoilt) {
 #pragma unroll
-            for (int c = 0; c < VCH; ++c) {
-              const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
-              const u32x4 col = {__builtin_amdgcn_perm(x[1][c / 2], x[0][c / 2], sel),
-                                 __builtin_amdgcn_perm(x[3][c / 2], x[2][c / 2], sel),
-                                 __builtin_amdgcn_perm(x[5][c / 2], x[4][c / 2], sel),
-                                 __builtin_amdgcn_perm(x[7][c / 2], x[6][c / 2], sel)};
+          for (int c = 0; c < VCH; ++c) {
+            const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
+            const u32x4 col = {__builtin_amdgcn_perm(x[1][c / 2], x[0][c / 2], sel),
+                               __builtin_amdgcn_perm(x[3][c / 2], x[2][c / 2], sel),
+                               __builtin_amdgcn_perm(x[5][c / 2], x[4][c / 2], sel),
+                               __builtin_amdgcn_perm(x[7][c / 2], x[6][c / 2], sel)};
 #pragma unroll
-              for (int nb = 0; nb < NB; ++nb)
-                acc[nb][VCH * p + c] = mma16(__builtin_bit_cast(V8, col), weights[nb],
-                                             acc[nb][VCH * p + c]);
-            }
-          } else {
-            for (int key = 0; key < TK; ++key) {  // each key alone
-              const bool my_k = k == key / KPL;
-              const int j = key % KPL;
-#pragma unroll
-              for (int c = 0; c < VCH; ++c) {
-                const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
-                u32x4 col;
-#pragma unroll
-                for (int y = 0; y < 4; ++y)
-                  col[y] = __builtin_amdgcn_perm(my_k && j == 2 * y + 1 ? x[2 * y + 1][c / 2] : 0u,
-                                                 my_k && j == 2 * y ? x[2 * y][c / 2] : 0u, sel);
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                  const f32x4 y = mma16(__builtin_bit_cast(V8, col), weights[nb],
-                                        acc[nb][VCH * p + c]);
-                  if (key0 + key < seen[nb]) acc[nb][VCH * p + c] = y;
-                }
-              }
-            }
+            for (int nb = 0; nb < NB; ++nb)
+              acc[nb][VCH * p + c] =
+                  mma16(__builtin_bit_cast(V8, col), weights[nb], acc[nb][VCH * p + c]);
           }
         }
       }
-      if (more) load_v(next, na, nb_);
+      load_v(now, na, nb_);
       there_a = na >= 0, there_b = nb_ >= 0;
     }
 
     // --- the four waves' states, one column block at a time ---
-    const bool whole = t0 == 0 && t1 == tiles;
+    const bool whole = t0 == 0 && t1 == at.tiles;
     const int64_t slot = 2 * (int64_t)blockIdx.x + (t0 == 0 ? 1 : 0);
+    // (0, 0) unless values were zeroed above: the keys that they may be of
+    const bool fix = __syncthreads_or(spoilt);
+    const int fix_lo = fix ? max(min_seen / TK * TK, t0 * KT) : 0;
+    const int fix_hi = fix ? min(max_seen, t1 * KT) : 0;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       float sum = sums[nb][0];
@@ -1048,9 +1122,25 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
           l += rw == -INFINITY ? 0.f : s_sum[w][x] * exp2f(rw - m);
           o += *reinterpret_cast<const f32x4*>(&s_acc[w][x][dim]);
         }
+        const int t = (row0 + in) / a.G, g = (row0 + in) - t * a.G;
+        const int fix_end = fix ? min(fix_hi, seen_by(bt, a, past, t)) : 0;
+        for (int key = fix_lo; key < fix_end; ++key) {
+          const int page = table[key >> bt.page_log2];
+          if ((unsigned)page >= (unsigned)bt.n_pages) continue;
+          const int at = key & page_mask;
+          const char* block = bt.V + ((int64_t)page * bt.h_kv + head) * blk;
+          if constexpr (MX) {
+            if ((uint8_t)block[mx_scale_at<D>(true, bt.page_log2, at, dim / 32)] == 255u) o += NAN;
+          } else {
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const float v = (float)reinterpret_cast<const T*>(block)[(int64_t)at * D + dim + y];
+              if (!(fabsf(v) < INFINITY)) o[y] += v;
+            }
+          }
+        }
         if (whole) {
           o = l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o / l;
-          const int t = (int)((row0 + in) / a.G), g = (int)((row0 + in) % a.G);
           T* dst = static_cast<T*>(a.out) +
                    ((int64_t)(sr.start + t) * a.h_q + head * a.G + g) * D + dim;
           if constexpr (is_f32<T>)
@@ -1066,27 +1156,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
       }
     }
 
-    // --- the next item ---
-    cur += t1 - t0;
-    if (cur >= hi) break;
-    t0 = 0;
-    tiles = 0;
-    while (tiles == 0) {
-      if (++rt >= row_tiles<R>(a, sr.n)) {
-        rt = 0;
-        if (++head >= bt.h_kv) {
-          head = 0;
-          sr = seq_rows(bt, ++b);
-          past = bt.past[b];
-          if (sr.n == 0) {                        // (a later sequence has tiles: cur < hi)
-            head = bt.h_kv - 1;
-            continue;
-          }
-        }
-      }
-      tiles = key_tiles<R, KT>(bt, a, past, sr.n, rt);
-    }
-  }
+  } while (at.next(bt, a));
 }
 
 // Combines the parts of an item's rows: blockIdx.x names the item (sequence, KV
@@ -1103,21 +1173,25 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(Batch bt, AttnArg
   const int head = bh % bt.h_kv, b = bh / bt.h_kv;
   const SeqRows sr = seq_rows(bt, b);
   if (rt >= row_tiles<R>(a, sr.n)) return;
-  const int past = bt.past[b];
+  const int past = fixed(bt.past + b);
   const int count = key_tiles<R, KT>(bt, a, past, sr.n, rt);
-  const int64_t row0 = (int64_t)rt * R;
-  const int in_tile = (int)min((int64_t)sr.n * a.G - row0, (int64_t)R);
-  int64_t w0 = 0, w1 = -1;
+  const int row0 = rt * R;
+  const int in_tile = min(sr.n * a.G - row0, R);
+  int w0 = 0, w1 = -1;
   if (count > 0) {
-    const int64_t total = a.offsets[bt.B], first = a.offsets[b];
-    int64_t at = first + head * ((a.offsets[b + 1] - first) / bt.h_kv);
-    if (!a.causal)
+    Division<R, KT> d;
+    d.count(bt, a, lane);
+    int64_t at = d.before_seq(bt, a, b) + head * head_tiles<R, KT>(bt, a, past, sr.n);
+    if (!a.causal) {
       at += (int64_t)rt * count;
-    else
-      for (int x = 0; x < rt; ++x) at += key_tiles<R, KT>(bt, a, past, sr.n, x);
-    const int64_t share = min(total, (int64_t)a.grid);
-    w0 = ((at + 1) * share - 1) / total;
-    w1 = ((at + count) * share - 1) / total;
+    } else if (rt > 0) {
+      int64_t sum = sum_tiles<R, KT>(bt, a, past, sr.n, lane, rt, 64);
+#pragma unroll
+      for (int step = 32; step; step >>= 1) sum += __shfl_xor(sum, step);
+      at += lane_value(sum, 0);
+    }
+    w0 = d.owner(at);
+    w1 = d.owner(at + count - 1);
     if (w0 == w1) return;                          // one workgroup had it all
   }
   const float* ml = a.parts + (int64_t)2 * a.grid * R * D;
@@ -1125,7 +1199,7 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(Batch bt, AttnArg
     float m = -INFINITY, l = 0.f, o[kVec];
 #pragma unroll
     for (int e = 0; e < kVec; ++e) o[e] = 0.f;
-    for (int64_t w = w0 + wave; w <= w1; w += kWaves) {
+    for (int w = w0 + wave; w <= w1; w += kWaves) {
       const int64_t slot = 2 * w + (w == w0 ? 1 : 0);
       const f32x2 s = *reinterpret_cast<const f32x2*>(ml + (slot * R + in) * 2);
       const float* p = a.parts + (slot * R + in) * D + lane * kVec;
@@ -1157,7 +1231,7 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(Batch bt, AttnArg
         sum += s_l[w] * f;
         y += s_part[w][tid] * f;
       }
-      const int t = (int)((row0 + in) / a.G), g = (int)((row0 + in) % a.G);
+      const int t = (row0 + in) / a.G, g = (row0 + in) - t * a.G;
       static_cast<T*>(a.out)[((int64_t)(sr.start + t) * a.h_q + head * a.G + g) * D + tid] =
           (T)(sum == 0.f ? 0.f : y / sum);
     }
@@ -1169,7 +1243,6 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(Batch bt, AttnArg
 // ---------------------------------------------------------------------------
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-size_t pad256(size_t x) { return (x + 255) / 256 * 256; }
 bool dim_ok(int d) { return d == 64 || d == 128 || d == 256; }
 bool type_ok(int dtype) { return dtype >= DA_F32 && dtype <= DA_F16; }
 int type_bytes(int dtype) { return dtype == DA_F32 ? 4 : 2; }
@@ -1274,7 +1347,7 @@ constexpr int kGroupsPerCu = 2;       // workgroups of the attention kernel per 
 
 struct AttnPlan {
   int R;
-  size_t offsets_bytes, bytes;
+  size_t bytes;
 };
 
 da_status plan_attn(int B, int h_q, int h_kv, int d, int T, int dtype, AttnPlan* plan) {
@@ -1286,9 +1359,7 @@ da_status plan_attn(int B, int h_q, int h_kv, int d, int T, int dtype, AttnPlan*
   plan->R = tile_rows(per_head);
   // (the merge's grid is the items)
   if ((int64_t)B * h_kv * ceil_div(per_head, plan->R) > kMaxGroups) return DA_ERR_SHAPE;
-  plan->offsets_bytes = pad256(((size_t)B + 1) * sizeof(int64_t));
-  plan->bytes = plan->offsets_bytes +
-                (size_t)2 * kMaxCus * kGroupsPerCu * plan->R * ((size_t)d + 2) * sizeof(float);
+  plan->bytes = (size_t)2 * kMaxCus * kGroupsPerCu * plan->R * ((size_t)d + 2) * sizeof(float);
   return DA_OK;
 }
 
@@ -1403,8 +1474,7 @@ da_status da_paged_attn(const da_paged_kv* kv, const void* q, int64_t q_stride, 
                    h_q,
                    h_q / p.h_kv,
                    causal,
-                   static_cast<int64_t*>(workspace),
-                   reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.offsets_bytes),
+                   static_cast<float*>(workspace),
                    device_cus() * kGroupsPerCu};
   hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();

@@ -1,6 +1,5 @@
 """What the paged cache's entry points refuse, on the CPU: every call here fails
 its checks before anything is enqueued, so no pointer is read."""
-import ctypes
 import math
 
 import numpy as np
@@ -21,7 +20,9 @@ def batch(**kw):
     f = dict(K=FAKE, V=FAKE, pages=FAKE, past=FAKE, row_start=None, B=2, h_kv=2, d=64, n_pages=5,
              page_rows=16, max_pages=4, rows=6, T=3, dtype=1, format=0)
     f.update(kw)
-    return ctypes.byref(binding._PagedKV(**f))
+    for name in ("K", "V", "pages", "past", "row_start"):
+        f[name] = f[name] or 0
+    return binding._pack_kv(*f.values())
 
 
 def append(kv=None, k=FAKE, v=FAKE, ks=128, vs=128, q=FAKE, qs=512, h_q=8, q_out=FAKE, rotary=FAKE,
