@@ -9,6 +9,8 @@
 //   paged_attn_kernel     softmax(scale q.K) V over the pages of each (sequence,
 //                         KV head, tile of query rows), split evenly over a
 //                         resident grid, as partial states.
+//   paged_chunk_kernel    the same for many query rows per KV head, K and V
+//                         shared by four waves through LDS.
 //   paged_merge_kernel    combines the parts of each query row.
 //
 // Register layouts of the matrix instructions used below (lane = 0..63,
@@ -456,12 +458,22 @@ __device__ __forceinline__ uint32_t finite_part(uint32_t w) {
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
+// An item that ends in a workgroup but did not begin there: what the merge needs
+// to put its parts together.
+struct Closing {
+  int first;                  // the workgroup of its first part, or -1: none ends here
+  int head, row0, in_tile;    // its rows of the KV head
+  int start;                  // the sequence's first row
+  int unused[3];
+};
+
 struct AttnArgs {
   const void* q;
   void* out;
   int64_t q_stride;
   float scale;          // times log2(e)
   int h_q, G, causal;
+  Closing* closing;     // [grid]
   float* parts;         // [2 * grid][R][D], then [2 * grid][R][2]
   int grid;             // workgroups of the attention kernel
 };
@@ -520,6 +532,7 @@ struct Division {
   int64_t before, upto;       // tiles before the lane's run and up to its end
   int64_t total, each;        // all tiles; workgroup w takes each, the first
   int share, more;            //   `more` ones one more; share of them have work
+  bool blind;                 // a sequence of the lane's run sees nothing
 
   __device__ __forceinline__ static int64_t tiles_of(const Batch& bt, const AttnArgs& a, int b) {
     return bt.h_kv * head_tiles<R, KT>(bt, a, bt.past[b], seq_rows(bt, b).n);
@@ -528,7 +541,12 @@ struct Division {
     run = (bt.B + 63) / 64;
     const int lo = min(lane * run, bt.B), hi = min(lo + run, bt.B);
     int64_t mine = 0;
-    for (int b = lo; b < hi; ++b) mine += tiles_of(bt, a, b);
+    blind = false;
+    for (int b = lo; b < hi; ++b) {
+      const int64_t n = tiles_of(bt, a, b);
+      blind |= n == 0;
+      mine += n;
+    }
     upto = mine;
 #pragma unroll
     for (int step = 1; step < 64; step <<= 1) {
@@ -547,13 +565,6 @@ struct Division {
     const int64_t big = more * (each + 1);
     return (int)(x < big ? quotient(x, each + 1) : more + quotient(x - big, each));
   }
-  // Tiles before sequence b.
-  __device__ __forceinline__ int64_t before_seq(const Batch& bt, const AttnArgs& a, int b) const {
-    const int at = b / run;
-    int64_t n = lane_value(before, at);
-    for (int x = at * run; x < b; ++x) n += tiles_of(bt, a, x);
-    return n;
-  }
 };
 
 // The parts of items that a workgroup takes, one after the other.
@@ -566,11 +577,29 @@ struct Walk {
   int64_t left;               // tiles to take, from t0 on
 
   __device__ __forceinline__ void cut() { t1 = (int)min((int64_t)tiles, t0 + left); }
-  __device__ __forceinline__ bool begin(const Batch& bt, const AttnArgs& a, int lane) {
+  // Whether the workgroup has work.  Rows of sequences that see nothing, which
+  // are in no item, are zeroed here.
+  template <class T>
+  __device__ __forceinline__ bool begin(const Batch& bt, const AttnArgs& a, int lane, int d_head) {
     Division<R, KT> d;
     d.count(bt, a, lane);
     const int w = blockIdx.x;
-    if (w >= d.share) return false;
+    uint64_t blind = __ballot(d.blind);
+    while (blind) {
+      const int first = (__ffsll((unsigned long long)blind) - 1) * d.run;
+      blind &= blind - 1;
+      for (int x = first; x < min(first + d.run, bt.B); ++x) {
+        if (x % a.grid != w || Division<R, KT>::tiles_of(bt, a, x)) continue;
+        const SeqRows zr = seq_rows(bt, x);
+        T* dst = static_cast<T*>(a.out) + (int64_t)zr.start * a.h_q * d_head;
+        for (int64_t e = threadIdx.x; e < (int64_t)zr.n * a.h_q * d_head; e += kThreads)
+          dst[e] = (T)0.f;
+      }
+    }
+    if (w >= d.share) {
+      if (threadIdx.x == 0) a.closing[w].first = -1;
+      return false;
+    }
     const int64_t lo = d.begin_of(w);
     left = d.each + (w < d.more ? 1 : 0);
     const int at = __ffsll((unsigned long long)__ballot(d.upto > lo)) - 1;
@@ -595,6 +624,11 @@ struct Walk {
     }
     t0 = (int)rem;
     cut();
+    if (threadIdx.x == 0) {
+      const int row0 = rt * R;
+      a.closing[w] = {t0 > 0 && t1 == tiles ? d.owner(lo - t0) : -1, head, row0,
+                      min(sr.n * a.G - row0, R), sr.start, {0, 0, 0}};
+    }
     return true;
   }
   __device__ __forceinline__ bool next(const Batch& bt, const AttnArgs& a) {
@@ -639,7 +673,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
   const int i = lane & 15, k = lane >> 4;
 
   Walk<R, KT> at;
-  if (!at.begin(bt, a, lane)) return;
+  if (!at.template begin<T>(bt, a, lane, D)) return;
 
   const int64_t blk = block_bytes<T, MX, D>(bt.page_log2);
   const int page_mask = (1 << bt.page_log2) - 1;
@@ -1159,61 +1193,453 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
   } while (at.next(bt, a));
 }
 
-// Combines the parts of an item's rows: blockIdx.x names the item (sequence, KV
-// head, row tile), the rows are shared out over blockIdx.y; four waves share a
-// row's parts.  Rows that see nothing are written here.
-template <class T, int D, int R, int KT>
-__global__ __launch_bounds__(kThreads) void paged_merge_kernel(Batch bt, AttnArgs a,
-                                                               int max_row_tiles) {
-  constexpr int kVec = D / 64;
-  __shared__ float s_part[kWaves][D], s_m[kWaves], s_l[kWaves];
+// ---------------------------------------------------------------------------
+// Attention of many query rows (chunks of prompts), 16-bit products.
+//
+// Where a KV head has more than 32 query rows the matrix cores are the bound,
+// and what counts is how often a K or V value is fetched for a product.  Four
+// waves share an item's key tiles of KT keys in LDS and take 32 query rows each:
+//   S^T [KT x 32 rows] = K . Q^T,   O^T [D x 32 rows] += V^T . P^T
+// on 32 x 32 x 16 products (layouts: lane = 0..63, i = lane % 32, k = lane / 32,
+// A[i][8k..], B[8k..][i], and the result's component r is row
+// 8*(r/4) + 4k + r%4 of column i).  As in the kernel above, the keys that the
+// score product's rows stand for are chosen so that a lane ends up with the
+// scores of the keys whose weights the second product wants from it:
+// component r of score block s is key 32 s + 16 (r/8) + 8 k + r%8.
+//
+// Two waves bring in K, two V (turned on the way: V lies in LDS by dimensions,
+// eight keys side by side); the next tile's loads are in flight during a tile's
+// products, and the tiles alternate between two buffers: one barrier each.
+// Chunks of 16 bytes are stored at their index XOR a function of the row, so
+// that the eight lanes of every 128-byte LDS access hit different banks.
+// A key tile of 16-bit values is 32 KB: two workgroups fit a CU, and one's
+// softmax overlaps the other's products.
+// ---------------------------------------------------------------------------
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ f32x16 mma32(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma32(f16x8 a, f16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+template <int D>
+struct ChunkTile {
+  static constexpr int KT = D == 256 ? 32 : 64;   // keys
+  static constexpr int R = 32 * kWaves;           // query rows
+};
+
+template <class T, bool MX, int D>
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel(Batch bt, AttnArgs a) {
+  constexpr int KT = ChunkTile<D>::KT, R = ChunkTile<D>::R;
+  constexpr int NS = KT / 32;                // score blocks
+  constexpr int ND = D / 32;                 // output blocks
+  constexpr int NQ = D / 16;                 // steps of a score product
+  constexpr int NE = KT / 16;                // entries of the page table that a tile may span
+  constexpr int RB = kRowBytes<T, MX, D>;
+  constexpr int SB = D / 32;
+  constexpr int KG = KT / 8;                 // groups of eight keys
+  using V8 = typename Vec8<T>::type;
+
+  __shared__ u32x4 s_k[2][KT][D / 8];        // [key][16-byte chunk]
+  __shared__ u32x4 s_v[2][D][KG];            // [dimension][group of keys]
+
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const int rt = blockIdx.x % max_row_tiles;
-  const int bh = blockIdx.x / max_row_tiles;
-  const int head = bh % bt.h_kv, b = bh / bt.h_kv;
-  const SeqRows sr = seq_rows(bt, b);
-  if (rt >= row_tiles<R>(a, sr.n)) return;
-  const int past = fixed(bt.past + b);
-  const int count = key_tiles<R, KT>(bt, a, past, sr.n, rt);
-  const int row0 = rt * R;
-  const int in_tile = min(sr.n * a.G - row0, R);
-  int w0 = 0, w1 = -1;
-  if (count > 0) {
-    Division<R, KT> d;
-    d.count(bt, a, lane);
-    int64_t at = d.before_seq(bt, a, b) + head * head_tiles<R, KT>(bt, a, past, sr.n);
-    if (!a.causal) {
-      at += (int64_t)rt * count;
-    } else if (rt > 0) {
-      int64_t sum = sum_tiles<R, KT>(bt, a, past, sr.n, lane, rt, 64);
+  const int i = lane & 31, k = lane >> 5;
+
+  Walk<R, KT> at;
+  if (!at.template begin<T>(bt, a, lane, D)) return;
+  const int64_t blk = block_bytes<T, MX, D>(bt.page_log2);
+  const int page_mask = (1 << bt.page_log2) - 1;
+
+  // Where chunks lie in LDS: K row r at chunk ^ k_turn(r), V row d at group ^
+  // v_turn(d).
+  auto k_turn = [](int r) { return (r & 3) | (r >> 1 & 4); };
+  auto v_turn = [](int d) {
+    return KG == 8 ? (d ^ d >> 3) & 7 : (d >> 1 ^ d >> 3) & 3;
+  };
+  // Reading: K row of score row i (of block 0), V row of output row i.
+  const int k_row = 16 * (i >> 4) + 8 * (i >> 2 & 1) + 4 * (i >> 3 & 1) + (i & 3);
+
+  do {
+    const int b = at.b, head = at.head, past = at.past, t0 = at.t0, t1 = at.t1;
+    const SeqRows sr = at.sr;
+    const int row0 = at.rt * R;
+    const int in_tile = min(sr.n * a.G - row0, R);
+    const int min_seen = seen_by(bt, a, past, row0 / a.G);
+    const int max_seen = seen_by(bt, a, past, (row0 + in_tile - 1) / a.G);
+    const int32_t* table = bt.pages + (int64_t)b * bt.max_pages;
+
+    // This wave's rows.
+    const int my_rows = min(max(in_tile - 32 * wave, 0), 32);
+    const int my_row0 = row0 + 32 * wave;
+    const int my_min = my_rows ? seen_by(bt, a, past, my_row0 / a.G) : 0;
+    const int my_max = my_rows ? seen_by(bt, a, past, (my_row0 + my_rows - 1) / a.G) : 0;
+    const int t = (my_row0 + min(i, max(my_rows - 1, 0))) / a.G;
+    const int g = my_row0 + min(i, max(my_rows - 1, 0)) - t * a.G;
+    const int seen = i < my_rows ? seen_by(bt, a, past, t) : 0;
+    u32x4 q[NQ];
+    {
+      const T* src = static_cast<const T*>(a.q) + (int64_t)(sr.start + t) * a.q_stride +
+                     (int64_t)(head * a.G + g) * D + 8 * k;
 #pragma unroll
-      for (int step = 32; step; step >>= 1) sum += __shfl_xor(sum, step);
-      at += lane_value(sum, 0);
+      for (int w = 0; w < NQ; ++w)
+        q[w] = my_rows ? *reinterpret_cast<const u32x4*>(src + 16 * w) : u32x4{0u, 0u, 0u, 0u};
     }
-    w0 = d.owner(at);
-    w1 = d.owner(at + count - 1);
-    if (w0 == w1) return;                          // one workgroup had it all
-  }
+
+    f32x16 acc[ND];
+#pragma unroll
+    for (int c = 0; c < ND; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[c][r] = 0.f;
+    float limit = -INFINITY, ref = 0.f, sum = 0.f;
+    bool spoilt = false;
+
+    // --- staging: the loads of one tile, 128 bytes a thread of 16-bit values ---
+    // Waves 0 and 1, K: unit u of a thread is chunk u % (row's chunks) of a row
+    // (MX: a block of 32 dimensions).  Waves 2 and 3, V: one unit is eight keys
+    // by eight dimensions.
+    const int st = tid & 127;
+    constexpr int kPer = MX ? D / 32 : D / 8;             // units of a K row
+    constexpr int kUnits = KT * kPer / 128 ? KT * kPer / 128 : 1;
+    constexpr int kStepRows = 128 / kPer;                 // rows between a thread's units
+    constexpr int vChunks = D / 8;
+    constexpr int vUnits = KG * vChunks / 128 ? KG * vChunks / 128 : 1;
+    static_assert(vUnits == 1, "one V unit a thread");
+    u32x4 raw[8];
+    uint32_t raw_scale[2];
+    int there = 0;                                        // bits: pages that are there
+    int entry[NE];
+
+    auto fetch_entries = [&](int key0) {
+#pragma unroll
+      for (int e = 0; e < NE; ++e)
+        entry[e] = fixed(table + min((key0 + 16 * e) >> bt.page_log2, bt.max_pages - 1));
+    };
+    auto load_tile = [&](int key0) {
+      int page[NE];
+      there = 0;
+#pragma unroll
+      for (int e = 0; e < NE; ++e) {
+        const bool ok = ((key0 + 16 * e) >> bt.page_log2) < bt.max_pages &&
+                        (unsigned)entry[e] < (unsigned)bt.n_pages;
+        page[e] = ok ? entry[e] : 0;
+        there |= ok << e;
+      }
+      // offset of the page block, and slot, of 16 keys
+      auto block_at = [&](int e, const char* pool) {
+        return pool + ((int64_t)page[e] * bt.h_kv + head) * blk;
+      };
+      auto slot_at = [&](int e) { return (key0 + 16 * e) & page_mask; };
+      if (wave < 2) {
+#pragma unroll
+        for (int n = 0; n < kUnits; ++n) {
+          const int r = st / kPer + kStepRows * n;        // row in the tile
+          const int u = st % kPer;
+          const char* block = block_at(0, bt.K);
+          int slot = slot_at(0);
+#pragma unroll
+          for (int e = 1; e < NE; ++e)
+            if (r >> 4 == e) block = block_at(e, bt.K), slot = slot_at(e);
+          slot += r & 15;
+          if constexpr (MX) {
+            raw[n] = *reinterpret_cast<const u32x4*>(block + (int64_t)slot * RB + 16 * u);
+            raw_scale[n] = *reinterpret_cast<const uint8_t*>(
+                block + ((int64_t)RB << bt.page_log2) + slot * SB + u);
+          } else {
+            raw[n] = *reinterpret_cast<const u32x4*>(block + (int64_t)slot * RB + 16 * u);
+          }
+        }
+      } else if (st < KG * vChunks) {
+        const int grp = st / vChunks, c = st % vChunks;   // keys 8 grp .., dimensions 8 c ..
+        const char* block = block_at(0, bt.V);
+        int slot = slot_at(0);
+#pragma unroll
+        for (int e = 1; e < NE; ++e)
+          if (grp >> 1 == e) block = block_at(e, bt.V), slot = slot_at(e);
+        slot += 8 * (grp & 1);
+        if constexpr (MX) {
+          raw[0] = *reinterpret_cast<const u32x4*>(block + (int64_t)slot * RB + 32 * c);
+          raw[1] = *reinterpret_cast<const u32x4*>(block + (int64_t)slot * RB + 32 * c + 16);
+          const u32x2 s = *reinterpret_cast<const u32x2*>(
+              block + ((int64_t)RB << bt.page_log2) + slot * SB + 8 * (c / 4));
+          raw_scale[0] = s[0], raw_scale[1] = s[1];
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            raw[j] = *reinterpret_cast<const u32x4*>(block + (int64_t)(slot + j) * RB + 16 * c);
+        }
+      }
+    };
+    auto store_tile = [&](int key0, int buf) {
+      if (wave < 2) {
+#pragma unroll
+        for (int n = 0; n < kUnits; ++n) {
+          const int r = st / kPer + kStepRows * n;
+          const int u = st % kPer;
+          if constexpr (MX) {
+            const float scale = mx_scale(raw_scale[n]);
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+              s_k[buf][r][(4 * u + w) ^ k_turn(r)] =
+                  u32x4{widen2<T, 0>(raw[n][w], scale), widen2<T, 1>(raw[n][w], scale),
+                        widen2<T, 2>(raw[n][w], scale), widen2<T, 3>(raw[n][w], scale)};
+          } else {
+            s_k[buf][r][u ^ k_turn(r)] = raw[n];
+          }
+        }
+      } else if (st < KG * vChunks) {
+        const int grp = st / vChunks, c = st % vChunks;
+        const int first = key0 + 8 * grp;
+        u32x4 x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if constexpr (MX) {
+            const float scale = mx_scale(raw_scale[j / 4] >> (8 * (j % 4)) & 255u);
+            const uint32_t codes = raw[j / 4][j % 4];
+            x[j] = u32x4{widen2<T, 0>(codes, scale), widen2<T, 1>(codes, scale),
+                         widen2<T, 2>(codes, scale), widen2<T, 3>(codes, scale)};
+          } else {
+            x[j] = raw[j];
+          }
+        }
+        // Keys that no row sees are left out; where only some rows see a tile's
+        // keys, what a weight of 0 does not take out is zeroed here and added at
+        // the end to the rows that see it.
+        const bool here = there >> (grp >> 1) & 1;
+        if (key0 + KT > min_seen || there != (1 << NE) - 1) {
+          const bool some = min_seen < max_seen && key0 + KT > min_seen;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const bool keep = here && first + j < max_seen;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              if (!keep) x[j][w] = 0u;
+              if (some) {
+                spoilt |= not_finite<T>(x[j][w]);
+                x[j][w] = finite_part<T>(x[j][w]);
+              }
+            }
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t sel = e % 2 ? 0x07060302u : 0x05040100u;
+          const int d = 8 * c + e;
+          s_v[buf][d][grp ^ v_turn(d)] =
+              u32x4{__builtin_amdgcn_perm(x[1][e / 2], x[0][e / 2], sel),
+                    __builtin_amdgcn_perm(x[3][e / 2], x[2][e / 2], sel),
+                    __builtin_amdgcn_perm(x[5][e / 2], x[4][e / 2], sel),
+                    __builtin_amdgcn_perm(x[7][e / 2], x[6][e / 2], sel)};
+        }
+      }
+    };
+
+    fetch_entries(t0 * KT);
+    load_tile(t0 * KT);
+    fetch_entries(min(t0 + 1, t1 - 1) * KT);
+    __syncthreads();                         // the buffers are free (the last item's reads)
+    int pages_here = there;                  // of the tile whose products are next
+    store_tile(t0 * KT, 0);
+    __syncthreads();
+
+    for (int tile = t0; tile < t1; ++tile) {
+      const int key0 = tile * KT, buf = (tile - t0) & 1;
+      const bool more = tile + 1 < t1;
+      if (more) {
+        load_tile(key0 + KT);
+        fetch_entries(min(tile + 2, t1 - 1) * KT);
+      }
+      if (key0 < my_max) {
+        // --- scores ---
+        f32x16 s[NS];
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[n][r] = 0.f;
+#pragma unroll
+        for (int w = 0; w < NQ; ++w)
+#pragma unroll
+          for (int n = 0; n < NS; ++n) {
+            const u32x4 x = s_k[buf][k_row + 32 * n][(2 * w + k) ^ k_turn(k_row)];
+            s[n] = mma32(__builtin_bit_cast(V8, x), __builtin_bit_cast(V8, q[w]), s[n]);
+          }
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[n][r] *= a.scale;
+        if (key0 + KT > my_min || pages_here != (1 << NE) - 1) {
+#pragma unroll
+          for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (!((pages_here >> (2 * n + r / 8) & 1) &&
+                    key0 + 32 * n + 16 * (r / 8) + 8 * k + r % 8 < seen))
+                s[n][r] = -INFINITY;
+        }
+        // --- softmax, the reference raised as in the kernel above ---
+        float top = s[0][0];
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
+        if (__any(!(top <= limit))) {
+          top = fmaxf(top, __shfl_xor(top, 32));
+          if (!(top <= limit)) {
+            const float f = limit == -INFINITY ? 0.f : exp2f(ref - top);
+            ref = top;
+            limit = top + 8.f;
+            sum *= f;
+#pragma unroll
+            for (int c = 0; c < ND; ++c) acc[c] *= f;
+          }
+        }
+        u32x4 p[2 * NS];
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - ref);
+          float part = 0.f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) part += s[n][r];
+          sum += part;
+#pragma unroll
+          for (int r = 0; r < 16; r += 2) p[2 * n + r / 8][r % 8 / 2] = pack2<T>(s[n][r], s[n][r + 1]);
+        }
+        // --- O^T += V^T P^T ---
+#pragma unroll
+        for (int c = 0; c < ND; ++c)
+#pragma unroll
+          for (int n = 0; n < 2 * NS; ++n) {
+            const int d = 32 * c + i;
+            const u32x4 x = s_v[buf][d][(2 * n + k) ^ v_turn(d)];
+            acc[c] = mma32(__builtin_bit_cast(V8, x), __builtin_bit_cast(V8, p[n]), acc[c]);
+          }
+      }
+      if (more) {
+        pages_here = there;
+        store_tile(key0 + KT, buf ^ 1);
+      }
+      __syncthreads();
+    }
+
+    // --- each wave's rows are its own: out, or the workgroup's slot ---
+    const bool fix = __syncthreads_or(spoilt);
+    sum += __shfl_xor(sum, 32);
+    if (i < my_rows) {
+      const int fix_hi = fix ? min(min(max_seen, t1 * KT), seen) : 0;
+      for (int key = max(min_seen / KT, t0) * KT; key < fix_hi; ++key) {
+        const int id = table[key >> bt.page_log2];
+        if ((unsigned)id >= (unsigned)bt.n_pages) continue;
+        const int slot = key & page_mask;
+        const char* block = bt.V + ((int64_t)id * bt.h_kv + head) * blk;
+#pragma unroll
+        for (int c = 0; c < ND; ++c) {
+          if constexpr (MX) {
+            if ((uint8_t)block[mx_scale_at<D>(true, bt.page_log2, slot, c)] == 255u)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) acc[c][r] += NAN;
+          } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const float v = (float)reinterpret_cast<const T*>(
+                  block)[(int64_t)slot * D + 32 * c + 8 * (r / 4) + 4 * k + r % 4];
+              if (!(fabsf(v) < INFINITY)) acc[c][r] += v;
+            }
+          }
+        }
+      }
+      const float my_ref = limit == -INFINITY ? -INFINITY : ref;
+      if (t0 == 0 && t1 == at.tiles) {
+        const float scale = sum == 0.f ? 0.f : 1.f / sum;
+        T* dst = static_cast<T*>(a.out) +
+                 ((int64_t)(sr.start + t) * a.h_q + head * a.G + g) * D + 4 * k;
+#pragma unroll
+        for (int c = 0; c < ND; ++c)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4)
+            *reinterpret_cast<u32x2*>(dst + 32 * c + 2 * r) =
+                u32x2{pack2<T>(acc[c][r] * scale, acc[c][r + 1] * scale),
+                      pack2<T>(acc[c][r + 2] * scale, acc[c][r + 3] * scale)};
+      } else {
+        const int64_t slot = 2 * (int64_t)blockIdx.x + (t0 == 0 ? 1 : 0);
+        const int64_t row = slot * R + 32 * wave + i;
+        float* dst = a.parts + row * D + 4 * k;
+#pragma unroll
+        for (int c = 0; c < ND; ++c)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4)
+            *reinterpret_cast<f32x4*>(dst + 32 * c + 2 * r) =
+                f32x4{acc[c][r], acc[c][r + 1], acc[c][r + 2], acc[c][r + 3]};
+        if (k == 0)
+          *reinterpret_cast<f32x2*>(a.parts + (int64_t)2 * a.grid * R * D + row * 2) =
+              f32x2{my_ref, sum};
+      }
+    }
+  } while (at.next(bt, a));
+}
+
+// Puts the parts of the item that ends in workgroup blockIdx.x together, rows
+// shared out over blockIdx.y.  Few parts: a wave takes a row.  Many: the waves
+// share a row's parts.
+constexpr int kMergeWaves = 8;
+
+template <class T, int D, int R>
+__global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(AttnArgs a) {
+  constexpr int kVec = D / 64;
+  __shared__ float s_part[kMergeWaves][D], s_m[kMergeWaves], s_l[kMergeWaves];
+  const Closing item = a.closing[blockIdx.x];
+  if (item.first < 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int n = blockIdx.x - item.first + 1;
   const float* ml = a.parts + (int64_t)2 * a.grid * R * D;
-  for (int in = blockIdx.y; in < in_tile; in += gridDim.y) {
-    float m = -INFINITY, l = 0.f, o[kVec];
+
+  float m, l, o[kVec];
+  auto combine = [&](int row, int from, int step) {
+    m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int e = 0; e < kVec; ++e) o[e] = 0.f;
-    for (int w = w0 + wave; w <= w1; w += kWaves) {
-      const int64_t slot = 2 * w + (w == w0 ? 1 : 0);
-      const f32x2 s = *reinterpret_cast<const f32x2*>(ml + (slot * R + in) * 2);
-      const float* p = a.parts + (slot * R + in) * D + lane * kVec;
-      float v[kVec];
+    for (int p0 = from; p0 < n; p0 += 4 * step) {
+      f32x2 s[4];
+      float v[4][kVec];
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) v[e] = p[e];
-      if (s[0] == -INFINITY) continue;             // saw nothing
-      const float mn = s[0] <= m ? m : s[0];       // (a NaN stays)
-      const float fo = m == -INFINITY ? 0.f : exp2f(m - mn), fn = exp2f(s[0] - mn);
-      l = l * fo + s[1] * fn;
+      for (int y = 0; y < 4; ++y) {
+        const int p = min(p0 + y * step, n - 1);
+        const int64_t at = (int64_t)(2 * (item.first + p) + (p == 0)) * R + row;
+        s[y] = *reinterpret_cast<const f32x2*>(ml + at * 2);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) o[e] = o[e] * fo + v[e] * fn;
-      m = mn;
+        for (int e = 0; e < kVec; ++e) v[y][e] = a.parts[at * D + lane * kVec + e];
+      }
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        if (p0 + y * step >= n || s[y][0] == -INFINITY) continue;    // saw nothing
+        const float mn = s[y][0] <= m ? m : s[y][0];                 // (a NaN stays)
+        const float fo = m == -INFINITY ? 0.f : exp2f(m - mn), fn = exp2f(s[y][0] - mn);
+        l = l * fo + s[y][1] * fn;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) o[e] = o[e] * fo + v[y][e] * fn;
+        m = mn;
+      }
     }
+  };
+  auto out_at = [&](int row) {
+    const int t = (item.row0 + row) / a.G, g = (item.row0 + row) - t * a.G;
+    return static_cast<T*>(a.out) + ((int64_t)(item.start + t) * a.h_q + item.head * a.G + g) * D;
+  };
+
+  if (n <= 2 * kMergeWaves) {
+    for (int row = blockIdx.y * kMergeWaves + wave; row < item.in_tile;
+         row += gridDim.y * kMergeWaves) {
+      combine(row, 0, 1);
+      T* dst = out_at(row) + lane * kVec;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) dst[e] = (T)(l == 0.f ? 0.f : o[e] / l);
+    }
+    return;
+  }
+  for (int row = blockIdx.y; row < item.in_tile; row += gridDim.y) {
+    combine(row, wave, kMergeWaves);
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < kVec; ++e) s_part[wave][lane * kVec + e] = o[e];
@@ -1222,18 +1648,16 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(Batch bt, AttnArg
     if (tid < D) {
       float top = s_m[0];
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_m[w]);
+      for (int w = 1; w < kMergeWaves; ++w) top = fmaxf(top, s_m[w]);
       float sum = 0.f, y = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
+      for (int w = 0; w < kMergeWaves; ++w) {
         if (s_m[w] == -INFINITY) continue;
         const float f = exp2f(s_m[w] - top);
         sum += s_l[w] * f;
         y += s_part[w][tid] * f;
       }
-      const int t = (row0 + in) / a.G, g = (row0 + in) - t * a.G;
-      static_cast<T*>(a.out)[((int64_t)(sr.start + t) * a.h_q + head * a.G + g) * D + tid] =
-          (T)(sum == 0.f ? 0.f : y / sum);
+      out_at(row)[tid] = (T)(sum == 0.f ? 0.f : y / sum);
     }
   }
 }
@@ -1340,10 +1764,16 @@ void dispatch(const da_paged_kv& p, F&& f) {
     with_dim<false>(p.dtype, p.d, f);
 }
 
-// Query rows of a row tile: 16 for one column block, else 32.
-int tile_rows(int64_t rows_per_head) { return rows_per_head <= 16 ? 16 : 32; }
+// Query rows of a row tile: 16 for one column block, 32 for two; more than 32
+// per KV head of a 16-bit type go to the chunk kernel's tiles of 128.
+constexpr int kChunkRows = 32 * kWaves;
+int tile_rows(int64_t rows_per_head, int dtype) {
+  return rows_per_head <= 16 ? 16 : rows_per_head <= 32 || dtype == DA_F32 ? 32 : kChunkRows;
+}
 
 constexpr int kGroupsPerCu = 2;       // workgroups of the attention kernel per CU
+
+constexpr size_t kClosingBytes = kMaxCus * kGroupsPerCu * sizeof(Closing);
 
 struct AttnPlan {
   int R;
@@ -1356,25 +1786,33 @@ da_status plan_attn(int B, int h_q, int h_kv, int d, int T, int dtype, AttnPlan*
     return DA_ERR_SHAPE;
   if (!dim_ok(d) || !type_ok(dtype)) return DA_ERR_UNSUPPORTED;
   const int64_t per_head = (int64_t)(h_q / h_kv) * T;
-  plan->R = tile_rows(per_head);
-  // (the merge's grid is the items)
-  if ((int64_t)B * h_kv * ceil_div(per_head, plan->R) > kMaxGroups) return DA_ERR_SHAPE;
-  plan->bytes = (size_t)2 * kMaxCus * kGroupsPerCu * plan->R * ((size_t)d + 2) * sizeof(float);
+  plan->R = tile_rows(per_head, dtype);
+  plan->bytes = kClosingBytes + (size_t)2 * kMaxCus * kGroupsPerCu * plan->R * ((size_t)d + 2) * sizeof(float);
   return DA_OK;
 }
 
-template <class T, bool MX, int D, int NB>
-void launch_attn(const Batch& bt, const AttnArgs& a, hipStream_t s) {
-  constexpr int R = 16 * NB, KT = kWaves * Tile<T, MX, D>::TK;
-  hipLaunchKernelGGL((paged_attn_kernel<T, MX, D, NB>), dim3((unsigned)a.grid), dim3(kThreads), 0,
-                     s, bt, a);
-  const int64_t per_head = (int64_t)a.G * bt.T;
-  const int nr = (int)ceil_div(per_head, R);
-  // one row of a small tile each; the many tiles of long chunks share less
-  const unsigned split = nr > 1 ? 4u : (unsigned)per_head;
-  hipLaunchKernelGGL((paged_merge_kernel<T, D, R, KT>),
-                     dim3((unsigned)((int64_t)bt.B * bt.h_kv * nr), split), dim3(kThreads), 0, s,
-                     bt, a, nr);
+template <class T, int D, int R>
+void launch_merge(const Batch& bt, const AttnArgs& a, hipStream_t s) {
+  // two rows a workgroup where many parts share one, sixteen of long chunks
+  const int rows = (int)std::min<int64_t>((int64_t)a.G * bt.T, R);
+  const unsigned split = (unsigned)ceil_div(rows, R == kChunkRows ? 16 : 2);
+  hipLaunchKernelGGL((paged_merge_kernel<T, D, R>), dim3((unsigned)a.grid, split),
+                     dim3(64 * kMergeWaves), 0, s, a);
+}
+
+template <class T, bool MX, int D>
+void launch_attn(int R, const Batch& bt, const AttnArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)a.grid), block(kThreads);
+  if (R == 16) {
+    hipLaunchKernelGGL((paged_attn_kernel<T, MX, D, 1>), grid, block, 0, s, bt, a);
+    launch_merge<T, D, 16>(bt, a, s);
+  } else if (R == 32) {
+    hipLaunchKernelGGL((paged_attn_kernel<T, MX, D, 2>), grid, block, 0, s, bt, a);
+    launch_merge<T, D, 32>(bt, a, s);
+  } else if constexpr (!is_f32<T>) {
+    hipLaunchKernelGGL((paged_chunk_kernel<T, MX, D>), grid, block, 0, s, bt, a);
+    launch_merge<T, D, kChunkRows>(bt, a, s);
+  }
 }
 
 }  // namespace
@@ -1474,16 +1912,13 @@ da_status da_paged_attn(const da_paged_kv* kv, const void* q, int64_t q_stride, 
                    h_q,
                    h_q / p.h_kv,
                    causal,
-                   static_cast<float*>(workspace),
+                   static_cast<Closing*>(workspace),
+                   reinterpret_cast<float*>(static_cast<char*>(workspace) + kClosingBytes),
                    device_cus() * kGroupsPerCu};
   hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   dispatch(p, [&](auto t, auto mx, auto d) {
-    using T = typename decltype(t)::type;
-    if (plan.R == 16)
-      launch_attn<T, mx.value, d.value, 1>(bt, a, s);
-    else
-      launch_attn<T, mx.value, d.value, 2>(bt, a, s);
+    launch_attn<typename decltype(t)::type, mx.value, d.value>(plan.R, bt, a, s);
   });
   return launch_status();
 }
