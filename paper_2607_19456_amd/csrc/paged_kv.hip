@@ -70,6 +70,12 @@ __device__ __forceinline__ int fixed(const int32_t* p) {
   return *(constant_ptr)p;
 }
 
+// A load of what is read once: it leaves the caches to others.
+template <class V>
+__device__ __forceinline__ V once(const void* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+}
+
 __device__ __forceinline__ int capacity(const Batch& bt) { return bt.max_pages << bt.page_log2; }
 
 // First row and number of rows of sequence b, within the arrays whatever
@@ -81,6 +87,14 @@ __device__ __forceinline__ SeqRows seq_rows(const Batch& bt, int b) {
   if (!bt.row_start) return {b * bt.T, bt.T};
   const int s = min(max(bt.row_start[b], 0), bt.rows);
   const int e = min(max(bt.row_start[b + 1], s), bt.rows);
+  return {s, min(e - s, bt.T)};
+}
+
+// The same where b is the same for the whole wave.
+__device__ __forceinline__ SeqRows one_seq_rows(const Batch& bt, int b) {
+  if (!bt.row_start) return {b * bt.T, bt.T};
+  const int s = min(max(fixed(bt.row_start + b), 0), bt.rows);
+  const int e = min(max(fixed(bt.row_start + b + 1), s), bt.rows);
   return {s, min(e - s, bt.T)};
 }
 
@@ -458,13 +472,14 @@ __device__ __forceinline__ uint32_t finite_part(uint32_t w) {
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// An item that ends in a workgroup but did not begin there: what the merge needs
-// to put its parts together.
+// An item in parts: what the merge needs to put them together.  By workgroup,
+// the item that ends in it but did not begin there; or by item, where these are
+// fewer than the workgroups.
 struct Closing {
-  int first;                  // the workgroup of its first part, or -1: none ends here
+  int first, last;            // the workgroups of its parts; first -1: not in parts
   int head, row0, in_tile;    // its rows of the KV head
   int start;                  // the sequence's first row
-  int unused[3];
+  int unused[2];
 };
 
 struct AttnArgs {
@@ -473,10 +488,18 @@ struct AttnArgs {
   int64_t q_stride;
   float scale;          // times log2(e)
   int h_q, G, causal;
-  Closing* closing;     // [grid]
+  uint32_t G_mul, G_shift;
+  int few_tiles;        // their number fits 31 bits, whatever the lengths
+  int by_item;          // closing is [B][h_kv] (one row tile each), else [grid]
+  Closing* closing;
   float* parts;         // [2 * grid][R][D], then [2 * grid][R][2]
   int grid;             // workgroups of the attention kernel
 };
+
+// x / G, 0 <= x < 2^31 (the host's multiplier: floor(2^shift / G) + 1).
+__device__ __forceinline__ int token_of(const AttnArgs& a, int x) {
+  return (int)((uint64_t)(uint32_t)x * a.G_mul >> a.G_shift);
+}
 
 // Keys that token t of a sequence sees.
 __device__ __forceinline__ int seen_by(const Batch& bt, const AttnArgs& a, int past, int t) {
@@ -486,37 +509,37 @@ __device__ __forceinline__ int seen_by(const Batch& bt, const AttnArgs& a, int p
   return past >= cap - t - 1 ? cap : past + t + 1;
 }
 
-// Row tiles of a sequence (each of R rows), tiles of keys of one of them, and
-// of row tiles lo, lo + step, ... below hi.
-template <int R>
+// Row tiles of a sequence (each of R rows; one where not MANY), tiles of keys of
+// one of them, and of all of them (for one KV head).
+template <int R, bool MANY>
 __device__ __forceinline__ int row_tiles(const AttnArgs& a, int n) {
-  return (n * a.G + R - 1) / R;
+  return MANY ? (n * a.G + R - 1) / R : n > 0;
 }
-template <int R, int KT>
+template <int R, int KT, bool MANY>
 __device__ __forceinline__ int key_tiles(const Batch& bt, const AttnArgs& a, int past, int n,
                                          int rt) {
-  // (the last row of most tiles is a token's last: no division)
-  const int last = min(n * a.G, (rt + 1) * R) - 1;
-  return (seen_by(bt, a, past, last == n * a.G - 1 ? n - 1 : last / a.G) + KT - 1) / KT;
+  int t = n - 1;                             // the tile's last token
+  if (MANY && (rt + 1) * R < n * a.G) t = token_of(a, (rt + 1) * R - 1);
+  return (seen_by(bt, a, past, t) + KT - 1) / KT;
 }
-template <int R, int KT>
-__device__ __forceinline__ int64_t sum_tiles(const Batch& bt, const AttnArgs& a, int past, int n,
-                                             int lo, int hi, int step) {
+template <int R, int KT, bool MANY>
+__device__ __forceinline__ int64_t head_tiles(const Batch& bt, const AttnArgs& a, int past, int n) {
+  const int nr = row_tiles<R, MANY>(a, n);
+  if (nr == 0) return 0;
+  if (!MANY || !a.causal) return (int64_t)nr * key_tiles<R, KT, MANY>(bt, a, past, n, 0);
   int64_t sum = 0;
-  for (int rt = lo; rt < hi; rt += step) sum += key_tiles<R, KT>(bt, a, past, n, rt);
+  for (int rt = 0; rt < nr; ++rt) sum += key_tiles<R, KT, MANY>(bt, a, past, n, rt);
   return sum;
 }
-template <int R, int KT>
-__device__ __forceinline__ int64_t head_tiles(const Batch& bt, const AttnArgs& a, int past, int n) {
-  const int nr = row_tiles<R>(a, n);
-  if (nr <= 1) return nr ? key_tiles<R, KT>(bt, a, past, n, 0) : 0;
-  if (!a.causal) return (int64_t)nr * key_tiles<R, KT>(bt, a, past, n, 0);
-  return sum_tiles<R, KT>(bt, a, past, n, 0, nr, 1);
-}
 
+// floor(a / b) for 0 <= a < 2^52, b > 0: by the quotient in 64-bit floating
+// point, off by at most one.
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
-  if ((a | b) >> 32) return a / b;
-  return (int64_t)((uint32_t)a / (uint32_t)b);
+  int64_t q = (int64_t)((double)a / (double)b);
+  const int64_t rest = a - q * b;
+  q += rest >= b;
+  q -= rest < 0;
+  return q;
 }
 __device__ __forceinline__ int64_t lane_value(int64_t x, int lane) {
   const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)x, lane);
@@ -524,40 +547,76 @@ __device__ __forceinline__ int64_t lane_value(int64_t x, int lane) {
   return (int64_t)hi << 32 | lo;
 }
 
+// Inclusive sum over the wave's lanes.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);   // row_shr:2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);   // row_shr:4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);   // row_shr:8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast:31
+  return x;
+}
+
 // The division of all items' tiles over the workgroups, counted by each wave
 // for itself: a lane counts a run of sequences.
-template <int R, int KT>
+template <int R, int KT, bool MANY>
 struct Division {
   int run;                    // sequences of a lane
+  int past;                   // the lane's sequence's, where that is one
+  SeqRows sr;
   int64_t before, upto;       // tiles before the lane's run and up to its end
   int64_t total, each;        // all tiles; workgroup w takes each, the first
   int share, more;            //   `more` ones one more; share of them have work
   bool blind;                 // a sequence of the lane's run sees nothing
 
   __device__ __forceinline__ static int64_t tiles_of(const Batch& bt, const AttnArgs& a, int b) {
-    return bt.h_kv * head_tiles<R, KT>(bt, a, bt.past[b], seq_rows(bt, b).n);
+    return bt.h_kv * head_tiles<R, KT, MANY>(bt, a, bt.past[b], seq_rows(bt, b).n);
   }
   __device__ __forceinline__ void count(const Batch& bt, const AttnArgs& a, int lane) {
     run = (bt.B + 63) / 64;
-    const int lo = min(lane * run, bt.B), hi = min(lo + run, bt.B);
     int64_t mine = 0;
     blind = false;
-    for (int b = lo; b < hi; ++b) {
-      const int64_t n = tiles_of(bt, a, b);
-      blind |= n == 0;
-      mine += n;
+    past = 0;
+    sr = {0, 0};
+    if (run == 1) {
+      if (lane < bt.B) {
+        past = bt.past[lane];
+        sr = seq_rows(bt, lane);
+        mine = bt.h_kv * head_tiles<R, KT, MANY>(bt, a, past, sr.n);
+        blind = mine == 0;
+      }
+    } else {
+      const int lo = min(lane * run, bt.B), hi = min(lo + run, bt.B);
+      for (int b = lo; b < hi; ++b) {
+        const int64_t n = tiles_of(bt, a, b);
+        blind |= n == 0;
+        mine += n;
+      }
     }
-    upto = mine;
+    if (a.few_tiles) {
+      upto = wave_scan((int)mine);
+    } else {
+      upto = mine;
 #pragma unroll
-    for (int step = 1; step < 64; step <<= 1) {
-      const int64_t other = __shfl_up(upto, step);
-      if (lane >= step) upto += other;
+      for (int step = 1; step < 64; step <<= 1) {
+        const int64_t other = __shfl_up(upto, step);
+        if (lane >= step) upto += other;
+      }
     }
     before = upto - mine;
     total = lane_value(upto, 63);
     share = (int)min(total, (int64_t)a.grid);
     each = share ? quotient(total, share) : 0;
     more = (int)(total - each * share);
+  }
+  // Sequence b's past and rows (run == 1: from its lane).
+  __device__ __forceinline__ int past_of(const Batch& bt, int b) const {
+    return run == 1 ? __builtin_amdgcn_readlane(past, b) : fixed(bt.past + b);
+  }
+  __device__ __forceinline__ SeqRows rows_of(const Batch& bt, int b) const {
+    if (run != 1) return one_seq_rows(bt, b);
+    return {__builtin_amdgcn_readlane(sr.start, b), __builtin_amdgcn_readlane(sr.n, b)};
   }
   __device__ __forceinline__ int64_t begin_of(int w) const { return w * each + min(w, more); }
   // The workgroup that takes tile x.
@@ -568,20 +627,30 @@ struct Division {
 };
 
 // The parts of items that a workgroup takes, one after the other.
-template <int R, int KT>
+template <int R, int KT, bool MANY>
 struct Walk {
   int b, head, rt;            // the item: sequence, KV head, row tile
   int tiles, t0, t1;          // its key tiles; those taken are t0 .. t1-1
   int past;
   SeqRows sr;
   int64_t left;               // tiles to take, from t0 on
+  int first;                  // the workgroup of the item's first part, if another
+  bool fresh;                 // the workgroup's first item
 
-  __device__ __forceinline__ void cut() { t1 = (int)min((int64_t)tiles, t0 + left); }
+  // The part's end.  All of these are the same in every lane, and said to be:
+  // addresses and branches made of them then stay with the scalar unit.
+  __device__ __forceinline__ void cut() {
+    left = lane_value(left, 0);
+    b = uniform(b), head = uniform(head), rt = uniform(rt);
+    tiles = uniform(tiles), t0 = uniform(t0), past = uniform(past);
+    sr = {uniform(sr.start), uniform(sr.n)};
+    t1 = uniform((int)min((int64_t)tiles, t0 + left));
+  }
   // Whether the workgroup has work.  Rows of sequences that see nothing, which
   // are in no item, are zeroed here.
   template <class T>
   __device__ __forceinline__ bool begin(const Batch& bt, const AttnArgs& a, int lane, int d_head) {
-    Division<R, KT> d;
+    Division<R, KT, MANY> d;
     d.count(bt, a, lane);
     const int w = blockIdx.x;
     uint64_t blind = __ballot(d.blind);
@@ -589,15 +658,16 @@ struct Walk {
       const int first = (__ffsll((unsigned long long)blind) - 1) * d.run;
       blind &= blind - 1;
       for (int x = first; x < min(first + d.run, bt.B); ++x) {
-        if (x % a.grid != w || Division<R, KT>::tiles_of(bt, a, x)) continue;
+        if (x % a.grid != w || Division<R, KT, MANY>::tiles_of(bt, a, x)) continue;
         const SeqRows zr = seq_rows(bt, x);
         T* dst = static_cast<T*>(a.out) + (int64_t)zr.start * a.h_q * d_head;
         for (int64_t e = threadIdx.x; e < (int64_t)zr.n * a.h_q * d_head; e += kThreads)
           dst[e] = (T)0.f;
+        if (a.by_item && (int)threadIdx.x < bt.h_kv) a.closing[x * bt.h_kv + threadIdx.x].first = -1;
       }
     }
     if (w >= d.share) {
-      if (threadIdx.x == 0) a.closing[w].first = -1;
+      if (!a.by_item && threadIdx.x == 0) a.closing[w].first = -1;
       return false;
     }
     const int64_t lo = d.begin_of(w);
@@ -605,31 +675,37 @@ struct Walk {
     const int at = __ffsll((unsigned long long)__ballot(d.upto > lo)) - 1;
     int64_t rem = lo - lane_value(d.before, at);
     b = at * d.run;
-    sr = seq_rows(bt, b);
-    past = fixed(bt.past + b);
-    int64_t per_head = head_tiles<R, KT>(bt, a, past, sr.n);
+    sr = d.rows_of(bt, b);
+    past = d.past_of(bt, b);
+    int64_t per_head = head_tiles<R, KT, MANY>(bt, a, past, sr.n);
     while (rem >= bt.h_kv * per_head) {          // (ends: d.upto > lo)
       rem -= bt.h_kv * per_head;
-      sr = seq_rows(bt, ++b);
-      past = fixed(bt.past + b);
-      per_head = head_tiles<R, KT>(bt, a, past, sr.n);
+      sr = d.rows_of(bt, ++b);
+      past = d.past_of(bt, b);
+      per_head = head_tiles<R, KT, MANY>(bt, a, past, sr.n);
     }
     head = (int)quotient(rem, per_head);
     rem -= head * per_head;
     rt = 0;
-    tiles = key_tiles<R, KT>(bt, a, past, sr.n, 0);
+    tiles = key_tiles<R, KT, MANY>(bt, a, past, sr.n, 0);
     while (rem >= tiles) {
       rem -= tiles;
-      tiles = key_tiles<R, KT>(bt, a, past, sr.n, ++rt);
+      tiles = key_tiles<R, KT, MANY>(bt, a, past, sr.n, ++rt);
     }
     t0 = (int)rem;
     cut();
-    if (threadIdx.x == 0) {
-      const int row0 = rt * R;
-      a.closing[w] = {t0 > 0 && t1 == tiles ? d.owner(lo - t0) : -1, head, row0,
-                      min(sr.n * a.G - row0, R), sr.start, {0, 0, 0}};
-    }
+    fresh = true;
+    first = t0 ? uniform(d.owner(lo - t0)) : -1;
     return true;
+  }
+  // What the merge is told: of every item that ends here, or (by workgroup) of
+  // the first, the only one that may have begun elsewhere.
+  __device__ __forceinline__ void close(const Batch& bt, const AttnArgs& a) const {
+    const bool ends = t1 == tiles;
+    if ((a.by_item ? ends : fresh) && threadIdx.x == 0)
+      a.closing[a.by_item ? b * bt.h_kv + head : (int)blockIdx.x] =
+          {ends ? first : -1, (int)blockIdx.x, head, rt * R, min(sr.n * a.G - rt * R, R), sr.start,
+           {0, 0}};
   }
   __device__ __forceinline__ bool next(const Batch& bt, const AttnArgs& a) {
     left -= t1 - t0;
@@ -637,11 +713,11 @@ struct Walk {
     t0 = 0;
     tiles = 0;
     while (tiles == 0) {
-      if (++rt >= row_tiles<R>(a, sr.n)) {
+      if (++rt >= row_tiles<R, MANY>(a, sr.n)) {
         rt = 0;
         if (++head >= bt.h_kv) {
           head = 0;
-          sr = seq_rows(bt, ++b);
+          sr = one_seq_rows(bt, ++b);
           past = fixed(bt.past + b);
           if (sr.n == 0) {                       // (a later sequence has tiles: left > 0)
             head = bt.h_kv - 1;
@@ -649,9 +725,11 @@ struct Walk {
           }
         }
       }
-      tiles = key_tiles<R, KT>(bt, a, past, sr.n, rt);
+      tiles = key_tiles<R, KT, MANY>(bt, a, past, sr.n, rt);
     }
     cut();
+    fresh = false;
+    first = -1;
     return true;
   }
 };
@@ -663,6 +741,8 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
   constexpr int KT = kWaves * TK, R = 16 * NB;
   constexpr int RB = kRowBytes<T, MX, D>;
   constexpr int SB = D / 32;                // scale bytes of a 4-bit row
+  // 4-bit tiles are small: two under way for each wave
+  constexpr int DEPTH = MX && D <= 128 ? 2 : 1;
   constexpr int kLdsRow = D + 4;            // floats: 16-byte accesses of 16 rows spread evenly
 
   __shared__ float s_acc[kWaves][16][kLdsRow];
@@ -672,7 +752,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
   const int lane = tid & 63, wave = uniform(tid >> 6);
   const int i = lane & 15, k = lane >> 4;
 
-  Walk<R, KT> at;
+  Walk<R, KT, is_f32<T> && NB == 2> at;     // (16-bit types: one row tile, by tile_rows)
   if (!at.template begin<T>(bt, a, lane, D)) return;
 
   const int64_t blk = block_bytes<T, MX, D>(bt.page_log2);
@@ -689,8 +769,8 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
     const SeqRows sr = at.sr;
     const int row0 = at.rt * R;
     const int in_tile = min(sr.n * a.G - row0, R);
-    const int min_seen = seen_by(bt, a, past, row0 / a.G);
-    const int max_seen = seen_by(bt, a, past, (row0 + in_tile - 1) / a.G);
+    const int min_seen = seen_by(bt, a, past, token_of(a, row0));
+    const int max_seen = seen_by(bt, a, past, token_of(a, row0 + in_tile - 1));
     const int32_t* table = bt.pages + (int64_t)b * bt.max_pages;
 
     // q: lane (i, k) holds row i's share of the score products' summed index.
@@ -703,7 +783,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
 #pragma unroll
       for (int w = 0; w < L::QW; ++w) q[nb][w] = 0u;
       if (x < in_tile) {
-        const int t = (row0 + x) / a.G, g = (row0 + x) - t * a.G;
+        const int t = token_of(a, row0 + x), g = (row0 + x) - t * a.G;
         seen[nb] = seen_by(bt, a, past, t);
         const T* src = static_cast<const T*>(a.q) + (int64_t)(sr.start + t) * a.q_stride +
                        (int64_t)(head * a.G + g) * D;
@@ -729,9 +809,14 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
       for (int c = 0; c < NC; ++c) acc[nb][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    uint32_t kw[NH][L::KW], vw[KPL][L::VW];
-    uint32_t ks[NH], vs[NP][2];
-    bool there_a = false, there_b = false;
+    // A wave tile as it was loaded, and the tile to load in its place next.
+    struct Raw {
+      uint32_t kw[NH][L::KW], vw[KPL][L::VW];
+      uint32_t ks[NH], vs[NP][2];
+      bool there_a, there_b;
+      int next, next_a, next_b;       // its first key and its entries of the table
+    };
+    Raw raw[DEPTH];
     bool spoilt = false;        // V rows that only some rows see held infinities or NaN
 
     // The table's entry for positions p .. p+15 of the sequence, and the page
@@ -745,7 +830,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
     auto base_of = [&](int page, int slot, const char* pool) -> const char* {
       return pool + ((int64_t)max(page, 0) * bt.h_kv + head) * blk + slot * RB;
     };
-    auto load_k = [&](int key0, int pa, int pb) {
+    auto load_k = [&](Raw& x, int key0, int pa, int pb) {
       const int sa = key0 & page_mask, sb = (key0 + 16) & page_mask;
       const char* base = base_of(pa, sa, bt.K);
       const char* scales = nullptr;
@@ -762,32 +847,32 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
         if constexpr (MX) {
           row += k * (D / 8);
           if constexpr (D == 64) {
-            const u32x2 v = *reinterpret_cast<const u32x2*>(row);
-            kw[h][0] = v[0], kw[h][1] = v[1];
+            const u32x2 v = once<u32x2>(row);
+            x.kw[h][0] = v[0], x.kw[h][1] = v[1];
           } else {
 #pragma unroll
             for (int w = 0; w < L::KW / 4; ++w) {
-              const u32x4 v = *reinterpret_cast<const u32x4*>(row + 16 * w);
+              const u32x4 v = once<u32x4>(row + 16 * w);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) kw[h][4 * w + e] = v[e];
+              for (int e = 0; e < 4; ++e) x.kw[h][4 * w + e] = v[e];
             }
           }
           const char* s = scales + (k_key + 4 * h) * SB;
           if constexpr (D == 256)
-            ks[h] = *reinterpret_cast<const uint16_t*>(s + 2 * k);
+            x.ks[h] = once<uint16_t>(s + 2 * k);
           else
-            ks[h] = *reinterpret_cast<const uint8_t*>(s + (D == 64 ? k >> 1 : k));
+            x.ks[h] = once<uint8_t>(s + (D == 64 ? k >> 1 : k));
         } else {
 #pragma unroll
           for (int w = 0; w < L::KW / 4; ++w) {
             const u32x4 v = *reinterpret_cast<const u32x4*>(row + 64 * w + 16 * k);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) kw[h][4 * w + e] = v[e];
+            for (int e = 0; e < 4; ++e) x.kw[h][4 * w + e] = v[e];
           }
         }
       }
     };
-    auto load_v = [&](int key0, int pa, int pb) {
+    auto load_v = [&](Raw& x, int key0, int pa, int pb) {
       const int sa = key0 & page_mask, sb = (key0 + 16) & page_mask;
       const char* base = base_of(pa, sa, bt.V);
       const char* scales = nullptr;
@@ -804,12 +889,12 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
           const int chunk = D == 64 ? i >> 1 : 16 * p + i;      // of 8 dimensions
-          const u32x4 lo4 = *reinterpret_cast<const u32x4*>(base + 32 * chunk);
-          const u32x4 hi4 = *reinterpret_cast<const u32x4*>(base + 32 * chunk + 16);
+          const u32x4 lo4 = once<u32x4>(base + 32 * chunk);
+          const u32x4 hi4 = once<u32x4>(base + 32 * chunk + 16);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) vw[e][p] = lo4[e], vw[4 + e][p] = hi4[e];
-          const u32x2 s = *reinterpret_cast<const u32x2*>(scales + 8 * (chunk / 4));
-          vs[p][0] = s[0], vs[p][1] = s[1];
+          for (int e = 0; e < 4; ++e) x.vw[e][p] = lo4[e], x.vw[4 + e][p] = hi4[e];
+          const u32x2 s = once<u32x2>(scales + 8 * (chunk / 4));
+          x.vs[p][0] = s[0], x.vs[p][1] = s[1];
         }
       } else {
 #pragma unroll
@@ -818,12 +903,12 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
           for (int p = 0; p < NP; ++p) {
             const char* at = base + j * RB + (VCH * i + 16 * VCH * p) * (int)sizeof(T);
             if constexpr (VCH * sizeof(T) == 8) {
-              const u32x2 v = *reinterpret_cast<const u32x2*>(at);
-              vw[j][2 * p] = v[0], vw[j][2 * p + 1] = v[1];
+              const u32x2 v = once<u32x2>(at);
+              x.vw[j][2 * p] = v[0], x.vw[j][2 * p + 1] = v[1];
             } else {
-              const u32x4 v = *reinterpret_cast<const u32x4*>(at);
+              const u32x4 v = once<u32x4>(at);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) vw[j][4 * p + e] = v[e];
+              for (int e = 0; e < 4; ++e) x.vw[j][4 * p + e] = v[e];
             }
           }
       }
@@ -831,78 +916,87 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
 
     // The V rows' words of piece p as values of T (16-bit types): word w of key
     // j holds dimensions 2w and 2w+1 of the piece.
-    auto v_words = [&](int p, uint32_t (&x)[KPL][VCH / 2]) {
+    auto v_words = [&](const Raw& x, int p, uint32_t (&out)[KPL][VCH / 2]) {
       if constexpr (!is_f32<T>) {
 #pragma unroll
         for (int j = 0; j < KPL; ++j) {
           if constexpr (MX) {
-            const float scale = mx_scale(vs[p][j / 4] >> (8 * (j % 4)) & 255u);
-            const uint32_t codes = D == 64 ? vw[j][p] >> (16 * (i & 1)) : vw[j][p];
-            x[j][0] = widen2<T, 0>(codes, scale);
-            x[j][1] = widen2<T, 1>(codes, scale);
+            const float scale = mx_scale(x.vs[p][j / 4] >> (8 * (j % 4)) & 255u);
+            const uint32_t codes = D == 64 ? x.vw[j][p] >> (16 * (i & 1)) : x.vw[j][p];
+            out[j][0] = widen2<T, 0>(codes, scale);
+            out[j][1] = widen2<T, 1>(codes, scale);
             if constexpr (VCH == 8) {
-              x[j][2] = widen2<T, 2>(codes, scale);
-              x[j][3] = widen2<T, 3>(codes, scale);
+              out[j][2] = widen2<T, 2>(codes, scale);
+              out[j][3] = widen2<T, 3>(codes, scale);
             }
           } else {
 #pragma unroll
-            for (int w = 0; w < VCH / 2; ++w) x[j][w] = vw[j][VCH / 2 * p + w];
+            for (int w = 0; w < VCH / 2; ++w) out[j][w] = x.vw[j][VCH / 2 * p + w];
           }
         }
       }
     };
     // float32: the VCH values of key j in piece p.
-    auto v_floats = [&](int p, int j, float (&x)[VCH]) {
+    auto v_floats = [&](const Raw& x, int p, int j, float (&out)[VCH]) {
       if constexpr (MX) {
-        const float scale = mx_scale(vs[p][j / 4] >> (8 * (j % 4)) & 255u);
-        const uint32_t codes = D == 64 ? vw[j][p] >> (16 * (i & 1)) : vw[j][p];
+        const float scale = mx_scale(x.vs[p][j / 4] >> (8 * (j % 4)) & 255u);
+        const uint32_t codes = D == 64 ? x.vw[j][p] >> (16 * (i & 1)) : x.vw[j][p];
         const f32x2 a0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0);
         const f32x2 a1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1);
-        x[0] = a0[0], x[1] = a0[1], x[2] = a1[0], x[3] = a1[1];
+        out[0] = a0[0], out[1] = a0[1], out[2] = a1[0], out[3] = a1[1];
         if constexpr (VCH == 8) {
           const f32x2 a2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 2);
           const f32x2 a3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 3);
-          x[4] = a2[0], x[5] = a2[1], x[6] = a3[0], x[7] = a3[1];
+          out[4] = a2[0], out[5] = a2[1], out[6] = a3[0], out[7] = a3[1];
         }
       } else {
 #pragma unroll
-        for (int e = 0; e < VCH; ++e) x[e] = __uint_as_float(vw[j][VCH * p + e]);
+        for (int e = 0; e < VCH; ++e) out[e] = __uint_as_float(x.vw[j][VCH * p + e]);
       }
     };
 
-    // Wave w takes wave tiles w, w + 4, ...  A tile's K is loaded as soon as the
-    // last one's is used up, its V likewise, and its entries of the page table
-    // a tile before that.  The last tile loads itself once more (from the cache):
-    // with a branch around the loads, the products would wait for all of them.
+    // Wave w takes wave tiles w, w + 4, ..., DEPTH of them under way.  A tile's K
+    // is loaded as soon as the last one's in its registers is used up, its V
+    // likewise, and its entries of the page table DEPTH tiles before that.  The
+    // last tiles load themselves once more (from the cache): with a branch
+    // around the loads, the products would wait for all of them.
     const int wt_end = min(t1 * kWaves, (max_seen + TK - 1) / TK);
     int wt = t0 * kWaves + wave;
-    int next = wt * TK, next_a = 0, next_b = 0;    // the next tile and its entries
-    auto advance = [&](int tile) {
-      next = tile * TK;
-      next_a = entry_of(next);
-      next_b = TK == 32 ? entry_of(next + 16) : next_a;
+    auto aim = [&](Raw& x, int tile) {
+      x.next = min(tile, wt_end - 1) * TK;
+      x.next_a = entry_of(x.next);
+      x.next_b = TK == 32 ? entry_of(x.next + 16) : x.next_a;
     };
     if (wt < wt_end) {
-      const int pa = page_of(next, entry_of(next));
-      const int pb = TK == 32 ? page_of(next + 16, entry_of(next + 16)) : pa;
-      // K before V, here as in the loop: the wait for K is a count of the loads
-      // behind it, and the compiler takes the smaller of the two places'.
-      load_k(next, pa, pb);
-      asm volatile("" ::: "memory");
-      load_v(next, pa, pb);
-      there_a = pa >= 0, there_b = pb >= 0;
-      advance(wt + kWaves < wt_end ? wt + kWaves : wt);
+#pragma unroll
+      for (int y = 0; y < DEPTH; ++y) aim(raw[y], wt + y * kWaves);
+#pragma unroll
+      for (int y = 0; y < DEPTH; ++y) {
+        Raw& x = raw[y];
+        const int pa = page_of(x.next, x.next_a);
+        const int pb = TK == 32 ? page_of(x.next + 16, x.next_b) : pa;
+        // K before V, here as in the loop: the wait for K is a count of the loads
+        // behind it, and the compiler takes the smaller of the two places'.
+        load_k(x, x.next, pa, pb);
+        asm volatile("" ::: "memory");
+        load_v(x, x.next, pa, pb);
+        asm volatile("" ::: "memory");
+        x.there_a = pa >= 0, x.there_b = pb >= 0;
+      }
+#pragma unroll
+      for (int y = 0; y < DEPTH; ++y) aim(raw[y], wt + (y + DEPTH) * kWaves);
     }
     // (q is waited for here, not by its uses in the loop)
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int w = 0; w < L::QW; ++w) asm volatile("" : "+v"(q[nb][w]));
-    for (; wt < wt_end; wt += kWaves) {
-      const int key0 = wt * TK;
-      const int now = next, na = page_of(now, next_a);
-      const int nb_ = TK == 32 ? page_of(now + 16, next_b) : na;
-      advance(wt + 2 * kWaves < wt_end ? wt + 2 * kWaves : wt);
+
+    auto process = [&](Raw& tw, int tile) {
+      const int key0 = tile * TK;
+      const int now = tw.next, na = page_of(now, tw.next_a);
+      const int nb_ = TK == 32 ? page_of(now + 16, tw.next_b) : na;
+      aim(tw, tile + 2 * DEPTH * kWaves);
       // --- scores ---
       f32x4 s[NB][NH];
 #pragma unroll
@@ -915,11 +1009,11 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
           if constexpr (MX) {
 #pragma unroll
             for (int w = 0; w < L::KW; ++w) {
-              const float scale = mx_scale(D == 256 ? ks[h] >> (8 * (w / 4)) & 255u : ks[h]);
-              const f32x2 a0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(kw[h][w], scale, 0);
-              const f32x2 a1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(kw[h][w], scale, 1);
-              const f32x2 a2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(kw[h][w], scale, 2);
-              const f32x2 a3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(kw[h][w], scale, 3);
+              const float scale = mx_scale(D == 256 ? tw.ks[h] >> (8 * (w / 4)) & 255u : tw.ks[h]);
+              const f32x2 a0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(tw.kw[h][w], scale, 0);
+              const f32x2 a1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(tw.kw[h][w], scale, 1);
+              const f32x2 a2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(tw.kw[h][w], scale, 2);
+              const f32x2 a3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(tw.kw[h][w], scale, 3);
               const float x[8] = {a0[0], a0[1], a1[0], a1[1], a2[0], a2[1], a3[0], a3[1]};
 #pragma unroll
               for (int nb = 0; nb < NB; ++nb)
@@ -934,7 +1028,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
 #pragma unroll
               for (int nb = 0; nb < NB; ++nb)
                 s[nb][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                    __uint_as_float(kw[h][w]), __uint_as_float(q[nb][w]), s[nb][h], 0, 0, 0);
+                    __uint_as_float(tw.kw[h][w]), __uint_as_float(q[nb][w]), s[nb][h], 0, 0, 0);
           }
         } else {
           using V8 = typename Vec8<T>::type;
@@ -942,11 +1036,11 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
           for (int w = 0; w < D / 32; ++w) {
             u32x4 x;
             if constexpr (MX) {
-              const float scale = mx_scale(D == 256 ? ks[h] >> (8 * (w / 4)) & 255u : ks[h]);
-              x = u32x4{widen2<T, 0>(kw[h][w], scale), widen2<T, 1>(kw[h][w], scale),
-                        widen2<T, 2>(kw[h][w], scale), widen2<T, 3>(kw[h][w], scale)};
+              const float scale = mx_scale(D == 256 ? tw.ks[h] >> (8 * (w / 4)) & 255u : tw.ks[h]);
+              x = u32x4{widen2<T, 0>(tw.kw[h][w], scale), widen2<T, 1>(tw.kw[h][w], scale),
+                        widen2<T, 2>(tw.kw[h][w], scale), widen2<T, 3>(tw.kw[h][w], scale)};
             } else {
-              x = u32x4{kw[h][4 * w], kw[h][4 * w + 1], kw[h][4 * w + 2], kw[h][4 * w + 3]};
+              x = u32x4{tw.kw[h][4 * w], tw.kw[h][4 * w + 1], tw.kw[h][4 * w + 2], tw.kw[h][4 * w + 3]};
             }
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
@@ -957,11 +1051,11 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
           }
         }
       }
-      load_k(now, na, nb_);
+      load_k(tw, now, na, nb_);
 
       // --- masks: only where a row does not see every key of the tile ---
-      const bool edge = key0 + TK > min_seen || !there_a || !there_b;
-      const bool here = v_half ? there_b : there_a;
+      const bool edge = key0 + TK > min_seen || !tw.there_a || !tw.there_b;
+      const bool here = v_half ? tw.there_b : tw.there_a;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -981,12 +1075,12 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
         for (int j = 0; j < KPL; ++j)
           if (!(here && key0 + KPL * k + j < max_seen)) {
 #pragma unroll
-            for (int w = 0; w < L::VW; ++w) vw[j][w] = 0u;
+            for (int w = 0; w < L::VW; ++w) tw.vw[j][w] = 0u;
             if constexpr (MX)
 #pragma unroll
               for (int p = 0; p < NP; ++p) {
-                vs[p][j / 4] &= ~(255u << (8 * (j % 4)));
-                vs[p][j / 4] |= 127u << (8 * (j % 4));
+                tw.vs[p][j / 4] &= ~(255u << (8 * (j % 4)));
+                tw.vs[p][j / 4] |= 127u << (8 * (j % 4));
               }
           }
         // ... and where only some rows see a tile's keys, infinities and NaN,
@@ -999,16 +1093,16 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
             if constexpr (MX) {
 #pragma unroll
               for (int p = 0; p < NP; ++p)
-                if ((vs[p][j / 4] >> (8 * (j % 4)) & 255u) == 255u) {
+                if ((tw.vs[p][j / 4] >> (8 * (j % 4)) & 255u) == 255u) {
                   bad = true;
-                  vw[j][p] = 0u;
-                  vs[p][j / 4] &= ~(128u << (8 * (j % 4)));
+                  tw.vw[j][p] = 0u;
+                  tw.vs[p][j / 4] &= ~(128u << (8 * (j % 4)));
                 }
             } else {
 #pragma unroll
               for (int w = 0; w < L::VW; ++w) {
-                bad |= not_finite<T>(vw[j][w]);
-                vw[j][w] = finite_part<T>(vw[j][w]);
+                bad |= not_finite<T>(tw.vw[j][w]);
+                tw.vw[j][w] = finite_part<T>(tw.vw[j][w]);
               }
             }
           }
@@ -1061,7 +1155,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
 #pragma unroll
           for (int j = 0; j < KPL; ++j) {
             float x[VCH];
-            v_floats(p, j, x);
+            v_floats(tw, p, j, x);
 #pragma unroll
             for (int c = 0; c < VCH; ++c)
 #pragma unroll
@@ -1085,7 +1179,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
           uint32_t x[KPL][VCH / 2];
-          v_words(p, x);
+          v_words(tw, p, x);
 #pragma unroll
           for (int c = 0; c < VCH; ++c) {
             const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
@@ -1100,13 +1194,23 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
           }
         }
       }
-      load_v(now, na, nb_);
-      there_a = na >= 0, there_b = nb_ >= 0;
+      load_v(tw, now, na, nb_);
+      tw.there_a = na >= 0, tw.there_b = nb_ >= 0;
+    };
+    while (wt < wt_end) {
+      process(raw[0], wt);
+      wt += kWaves;
+      if constexpr (DEPTH == 2) {
+        if (wt >= wt_end) break;
+        process(raw[1], wt);
+        wt += kWaves;
+      }
     }
 
     // --- the four waves' states, one column block at a time ---
     const bool whole = t0 == 0 && t1 == at.tiles;
     const int64_t slot = 2 * (int64_t)blockIdx.x + (t0 == 0 ? 1 : 0);
+    at.close(bt, a);
     // (0, 0) unless values were zeroed above: the keys that they may be of
     const bool fix = __syncthreads_or(spoilt);
     const int fix_lo = fix ? max(min_seen / TK * TK, t0 * KT) : 0;
@@ -1140,7 +1244,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
               f32x4{acc[nb][c][r], acc[nb][c + 1][r], acc[nb][c + 2][r], acc[nb][c + 3][r]} * f;
         }
       __syncthreads();
-#pragma unroll
+#pragma unroll 1
       for (int e = tid; e < 16 * D / 4; e += kThreads) {
         const int x = e / (D / 4), dim = e % (D / 4) * 4;
         const int in = nb * 16 + x;
@@ -1156,7 +1260,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
           l += rw == -INFINITY ? 0.f : s_sum[w][x] * exp2f(rw - m);
           o += *reinterpret_cast<const f32x4*>(&s_acc[w][x][dim]);
         }
-        const int t = (row0 + in) / a.G, g = (row0 + in) - t * a.G;
+        const int t = token_of(a, row0 + in), g = (row0 + in) - t * a.G;
         const int fix_end = fix ? min(fix_hi, seen_by(bt, a, past, t)) : 0;
         for (int key = fix_lo; key < fix_end; ++key) {
           const int page = table[key >> bt.page_log2];
@@ -1248,7 +1352,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int i = lane & 31, k = lane >> 5;
 
-  Walk<R, KT> at;
+  Walk<R, KT, true> at;
   if (!at.template begin<T>(bt, a, lane, D)) return;
   const int64_t blk = block_bytes<T, MX, D>(bt.page_log2);
   const int page_mask = (1 << bt.page_log2) - 1;
@@ -1267,16 +1371,16 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
     const SeqRows sr = at.sr;
     const int row0 = at.rt * R;
     const int in_tile = min(sr.n * a.G - row0, R);
-    const int min_seen = seen_by(bt, a, past, row0 / a.G);
-    const int max_seen = seen_by(bt, a, past, (row0 + in_tile - 1) / a.G);
+    const int min_seen = seen_by(bt, a, past, token_of(a, row0));
+    const int max_seen = seen_by(bt, a, past, token_of(a, row0 + in_tile - 1));
     const int32_t* table = bt.pages + (int64_t)b * bt.max_pages;
 
     // This wave's rows.
     const int my_rows = min(max(in_tile - 32 * wave, 0), 32);
     const int my_row0 = row0 + 32 * wave;
-    const int my_min = my_rows ? seen_by(bt, a, past, my_row0 / a.G) : 0;
-    const int my_max = my_rows ? seen_by(bt, a, past, (my_row0 + my_rows - 1) / a.G) : 0;
-    const int t = (my_row0 + min(i, max(my_rows - 1, 0))) / a.G;
+    const int my_min = my_rows ? seen_by(bt, a, past, token_of(a, my_row0)) : 0;
+    const int my_max = my_rows ? seen_by(bt, a, past, token_of(a, my_row0 + my_rows - 1)) : 0;
+    const int t = token_of(a, my_row0 + min(i, max(my_rows - 1, 0)));
     const int g = my_row0 + min(i, max(my_rows - 1, 0)) - t * a.G;
     const int seen = i < my_rows ? seen_by(bt, a, past, t) : 0;
     u32x4 q[NQ];
@@ -1525,6 +1629,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
     }
 
     // --- each wave's rows are its own: out, or the workgroup's slot ---
+    at.close(bt, a);
     const bool fix = __syncthreads_or(spoilt);
     sum += __shfl_xor(sum, 32);
     if (i < my_rows) {
@@ -1580,8 +1685,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
   } while (at.next(bt, a));
 }
 
-// Puts the parts of the item that ends in workgroup blockIdx.x together, rows
-// shared out over blockIdx.y.  Few parts: a wave takes a row.  Many: the waves
+// Puts the parts of item closing[blockIdx.x] together, rows shared out over
+// blockIdx.y.  Few parts: a wave takes a row.  Many: the waves
 // share a row's parts.
 constexpr int kMergeWaves = 8;
 
@@ -1592,7 +1697,7 @@ __global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(AttnArgs 
   const Closing item = a.closing[blockIdx.x];
   if (item.first < 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const int n = blockIdx.x - item.first + 1;
+  const int n = item.last - item.first + 1;
   const float* ml = a.parts + (int64_t)2 * a.grid * R * D;
 
   float m, l, o[kVec];
@@ -1624,7 +1729,7 @@ __global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(AttnArgs 
     }
   };
   auto out_at = [&](int row) {
-    const int t = (item.row0 + row) / a.G, g = (item.row0 + row) - t * a.G;
+    const int t = token_of(a, item.row0 + row), g = (item.row0 + row) - t * a.G;
     return static_cast<T*>(a.out) + ((int64_t)(item.start + t) * a.h_q + item.head * a.G + g) * D;
   };
 
@@ -1793,10 +1898,12 @@ da_status plan_attn(int B, int h_q, int h_kv, int d, int T, int dtype, AttnPlan*
 
 template <class T, int D, int R>
 void launch_merge(const Batch& bt, const AttnArgs& a, hipStream_t s) {
-  // two rows a workgroup where many parts share one, sixteen of long chunks
+  // A row a wave; few items have rows of many parts, and a workgroup for each.
   const int rows = (int)std::min<int64_t>((int64_t)a.G * bt.T, R);
-  const unsigned split = (unsigned)ceil_div(rows, R == kChunkRows ? 16 : 2);
-  hipLaunchKernelGGL((paged_merge_kernel<T, D, R>), dim3((unsigned)a.grid, split),
+  const int items = a.by_item ? bt.B * bt.h_kv : a.grid;
+  const bool many = (int64_t)bt.B * bt.h_kv * kMergeWaves < a.grid;
+  const unsigned split = (unsigned)ceil_div(rows, many ? 1 : R == kChunkRows ? 16 : kMergeWaves);
+  hipLaunchKernelGGL((paged_merge_kernel<T, D, R>), dim3((unsigned)items, split),
                      dim3(64 * kMergeWaves), 0, s, a);
 }
 
@@ -1905,6 +2012,15 @@ da_status da_paged_attn(const da_paged_kv* kv, const void* q, int64_t q_stride, 
   if (!workspace || workspace_bytes < plan.bytes) return DA_ERR_WORKSPACE;
   if (!aligned(workspace, 16)) return DA_ERR_ALIGN;
   const Batch bt = device_batch(p);
+  const int grid = device_cus() * kGroupsPerCu;
+  const int64_t row_tiles = ceil_div((int64_t)(h_q / p.h_kv) * p.T, plan.R);
+  const int few_tiles =
+      (double)p.B * p.h_kv * row_tiles * ceil_div((int64_t)p.max_pages * p.page_rows, 32) < 2e9;
+  const uint32_t G = h_q / p.h_kv;
+  uint32_t G_shift = 31;
+  while (G > 1u << (G_shift - 31)) ++G_shift;
+  const uint32_t G_mul = (uint32_t)((uint64_t(1) << G_shift) / G + 1);
+  const int by_item = row_tiles == 1 && (int64_t)p.B * p.h_kv <= grid && p.h_kv <= kThreads;
   const AttnArgs a{q,
                    out,
                    q_stride,
@@ -1912,9 +2028,13 @@ da_status da_paged_attn(const da_paged_kv* kv, const void* q, int64_t q_stride, 
                    h_q,
                    h_q / p.h_kv,
                    causal,
+                   G_mul,
+                   G_shift,
+                   few_tiles,
+                   by_item,
                    static_cast<Closing*>(workspace),
                    reinterpret_cast<float*>(static_cast<char*>(workspace) + kClosingBytes),
-                   device_cus() * kGroupsPerCu};
+                   grid};
   hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   dispatch(p, [&](auto t, auto mx, auto d) {
