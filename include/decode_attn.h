@@ -422,13 +422,18 @@ da_status da_paged_gather(const da_paged_kv *kv, void *k_out, void *v_out,
  * row that sees nothing, or whose scores are all -infinity, gives 0.  What a
  * row does not see stays out of it, infinities and NaN included.
  * q [rows][h_q][d] with a token stride in elements, out [rows][h_q][d]
- * contiguous.  Two launches: the work, counted from past and row_start on the
- * device, is divided evenly over a resident grid whatever the lengths, and
- * the parts of a row are then combined in a fixed order: equal calls give equal
- * bits.  Scores, softmax and sums in 32 bits; 16-bit types multiply in
- * their own type (weights rounded to it, once), float32 in float32.
- * workspace: da_paged_workspace_bytes(...) bytes, 16-byte aligned, of any
- * content; one call at a time.
+ * contiguous.  The work, counted from past and row_start on the device, is
+ * divided evenly over a resident grid whatever the lengths, and the parts of a
+ * row are put together in a fixed order: equal calls give equal bits.  One
+ * launch where a KV head has at most 16 query rows and a row few parts
+ * (4*B*h_kv at least twice the compute units, or page_rows*max_pages <= 1024),
+ * else two.  Scores, softmax and
+ * sums in 32 bits; 16-bit types multiply in their own type (weights rounded to
+ * it, once), float32 in float32.
+ * workspace: da_paged_workspace_bytes(...) bytes, 16-byte aligned, one call at
+ * a time.  Its leading da_paged_workspace_counter_bytes(...) bytes must be zero
+ * when a call starts, and are zero again when it is done; the rest may hold
+ * anything.
  */
 da_status da_paged_attn(const da_paged_kv *kv, const void *q, int64_t q_stride,
                         int h_q, float scale, int causal, void *out,
@@ -438,6 +443,11 @@ da_status da_paged_attn(const da_paged_kv *kv, const void *q, int64_t q_stride,
  * lengths, page table and format; no smaller for a larger B.  0 if invalid. */
 size_t da_paged_workspace_bytes(int B, int h_q, int h_kv, int d, int T,
                                 int dtype);
+
+/* Its leading bytes that must be zero before the first call on it.  0 if
+ * invalid. */
+size_t da_paged_workspace_counter_bytes(int B, int h_q, int h_kv, int d, int T,
+                                        int dtype);
 
 /*
  * ---------------------------------------------------------------------------

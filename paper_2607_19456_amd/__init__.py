@@ -16,7 +16,7 @@ _BINDING_NAMES = {
     "chunk_rows", "workspace_bytes", "workspace_counter_bytes", "workspace_reset",
     "alloc_workspace", "DecodeAttnError",
     "paged_alloc", "paged_append", "paged_attn", "paged_gather", "paged_workspace",
-    "paged_workspace_bytes", "rotary_table",
+    "paged_workspace_bytes", "paged_workspace_counter_bytes", "rotary_table",
     "LIBRARY_PATH",
 }
 

@@ -49,6 +49,7 @@ SIGNATURES = {
     "da_paged_gather": (_ci, [_vp] * 4),
     "da_paged_attn": (_ci, [_vp, _vp, _i64, _ci, _cf, _ci, _vp, _vp, _sz, _vp]),
     "da_paged_workspace_bytes": (_sz, [_ci] * 6),
+    "da_paged_workspace_counter_bytes": (_sz, [_ci] * 6),
     # tuning and testing only (explicit segment size)
     "da_decode_chunk_rows": (_ci, [_ci] * 6),
     "da_decode_workspace_bytes_ex": (_sz, [_ci] * 7),
@@ -575,15 +576,23 @@ def paged_workspace_bytes(B, h_q, h_kv, d, T: int = 1, dtype=torch.bfloat16) -> 
     return int(_lib.da_paged_workspace_bytes(B, h_q, h_kv, d, T, _DTYPES[dtype]))
 
 
+def paged_workspace_counter_bytes(B, h_q, h_kv, d, T: int = 1, dtype=torch.bfloat16) -> int:
+    """Leading workspace bytes that must be zero before first use."""
+    return int(_lib.da_paged_workspace_counter_bytes(B, h_q, h_kv, d, T, _DTYPES[dtype]))
+
+
 def paged_workspace(q, K, pages, T: int = 0) -> torch.Tensor:
     """A workspace for paged_attn with q [rows,h_q,d] and these pools and sequences
-    (T: most rows of a sequence; 0: rows / B)."""
-    B = pages.shape[0]
-    n = paged_workspace_bytes(B, q.shape[1], K.shape[1], q.shape[2], T or q.shape[0] // B,
-                              q.dtype)
+    (T: most rows of a sequence; 0: rows / B), its counters zeroed: reusable call
+    after call, by one call at a time."""
+    sizes = (pages.shape[0], q.shape[1], K.shape[1], q.shape[2], T or q.shape[0] // pages.shape[0],
+             q.dtype)
+    n = paged_workspace_bytes(*sizes)
     if n == 0:
         _check("da_paged_workspace_bytes", 2)
-    return torch.empty(n, dtype=torch.uint8, device=q.device)
+    ws = torch.empty(n, dtype=torch.uint8, device=q.device)
+    ws[:paged_workspace_counter_bytes(*sizes)].zero_()
+    return ws
 
 
 def paged_attn(q, K, V, pages, past, scale: float, causal: bool = True, row_start=None,

@@ -490,6 +490,10 @@ struct AttnArgs {
   int h_q, G, causal;
   uint32_t G_mul, G_shift;
   int few_tiles;        // their number fits 31 bits, whatever the lengths
+  // How the parts of an item are put together: by the workgroup that finishes
+  // last, counted in arrived[workgroup of the first part] (0 between calls), or,
+  // arrived NULL, by the merge kernel, which is told of them in closing.
+  unsigned* arrived;
   int by_item;          // closing is [B][h_kv] (one row tile each), else [grid]
   Closing* closing;
   float* parts;         // [2 * grid][R][D], then [2 * grid][R][2]
@@ -558,6 +562,13 @@ __device__ __forceinline__ int wave_scan(int x) {
   return x;
 }
 
+// The workgroup that takes tile x where each takes `each`, the first `more` one
+// more.
+__device__ __forceinline__ int owner_of(int64_t x, int64_t each, int more) {
+  const int64_t big = more * (each + 1);
+  return (int)(x < big ? quotient(x, each + 1) : more + quotient(x - big, each));
+}
+
 // The division of all items' tiles over the workgroups, counted by each wave
 // for itself: a lane counts a run of sequences.
 template <int R, int KT, bool MANY>
@@ -619,11 +630,7 @@ struct Division {
     return {__builtin_amdgcn_readlane(sr.start, b), __builtin_amdgcn_readlane(sr.n, b)};
   }
   __device__ __forceinline__ int64_t begin_of(int w) const { return w * each + min(w, more); }
-  // The workgroup that takes tile x.
-  __device__ __forceinline__ int owner(int64_t x) const {
-    const int64_t big = more * (each + 1);
-    return (int)(x < big ? quotient(x, each + 1) : more + quotient(x - big, each));
-  }
+  __device__ __forceinline__ int owner(int64_t x) const { return owner_of(x, each, more); }
 };
 
 // The parts of items that a workgroup takes, one after the other.
@@ -634,13 +641,17 @@ struct Walk {
   int past;
   SeqRows sr;
   int64_t left;               // tiles to take, from t0 on
+  int64_t at;                 // t0's number among all tiles
   int first;                  // the workgroup of the item's first part, if another
   bool fresh;                 // the workgroup's first item
+  int64_t each;               // of the division
+  int more;
 
   // The part's end.  All of these are the same in every lane, and said to be:
   // addresses and branches made of them then stay with the scalar unit.
   __device__ __forceinline__ void cut() {
-    left = lane_value(left, 0);
+    left = lane_value(left, 0), at = lane_value(at, 0), each = lane_value(each, 0);
+    more = uniform(more);
     b = uniform(b), head = uniform(head), rt = uniform(rt);
     tiles = uniform(tiles), t0 = uniform(t0), past = uniform(past);
     sr = {uniform(sr.start), uniform(sr.n)};
@@ -663,18 +674,20 @@ struct Walk {
         T* dst = static_cast<T*>(a.out) + (int64_t)zr.start * a.h_q * d_head;
         for (int64_t e = threadIdx.x; e < (int64_t)zr.n * a.h_q * d_head; e += kThreads)
           dst[e] = (T)0.f;
-        if (a.by_item && (int)threadIdx.x < bt.h_kv) a.closing[x * bt.h_kv + threadIdx.x].first = -1;
+        if (!a.arrived && a.by_item && (int)threadIdx.x < bt.h_kv)
+          a.closing[x * bt.h_kv + threadIdx.x].first = -1;
       }
     }
     if (w >= d.share) {
-      if (!a.by_item && threadIdx.x == 0) a.closing[w].first = -1;
+      if (!a.arrived && !a.by_item && threadIdx.x == 0) a.closing[w].first = -1;
       return false;
     }
     const int64_t lo = d.begin_of(w);
     left = d.each + (w < d.more ? 1 : 0);
-    const int at = __ffsll((unsigned long long)__ballot(d.upto > lo)) - 1;
-    int64_t rem = lo - lane_value(d.before, at);
-    b = at * d.run;
+    const int in = __ffsll((unsigned long long)__ballot(d.upto > lo)) - 1;
+    int64_t rem = lo - lane_value(d.before, in);
+    b = in * d.run;
+    at = lo, each = d.each, more = d.more;
     sr = d.rows_of(bt, b);
     past = d.past_of(bt, b);
     int64_t per_head = head_tiles<R, KT, MANY>(bt, a, past, sr.n);
@@ -702,12 +715,17 @@ struct Walk {
   // the first, the only one that may have begun elsewhere.
   __device__ __forceinline__ void close(const Batch& bt, const AttnArgs& a) const {
     const bool ends = t1 == tiles;
-    if ((a.by_item ? ends : fresh) && threadIdx.x == 0)
+    if (!a.arrived && (a.by_item ? ends : fresh) && threadIdx.x == 0)
       a.closing[a.by_item ? b * bt.h_kv + head : (int)blockIdx.x] =
           {ends ? first : -1, (int)blockIdx.x, head, rt * R, min(sr.n * a.G - rt * R, R), sr.start,
            {0, 0}};
   }
+  // The workgroup of the item's last part.
+  __device__ __forceinline__ int last() const {
+    return t1 == tiles ? (int)blockIdx.x : uniform(owner_of(at - t0 + tiles - 1, each, more));
+  }
   __device__ __forceinline__ bool next(const Batch& bt, const AttnArgs& a) {
+    at += t1 - t0;
     left -= t1 - t0;
     if (left <= 0) return false;
     t0 = 0;
@@ -733,6 +751,84 @@ struct Walk {
     return true;
   }
 };
+
+// Parts pass between workgroups on different dies, whose L2 caches do not see
+// each other's lines: they are written through to memory and read from there,
+// 8 bytes at a time, which costs a few KB an item.  (Fences would write back and
+// empty whole caches: measured 130 us a launch of 512 workgroups.)
+__device__ __forceinline__ void store_part(float* p, f32x2 v) {
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), __builtin_bit_cast(uint64_t, v),
+                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void store_part(float* p, f32x4 v) {
+  store_part(p, f32x2{v[0], v[1]});
+  store_part(p + 2, f32x2{v[2], v[3]});
+}
+__device__ __forceinline__ f32x2 load_part(const float* p) {
+  return __builtin_bit_cast(
+      f32x2, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED,
+                               __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// After a workgroup's part of an item has been written: the one that finishes
+// last puts the item's n parts together, in their order, four values of a row a
+// thread.  Every wave waits until its stores are in memory before the workgroup
+// is counted.
+template <class T, int D, int R, class W>
+__device__ __forceinline__ void finish(const Batch& bt, const AttnArgs& a, const W& at) {
+  __shared__ unsigned s_arrived;
+  const int first = at.t0 ? at.first : (int)blockIdx.x;
+  const int n = at.last() - first + 1;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0)
+    s_arrived = __hip_atomic_fetch_add(a.arrived + first, 1u, __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (uniform((int)s_arrived) != n - 1) return;
+  if (threadIdx.x == 0)
+    __hip_atomic_store(a.arrived + first, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const float* ml = a.parts + (int64_t)2 * a.grid * R * D;
+  const int row0 = at.rt * R, in_tile = min(at.sr.n * a.G - row0, R);
+#pragma unroll 1
+  for (int e = threadIdx.x; e < in_tile * (D / 4); e += kThreads) {
+    const int in = e / (D / 4), dim = e % (D / 4) * 4;
+    float m = -INFINITY, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int p0 = 0; p0 < n; p0 += 4) {
+      f32x2 s[4];
+      f32x4 v[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const int p = min(p0 + y, n - 1);
+        const int64_t row = (int64_t)(2 * (first + p) + (p == 0)) * R + in;
+        s[y] = load_part(ml + row * 2);
+        const f32x2 lo = load_part(a.parts + row * D + dim);
+        const f32x2 hi = load_part(a.parts + row * D + dim + 2);
+        v[y] = f32x4{lo[0], lo[1], hi[0], hi[1]};
+      }
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        if (p0 + y >= n || s[y][0] == -INFINITY) continue;           // saw nothing
+        const float mn = s[y][0] <= m ? m : s[y][0];                 // (a NaN stays)
+        const float fo = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+        const float fn = __builtin_amdgcn_exp2f(s[y][0] - mn);
+        l = l * fo + s[y][1] * fn;
+        o = o * fo + v[y] * fn;
+        m = mn;
+      }
+    }
+    o = l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o / l;
+    const int t = token_of(a, row0 + in), g = (row0 + in) - t * a.G;
+    T* dst = static_cast<T*>(a.out) +
+             ((int64_t)(at.sr.start + t) * a.h_q + at.head * a.G + g) * D + dim;
+    if constexpr (is_f32<T>)
+      *reinterpret_cast<f32x4*>(dst) = o;
+    else
+      *reinterpret_cast<u32x2*>(dst) = u32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
+  }
+}
 
 template <class T, bool MX, int D, int NB>
 __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs a) {
@@ -1286,14 +1382,20 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
           else
             *reinterpret_cast<u32x2*>(dst) = u32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
         } else {
-          *reinterpret_cast<f32x4*>(a.parts + (slot * R + in) * D + dim) = o;
-          if (dim == 0)
-            *reinterpret_cast<f32x2*>(a.parts + (int64_t)2 * a.grid * R * D +
-                                      (slot * R + in) * 2) = f32x2{m, l};
+          float* part = a.parts + (slot * R + in) * D + dim;
+          float* ml = a.parts + (int64_t)2 * a.grid * R * D + (slot * R + in) * 2;
+          if (NB == 1 && a.arrived) {
+            store_part(part, o);
+            if (dim == 0) store_part(ml, f32x2{m, l});
+          } else {
+            *reinterpret_cast<f32x4*>(part) = o;
+            if (dim == 0) *reinterpret_cast<f32x2*>(ml) = f32x2{m, l};
+          }
         }
       }
     }
-
+    if constexpr (NB == 1)
+      if (a.arrived && !whole) finish<T, D, R>(bt, a, at);
   } while (at.next(bt, a));
 }
 
@@ -1878,6 +1980,7 @@ int tile_rows(int64_t rows_per_head, int dtype) {
 
 constexpr int kGroupsPerCu = 2;       // workgroups of the attention kernel per CU
 
+constexpr size_t kArrivedBytes = kMaxCus * kGroupsPerCu * sizeof(unsigned);
 constexpr size_t kClosingBytes = kMaxCus * kGroupsPerCu * sizeof(Closing);
 
 struct AttnPlan {
@@ -1892,12 +1995,13 @@ da_status plan_attn(int B, int h_q, int h_kv, int d, int T, int dtype, AttnPlan*
   if (!dim_ok(d) || !type_ok(dtype)) return DA_ERR_UNSUPPORTED;
   const int64_t per_head = (int64_t)(h_q / h_kv) * T;
   plan->R = tile_rows(per_head, dtype);
-  plan->bytes = kClosingBytes + (size_t)2 * kMaxCus * kGroupsPerCu * plan->R * ((size_t)d + 2) * sizeof(float);
+  plan->bytes = kArrivedBytes + kClosingBytes + (size_t)2 * kMaxCus * kGroupsPerCu * plan->R * ((size_t)d + 2) * sizeof(float);
   return DA_OK;
 }
 
 template <class T, int D, int R>
 void launch_merge(const Batch& bt, const AttnArgs& a, hipStream_t s) {
+  if (a.arrived) return;
   // A row a wave; few items have rows of many parts, and a workgroup for each.
   const int rows = (int)std::min<int64_t>((int64_t)a.G * bt.T, R);
   const int items = a.by_item ? bt.B * bt.h_kv : a.grid;
@@ -1994,6 +2098,11 @@ size_t da_paged_workspace_bytes(int B, int h_q, int h_kv, int d, int T, int dtyp
   return plan_attn(B, h_q, h_kv, d, T, dtype, &plan) == DA_OK ? plan.bytes : 0;
 }
 
+size_t da_paged_workspace_counter_bytes(int B, int h_q, int h_kv, int d, int T, int dtype) {
+  AttnPlan plan;
+  return plan_attn(B, h_q, h_kv, d, T, dtype, &plan) == DA_OK ? kArrivedBytes : 0;
+}
+
 da_status da_paged_attn(const da_paged_kv* kv, const void* q, int64_t q_stride, int h_q,
                         float scale, int causal, void* out, void* workspace,
                         size_t workspace_bytes, void* stream) {
@@ -2016,6 +2125,14 @@ da_status da_paged_attn(const da_paged_kv* kv, const void* q, int64_t q_stride, 
   const int64_t row_tiles = ceil_div((int64_t)(h_q / p.h_kv) * p.T, plan.R);
   const int few_tiles =
       (double)p.B * p.h_kv * row_tiles * ceil_div((int64_t)p.max_pages * p.page_rows, 32) < 2e9;
+  // Items of few rows and few parts are put together by the workgroups that have
+  // them: one launch for two (one sequence of 700 rows 10.6 -> 9.5 us, 16 of
+  // 200-4000 30.8 -> 30.0; but with tiles of 32 rows 52.6 -> 56.6, of 128 rows
+  // 23.3 -> 26.4, where the last workgroup has too much to read).
+  const bool few_parts =
+      plan.R == 16 && (ceil_div((int64_t)p.max_pages * p.page_rows, 64) <= 16 ||
+                       4 * (int64_t)p.B * p.h_kv >= grid);
+  char* ws = static_cast<char*>(workspace);
   const uint32_t G = h_q / p.h_kv;
   uint32_t G_shift = 31;
   while (G > 1u << (G_shift - 31)) ++G_shift;
@@ -2031,9 +2148,10 @@ da_status da_paged_attn(const da_paged_kv* kv, const void* q, int64_t q_stride, 
                    G_mul,
                    G_shift,
                    few_tiles,
+                   few_parts ? reinterpret_cast<unsigned*>(ws) : nullptr,
                    by_item,
-                   static_cast<Closing*>(workspace),
-                   reinterpret_cast<float*>(static_cast<char*>(workspace) + kClosingBytes),
+                   reinterpret_cast<Closing*>(ws + kArrivedBytes),
+                   reinterpret_cast<float*>(ws + kArrivedBytes + kClosingBytes),
                    grid};
   hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();

@@ -206,17 +206,28 @@ def test_many_sequences(cuda_device):
     check_attn(cuda_device, d=64, h_q=2, h_kv=1, past=past[:300], T=2, counts=counts, seed=7)
 
 
-def test_equal_calls_give_equal_bits_and_workspaces_need_no_care(cuda_device):
-    c = ref.Cache(2, "bf16", "dense", 128, 2, 64, [3000, 500])
+@pytest.mark.parametrize("B,past", [(2, [2999, 499]), (70, None)])
+@pytest.mark.parametrize("dtype,T", [("bf16", 1), ("f16", 3), ("bf16", 40), ("f32", 9)])
+def test_equal_calls_give_equal_bits(cuda_device, dtype, T, B, past):
+    """Whatever the workspace holds behind its counters, which every call leaves
+    zeroed; rows of many parts, put together by the merge, and of few, put
+    together by the workgroup that finishes last."""
+    past = past or [int(x) for x in np.random.default_rng(4).integers(0, 900, B)]
+    c = ref.Cache(2, dtype, "dense", 64, 2, 64, [p + T for p in past])
     K, V, pages = c.to(cuda_device)
-    q = torch.randn(2, 16, 128, device=cuda_device).bfloat16()
-    past = torch.tensor([2999, 499], dtype=torch.int32, device=cuda_device)
-    ws = lib.paged_workspace(q, K, pages)
+    q = torch.randn(B * T, 8, 64, device=cuda_device).to(ref.DTYPES[dtype])
+    dpast = torch.tensor(past, dtype=torch.int32, device=cuda_device)
+    ws = lib.paged_workspace(q, K, pages, T)
+    n = lib.paged_workspace_counter_bytes(B, 8, 2, 64, T, q.dtype)
+    assert 0 < n < ws.numel() and int(ws[:n].max()) == 0
     outs = []
     for fill in (0, 255, 127):
-        ws.fill_(fill)
-        outs.append(lib.paged_attn(q, K, V, pages, past, 0.09, workspace=ws).clone())
+        ws[n:].fill_(fill)
+        outs.append(lib.paged_attn(q, K, V, pages, dpast, 0.09, T=T, workspace=ws).clone())
+        assert int(ws[:n].max()) == 0
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    check_attn(cuda_device, dtype=dtype, d=64, h_q=8, h_kv=2, P=64, past=past, T=T, cache=c,
+               scale=0.09, q=q.cpu())
 
 
 def test_queries_with_a_stride_and_another_stream(cuda_device):

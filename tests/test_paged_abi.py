@@ -107,11 +107,12 @@ def test_sizes():
         before = 0
         for B in (1, 2, 7, 300, 4000):
             n = size(B, h_q, h_kv, d, T, 1)
+            assert 0 < lib.da_paged_workspace_counter_bytes(B, h_q, h_kv, d, T, 1) < n
             assert n >= before > -1 and n > 0
             before = n
     for bad in ((0, 8, 2, 64, 1, 0), (1, 8, 3, 64, 1, 0), (1, 8, 2, 80, 1, 0),
                 (1, 8, 2, 64, 0, 0), (1, 8, 2, 64, 32769, 0), (1, 8, 2, 64, 1, 7)):
-        assert size(*bad) == 0, bad
+        assert size(*bad) == lib.da_paged_workspace_counter_bytes(*bad) == 0, bad
 
 
 def test_binding_refuses_tensors_that_are_not_on_the_gpu_or_do_not_fit():
