@@ -385,6 +385,13 @@ def kv_append_rows(K, V, k_new, v_new, lens, stream=None) -> None:
 
 # --- paged cache ----------------------------------------------------------------
 
+try:
+    from . import paged_call as _call
+except ImportError as e:
+    raise ImportError("paged_call.so is not built; run __graft_entry__.build()") from e
+_call.use(*(ctypes.cast(getattr(_lib, f), _vp).value
+            for f in ("da_paged_append", "da_paged_gather", "da_paged_attn")))
+
 # da_paged_kv: five pointers, ten ints.  Packed as bytes: filling a
 # ctypes.Structure of 15 fields takes twice as long.
 _pack_kv = struct.Struct("=5Q10i").pack
@@ -504,6 +511,15 @@ def _paged_stream(stream, gpu) -> int:
     return _stream(stream) if stream is not None or _raw_stream is None else _raw_stream(gpu)
 
 
+def _fast(K, stream):
+    """(gpu, stream) of a call that paged_call may take: K on the current device."""
+    if isinstance(K, torch.Tensor):
+        gpu = K.get_device()
+        if gpu >= 0 and gpu == torch._C._cuda_getDevice():
+            return gpu, _paged_stream(stream, gpu)
+    return None
+
+
 def _rows(t, name):
     if not isinstance(t, torch.Tensor) or t.dim() != 3:
         raise ValueError(f"{name} must be [rows, heads, d]")
@@ -516,6 +532,16 @@ def paged_append(K, V, pages, past, k_new, v_new, q=None, rotary=None, interleav
     turned by ``rotary`` [positions, rot_dim] on the way, and q [rows,h_q,d] turned
     into q_out (returned).  ``row_start`` [B+1]: each sequence's rows, at most ``T``;
     else T rows each.  past is not changed."""
+    if q is not None and q_out is None:
+        q_out = torch.empty(_rows(q, "q"), dtype=q.dtype, device=q.device)
+    fast = _fast(K, stream)
+    if fast is not None:
+        status = _call.append(K, V, pages, past, k_new, v_new, q, rotary, interleaved, row_start,
+                              T, q_out, *fast)
+        if status == 0:
+            return q_out
+        if status > 0:
+            _check("da_paged_append", status)
     shape = _rows(k_new, "k_new")
     rows, heads, d = shape
     dtype = k_new.dtype
@@ -539,8 +565,6 @@ def paged_append(K, V, pages, past, k_new, v_new, q=None, rotary=None, interleav
             _refuse(q, "q", dtype, gpu)
         qs = h_q * d if q.is_contiguous() else _stride(q, "q", shape)
         qp = q.data_ptr()
-        if q_out is None:
-            q_out = torch.empty(shape, dtype=dtype, device=q.device)
         qo = _here(q_out, "q_out", dtype, gpu)
         _need(q_out.shape == shape, "q_out must have q's shape")
     if rotary is not None:
@@ -559,6 +583,13 @@ def paged_gather(K, V, pages, past, k_out, v_out, row_start=None, T: int = 0, st
     """The rows at positions past[b] + r into k_out and v_out [rows,h_kv,d] (zeros
     where there is no page): the places that paged_append with the same
     ``past``, ``row_start`` and ``T`` writes."""
+    fast = _fast(K, stream)
+    if fast is not None:
+        status = _call.gather(K, V, pages, past, k_out, v_out, row_start, T, *fast)
+        if status == 0:
+            return k_out, v_out
+        if status > 0:
+            _check("da_paged_gather", status)
     rows, heads, d = _rows(k_out, "k_out")
     dtype = k_out.dtype
     kv, gpu, h_kv, T = _paged(K, V, pages, past, rows, d, dtype, row_start, T)
@@ -600,14 +631,22 @@ def paged_attn(q, K, V, pages, past, scale: float, causal: bool = True, row_star
     """out[n,h,:] = softmax(scale * q[n,h].K) V over the sequence's positions up to
     the row's own, past[b] + r (causal; append first), or over all past[b] of
     them.  q [rows,h_q,d], any stride between tokens."""
+    if out is None:
+        out = torch.empty(_rows(q, "q"), dtype=q.dtype, device=q.device)
+    fast = _fast(K, stream) if workspace is not None else None
+    if fast is not None:
+        status = _call.attn(K, V, pages, past, q, scale, causal, row_start, T, out, workspace,
+                            *fast)
+        if status == 0:
+            return out
+        if status > 0:
+            _check("da_paged_attn", status)
     shape = _rows(q, "q")
     rows, h_q, d = shape
     dtype = q.dtype
     kv, gpu, _, T = _paged(K, V, pages, past, rows, d, dtype, row_start, T)
     if q.get_device() != gpu:
         _refuse(q, "q", dtype, gpu)
-    if out is None:
-        out = torch.empty(shape, dtype=dtype, device=q.device)
     op = _here(out, "out", dtype, gpu)
     _need(out.shape == shape, "out must have q's shape")
     if workspace is None:

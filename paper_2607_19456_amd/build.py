@@ -20,6 +20,9 @@ LIB = os.path.join(PKG, "libdecode_attn.so")
 # the decode).
 PROBE_SRC = os.path.join(PKG, "csrc", "hbm_probe.hip")
 PROBE_LIB = os.path.join(PKG, "libhbm_probe.so")
+# The paged calls' argument handling (a Python extension: host code only).
+CALL_SRC = os.path.join(PKG, "csrc", "paged_call.cpp")
+CALL_LIB = os.path.join(PKG, "paged_call.so")
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -53,22 +56,39 @@ def _finish(jobs: list) -> None:
         raise subprocess.CalledProcessError(1, failed[0])
 
 
+def _call_command(out: str) -> list:
+    import sysconfig
+
+    import torch
+    from torch.utils.cpp_extension import include_paths
+
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            *(f"-isystem{p}" for p in include_paths()),
+            f"-isystem{sysconfig.get_paths()['include']}", f"-I{INCLUDE}", "-o", out, CALL_SRC,
+            f"-L{lib}", "-ltorch_python", "-ltorch_cpu", "-lc10", f"-Wl,-rpath,{lib}"]
+
+
 def build(verbose: bool = False) -> str:
-    """Compile the decode library and the read-ceiling probe (always; a stale
-    build must never be used).  Returns the decode library's path."""
+    """Compile the decode library, the read-ceiling probe and the paged calls'
+    argument handling (always; a stale build must never be used).  Returns the
+    decode library's path."""
     tag = ".tmp%d" % os.getpid()
     objects = [LIB + tag + ".%d.o" % i for i in range(2)]
     compile_flags = [f for f in FLAGS if f != "-shared"]
     try:
         _finish([_start([HIPCC, *compile_flags, "-c", "-o", obj, src], verbose)
                  for obj, src in zip(objects, (SRC, PAGED_SRC))]
-                + [_start([HIPCC, *FLAGS, "-o", PROBE_LIB + tag, PROBE_SRC], verbose)])
+                + [_start([HIPCC, *FLAGS, "-o", PROBE_LIB + tag, PROBE_SRC], verbose),
+                   _start(_call_command(CALL_LIB + tag), verbose)])
         _finish([_start([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", LIB + tag,
                          *objects], verbose)])
         os.replace(PROBE_LIB + tag, PROBE_LIB)
+        os.replace(CALL_LIB + tag, CALL_LIB)
         os.replace(LIB + tag, LIB)
     finally:
-        for path in (*objects, LIB + tag, PROBE_LIB + tag):
+        for path in (*objects, LIB + tag, PROBE_LIB + tag, CALL_LIB + tag):
             if os.path.exists(path):
                 os.unlink(path)
     return LIB

@@ -447,8 +447,12 @@ __device__ __forceinline__ uint32_t widen2(uint32_t codes, float scale) {
 }
 
 // A scale byte as the factor that the conversions take: they read its exponent
-// alone, 255 as not a number and 0 as 2^-127.
+// alone (not sign or mantissa), 255 as not a number and 0 as 2^-127.
 __device__ __forceinline__ float mx_scale(uint32_t byte) { return power_of(byte); }
+// Byte j % 4 of w as that: what stands beside it falls on sign and mantissa.
+__device__ __forceinline__ float mx_scale_of(uint32_t w, int j) {
+  return __uint_as_float(j % 4 == 3 ? w >> 1 : w << (23 - 8 * (j % 4)));
+}
 
 template <class T>
 __device__ __forceinline__ bool not_finite(uint32_t w) {
@@ -486,7 +490,10 @@ struct AttnArgs {
   const void* q;
   void* out;
   int64_t q_stride;
-  float scale;          // times log2(e)
+  // |scale| times log2(e), or 1 for a scale of 0; q's words are taken as
+  // (q & q_keep) ^ q_flip: negated for a negative scale, 0 for that of 0.
+  float scale;
+  uint32_t q_keep, q_flip;
   int h_q, G, causal;
   uint32_t G_mul, G_shift;
   int few_tiles;        // their number fits 31 bits, whatever the lengths
@@ -838,7 +845,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
   constexpr int RB = kRowBytes<T, MX, D>;
   constexpr int SB = D / 32;                // scale bytes of a 4-bit row
   // 4-bit tiles are small: two under way for each wave
-  constexpr int DEPTH = MX && D <= 128 ? 2 : 1;
+  constexpr int DEPTH = MX && D <= 128 && !(is_f32<T> && NB == 2) ? 2 : 1;
   constexpr int kLdsRow = D + 4;            // floats: 16-byte accesses of 16 rows spread evenly
 
   __shared__ float s_acc[kWaves][16][kLdsRow];
@@ -889,7 +896,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
           const int dim = MX ? D / 4 * k + per16 * w : 4 * per16 * w + per16 * k;
           const u32x4 v = *reinterpret_cast<const u32x4*>(src + dim);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) q[nb][4 * w + e] = v[e];
+          for (int e = 0; e < 4; ++e) q[nb][4 * w + e] = (v[e] & a.q_keep) ^ a.q_flip;
         }
       }
     }
@@ -1017,7 +1024,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
 #pragma unroll
         for (int j = 0; j < KPL; ++j) {
           if constexpr (MX) {
-            const float scale = mx_scale(x.vs[p][j / 4] >> (8 * (j % 4)) & 255u);
+            const float scale = mx_scale_of(x.vs[p][j / 4], j);
             const uint32_t codes = D == 64 ? x.vw[j][p] >> (16 * (i & 1)) : x.vw[j][p];
             out[j][0] = widen2<T, 0>(codes, scale);
             out[j][1] = widen2<T, 1>(codes, scale);
@@ -1035,7 +1042,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
     // float32: the VCH values of key j in piece p.
     auto v_floats = [&](const Raw& x, int p, int j, float (&out)[VCH]) {
       if constexpr (MX) {
-        const float scale = mx_scale(x.vs[p][j / 4] >> (8 * (j % 4)) & 255u);
+        const float scale = mx_scale_of(x.vs[p][j / 4], j);
         const uint32_t codes = D == 64 ? x.vw[j][p] >> (16 * (i & 1)) : x.vw[j][p];
         const f32x2 a0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0);
         const f32x2 a1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1);
@@ -1088,135 +1095,147 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
 #pragma unroll
       for (int w = 0; w < L::QW; ++w) asm volatile("" : "+v"(q[nb][w]));
 
-    auto process = [&](Raw& tw, int tile) {
-      const int key0 = tile * TK;
-      const int now = tw.next, na = page_of(now, tw.next_a);
-      const int nb_ = TK == 32 ? page_of(now + 16, tw.next_b) : na;
-      aim(tw, tile + 2 * DEPTH * kWaves);
-      // --- scores ---
-      f32x4 s[NB][NH];
+    const int end_key = wt_end * TK;       // (a step's second tile may lie beyond)
+    auto process = [&](int tile) {
+      int now[DEPTH], na[DEPTH], nb_[DEPTH];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int h = 0; h < NH; ++h) s[nb][h] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int h = 0; h < NH; ++h) {
-        if constexpr (is_f32<T>) {
-          if constexpr (MX) {
-#pragma unroll
-            for (int w = 0; w < L::KW; ++w) {
-              const float scale = mx_scale(D == 256 ? tw.ks[h] >> (8 * (w / 4)) & 255u : tw.ks[h]);
-              const f32x2 a0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(tw.kw[h][w], scale, 0);
-              const f32x2 a1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(tw.kw[h][w], scale, 1);
-              const f32x2 a2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(tw.kw[h][w], scale, 2);
-              const f32x2 a3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(tw.kw[h][w], scale, 3);
-              const float x[8] = {a0[0], a0[1], a1[0], a1[1], a2[0], a2[1], a3[0], a3[1]};
-#pragma unroll
-              for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                  s[nb][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                      x[e], __uint_as_float(q[nb][8 * w + e]), s[nb][h], 0, 0, 0);
-            }
-          } else {
-#pragma unroll
-            for (int w = 0; w < L::KW; ++w)
-#pragma unroll
-              for (int nb = 0; nb < NB; ++nb)
-                s[nb][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                    __uint_as_float(tw.kw[h][w]), __uint_as_float(q[nb][w]), s[nb][h], 0, 0, 0);
-          }
-        } else {
-          using V8 = typename Vec8<T>::type;
-#pragma unroll
-          for (int w = 0; w < D / 32; ++w) {
-            u32x4 x;
-            if constexpr (MX) {
-              const float scale = mx_scale(D == 256 ? tw.ks[h] >> (8 * (w / 4)) & 255u : tw.ks[h]);
-              x = u32x4{widen2<T, 0>(tw.kw[h][w], scale), widen2<T, 1>(tw.kw[h][w], scale),
-                        widen2<T, 2>(tw.kw[h][w], scale), widen2<T, 3>(tw.kw[h][w], scale)};
-            } else {
-              x = u32x4{tw.kw[h][4 * w], tw.kw[h][4 * w + 1], tw.kw[h][4 * w + 2], tw.kw[h][4 * w + 3]};
-            }
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-              const u32x4 y = {q[nb][4 * w], q[nb][4 * w + 1], q[nb][4 * w + 2],
-                               q[nb][4 * w + 3]};
-              s[nb][h] = mma16(__builtin_bit_cast(V8, x), __builtin_bit_cast(V8, y), s[nb][h]);
-            }
-          }
-        }
+      for (int y = 0; y < DEPTH; ++y) {
+        now[y] = raw[y].next;
+        na[y] = page_of(now[y], raw[y].next_a);
+        nb_[y] = TK == 32 ? page_of(now[y] + 16, raw[y].next_b) : na[y];
+        aim(raw[y], tile + (y + 2 * DEPTH) * kWaves);
       }
-      load_k(tw, now, na, nb_);
-
-      // --- masks: only where a row does not see every key of the tile ---
-      const bool edge = key0 + TK > min_seen || !tw.there_a || !tw.there_b;
-      const bool here = v_half ? tw.there_b : tw.there_a;
+      // --- scores ---
+      f32x4 s[DEPTH][NB][NH];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int h = 0; h < NH; ++h)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) s[nb][h][r] *= a.scale;
-      if (edge) {
+      for (int y = 0; y < DEPTH; ++y) {
+        Raw& tw = raw[y];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int h = 0; h < NH; ++h)
+          for (int h = 0; h < NH; ++h) s[y][nb][h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (!(here && key0 + KPL * k + 4 * h + r < seen[nb])) s[nb][h][r] = -INFINITY;
-        // V rows that no row sees are left out ...
-#pragma unroll
-        for (int j = 0; j < KPL; ++j)
-          if (!(here && key0 + KPL * k + j < max_seen)) {
-#pragma unroll
-            for (int w = 0; w < L::VW; ++w) tw.vw[j][w] = 0u;
-            if constexpr (MX)
-#pragma unroll
-              for (int p = 0; p < NP; ++p) {
-                tw.vs[p][j / 4] &= ~(255u << (8 * (j % 4)));
-                tw.vs[p][j / 4] |= 127u << (8 * (j % 4));
-              }
-          }
-        // ... and where only some rows see a tile's keys, infinities and NaN,
-        // which a weight of 0 does not take out (0 * infinity), are zeroed here
-        // and added at the end to the rows that see them.
-        if (min_seen < max_seen && key0 + TK > min_seen) {
-          bool bad = false;
-#pragma unroll
-          for (int j = 0; j < KPL; ++j) {
+        for (int h = 0; h < NH; ++h) {
+          if constexpr (is_f32<T>) {
             if constexpr (MX) {
 #pragma unroll
-              for (int p = 0; p < NP; ++p)
-                if ((tw.vs[p][j / 4] >> (8 * (j % 4)) & 255u) == 255u) {
-                  bad = true;
-                  tw.vw[j][p] = 0u;
-                  tw.vs[p][j / 4] &= ~(128u << (8 * (j % 4)));
-                }
+              for (int w = 0; w < L::KW; ++w) {
+                const float scale = mx_scale(D == 256 ? tw.ks[h] >> (8 * (w / 4)) & 255u : tw.ks[h]);
+                const f32x2 a0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(tw.kw[h][w], scale, 0);
+                const f32x2 a1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(tw.kw[h][w], scale, 1);
+                const f32x2 a2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(tw.kw[h][w], scale, 2);
+                const f32x2 a3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(tw.kw[h][w], scale, 3);
+                const float x[8] = {a0[0], a0[1], a1[0], a1[1], a2[0], a2[1], a3[0], a3[1]};
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                  for (int e = 0; e < 8; ++e)
+                    s[y][nb][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                        x[e], __uint_as_float(q[nb][8 * w + e]), s[y][nb][h], 0, 0, 0);
+              }
             } else {
 #pragma unroll
-              for (int w = 0; w < L::VW; ++w) {
-                bad |= not_finite<T>(tw.vw[j][w]);
-                tw.vw[j][w] = finite_part<T>(tw.vw[j][w]);
+              for (int w = 0; w < L::KW; ++w)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+                  s[y][nb][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                      __uint_as_float(tw.kw[h][w]), __uint_as_float(q[nb][w]), s[y][nb][h], 0, 0, 0);
+            }
+          } else {
+            using V8 = typename Vec8<T>::type;
+#pragma unroll
+            for (int w = 0; w < D / 32; ++w) {
+              u32x4 x;
+              if constexpr (MX) {
+                const float scale = mx_scale(D == 256 ? tw.ks[h] >> (8 * (w / 4)) & 255u : tw.ks[h]);
+                x = u32x4{widen2<T, 0>(tw.kw[h][w], scale), widen2<T, 1>(tw.kw[h][w], scale),
+                          widen2<T, 2>(tw.kw[h][w], scale), widen2<T, 3>(tw.kw[h][w], scale)};
+              } else {
+                x = u32x4{tw.kw[h][4 * w], tw.kw[h][4 * w + 1], tw.kw[h][4 * w + 2], tw.kw[h][4 * w + 3]};
+              }
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) {
+                const u32x4 z = {q[nb][4 * w], q[nb][4 * w + 1], q[nb][4 * w + 2],
+                                 q[nb][4 * w + 3]};
+                s[y][nb][h] = mma16(__builtin_bit_cast(V8, x), __builtin_bit_cast(V8, z), s[y][nb][h]);
               }
             }
           }
-          spoilt |= bad;
         }
+        load_k(tw, now[y], na[y], nb_[y]);
+      }
+
+      // --- masks: only where a row does not see every key of the tile ---
+#pragma unroll
+      for (int y = 0; y < DEPTH; ++y) {
+        Raw& tw = raw[y];
+        const int key0 = (tile + y * kWaves) * TK;
+        const bool edge = key0 + TK > min(min_seen, end_key) || !tw.there_a || !tw.there_b;
+        const bool here = v_half ? tw.there_b : tw.there_a;
+        if (edge) {
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int h = 0; h < NH; ++h)
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                if (!(here && key0 + KPL * k + 4 * h + r < min(seen[nb], end_key))) s[y][nb][h][r] = -INFINITY;
+          // V rows that no row sees are left out ...
+#pragma unroll
+          for (int j = 0; j < KPL; ++j)
+            if (!(here && key0 + KPL * k + j < min(max_seen, end_key))) {
+#pragma unroll
+              for (int w = 0; w < L::VW; ++w) tw.vw[j][w] = 0u;
+              if constexpr (MX)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                  tw.vs[p][j / 4] &= ~(255u << (8 * (j % 4)));
+                  tw.vs[p][j / 4] |= 127u << (8 * (j % 4));
+                }
+            }
+          // ... and where only some rows see a tile's keys, infinities and NaN,
+          // which a weight of 0 does not take out (0 * infinity), are zeroed here
+          // and added at the end to the rows that see them.
+          if (min_seen < max_seen && key0 + TK > min_seen) {
+            bool bad = false;
+#pragma unroll
+            for (int j = 0; j < KPL; ++j) {
+              if constexpr (MX) {
+#pragma unroll
+                for (int p = 0; p < NP; ++p)
+                  if ((tw.vs[p][j / 4] >> (8 * (j % 4)) & 255u) == 255u) {
+                    bad = true;
+                    tw.vw[j][p] = 0u;
+                    tw.vs[p][j / 4] &= ~(128u << (8 * (j % 4)));
+                  }
+              } else {
+#pragma unroll
+                for (int w = 0; w < L::VW; ++w) {
+                  bad |= not_finite<T>(tw.vw[j][w]);
+                  tw.vw[j][w] = finite_part<T>(tw.vw[j][w]);
+                }
+              }
+            }
+            spoilt |= bad;
+          }
+        }
+
       }
 
       // --- softmax against a reference that is raised only by a score more
       // than 8 above it (in base-2 units): the weights stay below 2^8, and
       // most tiles need neither the maximum over the lanes nor a rescaling ---
-      uint32_t pw[NB][NH * 2];                   // weights, two to a word (16-bit types)
+      uint32_t pw[DEPTH][NB][NH * 2];            // weights, two to a word (16-bit types)
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        float top = s[nb][0][0];
+        float top = s[0][nb][0][0];
 #pragma unroll
-        for (int h = 0; h < NH; ++h)
+        for (int y = 0; y < DEPTH; ++y)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) top = fmaxf(top, s[nb][h][r]);
+          for (int h = 0; h < NH; ++h)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, s[y][nb][h][r]);
+        top *= a.scale;
         // (a NaN among only NaN becomes the reference, and spoils the row)
         if (__any(!(top <= limit[nb]))) {
           top = fmaxf(top, __shfl_xor(top, 16));
@@ -1231,77 +1250,76 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
           }
         }
 #pragma unroll
-        for (int h = 0; h < NH; ++h) {
+        for (int y = 0; y < DEPTH; ++y)
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            s[nb][h][r] = __builtin_amdgcn_exp2f(s[nb][h][r] - ref[nb]);
-          if constexpr (is_f32<T>) {
-            sums[nb] += s[nb][h];
-          } else {
-            pw[nb][2 * h] = pack2<T>(s[nb][h][0], s[nb][h][1]);
-            pw[nb][2 * h + 1] = pack2<T>(s[nb][h][2], s[nb][h][3]);
+          for (int h = 0; h < NH; ++h) {
+            f32x4& w = s[y][nb][h];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              w[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(w[r], a.scale, -ref[nb]));
+            if constexpr (is_f32<T>) {
+              sums[nb] += w;
+            } else {
+              pw[y][nb][2 * h] = pack2<T>(w[0], w[1]);
+              pw[y][nb][2 * h + 1] = pack2<T>(w[2], w[3]);
+            }
           }
-        }
       }
 
       // --- O^T += V^T P^T ---
-      if constexpr (is_f32<T>) {
 #pragma unroll
-        for (int p = 0; p < NP; ++p)
+      for (int y = 0; y < DEPTH; ++y) {
+        Raw& tw = raw[y];
+        if constexpr (is_f32<T>) {
 #pragma unroll
-          for (int j = 0; j < KPL; ++j) {
-            float x[VCH];
-            v_floats(tw, p, j, x);
+          for (int p = 0; p < NP; ++p)
 #pragma unroll
-            for (int c = 0; c < VCH; ++c)
+            for (int j = 0; j < KPL; ++j) {
+              float x[VCH];
+              v_floats(tw, p, j, x);
+#pragma unroll
+              for (int c = 0; c < VCH; ++c)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+                  acc[nb][VCH * p + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                      x[c], s[y][nb][j / 4][j % 4], acc[nb][VCH * p + c], 0, 0, 0);
+            }
+        } else {
+          using V8 = typename Vec8<T>::type;
+          V8 weights[NB];
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+            weights[nb] =
+                __builtin_bit_cast(V8, (u32x4{pw[y][nb][0], pw[y][nb][1], pw[y][nb][2], pw[y][nb][3]}));
+          V8 ones;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) ones[e] = (T)1.f;
+          // the sum of the weights as they are multiplied, in every lane
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) sums[nb] = mma16(ones, weights[nb], sums[nb]);
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            uint32_t x[KPL][VCH / 2];
+            v_words(tw, p, x);
+#pragma unroll
+            for (int c = 0; c < VCH; ++c) {
+              const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
+              const u32x4 col = {__builtin_amdgcn_perm(x[1][c / 2], x[0][c / 2], sel),
+                                 __builtin_amdgcn_perm(x[3][c / 2], x[2][c / 2], sel),
+                                 __builtin_amdgcn_perm(x[5][c / 2], x[4][c / 2], sel),
+                                 __builtin_amdgcn_perm(x[7][c / 2], x[6][c / 2], sel)};
 #pragma unroll
               for (int nb = 0; nb < NB; ++nb)
-                acc[nb][VCH * p + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                    x[c], s[nb][j / 4][j % 4], acc[nb][VCH * p + c], 0, 0, 0);
-          }
-      } else {
-        using V8 = typename Vec8<T>::type;
-        V8 weights[NB];
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-          weights[nb] =
-              __builtin_bit_cast(V8, (u32x4{pw[nb][0], pw[nb][1], pw[nb][2], pw[nb][3]}));
-        V8 ones;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ones[e] = (T)1.f;
-        // the sum of the weights as they are multiplied, in every lane
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) sums[nb] = mma16(ones, weights[nb], sums[nb]);
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
-          uint32_t x[KPL][VCH / 2];
-          v_words(tw, p, x);
-#pragma unroll
-          for (int c = 0; c < VCH; ++c) {
-            const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
-            const u32x4 col = {__builtin_amdgcn_perm(x[1][c / 2], x[0][c / 2], sel),
-                               __builtin_amdgcn_perm(x[3][c / 2], x[2][c / 2], sel),
-                               __builtin_amdgcn_perm(x[5][c / 2], x[4][c / 2], sel),
-                               __builtin_amdgcn_perm(x[7][c / 2], x[6][c / 2], sel)};
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-              acc[nb][VCH * p + c] =
-                  mma16(__builtin_bit_cast(V8, col), weights[nb], acc[nb][VCH * p + c]);
+                acc[nb][VCH * p + c] =
+                    mma16(__builtin_bit_cast(V8, col), weights[nb], acc[nb][VCH * p + c]);
+            }
           }
         }
+        load_v(tw, now[y], na[y], nb_[y]);
+        tw.there_a = na[y] >= 0, tw.there_b = nb_[y] >= 0;
       }
-      load_v(tw, now, na, nb_);
-      tw.there_a = na >= 0, tw.there_b = nb_ >= 0;
     };
-    while (wt < wt_end) {
-      process(raw[0], wt);
-      wt += kWaves;
-      if constexpr (DEPTH == 2) {
-        if (wt >= wt_end) break;
-        process(raw[1], wt);
-        wt += kWaves;
-      }
-    }
+    for (; wt < wt_end; wt += DEPTH * kWaves) process(wt);
 
     // --- the four waves' states, one column block at a time ---
     const bool whole = t0 == 0 && t1 == at.tiles;
@@ -1491,7 +1509,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
                      (int64_t)(head * a.G + g) * D + 8 * k;
 #pragma unroll
       for (int w = 0; w < NQ; ++w)
-        q[w] = my_rows ? *reinterpret_cast<const u32x4*>(src + 16 * w) : u32x4{0u, 0u, 0u, 0u};
+        q[w] = my_rows ? (*reinterpret_cast<const u32x4*>(src + 16 * w) & a.q_keep) ^ a.q_flip
+                       : u32x4{0u, 0u, 0u, 0u};
     }
 
     f32x16 acc[ND];
@@ -1602,7 +1621,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           if constexpr (MX) {
-            const float scale = mx_scale(raw_scale[j / 4] >> (8 * (j % 4)) & 255u);
+            const float scale = mx_scale_of(raw_scale[j / 4], j);
             const uint32_t codes = raw[j / 4][j % 4];
             x[j] = u32x4{widen2<T, 0>(codes, scale), widen2<T, 1>(codes, scale),
                          widen2<T, 2>(codes, scale), widen2<T, 3>(codes, scale)};
@@ -1671,10 +1690,6 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
             const u32x4 x = s_k[buf][k_row + 32 * n][(2 * w + k) ^ k_turn(k_row)];
             s[n] = mma32(__builtin_bit_cast(V8, x), __builtin_bit_cast(V8, q[w]), s[n]);
           }
-#pragma unroll
-        for (int n = 0; n < NS; ++n)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[n][r] *= a.scale;
         if (key0 + KT > my_min || pages_here != (1 << NE) - 1) {
 #pragma unroll
           for (int n = 0; n < NS; ++n)
@@ -1690,6 +1705,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
         for (int n = 0; n < NS; ++n)
 #pragma unroll
           for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
+        top *= a.scale;
         if (__any(!(top <= limit))) {
           top = fmaxf(top, __shfl_xor(top, 32));
           if (!(top <= limit)) {
@@ -1705,7 +1721,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - ref);
+          for (int r = 0; r < 16; ++r)
+            s[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], a.scale, -ref));
           float part = 0.f;
 #pragma unroll
           for (int r = 0; r < 16; ++r) part += s[n][r];
@@ -2141,7 +2158,9 @@ da_status da_paged_attn(const da_paged_kv* kv, const void* q, int64_t q_stride, 
   const AttnArgs a{q,
                    out,
                    q_stride,
-                   scale * kLog2e,
+                   scale == 0.f ? 1.f : std::fabs(scale) * kLog2e,
+                   scale == 0.f ? 0u : ~0u,
+                   scale < 0.f ? (p.dtype == DA_F32 ? 0x80000000u : 0x80008000u) : 0u,
                    h_q,
                    h_q / p.h_kv,
                    causal,
