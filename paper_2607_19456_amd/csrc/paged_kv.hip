@@ -107,8 +107,9 @@ __device__ __forceinline__ int64_t block_bytes(int page_log2) {
 }
 
 // ---------------------------------------------------------------------------
-// Append: one thread turns and writes 8 dimensions of one head of one row.
-// Memory-bound: 6 operations for each pair of values that it reads and writes.
+// Append: one thread turns and writes 16 dimensions of one head of one row (8
+// of a 4-bit row, whose blocks of 32 are then four lanes' work).  Memory-bound: 6
+// operations for each pair of values that it reads and writes.
 // ---------------------------------------------------------------------------
 template <class T>
 __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
@@ -147,11 +148,11 @@ struct AppendArgs {
   int h_q, rot_dim, interleaved;
 };
 
-// Dimensions 8*piece .. +7 of a row after the rotation, in W (the type of the
-// products and sums).
-template <class T, class W>
+// Dimensions 8*piece .. +7 of a row after the rotation, in 64 bits.
+template <class T>
 __device__ __forceinline__ void turned8(const T* row, int piece, const AppendArgs& a,
-                                        const float* angles, W (&y)[8]) {
+                                        const float* angles, double (&y)[8]) {
+  typedef double W;
   float x[8];
   load8(row + 8 * piece, x);
   const int half = a.rot_dim / 2;
@@ -202,8 +203,7 @@ __device__ __forceinline__ float to_odd(float y) { return y; }
 __device__ __forceinline__ float power_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // Codes and scale byte of 8 values whose block of 32 lies in four lanes in
-// turn.  The block's largest exponent is found on the bits; the codes count
-// the levels' midpoints that a value has passed, ties to the even code.
+// turn.  The block's largest exponent is found on the bits.
 template <class W>
 __device__ __forceinline__ uint32_t quantise8(const W (&y)[8], uint32_t* scale_byte) {
   float f[8];
@@ -221,23 +221,14 @@ __device__ __forceinline__ uint32_t quantise8(const W (&y)[8], uint32_t* scale_b
   }
   const int byte = max((int)(top >> 23) - 2, 1);
   *scale_byte = (uint32_t)byte;
-  // 2^-(byte - 127) in two factors, either of them a normal number
-  const float down = power_of((uint32_t)(254 - max(byte, 127)));
-  const float up = power_of((uint32_t)(254 - min(byte, 127)));
+  // the conversion divides by the scale, rounds to the nearest level, ties to
+  // the even code, and stops at the largest
+  const float scale = power_of((uint32_t)byte);
   uint32_t codes = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float z = fabsf(f[e]) * down * up;
-    uint32_t c = z > 0.25f;
-    c += z >= 0.75f;
-    c += z > 1.25f;
-    c += z >= 1.75f;
-    c += z > 2.5f;
-    c += z >= 3.5f;
-    c += z > 5.f;
-    codes |= (c | (__float_as_uint(f[e]) >> 31) << 3) << (4 * e);
-  }
-  return codes;
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[0], f[1], scale, 0);
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[2], f[3], scale, 1);
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[4], f[5], scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[6], f[7], scale, 3);
 }
 
 // Offsets of a 4-bit row's codes and scale bytes in its page.
@@ -253,34 +244,70 @@ __device__ __forceinline__ int64_t mx_scale_at(bool value, int page_log2, int sl
                 : (int64_t)slot * (D / 32) + block);
 }
 
+// Unit u (of D/16) of a row into dst, where dst may be src: 16 dimensions, and
+// of a rotated part both of each pair, so that the angles are read once for two
+// values and nobody else reads what is written.
+template <class T>
+__device__ __forceinline__ void turn16(const T* src, T* dst, int u, const AppendArgs& a,
+                                       const float* angles, bool rotate) {
+  const int half = a.rot_dim / 2;
+  const bool turn = rotate && 16 * u < a.rot_dim;
+  const bool pairs = turn && !a.interleaved;          // dimensions 8u.. and half + 8u..
+  const int at1 = pairs ? 8 * u : 16 * u, at2 = pairs ? half + 8 * u : 16 * u + 8;
+  float x[8], y[8];
+  load8(src + at1, x);
+  load8(src + at2, y);
+  if (turn) {
+    float c[8], s[8];
+    load8(angles + 8 * u, c);
+    load8(angles + half + 8 * u, s);
+    if (pairs) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x1 = x[e], x2 = y[e];
+        x[e] = x1 * c[e] - x2 * s[e];
+        y[e] = x2 * c[e] + x1 * s[e];
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float(&z)[8] = e < 4 ? x : y;
+        const float x1 = z[2 * e % 8], x2 = z[2 * e % 8 + 1];
+        z[2 * e % 8] = x1 * c[e] - x2 * s[e];
+        z[2 * e % 8 + 1] = x2 * c[e] + x1 * s[e];
+      }
+    }
+  }
+  store8(dst + at1, x);
+  store8(dst + at2, y);
+}
+
 template <class T, bool MX, int D>
 __global__ __launch_bounds__(kThreads) void paged_append_kernel(Batch bt, AppendArgs a,
                                                                 unsigned seq_groups) {
-  constexpr int kPieces = D / 8;
+  constexpr int kPairs = D / 16;                      // units of a row of q, and of dense ones
+  constexpr int kPieces = MX ? D / 8 : kPairs;        // units of a row of K or V
   const int b = blockIdx.x / seq_groups;
   const SeqRows sr = seq_rows(bt, b);
-  const int per_row = (a.h_q + 2 * bt.h_kv) * kPieces;
-  const int64_t unit = (int64_t)(blockIdx.x % seq_groups) * kThreads + threadIdx.x;
-  const int r = (int)(unit / per_row);
+  const int of_q = a.h_q * kPairs, per_row = of_q + 2 * bt.h_kv * kPieces;
+  const uint32_t unit = blockIdx.x % seq_groups * kThreads + threadIdx.x;
+  const int r = (int)(unit / (uint32_t)per_row);
   if (r >= sr.n) return;
   const int past = bt.past[b];
   if (past < 0 || past >= capacity(bt) - r) return;
   const int pos = past + r;
-  const int u = (int)(unit - (int64_t)r * per_row);
-  const int piece = u % kPieces;
-  int head = u / kPieces;
+  int u = (int)(unit - (uint32_t)r * (uint32_t)per_row);
   const int64_t row = sr.start + r;
   const float* angles = a.rotary + (int64_t)pos * a.rot_dim;
-  if (head < a.h_q) {
-    float y[8];
-    turned8<T, float>(static_cast<const T*>(a.q) + row * a.q_stride + (int64_t)head * D, piece, a,
-                      angles, y);
-    // Where q_out is q, another lane of this wave may still read what is
-    // written here: all lanes of a head are in one wave, and have loaded.
-    store8(static_cast<T*>(a.q_out) + (row * a.h_q + head) * D + 8 * piece, y);
+  if (u < of_q) {
+    const int head = u / kPairs;
+    turn16(static_cast<const T*>(a.q) + row * a.q_stride + (int64_t)head * D,
+           static_cast<T*>(a.q_out) + (row * a.h_q + head) * D, u % kPairs, a, angles, true);
     return;
   }
-  head -= a.h_q;
+  u -= of_q;
+  const int piece = u % kPieces;
+  int head = u / kPieces;
   const bool value = head >= bt.h_kv;
   if (value) head -= bt.h_kv;
   const int page = bt.pages[(int64_t)b * bt.max_pages + (pos >> bt.page_log2)];
@@ -300,20 +327,14 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(Batch bt, Append
       codes = quantise8(y, &scale);
     } else {
       double y[8];
-      turned8<T, double>(src, piece, a, angles, y);
+      turned8(src, piece, a, angles, y);
       codes = quantise8(y, &scale);
     }
     *reinterpret_cast<uint32_t*>(block + mx_code_at<D>(value, slot, piece)) = codes;
     if (piece % 4 == 0)
       block[mx_scale_at<D>(value, bt.page_log2, slot, piece / 4)] = (char)scale;
   } else {
-    T* dst = reinterpret_cast<T*>(block) + (int64_t)slot * D + 8 * piece;
-    float y[8];
-    if (value)
-      load8(src + 8 * piece, y);
-    else
-      turned8<T, float>(src, piece, a, angles, y);
-    store8(dst, y);
+    turn16(src, reinterpret_cast<T*>(block) + (int64_t)slot * D, piece, a, angles, !value);
   }
 }
 
@@ -328,10 +349,10 @@ __global__ __launch_bounds__(kThreads) void paged_gather_kernel(Batch bt, void* 
   const int b = blockIdx.x / seq_groups;
   const SeqRows sr = seq_rows(bt, b);
   const int per_row = 2 * bt.h_kv * kPieces;
-  const int64_t unit = (int64_t)(blockIdx.x % seq_groups) * kThreads + threadIdx.x;
-  const int r = (int)(unit / per_row);
+  const uint32_t unit = blockIdx.x % seq_groups * kThreads + threadIdx.x;
+  const int r = (int)(unit / (uint32_t)per_row);
   if (r >= sr.n) return;
-  const int u = (int)(unit - (int64_t)r * per_row);
+  const int u = (int)(unit - (uint32_t)r * (uint32_t)per_row);
   const int piece = u % kPieces;
   int head = u / kPieces;
   const bool value = head >= bt.h_kv;
@@ -2080,7 +2101,9 @@ da_status da_paged_append(const da_paged_kv* kv, const void* k_new, const void* 
   const AppendArgs a{q,        k_new,    v_new,  q_out, q_stride, k_stride,
                      v_stride, rotary, h_q, rot_dim, interleaved};
   const Batch bt = device_batch(p);
-  const int64_t units = (int64_t)p.T * (h_q + 2 * (int64_t)p.h_kv) * (p.d / 8);
+  const int64_t units =
+      (int64_t)p.T * ((int64_t)h_q * (p.d / 16) +
+                      2 * (int64_t)p.h_kv * (p.d / (p.format == DA_KV_MX4 ? 8 : 16)));
   const int64_t groups = ceil_div(units, kThreads);
   if (groups > kMaxGroups || groups * p.B > kMaxGroups) return DA_ERR_SHAPE;
   (void)hipGetLastError();
