@@ -397,8 +397,8 @@ __global__ __launch_bounds__(kThreads) void paged_gather_kernel(Batch bt, void* 
 // Items.  An item is (sequence, KV head, tile of up to R = 16*NB query rows);
 // row x of a KV head's rows is (token x / G, query head x % G of the group), so
 // a tile's rows see nearly the same keys.  An item's keys are cut into tiles of
-// KT = 4*TK, and all items' tiles, laid end to end (sequences, heads, row
-// tiles), are divided evenly over the resident workgroups, which count for
+// KT = 4*TK, and all items' costs (kItemCost), laid end to end (sequences, heads,
+// row tiles), are divided evenly over the resident workgroups, which count for
 // themselves, from past and row_start, where each one's share begins.  A workgroup begins and ends inside at most
 // one item each; those parts go to its two slots of the workspace, the rest
 // straight to out.  The parts of an item are then those of consecutive
@@ -541,8 +541,8 @@ __device__ __forceinline__ int seen_by(const Batch& bt, const AttnArgs& a, int p
   return past >= cap - t - 1 ? cap : past + t + 1;
 }
 
-// Row tiles of a sequence (each of R rows; one where not MANY), tiles of keys of
-// one of them, and of all of them (for one KV head).
+// Row tiles of a sequence (each of R rows; one where not MANY), and tiles of keys
+// of one of them.
 template <int R, bool MANY>
 __device__ __forceinline__ int row_tiles(const AttnArgs& a, int n) {
   return MANY ? (n * a.G + R - 1) / R : n > 0;
@@ -554,12 +554,22 @@ __device__ __forceinline__ int key_tiles(const Batch& bt, const AttnArgs& a, int
   if (MANY && (rt + 1) * R < n * a.G) t = token_of(a, (rt + 1) * R - 1);
   return (seen_by(bt, a, past, t) + KT - 1) / KT;
 }
+
+// An item costs its tiles and, for the loads before the first and the exchange
+// after the last, as much as kItemCost tiles: what the workgroups share out is
+// cost, and every item begins with its fixed part.  (Measured: 4 to 6 us an item,
+// 1.7 to 2.7 us a tile.  256 items of 1 to 12 tiles take 50 us if this is left
+// out and 33 with 1 to 3; 8 sequences of 15 rows a head over 500 to 4000 keys 43,
+// 42, 39 and 39 us with 0, 1, 2 and 3.)
+constexpr int kItemCost = 3;
+
 template <int R, int KT, bool MANY>
-__device__ __forceinline__ int64_t head_tiles(const Batch& bt, const AttnArgs& a, int past, int n) {
+__device__ __forceinline__ int64_t head_cost(const Batch& bt, const AttnArgs& a, int past, int n) {
   const int nr = row_tiles<R, MANY>(a, n);
-  if (nr == 0) return 0;
-  if (!MANY || !a.causal) return (int64_t)nr * key_tiles<R, KT, MANY>(bt, a, past, n, 0);
-  int64_t sum = 0;
+  const int one = nr ? key_tiles<R, KT, MANY>(bt, a, past, n, 0) : 0;
+  if (one == 0) return 0;                    // (the first row sees least: so it is with all)
+  if (!MANY || !a.causal) return (int64_t)nr * (one + kItemCost);
+  int64_t sum = (int64_t)nr * kItemCost;
   for (int rt = 0; rt < nr; ++rt) sum += key_tiles<R, KT, MANY>(bt, a, past, n, rt);
   return sum;
 }
@@ -590,8 +600,8 @@ __device__ __forceinline__ int wave_scan(int x) {
   return x;
 }
 
-// The workgroup that takes tile x where each takes `each`, the first `more` one
-// more.
+// The workgroup that takes unit x of the cost where each takes `each`, the first
+// `more` one more.
 __device__ __forceinline__ int owner_of(int64_t x, int64_t each, int more) {
   const int64_t big = more * (each + 1);
   return (int)(x < big ? quotient(x, each + 1) : more + quotient(x - big, each));
@@ -604,13 +614,13 @@ struct Division {
   int run;                    // sequences of a lane
   int past;                   // the lane's sequence's, where that is one
   SeqRows sr;
-  int64_t before, upto;       // tiles before the lane's run and up to its end
-  int64_t total, each;        // all tiles; workgroup w takes each, the first
-  int share, more;            //   `more` ones one more; share of them have work
+  int64_t before, upto;       // cost before the lane's run and up to its end
+  int64_t total, each;        // all cost; workgroup w takes each, the first
+  int share, more;            //   `more` ones one more; share of them have some
   bool blind;                 // a sequence of the lane's run sees nothing
 
-  __device__ __forceinline__ static int64_t tiles_of(const Batch& bt, const AttnArgs& a, int b) {
-    return bt.h_kv * head_tiles<R, KT, MANY>(bt, a, bt.past[b], seq_rows(bt, b).n);
+  __device__ __forceinline__ static int64_t cost_of(const Batch& bt, const AttnArgs& a, int b) {
+    return bt.h_kv * head_cost<R, KT, MANY>(bt, a, bt.past[b], seq_rows(bt, b).n);
   }
   __device__ __forceinline__ void count(const Batch& bt, const AttnArgs& a, int lane) {
     run = (bt.B + 63) / 64;
@@ -622,13 +632,13 @@ struct Division {
       if (lane < bt.B) {
         past = bt.past[lane];
         sr = seq_rows(bt, lane);
-        mine = bt.h_kv * head_tiles<R, KT, MANY>(bt, a, past, sr.n);
+        mine = bt.h_kv * head_cost<R, KT, MANY>(bt, a, past, sr.n);
         blind = mine == 0;
       }
     } else {
       const int lo = min(lane * run, bt.B), hi = min(lo + run, bt.B);
       for (int b = lo; b < hi; ++b) {
-        const int64_t n = tiles_of(bt, a, b);
+        const int64_t n = cost_of(bt, a, b);
         blind |= n == 0;
         mine += n;
       }
@@ -668,22 +678,48 @@ struct Walk {
   int tiles, t0, t1;          // its key tiles; those taken are t0 .. t1-1
   int past;
   SeqRows sr;
-  int64_t left;               // tiles to take, from t0 on
-  int64_t at;                 // t0's number among all tiles
   int first;                  // the workgroup of the item's first part, if another
-  bool fresh;                 // the workgroup's first item
-  int64_t each;               // of the division
+  bool fresh;                 // the workgroup's first part
+  // The division: where the item's cost begins, what of it lies before the
+  // workgroup's, and how much the workgroup still takes from there on.
+  int64_t start, skip, left, each;
   int more;
 
-  // The part's end.  All of these are the same in every lane, and said to be:
-  // addresses and branches made of them then stay with the scalar unit.
+  // The part.  All of these are the same in every lane, and said to be: addresses
+  // and branches made of them then stay with the scalar unit.
   __device__ __forceinline__ void cut() {
-    left = lane_value(left, 0), at = lane_value(at, 0), each = lane_value(each, 0);
-    more = uniform(more);
+    left = lane_value(left, 0), skip = lane_value(skip, 0), start = lane_value(start, 0);
+    each = lane_value(each, 0), more = uniform(more);
     b = uniform(b), head = uniform(head), rt = uniform(rt);
-    tiles = uniform(tiles), t0 = uniform(t0), past = uniform(past);
+    tiles = uniform(tiles), past = uniform(past);
     sr = {uniform(sr.start), uniform(sr.n)};
-    t1 = uniform((int)min((int64_t)tiles, t0 + left));
+    t0 = uniform((int)max(skip - kItemCost, (int64_t)0));
+    t1 = uniform((int)max(min((int64_t)tiles, skip + left - kItemCost), (int64_t)0));
+  }
+  // The next item that has tiles (there is one while left > 0).
+  __device__ __forceinline__ void forward(const Batch& bt, const AttnArgs& a) {
+    const int64_t used = min(tiles + kItemCost - skip, left);
+    left -= used;
+    if (left <= 0) return;
+    start += tiles + kItemCost;
+    skip = 0;
+    tiles = 0;
+    while (tiles == 0) {
+      if (++rt >= row_tiles<R, MANY>(a, sr.n)) {
+        rt = 0;
+        if (++head >= bt.h_kv) {
+          head = 0;
+          sr = one_seq_rows(bt, ++b);
+          past = fixed(bt.past + b);
+          if (sr.n == 0) {
+            head = bt.h_kv - 1;
+            continue;
+          }
+        }
+      }
+      tiles = key_tiles<R, KT, MANY>(bt, a, past, sr.n, rt);
+    }
+    cut();
   }
   // Whether the workgroup has work.  Rows of sequences that see nothing, which
   // are in no item, are zeroed here.
@@ -694,10 +730,10 @@ struct Walk {
     const int w = blockIdx.x;
     uint64_t blind = __ballot(d.blind);
     while (blind) {
-      const int first = (__ffsll((unsigned long long)blind) - 1) * d.run;
+      const int from = (__ffsll((unsigned long long)blind) - 1) * d.run;
       blind &= blind - 1;
-      for (int x = first; x < min(first + d.run, bt.B); ++x) {
-        if (x % a.grid != w || Division<R, KT, MANY>::tiles_of(bt, a, x)) continue;
+      for (int x = from; x < min(from + d.run, bt.B); ++x) {
+        if (x % a.grid != w || Division<R, KT, MANY>::cost_of(bt, a, x)) continue;
         const SeqRows zr = seq_rows(bt, x);
         T* dst = static_cast<T*>(a.out) + (int64_t)zr.start * a.h_q * d_head;
         for (int64_t e = threadIdx.x; e < (int64_t)zr.n * a.h_q * d_head; e += kThreads)
@@ -706,38 +742,41 @@ struct Walk {
           a.closing[x * bt.h_kv + threadIdx.x].first = -1;
       }
     }
-    if (w >= d.share) {
-      if (!a.arrived && !a.by_item && threadIdx.x == 0) a.closing[w].first = -1;
-      return false;
-    }
-    const int64_t lo = d.begin_of(w);
-    left = d.each + (w < d.more ? 1 : 0);
-    const int in = __ffsll((unsigned long long)__ballot(d.upto > lo)) - 1;
-    int64_t rem = lo - lane_value(d.before, in);
-    b = in * d.run;
-    at = lo, each = d.each, more = d.more;
-    sr = d.rows_of(bt, b);
-    past = d.past_of(bt, b);
-    int64_t per_head = head_tiles<R, KT, MANY>(bt, a, past, sr.n);
-    while (rem >= bt.h_kv * per_head) {          // (ends: d.upto > lo)
-      rem -= bt.h_kv * per_head;
-      sr = d.rows_of(bt, ++b);
-      past = d.past_of(bt, b);
-      per_head = head_tiles<R, KT, MANY>(bt, a, past, sr.n);
-    }
-    head = (int)quotient(rem, per_head);
-    rem -= head * per_head;
-    rt = 0;
-    tiles = key_tiles<R, KT, MANY>(bt, a, past, sr.n, 0);
-    while (rem >= tiles) {
-      rem -= tiles;
-      tiles = key_tiles<R, KT, MANY>(bt, a, past, sr.n, ++rt);
-    }
-    t0 = (int)rem;
-    cut();
     fresh = true;
-    first = t0 ? uniform(d.owner(lo - t0)) : -1;
-    return true;
+    first = -1;
+    left = 0;
+    if (w < d.share) {
+      const int64_t lo = d.begin_of(w);
+      left = d.each + (w < d.more ? 1 : 0);
+      const int in = __ffsll((unsigned long long)__ballot(d.upto > lo)) - 1;
+      int64_t rem = lo - lane_value(d.before, in);
+      b = in * d.run;
+      each = d.each, more = d.more;
+      sr = d.rows_of(bt, b);
+      past = d.past_of(bt, b);
+      int64_t per_head = head_cost<R, KT, MANY>(bt, a, past, sr.n);
+      while (rem >= bt.h_kv * per_head) {        // (ends: d.upto > lo)
+        rem -= bt.h_kv * per_head;
+        sr = d.rows_of(bt, ++b);
+        past = d.past_of(bt, b);
+        per_head = head_cost<R, KT, MANY>(bt, a, past, sr.n);
+      }
+      head = (int)quotient(rem, per_head);
+      rem -= head * per_head;
+      rt = 0;
+      tiles = key_tiles<R, KT, MANY>(bt, a, past, sr.n, 0);
+      while (rem >= tiles + kItemCost) {
+        rem -= tiles + kItemCost;
+        tiles = key_tiles<R, KT, MANY>(bt, a, past, sr.n, ++rt);
+      }
+      skip = rem;
+      start = lo - rem;
+      cut();
+      while (left > 0 && t0 >= t1) forward(bt, a);       // (only the fixed part of an item)
+      if (left > 0 && t0 > 0) first = uniform(d.owner(start + kItemCost));
+    }
+    if (left <= 0 && !a.arrived && !a.by_item && threadIdx.x == 0) a.closing[w].first = -1;
+    return left > 0;
   }
   // What the merge is told: of every item that ends here, or (by workgroup) of
   // the first, the only one that may have begun elsewhere.
@@ -750,33 +789,16 @@ struct Walk {
   }
   // The workgroup of the item's last part.
   __device__ __forceinline__ int last() const {
-    return t1 == tiles ? (int)blockIdx.x : uniform(owner_of(at - t0 + tiles - 1, each, more));
+    return t1 == tiles ? (int)blockIdx.x
+                       : uniform(owner_of(start + kItemCost + tiles - 1, each, more));
   }
   __device__ __forceinline__ bool next(const Batch& bt, const AttnArgs& a) {
-    at += t1 - t0;
-    left -= t1 - t0;
-    if (left <= 0) return false;
-    t0 = 0;
-    tiles = 0;
-    while (tiles == 0) {
-      if (++rt >= row_tiles<R, MANY>(a, sr.n)) {
-        rt = 0;
-        if (++head >= bt.h_kv) {
-          head = 0;
-          sr = one_seq_rows(bt, ++b);
-          past = fixed(bt.past + b);
-          if (sr.n == 0) {                       // (a later sequence has tiles: left > 0)
-            head = bt.h_kv - 1;
-            continue;
-          }
-        }
-      }
-      tiles = key_tiles<R, KT, MANY>(bt, a, past, sr.n, rt);
-    }
-    cut();
     fresh = false;
     first = -1;
-    return true;
+    do {
+      forward(bt, a);
+    } while (left > 0 && t0 >= t1);
+    return left > 0;
   }
 };
 
@@ -2163,8 +2185,8 @@ da_status da_paged_attn(const da_paged_kv* kv, const void* q, int64_t q_stride, 
   const Batch bt = device_batch(p);
   const int grid = device_cus() * kGroupsPerCu;
   const int64_t row_tiles = ceil_div((int64_t)(h_q / p.h_kv) * p.T, plan.R);
-  const int few_tiles =
-      (double)p.B * p.h_kv * row_tiles * ceil_div((int64_t)p.max_pages * p.page_rows, 32) < 2e9;
+  const int64_t most_tiles = ceil_div((int64_t)p.max_pages * p.page_rows, 32) + kItemCost;
+  const int few_tiles = (double)p.B * p.h_kv * row_tiles * most_tiles < 2e9;
   // Items of few rows and few parts are put together by the workgroups that have
   // them: one launch for two (one sequence of 700 rows 10.6 -> 9.5 us, 16 of
   // 200-4000 30.8 -> 30.0; but with tiles of 32 rows 52.6 -> 56.6, of 128 rows
