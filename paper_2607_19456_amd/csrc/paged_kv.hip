@@ -825,7 +825,7 @@ __device__ __forceinline__ f32x2 load_part(const float* p) {
 // thread.  Every wave waits until its stores are in memory before the workgroup
 // is counted.
 template <class T, int D, int R, class W>
-__device__ __forceinline__ void finish(const Batch& bt, const AttnArgs& a, const W& at) {
+__device__ __forceinline__ void finish(const AttnArgs& a, const W& at) {
   __shared__ unsigned s_arrived;
   const int first = at.t0 ? at.first : (int)blockIdx.x;
   const int n = at.last() - first + 1;
@@ -1456,7 +1456,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
       }
     }
     if constexpr (NB == 1)
-      if (a.arrived && !whole) finish<T, D, R>(bt, a, at);
+      if (a.arrived && !whole) finish<T, D, R>(a, at);
   } while (at.next(bt, a));
 }
 

@@ -230,6 +230,51 @@ def test_equal_calls_give_equal_bits(cuda_device, dtype, T, B, past):
                scale=0.09, q=q.cpu())
 
 
+def test_the_last_to_finish_has_all_parts(cuda_device):
+    """Many calls one after the other, each with new queries, the parts of a row on
+    different workgroups: all as from a workspace of their own."""
+    past = [int(x) for x in np.random.default_rng(9).integers(100, 1500, 40)]
+    c = ref.Cache(3, "bf16", "dense", 64, 4, 64, [p + 1 for p in past])
+    K, V, pages = c.to(cuda_device)
+    dpast = torch.tensor(past, dtype=torch.int32, device=cuda_device)
+    qs = torch.randn(60, 40, 16, 64, device=cuda_device).bfloat16()
+    ws = lib.paged_workspace(qs[0], K, pages)
+    got = torch.stack([lib.paged_attn(q, K, V, pages, dpast, 0.1, workspace=ws) for q in qs])
+    want = torch.stack([lib.paged_attn(q, K, V, pages, dpast, 0.1) for q in qs])
+    assert torch.equal(got, want)
+
+
+def test_calls_on_two_streams(cuda_device):
+    """Two calls at once, each with its own workspace."""
+    c = ref.Cache(5, "f16", "mx4", 128, 2, 32, [700, 300, 900])
+    K, V, pages = c.to(cuda_device)
+    past = torch.tensor([699, 299, 899], dtype=torch.int32, device=cuda_device)
+    q = torch.randn(2, 3, 16, 128, device=cuda_device).half()
+    want = [lib.paged_attn(x, K, V, pages, past, 0.09) for x in q]
+    ws = [lib.paged_workspace(q[0], K, pages) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(20):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(lib.paged_attn(q[i], K, V, pages, past, 0.09, workspace=ws[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(x, want[i]) for x in got[i])
+
+
+@pytest.mark.parametrize("P", [16, 64, 256])
+@pytest.mark.parametrize("dtype,fmt,d", [("bf16", "dense", 128), ("f16", "dense", 64),
+                                         ("bf16", "mx4", 128), ("f16", "mx4", 256),
+                                         ("f16", "dense", 256), ("bf16", "mx4", 64)])
+def test_chunks_over_page_sizes(cuda_device, dtype, fmt, d, P):
+    """Many rows a head: row tiles that end inside a token and inside a page."""
+    check_attn(cuda_device, dtype=dtype, fmt=fmt, d=d, h_q=10, h_kv=2, P=P,
+               past=[300, 0, 63], T=90, counts=[90, 77, 1], seed=P + d)
+
+
 def test_queries_with_a_stride_and_another_stream(cuda_device):
     """q as a view into a fused projection, the call on a stream of its own."""
     c = ref.Cache(12, "f16", "dense", 64, 2, 16, [90, 41])
@@ -422,6 +467,25 @@ def test_codes_of_values_of_every_size(cuda_device, dtype):
     for pool, value in ((K, False), (V, True)):
         c, s = ref.unpack_page(pool[0, 0].reshape(-1).cpu().numpy(), 16, 64, value)
         assert np.array_equal(c[:2], codes) and np.array_equal(s[:2], scales)
+
+
+def test_codes_of_the_smallest_values(cuda_device):
+    """Blocks whose largest value is at, above and below the smallest scale's, and
+    next to 2^127."""
+    rng = np.random.default_rng(8)
+    tops = [2.0 ** e for e in (-149, -130, -127, -126, -125, -124, -123, -100, 100, 127)]
+    x = np.stack([rng.uniform(-1, 1, 64) * t * (1.99 if t > 1 else 1.0) for t in tops])
+    x = torch.from_numpy(x).float()[:, None]
+    K, V = lib.paged_alloc(1, 16, 1, 64, dtype=torch.float32, format="mx4", device=cuda_device)
+    pages = torch.zeros(1, 1, dtype=torch.int32, device=cuda_device)
+    past = torch.zeros(1, dtype=torch.int32, device=cuda_device)
+    lib.paged_append(K, V, pages, past, x.to(cuda_device), x.to(cuda_device))
+    codes, scales = ref.quantise(x[:, 0].double().numpy())
+    for pool, value in ((K, False), (V, True)):
+        c, s = ref.unpack_page(pool[0, 0].reshape(-1).cpu().numpy(), 16, 64, value)
+        for n, t in enumerate(tops):
+            assert np.array_equal(s[n], scales[n]), (t, s[n], scales[n])
+            assert np.array_equal(c[n], codes[n]), (t, c[n], codes[n])
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
