@@ -502,9 +502,13 @@ def _paged(K, V, pages, past, rows, d, dtype, row_start, T):
         if T == 0 and B:
             T = rows // B
         _need(rows == B * T, "without row_start every sequence has T rows: rows must be B*T")
-    return _pack_kv(K.data_ptr(), V.data_ptr(), pages.data_ptr(), past.data_ptr(), start, B,
-                    h_kv, d, n_pages, page_rows, max_pages, rows, T, code,
-                    _MX4 if mx4 else _DENSE), gpu, h_kv, T
+    try:
+        kv = _pack_kv(K.data_ptr(), V.data_ptr(), pages.data_ptr(), past.data_ptr(), start, B,
+                      h_kv, d, n_pages, page_rows, max_pages, rows, T, code,
+                      _MX4 if mx4 else _DENSE)
+    except struct.error as e:
+        raise ValueError(f"sizes and T must be integers of 32 bits: {e}") from None
+    return kv, gpu, h_kv, T
 
 
 def _paged_stream(stream, gpu) -> int:
@@ -520,6 +524,15 @@ def _fast(K, stream):
     return None
 
 
+def _empty(t, name, stream):
+    """A result like t, in memory of the stream that will write it."""
+    shape = _rows(t, name)
+    if stream is None:
+        return torch.empty(shape, dtype=t.dtype, device=t.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=t.dtype, device=t.device)
+
+
 def _rows(t, name):
     if not isinstance(t, torch.Tensor) or t.dim() != 3:
         raise ValueError(f"{name} must be [rows, heads, d]")
@@ -531,9 +544,10 @@ def paged_append(K, V, pages, past, k_new, v_new, q=None, rotary=None, interleav
     """Rows k_new, v_new [rows,h_kv,d] into the pages of positions past[b] + r, k_new
     turned by ``rotary`` [positions, rot_dim] on the way, and q [rows,h_q,d] turned
     into q_out (returned).  ``row_start`` [B+1]: each sequence's rows, at most ``T``;
-    else T rows each.  past is not changed."""
+    else T rows each.  past is not changed.  A ``q_out`` not given is allocated on
+    ``stream``."""
     if q is not None and q_out is None:
-        q_out = torch.empty(_rows(q, "q"), dtype=q.dtype, device=q.device)
+        q_out = _empty(q, "q", stream)
     fast = _fast(K, stream)
     if fast is not None:
         status = _call.append(K, V, pages, past, k_new, v_new, q, rotary, interleaved, row_start,
@@ -604,20 +618,21 @@ def paged_gather(K, V, pages, past, k_out, v_out, row_start=None, T: int = 0, st
 
 def paged_workspace_bytes(B, h_q, h_kv, d, T: int = 1, dtype=torch.bfloat16) -> int:
     """Workspace bytes of paged_attn for these sizes (0: invalid)."""
-    return int(_lib.da_paged_workspace_bytes(B, h_q, h_kv, d, T, _DTYPES[dtype]))
+    return int(_lib.da_paged_workspace_bytes(B, h_q, h_kv, d, T, _DTYPES.get(dtype, -1)))
 
 
 def paged_workspace_counter_bytes(B, h_q, h_kv, d, T: int = 1, dtype=torch.bfloat16) -> int:
     """Leading workspace bytes that must be zero before first use."""
-    return int(_lib.da_paged_workspace_counter_bytes(B, h_q, h_kv, d, T, _DTYPES[dtype]))
+    return int(_lib.da_paged_workspace_counter_bytes(B, h_q, h_kv, d, T,
+                                                     _DTYPES.get(dtype, -1)))
 
 
 def paged_workspace(q, K, pages, T: int = 0) -> torch.Tensor:
     """A workspace for paged_attn with q [rows,h_q,d] and these pools and sequences
     (T: most rows of a sequence; 0: rows / B), its counters zeroed: reusable call
     after call, by one call at a time."""
-    sizes = (pages.shape[0], q.shape[1], K.shape[1], q.shape[2], T or q.shape[0] // pages.shape[0],
-             q.dtype)
+    B = pages.shape[0]
+    sizes = (B, q.shape[1], K.shape[1], q.shape[2], T or q.shape[0] // max(B, 1), q.dtype)
     n = paged_workspace_bytes(*sizes)
     if n == 0:
         _check("da_paged_workspace_bytes", 2)
@@ -630,9 +645,10 @@ def paged_attn(q, K, V, pages, past, scale: float, causal: bool = True, row_star
                T: int = 0, out=None, workspace=None, stream=None) -> torch.Tensor:
     """out[n,h,:] = softmax(scale * q[n,h].K) V over the sequence's positions up to
     the row's own, past[b] + r (causal; append first), or over all past[b] of
-    them.  q [rows,h_q,d], any stride between tokens."""
+    them.  q [rows,h_q,d], any stride between tokens.  An ``out`` or ``workspace`` not
+    given is allocated on ``stream``."""
     if out is None:
-        out = torch.empty(_rows(q, "q"), dtype=q.dtype, device=q.device)
+        out = _empty(q, "q", stream)
     fast = _fast(K, stream) if workspace is not None else None
     if fast is not None:
         status = _call.attn(K, V, pages, past, q, scale, causal, row_start, T, out, workspace,
@@ -650,7 +666,8 @@ def paged_attn(q, K, V, pages, past, scale: float, causal: bool = True, row_star
     op = _here(out, "out", dtype, gpu)
     _need(out.shape == shape, "out must have q's shape")
     if workspace is None:
-        workspace = paged_workspace(q, K, pages, T)
+        with torch.cuda.stream(stream):        # (None: the current one)
+            workspace = paged_workspace(q, K, pages, T)
     status = _lib.da_paged_attn(
         kv, q.data_ptr(), h_q * d if q.is_contiguous() else _stride(q, "q", shape), h_q, scale,
         1 if causal else 0, op, _here(workspace, "workspace", _u8, gpu), workspace.numel(),

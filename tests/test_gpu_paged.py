@@ -293,6 +293,50 @@ def test_queries_with_a_stride_and_another_stream(cuda_device):
     assert torch.equal(got, want) and torch.equal(also, want)
 
 
+def test_what_a_call_allocates_is_of_its_stream(cuda_device):
+    """A call on a stream that need not wait for the current one, which is busy: the
+    workspace's counters are zero when it runs, and its results are not memory that
+    the current stream has still to write."""
+    c = ref.Cache(13, "bf16", "dense", 64, 2, 16, [300, 200])
+    K, V, pages = c.to(cuda_device)
+    past = torch.tensor([299, 199], dtype=torch.int32, device=cuda_device)
+    q = torch.randn(2, 8, 64, device=cuda_device).bfloat16()
+    table = lib.rotary_table(K.shape[2] * pages.shape[1], 64, device=cuda_device)
+    k = torch.randn(2, 2, 64, device=cuda_device).bfloat16()
+    want_q = lib.paged_append(K, V, pages, past, k, k, q=q, rotary=table)
+    want = lib.paged_attn(q, K, V, pages, past, 0.125)
+    n = lib.paged_workspace(q, K, pages).numel()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    busy = torch.randn(4096, 4096, device=cuda_device)
+    # blocks of these sizes that the current stream fills late, and gives back
+    late = [torch.empty(n, dtype=torch.uint8, device=cuda_device), torch.empty_like(q),
+            torch.empty_like(q)]
+    torch.cuda.synchronize()
+    for _ in range(30):
+        busy = busy @ busy * 1e-4
+    for x in late:
+        x.fill_(1)
+    del late, x
+    got = lib.paged_attn(q, K, V, pages, past, 0.125, stream=side)
+    got_q = lib.paged_append(K, V, pages, past, k, k, q=q, rotary=table, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(got_q, want_q)
+
+
+def test_sizes_that_are_not_integers_of_32_bits(cuda_device):
+    K, V = lib.paged_alloc(2, 16, 1, 64, device=cuda_device)
+    pages = torch.tensor([[0]], dtype=torch.int32, device=cuda_device)
+    past = torch.zeros(1, dtype=torch.int32, device=cuda_device)
+    start = torch.tensor([0, 1], dtype=torch.int32, device=cuda_device)
+    q = torch.zeros(1, 1, 64, dtype=torch.bfloat16, device=cuda_device)
+    for T in (1 << 40, 1.5):
+        with pytest.raises(ValueError, match="32 bits"):
+            lib.paged_append(K, V, pages, past, q, q, row_start=start, T=T)
+        with pytest.raises(ValueError, match="32 bits"):
+            lib.paged_attn(q, K, V, pages, past, 1.0, row_start=start, T=T)
+
+
 def test_pool_beyond_32_bit_offsets(cuda_device):
     """Pages at both ends of pools of 6 GiB."""
     P, h_kv, d = 256, 8, 128

@@ -137,6 +137,17 @@ def test_binding_refuses_tensors_that_are_not_on_the_gpu_or_do_not_fit():
         binding.paged_alloc(4, 16, 2, 64, dtype=torch.float64, device="cpu")
 
 
+def test_workspaces_that_are_refused():
+    K, _ = binding.paged_alloc(4, 16, 2, 64, device="cpu")
+    q = torch.zeros(3, 4, 64, dtype=torch.bfloat16)
+    for rows, sequences, t in ((q, 0, None), (q, 5, None), (q, 3, torch.float64)):
+        pages = torch.zeros(sequences, 2, dtype=torch.int32)
+        with pytest.raises(binding.DecodeAttnError):
+            binding.paged_workspace(rows.to(t) if t else rows, K, pages)
+    assert binding.paged_workspace_bytes(1, 4, 2, 64, 1, torch.int8) == 0
+    assert binding.paged_workspace_counter_bytes(1, 4, 2, 64, 1, torch.int8) == 0
+
+
 def test_pools_have_the_size_that_the_library_names():
     for dtype in (torch.float32, torch.bfloat16, torch.float16):
         for fmt in ("dense", "mx4"):
