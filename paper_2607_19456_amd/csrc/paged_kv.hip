@@ -1864,11 +1864,12 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
 }
 
 // Puts the parts of item closing[blockIdx.x] together, rows shared out over
-// blockIdx.y.  Few parts: a wave takes a row.  Many: the waves share a row's
-// parts.  Memory-bound, from the caches: 5 to 8 us after decode steps, most of it a
-// launch; 48 to 57 us after chunks of four prompts (each part 66 KB, twice a
-// workgroup).
+// blockIdx.y.  Few parts: D/4 lanes take a row.  Many: the waves share a row's
+// parts.  What bounds it: 5 us after decode steps, of which loads that wait for each
+// other are most; after chunks of four prompts 41 us, 67 MB of parts at 1.6 TB/s
+// (each part 66 KB, two a workgroup; a row a wave, by 8 bytes a lane, took 48).
 constexpr int kMergeWaves = 8;
+constexpr int merge_rows(int d) { return kMergeWaves * 256 / d; }    // rows at once, of few parts
 
 template <class T, int D, int R>
 __global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(AttnArgs a) {
@@ -1880,30 +1881,33 @@ __global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(AttnArgs 
   const int n = item.last - item.first + 1;
   const float* ml = a.parts + (int64_t)2 * a.grid * R * D;
 
-  float m, l, o[kVec];
-  auto combine = [&](int row, int from, int step) {
+  // Parts from, from + step, .. of a row, o.size() dimensions from col on, the
+  // loads of Y parts in flight at once.
+  float m, l;
+  auto combine = [&](auto& o, auto Y, int row, int col, int from, int step) {
+    constexpr int kOut = sizeof(o) / sizeof(float);
+    typedef float vec __attribute__((ext_vector_type(kOut)));
     m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) o[e] = 0.f;
-    for (int p0 = from; p0 < n; p0 += 4 * step) {
-      f32x2 s[4];
-      float v[4][kVec];
+    for (int e = 0; e < kOut; ++e) o[e] = 0.f;
+    for (int p0 = from; p0 < n; p0 += Y * step) {
+      f32x2 s[Y];
+      vec v[Y];
 #pragma unroll
-      for (int y = 0; y < 4; ++y) {
+      for (int y = 0; y < Y; ++y) {
         const int p = min(p0 + y * step, n - 1);
         const int64_t at = (int64_t)(2 * (item.first + p) + (p == 0)) * R + row;
         s[y] = *reinterpret_cast<const f32x2*>(ml + at * 2);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) v[y][e] = a.parts[at * D + lane * kVec + e];
+        v[y] = *reinterpret_cast<const vec*>(a.parts + at * D + col);
       }
 #pragma unroll
-      for (int y = 0; y < 4; ++y) {
+      for (int y = 0; y < Y; ++y) {
         if (p0 + y * step >= n || s[y][0] == -INFINITY) continue;    // saw nothing
         const float mn = s[y][0] <= m ? m : s[y][0];                 // (a NaN stays)
         const float fo = m == -INFINITY ? 0.f : exp2f(m - mn), fn = exp2f(s[y][0] - mn);
         l = l * fo + s[y][1] * fn;
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) o[e] = o[e] * fo + v[y][e] * fn;
+        for (int e = 0; e < kOut; ++e) o[e] = o[e] * fo + v[y][e] * fn;
         m = mn;
       }
     }
@@ -1914,17 +1918,29 @@ __global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(AttnArgs 
   };
 
   if (n <= 2 * kMergeWaves) {
-    for (int row = blockIdx.y * kMergeWaves + wave; row < item.in_tile;
-         row += gridDim.y * kMergeWaves) {
-      combine(row, 0, 1);
-      T* dst = out_at(row) + lane * kVec;
+    // D / 4 lanes a row, so one, two or four rows a wave
+    constexpr int kLanes = D / 4, kRows = merge_rows(D);
+    const int col = lane % kLanes * 4;
+    for (int first = blockIdx.y * kRows; first < item.in_tile; first += gridDim.y * kRows) {
+      const int row = first + wave * (64 / kLanes) + lane / kLanes;
+      const int held = min(row, item.in_tile - 1);
+      float o[4];
+      if (n == 2)
+        combine(o, std::integral_constant<int, 2>{}, held, col, 0, 1);
+      else
+        combine(o, std::integral_constant<int, 4>{}, held, col, 0, 1);
+      if (row >= item.in_tile) continue;
+      typedef T t4 __attribute__((ext_vector_type(4)));
+      t4 y;
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) dst[e] = (T)(l == 0.f ? 0.f : o[e] / l);
+      for (int e = 0; e < 4; ++e) y[e] = (T)(l == 0.f ? 0.f : o[e] / l);
+      *reinterpret_cast<t4*>(out_at(row) + col) = y;
     }
     return;
   }
+  float o[kVec];
   for (int row = blockIdx.y; row < item.in_tile; row += gridDim.y) {
-    combine(row, wave, kMergeWaves);
+    combine(o, std::integral_constant<int, 4>{}, row, lane * kVec, wave, kMergeWaves);
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < kVec; ++e) s_part[wave][lane * kVec + e] = o[e];
@@ -2085,7 +2101,7 @@ void launch_merge(const Batch& bt, const AttnArgs& a, hipStream_t s) {
   const int rows = (int)std::min<int64_t>((int64_t)a.G * bt.T, R);
   const int items = a.by_item ? bt.B * bt.h_kv : a.grid;
   const bool many = (int64_t)bt.B * bt.h_kv * kMergeWaves < a.grid;
-  const unsigned split = (unsigned)ceil_div(rows, many ? 1 : R == kChunkRows ? 16 : kMergeWaves);
+  const unsigned split = (unsigned)ceil_div(rows, many ? 1 : merge_rows(D));
   hipLaunchKernelGGL((paged_merge_kernel<T, D, R>), dim3((unsigned)items, split),
                      dim3(64 * kMergeWaves), 0, s, a);
 }
