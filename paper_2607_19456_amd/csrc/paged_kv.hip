@@ -25,6 +25,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <type_traits>
@@ -2238,7 +2239,7 @@ da_status da_paged_attn(const da_paged_kv* kv, const void* q, int64_t q_stride, 
   const AttnArgs a{q,
                    out,
                    q_stride,
-                   scale == 0.f ? 1.f : std::fabs(scale) * kLog2e,
+                   scale == 0.f ? 1.f : std::min(std::fabs(scale) * kLog2e, FLT_MAX),
                    scale == 0.f ? 0u : ~0u,
                    scale < 0.f ? (p.dtype == DA_F32 ? 0x80000000u : 0x80008000u) : 0u,
                    h_q,

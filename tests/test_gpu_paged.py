@@ -293,6 +293,21 @@ def test_queries_with_a_stride_and_another_stream(cuda_device):
     assert torch.equal(got, want) and torch.equal(also, want)
 
 
+@pytest.mark.parametrize("T", [1, 4, 40])
+def test_the_largest_scales(cuda_device, T):
+    """A finite scale whose product with log2(e) is not: scores of 0 stay 0, so
+    queries of zeros give the mean of V."""
+    c = ref.Cache(14, "bf16", "dense", 64, 1, 16, [96])
+    K, V, pages = c.to(cuda_device)
+    past = torch.tensor([96], dtype=torch.int32, device=cuda_device)
+    scale = float(np.finfo(np.float32).max)
+    q = torch.zeros(T, 8, 64, dtype=torch.bfloat16, device=cuda_device)
+    want = lib.paged_attn(q, K, V, pages, past, 0.125, causal=False)
+    for s in (scale, -scale):
+        got = lib.paged_attn(q, K, V, pages, past, s, causal=False)
+        assert torch.isfinite(got).all() and torch.equal(got, want)
+
+
 def test_what_a_call_allocates_is_of_its_stream(cuda_device):
     """A call on a stream that need not wait for the current one, which is busy: the
     workspace's counters are zero when it runs, and its results are not memory that
