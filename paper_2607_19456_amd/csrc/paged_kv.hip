@@ -1494,10 +1494,11 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
 // that the eight lanes of every 128-byte LDS access hit different banks.
 // A key tile of 16-bit values is 32 KB: two workgroups fit a CU, and one's
 // softmax overlaps the other's products.
-// Measured: chunks of four prompts, 359 GFLOP, 564 us with the merge (637 TFLOP/s;
-// the matrix pipes are busy for 35 % of the cycles, the vector units for 44 %).  64
-// rows a wave at one wave per SIMD halve the LDS reads and were 9 % slower to 9 %
-// faster by shape (605 -> 624 for these chunks); not taken.
+// Measured: chunks of four prompts, 359 GFLOP, 542 us with the merge (662 TFLOP/s;
+// the matrix pipes are busy for 35 % of the cycles, the vector units for 44 %, LDS
+// for 41 %).  64 rows a wave at one wave per SIMD halve the LDS reads and were 9 %
+// slower to 9 % faster by shape (605 -> 624 for these chunks); a tile's scores
+// between the weights of the one before were 2 to 9 % slower.  Neither is taken.
 // ---------------------------------------------------------------------------
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
