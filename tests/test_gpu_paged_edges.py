@@ -1,0 +1,75 @@
+"""The paged cache on the GPU at the edges of its numbers, where values are not
+finite: in every kernel that a call may take (16 and 32 query rows a KV head,
+chunks of more), on items that one workgroup holds and on items in parts."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_19456_amd as lib
+import paged_reference as ref
+from test_gpu_paged import check_attn
+
+pytestmark = pytest.mark.gpu
+
+P = 16
+# (rows before the step of each sequence): one workgroup or a few; in parts that
+# the last workgroup puts together (at most 1024 positions, where rows are few);
+# in parts that the merge puts together; many sequences
+PASTS = {"short": [40], "parts": [900], "merged": [2900], "many": [40 + 7 * b for b in range(70)]}
+
+
+def set_v(c, b, head, pos, block, x):
+    """Position pos of sequence b gets x in V, in the first dimensions of a block of
+    32 (of a 4-bit cache: the block becomes NaN)."""
+    page, slot = int(c.pages[b, pos // c.P]), pos % c.P
+    if c.fmt == "dense":
+        c.V[page, head, slot, 32 * block + 3] = x
+        c.V[page, head, slot, 32 * block + 9:32 * block + 13] = x
+        return
+    edit_scale(c, c.V, True, page, head, slot, block, 255)
+
+
+def edit_scale(c, pool, value, page, head, slot, block, byte):
+    codes, scales = ref.unpack_page(pool[page, head].reshape(-1).numpy(), c.P, c.d, value)
+    scales = scales.copy()
+    scales[slot, block] = byte
+    pool[page, head] = torch.from_numpy(ref.pack_page(codes, scales, value)).reshape(c.P, -1)
+
+
+def set_k_nan(c, b, head, pos):
+    page, slot = int(c.pages[b, pos // c.P]), pos % c.P
+    if c.fmt == "dense":
+        c.K[page, head, slot, 7] = math.nan
+    else:
+        edit_scale(c, c.K, False, page, head, slot, 1, 255)
+
+
+# --- what some rows see and others do not -------------------------------------------
+
+@pytest.mark.parametrize("past", PASTS)
+@pytest.mark.parametrize("T", [4, 10, 70])
+@pytest.mark.parametrize("dtype,fmt,d", [("bf16", "dense", 64), ("bf16", "dense", 128),
+                                         ("f16", "dense", 128), ("f16", "dense", 256),
+                                         ("f32", "dense", 64), ("bf16", "mx4", 64),
+                                         ("f16", "mx4", 128), ("bf16", "mx4", 256),
+                                         ("f32", "mx4", 128)])
+def test_what_only_later_rows_see(cuda_device, dtype, fmt, d, T, past):
+    """Infinities and NaN in V among the step's own positions, on head 0, and
+    before them, on head 1 (which all rows see); NaN in K at the last position but
+    one, on head 1.  8, 20 and 140 rows a KV head."""
+    pasts = PASTS[past] if past != "many" or T < 70 else PASTS[past][:12]
+
+    def edit(c):
+        for b, p in enumerate(pasts):
+            if b % 3:
+                continue
+            set_v(c, b, 0, p + 1, 0, math.inf)
+            set_v(c, b, 0, p + T // 2, 1, math.nan)
+            set_v(c, b, 0, p + T - 2, 1, -math.inf)
+            set_v(c, b, 1, p // 2, 1, math.inf)
+            set_v(c, b, 1, p - 1, 0, -math.inf)
+            set_k_nan(c, b, 1, p + T - 2)
+    check_attn(cuda_device, dtype=dtype, fmt=fmt, d=d, h_q=4, h_kv=2, past=pasts, T=T, edit=edit,
+               seed=T + d)
