@@ -1837,7 +1837,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
       }
       const float my_ref = limit == -INFINITY ? -INFINITY : ref;
       if (t0 == 0 && t1 == at.tiles) {
-        const float scale = sum == 0.f ? 0.f : 1.f / sum;
+        // (scores that are all -infinity: 0, also where V is not finite)
+        const float inverse = 1.f / sum;
+        auto mean = [&](float x) { return sum == 0.f ? 0.f : x * inverse; };
         T* dst = static_cast<T*>(a.out) +
                  ((int64_t)(sr.start + t) * a.h_q + head * a.G + g) * D + 4 * k;
 #pragma unroll
@@ -1845,8 +1847,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
 #pragma unroll
           for (int r = 0; r < 16; r += 4)
             *reinterpret_cast<u32x2*>(dst + 32 * c + 2 * r) =
-                u32x2{pack2<T>(acc[c][r] * scale, acc[c][r + 1] * scale),
-                      pack2<T>(acc[c][r + 2] * scale, acc[c][r + 3] * scale)};
+                u32x2{pack2<T>(mean(acc[c][r]), mean(acc[c][r + 1])),
+                      pack2<T>(mean(acc[c][r + 2]), mean(acc[c][r + 3]))};
       } else {
         const int64_t slot = 2 * (int64_t)blockIdx.x + (t0 == 0 ? 1 : 0);
         const int64_t row = slot * R + 32 * wave + i;

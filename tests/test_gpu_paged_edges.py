@@ -8,6 +8,7 @@ import pytest
 import torch
 
 import paper_2607_19456_amd as lib
+import paper_2607_19456_amd as lib
 import paged_reference as ref
 from test_gpu_paged import check_attn
 
@@ -73,3 +74,43 @@ def test_what_only_later_rows_see(cuda_device, dtype, fmt, d, T, past):
             set_k_nan(c, b, 1, p + T - 2)
     check_attn(cuda_device, dtype=dtype, fmt=fmt, d=d, h_q=4, h_kv=2, past=pasts, T=T, edit=edit,
                seed=T + d)
+
+
+# --- rows whose scores are -infinity ------------------------------------------------
+
+def minus_inf_keys(c, b, lo, hi):
+    for pos in range(lo, hi):
+        page, slot = int(c.pages[b, pos // c.P]), pos % c.P
+        c.K[page, :, slot, 0] = -math.inf
+
+
+def attend(device, dtype, d, h_q, h_kv, past, T, edit):
+    """(result, cache, q) of queries whose first dimension is positive."""
+    q = torch.from_numpy(np.random.default_rng(5).standard_normal((len(past) * T, h_q, d)))
+    q[..., 0] = q[..., 0].abs() + 0.5
+    q = q.to(ref.DTYPES[dtype])
+    c = ref.Cache(T, dtype, "dense", d, h_kv, P, [p + T for p in past])
+    edit(c)
+    K, V, pages = c.to(device)
+    print("attn", dtype, "past", past[:6], "rows", T, flush=True)
+    out = lib.paged_attn(q.to(device), K, V, pages,
+                         torch.tensor(past, dtype=torch.int32, device=device), 1 / math.sqrt(d))
+    return out.cpu(), c, q
+
+
+@pytest.mark.parametrize("past", [[20], [900], [2900], [20 + b % 9 for b in range(300)]],
+                         ids=["one", "parts", "merged", "whole"])
+@pytest.mark.parametrize("T", [4, 10, 20])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_rows_of_scores_that_are_all_minus_infinity(cuda_device, dtype, T, past):
+    """They give 0, whatever V holds: 8, 20 and 40 rows a KV head."""
+    past = [20 + b % 9 for b in range(300)] if len(past) > 1 else past
+
+    def edit(c):
+        for b, p in enumerate(past):
+            minus_inf_keys(c, b, 0, p + T)
+            set_v(c, b, 0, 3, 0, math.inf)
+            set_v(c, b, 0, 3, 1, math.nan)
+            set_v(c, b, 0, p + 1, 1, math.inf)
+    out = attend(cuda_device, dtype, 64, 2, 1, past, T, edit)[0]
+    assert int(torch.count_nonzero(out)) == 0 and not torch.isnan(out).any()
