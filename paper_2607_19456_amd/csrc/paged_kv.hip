@@ -249,6 +249,32 @@ __device__ __forceinline__ int64_t mx_scale_at(bool value, int page_log2, int sl
                 : (int64_t)slot * (D / 32) + block);
 }
 
+// What a 4-bit code and a scale byte stand for.
+__device__ __forceinline__ float mx_level(uint32_t code) {
+  const uint32_t ex = code >> 1 & 3u;
+  const float m = ex ? (float)(2 + (code & 1u)) * (float)(1u << ex) * 0.25f
+                     : (float)(code & 1u) * 0.5f;
+  return code & 8u ? -m : m;
+}
+__device__ __forceinline__ float mx_factor(uint32_t byte) {
+  // the byte 255 as a scale is not a number, and so is what it scales
+  return byte == 255 ? __uint_as_float(0x7fc00000u) : power_of(byte);
+}
+
+// A dimension of a slot of a head's page, as a value of T.
+template <class T, bool MX, int D>
+__device__ __forceinline__ float held(const char* block, bool value, int page_log2, int slot,
+                                      int dim) {
+  if constexpr (MX) {
+    const uint32_t codes =
+        *reinterpret_cast<const uint32_t*>(block + mx_code_at<D>(value, slot, dim / 8));
+    const uint32_t byte = (uint8_t)block[mx_scale_at<D>(value, page_log2, slot, dim / 32)];
+    return (float)(T)(mx_level(codes >> (4 * (dim % 8)) & 15u) * mx_factor(byte));
+  } else {
+    return (float)reinterpret_cast<const T*>(block)[(int64_t)slot * D + dim];
+  }
+}
+
 // Unit u (of D/16) of a row into dst, where dst may be src: 16 dimensions, and
 // of a rotated part both of each pair, so that the angles are read once for two
 // values and nobody else reads what is written.
@@ -379,16 +405,9 @@ __global__ __launch_bounds__(kThreads) void paged_gather_kernel(Batch bt, void* 
             *reinterpret_cast<const uint32_t*>(block + mx_code_at<D>(value, slot, piece));
         const uint32_t byte =
             (uint8_t)block[mx_scale_at<D>(value, bt.page_log2, slot, piece / 4)];
-        // the byte 255 as a scale is not a number, and so is what it scales
-        const float scale = byte == 255 ? __uint_as_float(0x7fc00000u) : power_of(byte);
+        const float scale = mx_factor(byte);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t c = codes >> (4 * e) & 15u;
-          const uint32_t ex = c >> 1 & 3u;
-          const float m = ex ? (float)(2 + (c & 1u)) * (float)(1u << ex) * 0.25f
-                             : (float)(c & 1u) * 0.5f;
-          y[e] = (c & 8u ? -m : m) * scale;
-        }
+        for (int e = 0; e < 8; ++e) y[e] = mx_level(codes >> (4 * e) & 15u) * scale;
       } else {
         load8(reinterpret_cast<const T*>(block) + (int64_t)slot * D + 8 * piece, y);
       }
@@ -552,6 +571,24 @@ __device__ __forceinline__ int seen_by(const Batch& bt, const AttnArgs& a, int p
   if (past < 0) return 0;
   if (!a.causal) return min(past, cap);
   return past >= cap - t - 1 ? cap : past + t + 1;
+}
+
+// The weight of a key whose V is not finite, against the reference ref: computed
+// again, where the row's product had zeros in V's place.  (0 times an infinity is
+// NaN there too.)
+template <class T, bool MX, int D>
+__device__ __forceinline__ float weight_of(const Batch& bt, const AttnArgs& a, int64_t row,
+                                           int q_head, int kv_head, int page, int slot,
+                                           float ref) {
+  const T* q = static_cast<const T*>(a.q) + row * a.q_stride + (int64_t)q_head * D;
+  const char* block =
+      bt.K + ((int64_t)page * bt.h_kv + kv_head) * block_bytes<T, MX, D>(bt.page_log2);
+  float s = 0.f;
+#pragma unroll 1
+  for (int dim = 0; dim < D; ++dim)
+    s += (float)q[dim] * held<T, MX, D>(block, false, bt.page_log2, slot, dim);
+  s = a.q_keep ? a.q_flip ? -s : s : 0.f;
+  return (float)(T)exp2f(__builtin_fmaf(s, a.scale, -ref));
 }
 
 // Row tiles of a sequence (each of R rows; one where not MANY), and tiles of keys
@@ -873,10 +910,10 @@ __device__ __forceinline__ void finish(const AttnArgs& a, const W& at) {
       }
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
-        if (p0 + y >= n || s[y][0] == -INFINITY) continue;           // saw nothing
+        if (p0 + y >= n) continue;
         const float mn = s[y][0] <= m ? m : s[y][0];                 // (a NaN stays)
         const float fo = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-        const float fn = __builtin_amdgcn_exp2f(s[y][0] - mn);
+        const float fn = s[y][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s[y][0] - mn);
         l = l * fo + s[y][1] * fn;
         o = o * fo + v[y] * fn;
         m = mn;
@@ -1437,15 +1474,19 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
           if ((unsigned)page >= (unsigned)bt.n_pages) continue;
           const int at = key & page_mask;
           const char* block = bt.V + ((int64_t)page * bt.h_kv + head) * blk;
-          if constexpr (MX) {
-            if ((uint8_t)block[mx_scale_at<D>(true, bt.page_log2, at, dim / 32)] == 255u) o += NAN;
-          } else {
+          f32x4 v;
+          bool bad = false;
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              const float v = (float)reinterpret_cast<const T*>(block)[(int64_t)at * D + dim + y];
-              if (!(fabsf(v) < INFINITY)) o[y] += v;
-            }
+          for (int y = 0; y < 4; ++y) {
+            v[y] = held<T, MX, D>(block, true, bt.page_log2, at, dim + y);
+            bad |= !(fabsf(v[y]) < INFINITY);
           }
+          if (!bad) continue;
+          const float w =
+              weight_of<T, MX, D>(bt, a, sr.start + t, head * a.G + g, head, page, at, m);
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+            if (!(fabsf(v[y]) < INFINITY)) o[y] += w * v[y];
         }
         if (whole) {
           o = l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o / l;
@@ -1819,21 +1860,24 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
         if ((unsigned)id >= (unsigned)bt.n_pages) continue;
         const int slot = key & page_mask;
         const char* block = bt.V + ((int64_t)id * bt.h_kv + head) * blk;
+        auto value = [&](int c, int r) {
+          return held<T, MX, D>(block, true, bt.page_log2, slot, 32 * c + 8 * (r / 4) + 4 * k + r % 4);
+        };
+        bool bad = false;
 #pragma unroll
-        for (int c = 0; c < ND; ++c) {
-          if constexpr (MX) {
-            if ((uint8_t)block[mx_scale_at<D>(true, bt.page_log2, slot, c)] == 255u)
+        for (int c = 0; c < ND; ++c)
 #pragma unroll
-              for (int r = 0; r < 16; ++r) acc[c][r] += NAN;
-          } else {
+          for (int r = 0; r < 16; ++r) bad |= !(fabsf(value(c, r)) < INFINITY);
+        if (!bad) continue;
+        const float w =
+            weight_of<T, MX, D>(bt, a, sr.start + t, head * a.G + g, head, id, slot, ref);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const float v = (float)reinterpret_cast<const T*>(
-                  block)[(int64_t)slot * D + 32 * c + 8 * (r / 4) + 4 * k + r % 4];
-              if (!(fabsf(v) < INFINITY)) acc[c][r] += v;
-            }
+        for (int c = 0; c < ND; ++c)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float v = value(c, r);
+            if (!(fabsf(v) < INFINITY)) acc[c][r] += w * v;
           }
-        }
       }
       const float my_ref = limit == -INFINITY ? -INFINITY : ref;
       if (t0 == 0 && t1 == at.tiles) {
@@ -1906,9 +1950,10 @@ __global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(AttnArgs 
       }
 #pragma unroll
       for (int y = 0; y < Y; ++y) {
-        if (p0 + y * step >= n || s[y][0] == -INFINITY) continue;    // saw nothing
+        if (p0 + y * step >= n) continue;
         const float mn = s[y][0] <= m ? m : s[y][0];                 // (a NaN stays)
-        const float fo = m == -INFINITY ? 0.f : exp2f(m - mn), fn = exp2f(s[y][0] - mn);
+        const float fo = m == -INFINITY ? 0.f : exp2f(m - mn);
+        const float fn = s[y][0] == -INFINITY ? 0.f : exp2f(s[y][0] - mn);
         l = l * fo + s[y][1] * fn;
 #pragma unroll
         for (int e = 0; e < kOut; ++e) o[e] = o[e] * fo + v[y][e] * fn;
@@ -1957,8 +2002,7 @@ __global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(AttnArgs 
       float sum = 0.f, y = 0.f;
 #pragma unroll
       for (int w = 0; w < kMergeWaves; ++w) {
-        if (s_m[w] == -INFINITY) continue;
-        const float f = exp2f(s_m[w] - top);
+        const float f = s_m[w] == -INFINITY ? 0.f : exp2f(s_m[w] - top);
         sum += s_l[w] * f;
         y += s_part[w][tid] * f;
       }

@@ -114,3 +114,28 @@ def test_rows_of_scores_that_are_all_minus_infinity(cuda_device, dtype, T, past)
             set_v(c, b, 0, p + 1, 1, math.inf)
     out = attend(cuda_device, dtype, 64, 2, 1, past, T, edit)[0]
     assert int(torch.count_nonzero(out)) == 0 and not torch.isnan(out).any()
+
+
+@pytest.mark.parametrize("past", [[900], [2900], [40] * 130], ids=["parts", "merged", "short"])
+@pytest.mark.parametrize("T", [4, 10, 70])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_parts_of_scores_that_are_all_minus_infinity(cuda_device, dtype, T, past):
+    """The first half of the keys has weight 0, and 0 times an infinity or a NaN is
+    NaN: however the row is divided.  The other results are those without these
+    keys' scores."""
+    def edit(c):
+        for b, p in enumerate(past):
+            minus_inf_keys(c, b, 0, p // 2)
+            if b % 2 == 0:
+                set_v(c, b, 0, 3, 0, math.inf)
+                set_v(c, b, 1, 5, 1, math.nan)
+    out, c, q = attend(cuda_device, dtype, 64, 4, 2, past, T, edit)
+    want, mass, _, seen, _, top = ref.attention(q, c.K, c.V, c.pages.numpy(), past, 1 / 8, True,
+                                                None, T, 2)
+    finite_k = torch.where(torch.isinf(c.K), torch.zeros_like(c.K), c.K)
+    spread = ref.attention(q, finite_k, c.V, c.pages.numpy(), past, 1 / 8, True, None, T, 2)[2]
+    got, nan = out.double().numpy(), np.isnan(want)
+    assert nan.any() and np.array_equal(np.isnan(got), nan)
+    tol = ref.tolerance(np.where(nan, 0, want), np.where(nan, 0, mass), spread, seen, 0.0,
+                        ref.DTYPES[dtype], 64)
+    assert (np.abs(np.where(nan, 0, got - want)) <= tol).all()
