@@ -912,8 +912,9 @@ __device__ __forceinline__ void finish(const AttnArgs& a, const W& at) {
       for (int y = 0; y < 4; ++y) {
         if (p0 + y >= n) continue;
         const float mn = s[y][0] <= m ? m : s[y][0];                 // (a NaN stays)
-        const float fo = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-        const float fn = s[y][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s[y][0] - mn);
+        const float base = mn == -INFINITY ? 0.f : mn;               // (then both factors are 0)
+        const float fo = __builtin_amdgcn_exp2f(m - base);
+        const float fn = __builtin_amdgcn_exp2f(s[y][0] - base);
         l = l * fo + s[y][1] * fn;
         o = o * fo + v[y] * fn;
         m = mn;
@@ -1451,6 +1452,40 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
               f32x4{acc[nb][c][r], acc[nb][c + 1][r], acc[nb][c + 2][r], acc[nb][c + 3][r]} * f;
         }
       __syncthreads();
+      if (__builtin_expect(fix, 0)) {
+        // The zeroed values, times their weights, to the sums of the first wave.
+#pragma unroll 1
+        for (int e = tid; e < 16 * D / 4; e += kThreads) {
+          const int x = e / (D / 4), dim = e % (D / 4) * 4;
+          const int in = nb * 16 + x;
+          if (in >= in_tile) continue;
+          float m = s_ref[0][x];
+#pragma unroll
+          for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_ref[w][x]);
+          const int t = token_of(a, row0 + in), g = (row0 + in) - t * a.G;
+          const int end = min(fix_hi, seen_by(bt, a, past, t));
+#pragma unroll 1
+          for (int key = fix_lo; key < end; ++key) {
+            const int page = table[key >> bt.page_log2];
+            if ((unsigned)page >= (unsigned)bt.n_pages) continue;
+            const int at = key & page_mask;
+            const char* block = bt.V + ((int64_t)page * bt.h_kv + head) * blk;
+            float v[4];
+            bool bad = false;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              v[y] = held<T, MX, D>(block, true, bt.page_log2, at, dim + y);
+              bad |= !(fabsf(v[y]) < INFINITY);
+            }
+            if (!bad) continue;
+            const float w =
+                weight_of<T, MX, D>(bt, a, sr.start + t, head * a.G + g, head, page, at, m);
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              if (!(fabsf(v[y]) < INFINITY)) s_acc[0][x][dim + y] += w * v[y];
+          }
+        }
+      }
 #pragma unroll 1
       for (int e = tid; e < 16 * D / 4; e += kThreads) {
         const int x = e / (D / 4), dim = e % (D / 4) * 4;
@@ -1468,26 +1503,6 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
           o += *reinterpret_cast<const f32x4*>(&s_acc[w][x][dim]);
         }
         const int t = token_of(a, row0 + in), g = (row0 + in) - t * a.G;
-        const int fix_end = fix ? min(fix_hi, seen_by(bt, a, past, t)) : 0;
-        for (int key = fix_lo; key < fix_end; ++key) {
-          const int page = table[key >> bt.page_log2];
-          if ((unsigned)page >= (unsigned)bt.n_pages) continue;
-          const int at = key & page_mask;
-          const char* block = bt.V + ((int64_t)page * bt.h_kv + head) * blk;
-          f32x4 v;
-          bool bad = false;
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            v[y] = held<T, MX, D>(block, true, bt.page_log2, at, dim + y);
-            bad |= !(fabsf(v[y]) < INFINITY);
-          }
-          if (!bad) continue;
-          const float w =
-              weight_of<T, MX, D>(bt, a, sr.start + t, head * a.G + g, head, page, at, m);
-#pragma unroll
-          for (int y = 0; y < 4; ++y)
-            if (!(fabsf(v[y]) < INFINITY)) o[y] += w * v[y];
-        }
         if (whole) {
           o = l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o / l;
           T* dst = static_cast<T*>(a.out) +
@@ -1952,8 +1967,8 @@ __global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(AttnArgs 
       for (int y = 0; y < Y; ++y) {
         if (p0 + y * step >= n) continue;
         const float mn = s[y][0] <= m ? m : s[y][0];                 // (a NaN stays)
-        const float fo = m == -INFINITY ? 0.f : exp2f(m - mn);
-        const float fn = s[y][0] == -INFINITY ? 0.f : exp2f(s[y][0] - mn);
+        const float base = mn == -INFINITY ? 0.f : mn;               // (then both factors are 0)
+        const float fo = exp2f(m - base), fn = exp2f(s[y][0] - base);
         l = l * fo + s[y][1] * fn;
 #pragma unroll
         for (int e = 0; e < kOut; ++e) o[e] = o[e] * fo + v[y][e] * fn;
