@@ -488,6 +488,18 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), t2));
 }
 
+// Both values of a word of 16-bit ones, added to x.
+template <class T>
+__device__ __forceinline__ float add2(uint32_t w, float x) {
+  if constexpr (std::is_same<T, __bf16>::value) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w),
+                                           bf16x2{(__bf16)1.f, (__bf16)1.f}, x, false);
+  } else {
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, w), f16x2{(_Float16)1.f, (_Float16)1.f},
+                                  x, false);
+  }
+}
+
 // Two values of byte `sel` of `codes`, times the scale, as two T.
 template <class T, int sel>
 __device__ __forceinline__ uint32_t widen2(uint32_t codes, float scale) {
@@ -1840,12 +1852,15 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
 #pragma unroll
           for (int r = 0; r < 16; ++r)
             s[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], a.scale, -ref));
+          // the sum of the weights as they are multiplied: rounded to T
           float part = 0.f;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) part += s[n][r];
+          for (int r = 0; r < 16; r += 2) {
+            const uint32_t w = pack2<T>(s[n][r], s[n][r + 1]);
+            p[2 * n + r / 8][r % 8 / 2] = w;
+            part = add2<T>(w, part);
+          }
           sum += part;
-#pragma unroll
-          for (int r = 0; r < 16; r += 2) p[2 * n + r / 8][r % 8 / 2] = pack2<T>(s[n][r], s[n][r + 1]);
         }
         // --- O^T += V^T P^T ---
 #pragma unroll

@@ -139,3 +139,30 @@ def test_parts_of_scores_that_are_all_minus_infinity(cuda_device, dtype, T, past
     tol = ref.tolerance(np.where(nan, 0, want), np.where(nan, 0, mass), spread, seen, 0.0,
                         ref.DTYPES[dtype], 64)
     assert (np.abs(np.where(nan, 0, got - want)) <= tol).all()
+
+
+# --- the sum that divides is that of the weights as they are multiplied --------------
+
+@pytest.mark.parametrize("past", [[1400], [500] * 600], ids=["parts", "whole"])
+@pytest.mark.parametrize("T", [4, 10, 20, 70])
+@pytest.mark.parametrize("dtype,weight", [("bf16", 0.5 * (1 + 0.9 * 2.0 ** -8)),
+                                          ("f16", 0.5 * (1 + 0.9 * 2.0 ** -11)),
+                                          ("f16", 1.5 * 2.0 ** -16)])
+def test_weights_that_all_round_one_way(cuda_device, dtype, weight, T, past):
+    """One key at score 0 and all others where their weight is off by 0.9 of half a
+    step, or below the normal numbers of float16: V of ones gives ones, since both sums
+    are of the same weights and their roundings in 32 bits (at most n * 2^-24, n <
+    1500 keys) stay far from half a step of the result."""
+    t = ref.DTYPES[dtype]
+    B, n = len(past), past[0] + T
+    K = torch.zeros(B * -(-n // P), 1, P, 64, dtype=t, device=cuda_device)
+    K[..., 0] = -1
+    pages = torch.arange(K.shape[0], dtype=torch.int32, device=cuda_device).reshape(B, -1)
+    K[pages[:, 0].long(), 0, 0, 0] = 0
+    q = torch.zeros(B * T, 2, 64, dtype=t, device=cuda_device)
+    q[..., 0] = 1
+    out = lib.paged_attn(q, K, torch.ones_like(K), pages,
+                         torch.tensor(past, dtype=torch.int32, device=cuda_device),
+                         -math.log(weight))
+    print(dtype, weight, T, "off by", float((out.double() - 1).abs().max()), flush=True)
+    assert torch.equal(out, torch.ones_like(out))
