@@ -257,8 +257,9 @@ __device__ __forceinline__ float mx_level(uint32_t code) {
   return code & 8u ? -m : m;
 }
 __device__ __forceinline__ float mx_factor(uint32_t byte) {
-  // the byte 255 as a scale is not a number, and so is what it scales
-  return byte == 255 ? __uint_as_float(0x7fc00000u) : power_of(byte);
+  // the byte 255 as a scale is not a number, and so is what it scales; 0 is
+  // 2^-127, which is not a normal number
+  return __uint_as_float(byte == 255 ? 0x7fc00000u : byte == 0 ? 0x00400000u : byte << 23);
 }
 
 // A dimension of a slot of a head's page, as a value of T.

@@ -166,3 +166,63 @@ def test_weights_that_all_round_one_way(cuda_device, dtype, weight, T, past):
                          -math.log(weight))
     print(dtype, weight, T, "off by", float((out.double() - 1).abs().max()), flush=True)
     assert torch.equal(out, torch.ones_like(out))
+
+
+# --- 4-bit blocks at the ends of their range ------------------------------------------
+
+def every_code(rng, scales, rows, d):
+    """Codes and scale bytes of rows whose blocks have the given bytes in turn."""
+    codes = rng.integers(0, 16, (rows, d)).astype(np.uint8)
+    codes[:, :16] = np.arange(16)
+    return codes, np.resize(np.array(scales, np.uint8), (rows, d // 32))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_blocks_of_every_scale_read_back(cuda_device, dtype):
+    """All 256 bytes, all 16 codes: the values rounded to the type."""
+    t = ref.DTYPES[dtype]
+    rng = np.random.default_rng(3)
+    d, n = 64, 128
+    c = ref.Cache(1, dtype, "mx4", d, 1, n, [n], spare=0)
+    codes, scales = every_code(rng, range(256), n, d)
+    for pool, value in ((c.K, False), (c.V, True)):
+        pool[0, 0] = torch.from_numpy(ref.pack_page(codes, scales, value)).reshape(n, -1)
+    K, V, _ = c.to(cuda_device)
+    pages = torch.zeros(1, 1, dtype=torch.int32, device=cuda_device)
+    past = torch.zeros(1, dtype=torch.int32, device=cuda_device)
+    want = torch.from_numpy(ref.values(codes, scales)).to(t)
+    back = [torch.empty(n, 1, d, dtype=t, device=cuda_device) for _ in range(2)]
+    for got in lib.paged_gather(K, V, pages, past, *back):
+        got = got[:, 0].cpu()
+        same = (got == want) | (torch.isnan(got) & torch.isnan(want))
+        assert same.all(), [(int(scales[r, x // 32]), int(codes[r, x]), float(got[r, x]),
+                             float(want[r, x])) for r, x in (~same).nonzero().tolist()[:8]]
+
+
+@pytest.mark.parametrize("T", [1, 10, 40])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_attention_over_blocks_of_every_scale(cuda_device, dtype, T):
+    """One position, so a weight of 1: V comes out as paged_gather reads it, each
+    position of a sequence of its own."""
+    t = ref.DTYPES[dtype]
+    rng = np.random.default_rng(4)
+    d, n = 64, 128
+    codes, scales = every_code(rng, range(256), n, d)
+    c = ref.Cache(1, dtype, "mx4", d, 1, P, [P] * n, spare=0)
+    for b in range(n):
+        full_c, full_s = np.zeros((P, d), np.uint8), np.full((P, d // 32), 127, np.uint8)
+        full_c[0], full_s[0] = codes[b], scales[b]
+        c.V[int(c.pages[b, 0]), 0] = torch.from_numpy(
+            ref.pack_page(full_c, full_s, True)).reshape(P, -1)
+    K, V, pages = c.to(cuda_device)
+    want = torch.from_numpy(ref.values(codes, scales)).to(t)
+    past = torch.ones(n, dtype=torch.int32, device=cuda_device)
+    q = torch.zeros(n * T, 1, d, dtype=t, device=cuda_device)
+    out = lib.paged_attn(q, K, V, pages, past, 1.0, causal=False)
+    # a result below the normal numbers of 32 bits may be taken for 0
+    low = want.double().abs() < 2.0 ** -126
+    for got in out.reshape(n, T, d).cpu().unbind(1):
+        same = (got == want) | (torch.isnan(got) & torch.isnan(want)) \
+            | (low & (got.double().abs() <= 2.0 ** -126))
+        assert same.all(), [(int(scales[r, x // 32]), int(codes[r, x]), float(got[r, x]),
+                             float(want[r, x])) for r, x in (~same).nonzero().tolist()[:8]]
