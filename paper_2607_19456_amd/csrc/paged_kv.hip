@@ -520,6 +520,22 @@ __device__ __forceinline__ float mx_scale_of(uint32_t w, int j) {
   return __uint_as_float(j % 4 == 3 ? w >> 1 : w << (23 - 8 * (j % 4)));
 }
 
+// The least scale byte 2^X whose largest value, 6 * 2^X, is an infinity in T, and a
+// word of codes without those that are: from 4 * 2^X on there, 2 * 2^X with the
+// next byte, 2^X with the one after, and then all but 0.
+template <class T>
+constexpr uint32_t kFirstBeyond = 127 + (std::is_same<T, _Float16>::value ? 14 : 126);
+template <class T>
+__device__ __forceinline__ uint32_t codes_within(uint32_t codes, uint32_t byte) {
+  if (byte == 255u) return 0u;
+  const uint32_t more = byte - kFirstBeyond<T>;
+  const uint32_t first = more == 0 ? 6u : more == 1 ? 4u : more == 2 ? 2u : 1u;
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if ((codes >> (4 * e) & 7u) >= first) codes &= ~(15u << (4 * e));
+  return codes;
+}
+
 template <class T>
 __device__ __forceinline__ bool not_finite(uint32_t w) {
   if constexpr (is_f32<T>)
@@ -1309,12 +1325,13 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
             for (int j = 0; j < KPL; ++j) {
               if constexpr (MX) {
 #pragma unroll
-                for (int p = 0; p < NP; ++p)
-                  if ((tw.vs[p][j / 4] >> (8 * (j % 4)) & 255u) == 255u) {
-                    bad = true;
-                    tw.vw[j][p] = 0u;
-                    tw.vs[p][j / 4] &= ~(128u << (8 * (j % 4)));
-                  }
+                for (int p = 0; p < NP; ++p) {
+                  const uint32_t byte = tw.vs[p][j / 4] >> (8 * (j % 4)) & 255u;
+                  if (byte < kFirstBeyond<T>) continue;
+                  bad = true;
+                  tw.vw[j][p] = codes_within<T>(tw.vw[j][p], byte);
+                  if (byte == 255u) tw.vs[p][j / 4] &= ~(128u << (8 * (j % 4)));
+                }
               } else {
 #pragma unroll
                 for (int w = 0; w < L::VW; ++w) {

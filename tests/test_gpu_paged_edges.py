@@ -15,7 +15,7 @@ from test_gpu_paged import check_attn
 pytestmark = pytest.mark.gpu
 
 P = 16
-# (rows before the step of each sequence): one workgroup or a few; in parts that
+# Rows before the step of each sequence): one workgroup or a few; in parts that
 # the last workgroup puts together (at most 1024 positions, where rows are few);
 # in parts that the merge puts together; many sequences
 PASTS = {"short": [40], "parts": [900], "merged": [2900], "many": [40 + 7 * b for b in range(70)]}
@@ -37,6 +37,12 @@ def edit_scale(c, pool, value, page, head, slot, block, byte):
     scales = scales.copy()
     scales[slot, block] = byte
     pool[page, head] = torch.from_numpy(ref.pack_page(codes, scales, value)).reshape(c.P, -1)
+
+
+def edit_codes(c, page, head, slot, block, codes_in_turn):
+    codes, scales = ref.unpack_page(c.V[page, head].reshape(-1).numpy(), c.P, c.d, True)
+    codes[slot, 32 * block:32 * block + 32] = np.resize(np.array(codes_in_turn, np.uint8), 32)
+    c.V[page, head] = torch.from_numpy(ref.pack_page(codes, scales, True)).reshape(c.P, -1)
 
 
 def set_k_nan(c, b, head, pos):
@@ -170,6 +176,17 @@ def test_weights_that_all_round_one_way(cuda_device, dtype, weight, T, past):
 
 # --- 4-bit blocks at the ends of their range ------------------------------------------
 
+def dense_of(c, t):
+    """A dense cache of the same values, rounded to the type."""
+    K, V = (torch.zeros(c.K.shape[0], c.h_kv, c.P, c.d, dtype=t) for _ in range(2))
+    for page in range(c.K.shape[0]):
+        for h in range(c.h_kv):
+            for pool, to, value in ((c.K, K, False), (c.V, V, True)):
+                with np.errstate(over="ignore"):
+                    to[page, h] = torch.from_numpy(ref.page_rows(pool, page, h, c.d, value)).to(t)
+    return K, V
+
+
 def every_code(rng, scales, rows, d):
     """Codes and scale bytes of rows whose blocks have the given bytes in turn."""
     codes = rng.integers(0, 16, (rows, d)).astype(np.uint8)
@@ -226,3 +243,44 @@ def test_attention_over_blocks_of_every_scale(cuda_device, dtype, T):
             | (low & (got.double().abs() <= 2.0 ** -126))
         assert same.all(), [(int(scales[r, x // 32]), int(codes[r, x]), float(got[r, x]),
                              float(want[r, x])) for r, x in (~same).nonzero().tolist()[:8]]
+
+
+@pytest.mark.parametrize("past", [[40], [900], [2900]], ids=["short", "parts", "merged"])
+@pytest.mark.parametrize("T", [4, 10, 70])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("dtype,scales", [("f16", (141, 142, 143, 144, 180)), ("f32", (253, 254)),
+                                          ("bf16", (253, 254))])
+def test_4_bit_values_that_do_not_fit_the_type(cuda_device, dtype, scales, d, T, past):
+    """V values that are infinities in the rows' type, at positions that only some
+    rows see: infinite where they are seen, and nothing where they are not."""
+    t = ref.DTYPES[dtype]
+    c = ref.Cache(7, dtype, "mx4", d, 2, P, [past[0] + T])
+    rng = np.random.default_rng(T)
+    for n, byte in enumerate(scales):
+        pos = past[0] + 1 + (n * (T - 2)) // len(scales)
+        page, slot = int(c.pages[0, pos // P]), pos % P
+        block = n % (d // 32)
+        edit_scale(c, c.V, True, page, n % 2, slot, block, byte)
+        if dtype != "f16":
+            # sums in 32 bits of finite values as large as these would be infinite
+            edit_codes(c, page, n % 2, slot, block, (0, 7, 15))
+    K, V, pages = c.to(cuda_device)
+    q = torch.from_numpy(rng.standard_normal((T, 4, d))).to(t)
+    dK, dV = dense_of(c, t)
+    scale = 1 / math.sqrt(d)
+    want, mass, spread, seen, _, _ = ref.attention(q, dK, dV, c.pages.numpy(), past, scale, True,
+                                                   None, T, 2)
+    out = lib.paged_attn(q.to(cuda_device), K, V, pages,
+                         torch.tensor(past, dtype=torch.int32, device=cuda_device), scale)
+    got = out.cpu().double().numpy()
+    # the largest V that a finite output may hold is that of other dimensions of the
+    # same block: the bound goes by each output's own weights, and float16 weights
+    # below 2^-14 by the values that they may be of
+    with np.errstate(invalid="ignore"):
+        finite = np.isfinite(want)
+        mass = np.where(finite, mass, 0.0)
+        top = float(np.abs(np.nan_to_num(dV.double().numpy(), nan=0, posinf=0, neginf=0)).max())
+        tol = ref.tolerance(np.where(finite, want, 0.0), mass, spread, seen, top, t, d)
+        assert np.array_equal(np.isnan(got), np.isnan(want))
+        assert np.array_equal(got[~finite & ~np.isnan(want)], want[~finite & ~np.isnan(want)])
+        assert (np.abs(np.where(finite, got - want, 0.0)) <= tol).all()
