@@ -1482,10 +1482,12 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
               f32x4{acc[nb][c][r], acc[nb][c + 1][r], acc[nb][c + 2][r], acc[nb][c + 3][r]} * f;
         }
       __syncthreads();
+      int from = tid;                // (its rows and dimensions take registers only here)
+      asm volatile("" : "+v"(from));
       if (__builtin_expect(fix, 0)) {
         // The zeroed values, times their weights, to the sums of the first wave.
 #pragma unroll 1
-        for (int e = tid; e < 16 * D / 4; e += kThreads) {
+        for (int e = from; e < 16 * D / 4; e += kThreads) {
           const int x = e / (D / 4), dim = e % (D / 4) * 4;
           const int in = nb * 16 + x;
           if (in >= in_tile) continue;
@@ -1517,7 +1519,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
         }
       }
 #pragma unroll 1
-      for (int e = tid; e < 16 * D / 4; e += kThreads) {
+      for (int e = from; e < 16 * D / 4; e += kThreads) {
         const int x = e / (D / 4), dim = e % (D / 4) * 4;
         const int in = nb * 16 + x;
         if (in >= in_tile) continue;
