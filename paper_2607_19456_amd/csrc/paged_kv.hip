@@ -602,6 +602,15 @@ __device__ __forceinline__ int seen_by(const Batch& bt, const AttnArgs& a, int p
   return past >= cap - t - 1 ? cap : past + t + 1;
 }
 
+// A score's distance from the reference is taken in one multiply-add, which keeps
+// what the reference lost when it was rounded: the same factor for every key, small
+// enough below kFar (2^4 at most).  Beyond, the product is rounded as the reference
+// was, so that the largest score's weight is 1; scores beyond 32 bits give NaN.
+constexpr float kFar = 0x1p26f;
+__device__ __forceinline__ bool is_far(float ref) {
+  return fabsf(ref) > kFar && ref != -INFINITY;
+}
+
 // The weight of a key whose V is not finite, against the reference ref: computed
 // again, where the row's product had zeros in V's place.  (0 times an infinity is
 // NaN there too.)
@@ -617,7 +626,9 @@ __device__ __forceinline__ float weight_of(const Batch& bt, const AttnArgs& a, i
   for (int dim = 0; dim < D; ++dim)
     s += (float)q[dim] * held<T, MX, D>(block, false, bt.page_log2, slot, dim);
   s = a.q_keep ? a.q_flip ? -s : s : 0.f;
-  return (float)(T)exp2f(__builtin_fmaf(s, a.scale, -ref));
+  const bool far = is_far(ref);
+  if (far) s *= a.scale;
+  return (float)(T)exp2f(__builtin_fmaf(s, far ? 1.f : a.scale, -ref));
 }
 
 // Row tiles of a sequence (each of R rows; one where not MANY), and tiles of keys
@@ -1026,6 +1037,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
 
     f32x4 acc[NB][NC], sums[NB];
     float limit[NB], ref[NB];   // raise the reference above limit; scores are taken less ref
+    bool far = false;           // a reference is beyond kFar
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       limit[nb] = -INFINITY;
@@ -1364,6 +1376,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
         if (__any(!(top <= limit[nb]))) {
           top = fmaxf(top, __shfl_xor(top, 16));
           top = fmaxf(top, __shfl_xor(top, 32));
+          far |= __any(is_far(top));
           if (!(top <= limit[nb])) {
             const float f = limit[nb] == -INFINITY ? 0.f : exp2f(ref[nb] - top);
             ref[nb] = top;
@@ -1373,6 +1386,14 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
             for (int c = 0; c < NC; ++c) acc[nb][c] *= f;
           }
         }
+        float by = a.scale;
+        if (__builtin_expect(far, 0)) {
+          by = 1.f;
+#pragma unroll
+          for (int y = 0; y < DEPTH; ++y)
+#pragma unroll
+            for (int h = 0; h < NH; ++h) s[y][nb][h] *= a.scale;
+        }
 #pragma unroll
         for (int y = 0; y < DEPTH; ++y)
 #pragma unroll
@@ -1380,7 +1401,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
             f32x4& w = s[y][nb][h];
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-              w[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(w[r], a.scale, -ref[nb]));
+              w[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(w[r], by, -ref[nb]));
             if constexpr (is_f32<T>) {
               sums[nb] += w;
             } else {
@@ -1668,7 +1689,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[c][r] = 0.f;
     float limit = -INFINITY, ref = 0.f, sum = 0.f;
-    bool spoilt = false;
+    bool spoilt = false, far = false;
 
     // --- staging: the loads of one tile, 128 bytes a thread of 16-bit values ---
     // Waves 0 and 1, K: unit u of a thread is chunk u % (row's chunks) of a row
@@ -1857,6 +1878,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
         top *= a.scale;
         if (__any(!(top <= limit))) {
           top = fmaxf(top, __shfl_xor(top, 32));
+          far |= __any(is_far(top));
           if (!(top <= limit)) {
             const float f = limit == -INFINITY ? 0.f : exp2f(ref - top);
             ref = top;
@@ -1866,12 +1888,18 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
             for (int c = 0; c < ND; ++c) acc[c] *= f;
           }
         }
+        float by = a.scale;
+        if (__builtin_expect(far, 0)) {
+          by = 1.f;
+#pragma unroll
+          for (int n = 0; n < NS; ++n) s[n] *= a.scale;
+        }
         u32x4 p[2 * NS];
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            s[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], a.scale, -ref));
+            s[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], by, -ref));
           // the sum of the weights as they are multiplied: rounded to T
           float part = 0.f;
 #pragma unroll

@@ -1,6 +1,8 @@
-"""The paged cache on the GPU at the edges of its numbers, where values are not
-finite: in every kernel that a call may take (16 and 32 query rows a KV head,
-chunks of more), on items that one workgroup holds and on items in parts."""
+"""The paged cache on the GPU at the edges of its numbers: values that are not
+finite or do not fit the type of the rows, weights that all round one way, scores
+beyond what 32 bits resolve.  In every kernel that a call may take (16 and 32
+query rows a KV head, chunks of more), on items that one workgroup holds and on
+items in parts."""
 import math
 
 import numpy as np
@@ -284,3 +286,58 @@ def test_4_bit_values_that_do_not_fit_the_type(cuda_device, dtype, scales, d, T,
         assert np.array_equal(np.isnan(got), np.isnan(want))
         assert np.array_equal(got[~finite & ~np.isnan(want)], want[~finite & ~np.isnan(want)])
         assert (np.abs(np.where(finite, got - want, 0.0)) <= tol).all()
+
+
+# --- scores of any size ---------------------------------------------------------------
+
+@pytest.mark.parametrize("past", [[60, 3], [2900]], ids=["short", "merged"])
+@pytest.mark.parametrize("T", [4, 10, 70])
+@pytest.mark.parametrize("scale", [2.0 ** 24, -3.0e8, 1e12, 1e30])
+@pytest.mark.parametrize("dtype,fmt", [("bf16", "dense"), ("f16", "dense"), ("f32", "dense"),
+                                       ("f16", "mx4")])
+def test_scores_of_any_size(cuda_device, dtype, fmt, scale, T, past):
+    """Finite scores far apart: the one key with the largest has all the weight.
+    Rows are looked at whose two largest scores differ by more than the error of
+    sums of d products in 32 bits and of the scaling; of a row's next key exp(-100)
+    is left, so the result is that key's V, rounded in 32 bits three times."""
+    t, d = ref.DTYPES[dtype], 64
+    c = ref.Cache(11, dtype, fmt, d, 1, P, [p + T for p in past])
+    q = torch.from_numpy(np.random.default_rng(12).standard_normal((T * len(past), 2, d))).to(t)
+    K, V, pages = c.to(cuda_device)
+    out = lib.paged_attn(q.to(cuda_device), K, V, pages,
+                         torch.tensor(past, dtype=torch.int32, device=cuda_device), scale)
+    got, looked = out.cpu().double().numpy(), 0
+    assert np.isfinite(got).all()
+    for b, p in enumerate(past):
+        ids = [int(x) for x in c.pages[b, :-(-(p + T) // P)]]
+        k = np.concatenate([ref.page_rows(c.K, x, 0, d, False) for x in ids])
+        v = np.concatenate([ref.page_rows(c.V, x, 0, d, True) for x in ids])
+        for r in range(T):
+            n = p + r + 1
+            for h in range(2):
+                x = q[b * T + r, h].double().numpy()
+                s = scale * (k[:n] @ x)
+                at = np.argsort(s)
+                slack = 4 * (d + 16) * 2.0 ** -24 * abs(scale) * (np.abs(k[:n]) @ np.abs(x)).max()
+                if s[at[-1]] - s[at[-2]] <= slack + 100:
+                    continue
+                looked += 1
+                w = v[at[-1]]
+                err = np.abs(got[b * T + r, h] - w)
+                assert (err <= (ref.half_step(t) + 3 * 2.0 ** -24) * np.abs(w)).all()
+    print("rows looked at:", looked, flush=True)
+    assert looked > T
+
+
+@pytest.mark.parametrize("T", [4, 10, 70])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_scores_beyond_32_bits(cuda_device, dtype, T):
+    """Infinite in 32 bits, as their difference is then NaN: no row that has one
+    passes for one that sees nothing."""
+    t, d, past = ref.DTYPES[dtype], 64, 200
+    c = ref.Cache(13, dtype, "dense", d, 1, P, [past + T])
+    K, V, pages = c.to(cuda_device)
+    q = torch.from_numpy(np.random.default_rng(2).standard_normal((T, 2, d))).to(t)
+    out = lib.paged_attn(q.to(cuda_device), K, V, pages,
+                         torch.tensor([past], dtype=torch.int32, device=cuda_device), 3.0e38)
+    assert torch.isnan(out).all()
