@@ -385,12 +385,19 @@ def kv_append_rows(K, V, k_new, v_new, lens, stream=None) -> None:
 
 # --- paged cache ----------------------------------------------------------------
 
+# The paged calls' arguments, taken apart in C++.  It is made for one Python and one
+# torch; where it cannot be imported, the calls below do the same work in Python
+# (10 us more a call), and all others do not need it.
 try:
     from . import paged_call as _call
+    _call.use(*(ctypes.cast(getattr(_lib, f), _vp).value
+                for f in ("da_paged_append", "da_paged_gather", "da_paged_attn")))
 except ImportError as e:
-    raise ImportError("paged_call.so is not built; run __graft_entry__.build()") from e
-_call.use(*(ctypes.cast(getattr(_lib, f), _vp).value
-            for f in ("da_paged_append", "da_paged_gather", "da_paged_attn")))
+    import warnings
+
+    warnings.warn(f"paged_call cannot be imported ({e}); paged calls take their arguments apart "
+                  "in Python. Run __graft_entry__.build() to build it.", RuntimeWarning)
+    _call = None
 
 # da_paged_kv: five pointers, ten ints.  Packed as bytes: filling a
 # ctypes.Structure of 15 fields takes twice as long.
@@ -517,7 +524,7 @@ def _paged_stream(stream, gpu) -> int:
 
 def _fast(K, stream):
     """(gpu, stream) of a call that paged_call may take: K on the current device."""
-    if isinstance(K, torch.Tensor):
+    if _call is not None and isinstance(K, torch.Tensor):
         gpu = K.get_device()
         if gpu >= 0 and gpu == torch._C._cuda_getDevice():
             return gpu, _paged_stream(stream, gpu)

@@ -10,16 +10,15 @@ import pytest
 import torch
 
 import paper_2607_19456_amd as lib
-import paper_2607_19456_amd as lib
 import paged_reference as ref
 from test_gpu_paged import check_attn
 
 pytestmark = pytest.mark.gpu
 
 P = 16
-# Rows before the step of each sequence): one workgroup or a few; in parts that
-# the last workgroup puts together (at most 1024 positions, where rows are few);
-# in parts that the merge puts together; many sequences
+# Positions of each sequence before the step: one workgroup or a few; in parts that
+# the last workgroup puts together (at most 1024 positions, where rows are few); in
+# parts that the merge puts together; many sequences.
 PASTS = {"short": [40], "parts": [900], "merged": [2900], "many": [40 + 7 * b for b in range(70)]}
 
 
