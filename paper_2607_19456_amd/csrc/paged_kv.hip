@@ -1482,7 +1482,8 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
       }
-      const float my_ref = limit[nb] == -INFINITY ? -INFINITY : ref[nb];
+      // (no key, or scores that are all -infinity; but NaN among masked ones counts)
+      const float my_ref = limit[nb] == -INFINITY && sum == 0.f ? -INFINITY : ref[nb];
       __syncthreads();
       if (k == 0) {
         s_ref[wave][i] = my_ref;
@@ -1957,7 +1958,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_chunk_kernel
             if (!(fabsf(v) < INFINITY)) acc[c][r] += w * v;
           }
       }
-      const float my_ref = limit == -INFINITY ? -INFINITY : ref;
+      const float my_ref = limit == -INFINITY && sum == 0.f ? -INFINITY : ref;
       if (t0 == 0 && t1 == at.tiles) {
         // (scores that are all -infinity: 0, also where V is not finite)
         const float inverse = 1.f / sum;

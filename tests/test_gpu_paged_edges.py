@@ -340,3 +340,67 @@ def test_scores_beyond_32_bits(cuda_device, dtype, T):
     out = lib.paged_attn(q.to(cuda_device), K, V, pages,
                          torch.tensor([past], dtype=torch.int32, device=cuda_device), 3.0e38)
     assert torch.isnan(out).all()
+
+
+# --- calls that are allowed and rarely made ----------------------------------------------
+
+@pytest.mark.parametrize("past", [[40, 3], [2900, 700], [50 + 3 * b for b in range(70)]],
+                         ids=["short", "merged", "many"])
+@pytest.mark.parametrize("T", [1, 10, 40])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_result_in_the_place_of_q(cuda_device, dtype, T, past):
+    t = ref.DTYPES[dtype]
+    c = ref.Cache(3, dtype, "dense", 64, 2, P, [p + T for p in past])
+    K, V, pages = c.to(cuda_device)
+    past = torch.tensor(past, dtype=torch.int32, device=cuda_device)
+    q = torch.randn(len(past) * T, 8, 64, device=cuda_device).to(t)
+    want = lib.paged_attn(q, K, V, pages, past, 0.125)
+    assert lib.paged_attn(q, K, V, pages, past, 0.125, out=q) is q
+    assert torch.equal(q, want)
+
+
+@pytest.mark.parametrize("past", [0, 1, 5, 31, 64, 200, 500, 2900])
+@pytest.mark.parametrize("T", [1, 4, 10, 70])
+@pytest.mark.parametrize("dtype,fmt", [("bf16", "dense"), ("bf16", "mx4"), ("f16", "mx4"),
+                                       ("f32", "dense"), ("f32", "mx4")])
+def test_a_row_of_nan_leaves_the_others(cuda_device, dtype, fmt, T, past):
+    """Queries of NaN and of infinities of either sign: their own rows are NaN, the
+    others' as ever but for the rounding of their scores' scaling, which may be another
+    one: an error of 2^-23 of scores below 8, of their weights, twice."""
+    t = ref.DTYPES[dtype]
+    c = ref.Cache(3, dtype, fmt, 64, 2, P, [past + T, 9 + T])
+    K, V, pages = c.to(cuda_device)
+    past = torch.tensor([past, 9], dtype=torch.int32, device=cuda_device)
+    q = torch.randn(2 * T, 4, 64, device=cuda_device).to(t)
+    want = lib.paged_attn(q, K, V, pages, past, 0.125)
+    bad = torch.zeros(2 * T, 4, dtype=torch.bool, device=cuda_device)
+    bad[0, 1] = bad[T - 1, 2] = bad[T, 0] = True
+    q[0, 1, 5], q[T - 1, 2, 0::2], q[T - 1, 2, 1::2] = math.nan, math.inf, -math.inf
+    q[T, 0] = math.nan
+    got = lib.paged_attn(q, K, V, pages, past, 0.125)
+    assert torch.isnan(got[bad]).all()
+    got, want = got[~bad].double(), want[~bad].double()
+    slack = 2 * 8 * 2.0 ** -23 * 4 + 2 * ref.half_step(t)
+    assert ((got - want).abs() <= slack * want.abs().max()).all()
+
+
+@pytest.mark.parametrize("dtype,fmt,d", [("bf16", "dense", 128), ("f32", "mx4", 256),
+                                         ("f16", "mx4", 64)])
+def test_the_largest_pages(cuda_device, dtype, fmt, d):
+    """32768 rows a page: an append at its end, read back, and attention over it."""
+    n = 32768
+    c = ref.Cache(4, dtype, fmt, d, 1, n, [n - 3, 9], spare=0)
+    K, V, pages = c.to(cuda_device)
+    past = torch.tensor([n - 3, 9], dtype=torch.int32, device=cuda_device)
+    t = ref.DTYPES[dtype]
+    k, v, q = (torch.randn(6, h, d, device=cuda_device).to(t) for h in (1, 1, 2))
+    lib.paged_append(K, V, pages, past, k, v)
+    back = [torch.empty_like(k) for _ in range(2)]
+    lib.paged_gather(K, V, pages, past, *back)
+    if fmt == "dense":
+        assert torch.equal(back[0], k) and torch.equal(back[1], v)
+    out = lib.paged_attn(q, K, V, pages, past, 1 / math.sqrt(d))
+    want, mass, spread, seen, _, top = ref.attention(
+        q.cpu(), K.cpu(), V.cpu(), c.pages.numpy(), [n - 3, 9], 1 / math.sqrt(d), True, None, 3, 1)
+    tol = ref.tolerance(want, mass, spread, seen, top, t, d)
+    assert (np.abs(out.cpu().double().numpy() - want) <= tol).all()
