@@ -404,3 +404,29 @@ def test_the_largest_pages(cuda_device, dtype, fmt, d):
         q.cpu(), K.cpu(), V.cpu(), c.pages.numpy(), [n - 3, 9], 1 / math.sqrt(d), True, None, 3, 1)
     tol = ref.tolerance(want, mass, spread, seen, top, t, d)
     assert (np.abs(out.cpu().double().numpy() - want) <= tol).all()
+
+
+@pytest.mark.parametrize("T", [1, 4, 12])
+@pytest.mark.parametrize("dtype,fmt,pages", [("bf16", "dense", 512), ("f32", "mx4", 512),
+                                             ("f16", "mx4", 32768)])
+def test_as_many_positions_as_there_are(cuda_device, dtype, fmt, pages, T):
+    """Up to 2^30 positions of a sequence, one page of 32768 over and over: the
+    attention over that page once.  A wave's sums are chains of at most
+    positions / (512 * 4 * 32) additions, each off by 2^-24 of the sum, twice (value and
+    divisor); the merges add less; both results are rounded to the type, and the page's
+    own result may be off by the bound of its own sums."""
+    t, d, n = ref.DTYPES[dtype], 64, 32768
+    c = ref.Cache(6, dtype, fmt, d, 1, n, [n], spare=0)
+    K, V, _ = c.to(cuda_device)
+    q = torch.randn(T, 4, d, device=cuda_device).to(t)
+    out = []
+    for count in (1, pages):
+        table = torch.zeros(1, count, dtype=torch.int32, device=cuda_device)
+        past = torch.tensor([count * n], dtype=torch.int32, device=cuda_device)
+        print("positions", count * n, flush=True)
+        out.append(lib.paged_attn(q, K, V, table, past, 0.125, causal=False).double().cpu())
+    largest = float(np.abs(np.nan_to_num(ref.page_rows(c.V, 0, 0, d, True))).max())
+    steps = pages * n / (512 * 4 * 32) + n / 16 + 64
+    slack = 2 * steps * 2.0 ** -24 * largest + 2 * ref.half_step(t) * largest
+    print("off by", float((out[1] - out[0]).abs().max()), "of", slack, flush=True)
+    assert (out[1] - out[0]).abs().max() <= slack
