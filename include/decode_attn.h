@@ -347,7 +347,10 @@ da_status da_decode_attn_noalloc(const float *q, const float *K,
  * 2, 3, 4, 6 times 2^X (ties to the even code; above 6: 6), the code's low
  * three bits counting these levels and its bit 3 the sign (the OCP microscaling
  * format MXFP4).  A block with an infinity or a NaN has the byte 255 and reads
- * as NaN.  A page of one head is page_rows*(d/2 + d/32) bytes:
+ * as NaN.  A pool is not tied to a type of rows: a call takes its values rounded to
+ * its dtype, so 4-bit values that other rows or another program wrote, and that the
+ * dtype does not hold, are infinities in it.  A page of one head is
+ * page_rows*(d/2 + d/32) bytes:
  *     K: code bytes [page_rows][d/2] (dimension 2j in the low half of byte j),
  *        then scale bytes [page_rows][d/32];
  *     V: code bytes [page_rows/8][d/8][8][4]: for 8 rows, 8 dimensions of each
@@ -356,9 +359,10 @@ da_status da_decode_attn_noalloc(const float *q, const float *K,
  * those of the exact product with the table.
  *
  * Supported: d in {64, 128, 256}; page_rows a power of two from 16 to 32768;
- * page_rows*max_pages <= 2^30; T <= 32768; h_kv dividing h_q.  Pools, rows and
- * tables are 16-byte aligned, strides between tokens multiples of 16 bytes and
- * at least a token's own size.
+ * page_rows*max_pages <= 2^30; T <= 32768; h_kv dividing h_q.  All sizes are at
+ * least 1: sequences of a batch may have no rows, but arrays of no rows at all are
+ * DA_ERR_SHAPE.  Pools, rows and tables are 16-byte aligned, strides between tokens
+ * multiples of 16 bytes and at least a token's own size.
  * Errors are checked in the order of the enumeration (workspace last).
  * ---------------------------------------------------------------------------
  */
@@ -420,16 +424,21 @@ da_status da_paged_gather(const da_paged_kv *kv, void *k_out, void *v_out,
  * the step are in the cache already: append first), else 0 .. past[b] - 1 (cross
  * attention to past[b] states of an encoder, of any number per sequence).  A
  * row that sees nothing, or whose scores are all -infinity, gives 0.  What a
- * row does not see stays out of it, infinities and NaN included.
+ * row does not see stays out of it, infinities and NaN included; of what it sees,
+ * a NaN in q or K gives NaN, and a V that is not finite an infinity or (where its
+ * weight is 0) NaN in its dimension, however the row's work is divided.  Scores
+ * beyond 32 bits give NaN.  A scale of 0 takes q for 0.
  * q [rows][h_q][d] with a token stride in elements, out [rows][h_q][d]
- * contiguous.  The work, counted from past and row_start on the device, is
- * divided evenly over a resident grid whatever the lengths, and the parts of a
- * row are put together in a fixed order: equal calls give equal bits.  One
+ * contiguous (and may be q, where q is).  The work, counted from past and row_start
+ * on the device, is divided evenly over a grid of two workgroups a compute unit
+ * whatever the lengths (both resident for d of 64 and 128, one at a time for most
+ * of d = 256), and the parts of a row are put together in a fixed order: equal
+ * calls give equal bits.  One
  * launch where a KV head has at most 16 query rows and a row few parts
  * (4*B*h_kv at least twice the compute units, or page_rows*max_pages <= 1024),
- * else two.  Scores, softmax and
- * sums in 32 bits; 16-bit types multiply in their own type (weights rounded to
- * it, once), float32 in float32.
+ * else two.  Scores, softmax and sums in 32 bits; 16-bit types multiply in their
+ * own type (weights rounded to it, once, and divided by the sum of the rounded
+ * ones), float32 in float32.
  * workspace: da_paged_workspace_bytes(...) bytes, 16-byte aligned, one call at
  * a time.  Its leading da_paged_workspace_counter_bytes(...) bytes must be zero
  * when a call starts, and are zero again when it is done; the rest may hold

@@ -8,7 +8,7 @@
 //   paged_gather_kernel   the same places read back as dense rows.
 //   paged_attn_kernel     softmax(scale q.K) V over the pages of each (sequence,
 //                         KV head, tile of query rows), split evenly over a
-//                         resident grid, as partial states.
+//                         grid of two workgroups a CU, as partial states.
 //   paged_chunk_kernel    the same for many query rows per KV head, K and V
 //                         shared by four waves through LDS.
 //   paged_merge_kernel    combines the parts of each query row.
@@ -424,10 +424,12 @@ __global__ __launch_bounds__(kThreads) void paged_gather_kernel(Batch bt, void* 
 // row x of a KV head's rows is (token x / G, query head x % G of the group), so
 // a tile's rows see nearly the same keys.  An item's keys are cut into tiles of
 // KT = 4*TK, and all items' costs (kItemCost), laid end to end (sequences, heads,
-// row tiles), are divided evenly over the resident workgroups, which count for
-// themselves, from past and row_start, where each one's share begins.  A workgroup
-// begins and ends inside at most one item each; those parts go to its two slots of
-// the workspace, the rest straight to out.  The parts of an item are then those of
+// row tiles), are divided evenly over the grid's workgroups, which count for
+// themselves, from past and row_start, where each one's share begins.  The grid is
+// two workgroups a CU: all resident for d = 64 and 128; of d = 256 most instances
+// take more than 256 registers a lane, and one runs at a time.  A workgroup begins
+// and ends inside at most one item each; those parts go to its two slots of the
+// workspace, the rest straight to out.  The parts of an item are then those of
 // consecutive workgroups and are summed in their order, by whichever workgroup or
 // launch does it: equal calls give equal bits.
 //
@@ -440,12 +442,16 @@ __global__ __launch_bounds__(kThreads) void paged_gather_kernel(Batch bt, void* 
 // in by rows (lane (i, k): its keys, D/16 dimensions of each), which float32
 // products take as they are; 16-bit ones want a dimension's keys side by side
 // in a register, two byte permutes for four values.
+// Weights of 16-bit types are rounded to the type, as the second product takes
+// them: half a step each, with the same weights summed for the divisor.  Errors
+// against 64 bits are then 0.0020-0.0023 of the result (bfloat16; float16
+// 0.00028), where one rounding of the result alone gives 0.0017 (0.00021).
 //
 // What bounds it: the reading of the cache.  Kernel times over 4 sequences of
 // 65k-131k rows (64/8 heads, d = 128): bfloat16 261 us, 6.7 TB/s (the same loads
 // without the products 260); 4 bits 82 us, 5.7 TB/s (77); float32, 16 x 8192
 // rows, 32/8 heads: 168 us, 6.4 TB/s.  Small batches are bound by what is not
-// reading: of one sequence of 700 rows' 9 us, 1.7 are the launch, 1.4 the count of
+// reading: of one sequence of 700 rows' 9.2 us, 1.7 are the launch, 1.4 the count of
 // the work, 1.4 the way to the first loads and 3 the exchange at the end.
 // ---------------------------------------------------------------------------
 template <class T, bool MX, int D>
@@ -650,7 +656,8 @@ __device__ __forceinline__ int key_tiles(const Batch& bt, const AttnArgs& a, int
 // cost, and every item begins with its fixed part.  (Measured: 4 to 6 us an item,
 // 1.7 to 2.7 us a tile.  256 items of 1 to 12 tiles take 50 us if this is left
 // out and 33 with 1 to 3; 8 sequences of 15 rows a head over 500 to 4000 keys 43,
-// 42, 39 and 39 us with 0, 1, 2 and 3.)
+// 42, 39 and 39 us with 0, 1, 2 and 3.  The chunk kernel, whose tiles cost something
+// else, takes the same 3 unmeasured.)
 constexpr int kItemCost = 3;
 
 template <int R, int KT, bool MANY>
@@ -1600,15 +1607,17 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Batch bt, AttnArgs
 // Two waves bring in K, two V (turned on the way: V lies in LDS by dimensions,
 // eight keys side by side); the next tile's loads are in flight during a tile's
 // products, and the tiles alternate between two buffers: one barrier each.
-// Chunks of 16 bytes are stored at their index XOR a function of the row, so
-// that the eight lanes of every 128-byte LDS access hit different banks.
+// Chunks of 16 bytes are stored at their index XOR a function of the row, to
+// spread the eight lanes of a 128-byte LDS access over the banks.  (Not all are:
+// conflicts still take a fifth of LDS's busy cycles.)
 // A key tile of 16-bit values is 32 KB: two workgroups fit a CU, and one's
 // softmax overlaps the other's products.
-// Measured: chunks of four prompts, 359 GFLOP, 542 us with the merge (662 TFLOP/s;
-// the matrix pipes are busy for 35 % of the cycles, the vector units for 44 %, LDS
-// for 41 %).  64 rows a wave at one wave per SIMD halve the LDS reads and were 9 %
-// slower to 9 % faster by shape (605 -> 624 for these chunks); a tile's scores
-// between the weights of the one before were 2 to 9 % slower.  Neither is taken.
+// Measured: chunks of four prompts, 359 GFLOP, 547 us a call with the merge (657
+// TFLOP/s; 535 to 565 by the card's clock; the matrix pipes are busy for 35 % of the
+// cycles, the vector units for 43 %, LDS for 41 %).  64 rows a wave at one wave per
+// SIMD halve the LDS reads and were 9 % slower to 9 % faster by shape (605 -> 624 us
+// for these chunks, both before later steps); a tile's scores between the weights of
+// the one before were 2 to 9 % slower.  Neither is taken.
 // ---------------------------------------------------------------------------
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
