@@ -427,7 +427,8 @@ da_status da_paged_gather(const da_paged_kv *kv, void *k_out, void *v_out,
  * row does not see stays out of it, infinities and NaN included; of what it sees,
  * a NaN in q or K gives NaN, and a V that is not finite an infinity or (where its
  * weight is 0) NaN in its dimension, however the row's work is divided.  Scores
- * beyond 32 bits give NaN.  A scale of 0 takes q for 0.
+ * beyond 32 bits give NaN; weights and results below its normal numbers may be 0.
+ * A scale of 0 takes q for 0.
  * q [rows][h_q][d] with a token stride in elements, out [rows][h_q][d]
  * contiguous (and may be q, where q is).  The work, counted from past and row_start
  * on the device, is divided evenly over a grid of two workgroups a compute unit

@@ -610,7 +610,7 @@ __device__ __forceinline__ int seen_by(const Batch& bt, const AttnArgs& a, int p
 
 // A score's distance from the reference is taken in one multiply-add, which keeps
 // what the reference lost when it was rounded: the same factor for every key, small
-// enough below kFar (2^4 at most).  Beyond, the product is rounded as the reference
+// enough below kFar (2^2 at most).  Beyond, the product is rounded as the reference
 // was, so that the largest score's weight is 1; scores beyond 32 bits give NaN.
 constexpr float kFar = 0x1p26f;
 __device__ __forceinline__ bool is_far(float ref) {
