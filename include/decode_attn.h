@@ -461,6 +461,137 @@ size_t da_paged_workspace_counter_bytes(int B, int h_q, int h_kv, int d, int T,
 
 /*
  * ---------------------------------------------------------------------------
+ * Attention over whole prompts, without a cache, and its gradient.
+ *
+ * Sequences of different lengths lie packed one after the other, token-major
+ * ([rows][heads][d], heads of one token contiguous, any stride between tokens:
+ * views into a fused projection's output).  Sequence b has rows row_start[b] ..
+ * row_start[b+1]-1 of q, at most T of them, and keys key_start[b] ..
+ * key_start[b+1]-1 of k and v, at most N (a longer sequence's further rows and
+ * keys are not its own); row_start NULL: T rows each (rows = B*T), key_start
+ * NULL: N keys each (keys = B*N).  Self-attention gives the same array twice.
+ * What the starts hold is taken within the arrays, whatever it is.  Arrays may
+ * hold rows and keys behind the last sequence's: neither they nor their results
+ * are touched.
+ *
+ * Of a sequence of t rows and n keys, row r sees the keys 0 .. r + n - t if
+ * causal (the last row sees all), else all n.  Head map as above.
+ *
+ * Supported: d in {64, 128, 256}; types DA_F32, DA_BF16, DA_F16; h_kv dividing
+ * h_q; T*(h_q/h_kv) and N up to 2^30.  All sizes are at least 1: sequences may
+ * have no rows or no keys, but arrays of none at all are DA_ERR_SHAPE.  Arrays are
+ * 16-byte aligned (lse and the starts 4), strides between tokens multiples of 16
+ * bytes and at least a token's own size.  Errors are checked in the order of the
+ * enumeration (workspace last).
+ * ---------------------------------------------------------------------------
+ */
+typedef struct da_prompt {
+    const int32_t *row_start, *key_start; /* [B+1] each (device), or NULL    */
+    int B, h_q, h_kv, d;
+    int rows, keys;                       /* of the arrays                   */
+    int T, N;                             /* most rows, keys of a sequence   */
+    int dtype, causal;
+} da_prompt;
+
+/*
+ * out[n,h,:] = softmax_l(scale * q[n,h,:].k[l,:]) v[l,:] over the keys that the
+ * row sees, out [rows][h_q][d] contiguous (and may be q, where q is contiguous),
+ * and, where lse is given, lse[n,h] = ln sum_l exp(scale * q[n,h,:].k[l,:]),
+ * [rows][h_q] float.  A row that sees nothing, or whose scores are all -infinity,
+ * gives 0 and an lse of -infinity.  What a row does not see stays out of it,
+ * infinities and NaN included; of what it sees, a NaN in q or k gives NaN, and a
+ * v that is not finite an infinity or (where its weight is 0) NaN in its dimension.
+ * Scores beyond 32 bits give NaN; weights and results below the normal numbers
+ * of 32 bits may be 0.  A scale of 0 takes q for 0.
+ * Scores, softmax and sums in 32 bits; 16-bit types multiply in their own type
+ * (weights rounded to it, once, and divided by the sum of the rounded ones; lse
+ * is that of the unrounded ones), float32 in float32.  Every sum has one order:
+ * equal calls give equal bits.  One launch, or two where few rows see many keys.
+ * workspace: da_prompt_workspace_bytes(...) bytes, 16-byte aligned, one call at
+ * a time; it may hold anything.
+ */
+da_status da_prompt_attn(const da_prompt *prompt, const void *q,
+                         int64_t q_stride, const void *k, int64_t k_stride,
+                         const void *v, int64_t v_stride, float scale,
+                         void *out, float *lse, void *workspace,
+                         size_t workspace_bytes, void *stream);
+
+/* Workspace of da_prompt_attn for these sizes, on any device and for any
+ * lengths (what the starts point to is not read).  0 if invalid. */
+size_t da_prompt_workspace_bytes(const da_prompt *prompt);
+
+/*
+ * The gradient of out with respect to q, k and v, given d_out [rows][h_q][d],
+ * the q, k, v and scale of the call before, and the out and lse that it returned:
+ * with P = exp(scale q.k - lse), dP = d_out.v and delta = sum_d d_out*out,
+ *     dS = P (dP - delta),  dq = scale dS k,  dk = scale dS^T q,  dv = P^T d_out,
+ * dk and dv summed over the rows that see the key and the heads that share it.
+ * Keys that no row sees get 0.  dq, dk and dv have strides of their own (views
+ * into a fused projection's gradient); none may overlap an input or another.
+ * What a row does not see stays out of its dq, and a row out of dk and dv of keys
+ * that it does not see, infinities and NaN included; of the others a NaN gives NaN
+ * and an infinity what the formulas give.  P carries the error of lse, 2^-23 of
+ * its size.  Rows with an lse of -infinity have no weights.
+ * Sums in 32 bits; 16-bit types multiply in their own type (P and dS rounded to
+ * it, once), float32 in float32.  No atomics: equal calls give equal bits.
+ * workspace: da_prompt_grad_workspace_bytes(...), as above.
+ */
+da_status da_prompt_attn_grad(const da_prompt *prompt, const void *q,
+                              int64_t q_stride, const void *k,
+                              int64_t k_stride, const void *v,
+                              int64_t v_stride, const void *out,
+                              const float *lse, const void *d_out,
+                              int64_t d_out_stride, float scale, void *dq,
+                              int64_t dq_stride, void *dk, int64_t dk_stride,
+                              void *dv, int64_t dv_stride, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/* Workspace of da_prompt_attn_grad for these sizes.  0 if invalid. */
+size_t da_prompt_grad_workspace_bytes(const da_prompt *prompt);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Rotation of q and k by positions of several axes: time, height and width of
+ * images and video, all the same in text.
+ *
+ * A row has a position on each axis, positions[axis][row].  Of the rot_dim/2
+ * pairs of a head's first rot_dim dimensions, the first sections[0] turn by the
+ * first axis's position, the next sections[1] by the second's, and so on; pair i
+ * by the angle of column i of the table at that position ([n_table][rot_dim]
+ * float, cosines then sines, as in da_paged_append).  With half = rot_dim/2,
+ * pair i is the dimensions (i, i + half), or (2i, 2i+1) if interleaved, and becomes
+ *     x1*cos - x2*sin,  x2*cos + x1*sin,
+ * with inverse the sines negated: the rotation back, and the gradient.  Other
+ * dimensions are copied.  A position outside [0, n_table) turns nothing: its
+ * axis's pairs are copied.  Products and sums in 32 bits, one rounding.
+ *
+ * Supported: d in {64, 128, 256}, rot_dim a multiple of 16 up to d, 1 to 4 axes
+ * whose sections add up to rot_dim/2 (a section may be 0).
+ * ---------------------------------------------------------------------------
+ */
+typedef struct da_rotary {
+    const int32_t *positions;  /* [axes][rows] (device)          */
+    const float *table;        /* [n_table][rot_dim] (device)    */
+    int rows, d, dtype;
+    int n_table, rot_dim;
+    int axes, sections[4];
+    int interleaved, inverse;
+} da_rotary;
+
+/*
+ * q [rows][h_q][d] into q_out, k [rows][h_kv][d] into k_out (k NULL: q alone),
+ * strides between tokens in elements.  An output may be its input (with one
+ * stride); otherwise nothing may overlap.  Arrays 16-byte aligned, strides
+ * multiples of 16 bytes and at least a token's own size.  One launch.
+ */
+da_status da_rotary_axes(const da_rotary *rotary, const void *q,
+                         int64_t q_stride, int h_q, void *q_out,
+                         int64_t q_out_stride, const void *k, int64_t k_stride,
+                         int h_kv, void *k_out, int64_t k_out_stride,
+                         void *stream);
+
+/*
+ * ---------------------------------------------------------------------------
  * Tuning and testing only.  The entry points above choose their own segment
  * size (the most rows a workgroup reads from its static range in one go,
  * and for caches scheduled without a static share also the unit handed out

@@ -17,6 +17,8 @@ _BINDING_NAMES = {
     "alloc_workspace", "DecodeAttnError",
     "paged_alloc", "paged_append", "paged_attn", "paged_gather", "paged_workspace",
     "paged_workspace_bytes", "paged_workspace_counter_bytes", "rotary_table",
+    "prompt_attn", "prompt_attn_grad", "prompt_workspace", "prompt_workspace_bytes",
+    "rotary_axes",
     "LIBRARY_PATH",
 }
 

@@ -40,6 +40,13 @@ SIGNATURES = {
     "da_decode_merge": (_ci, [_vp, _vp] + [_ci] * 6 + [_vp, _sz, _vp]),
     "da_decode_multi": (_ci, [_vp, _vp, _vp, _vp, _cf, _vp] + [_ci] * 7 + [_vp, _sz, _vp]),
     "da_decode_multi_step": (_ci, [_vp] * 6 + [_cf, _vp] + [_ci] * 7 + [_vp, _sz, _vp]),
+    "da_prompt_attn": (_ci, [ctypes.c_char_p] + [_vp, _i64] * 3
+                       + [_cf, _vp, _vp, _vp, _sz, _vp]),
+    "da_prompt_workspace_bytes": (_sz, [ctypes.c_char_p]),
+    "da_prompt_attn_grad": (_ci, [ctypes.c_char_p] + [_vp, _i64] * 3
+                            + [_vp, _vp, _vp, _i64, _cf] + [_vp, _i64] * 3 + [_vp, _sz, _vp]),
+    "da_prompt_grad_workspace_bytes": (_sz, [ctypes.c_char_p]),
+    "da_rotary_axes": (_ci, [ctypes.c_char_p] + [_vp, _i64, _ci, _vp, _i64] * 2 + [_vp]),
     "da_kv_append": (_ci, [_vp] * 5 + [_ci] * 5 + [_vp]),
     "da_kv_append_rows": (_ci, [_vp] * 5 + [_ci] * 6 + [_vp]),
     "da_decode_attn_noalloc": (_ci, [_vp, _vp, _vp, _vp, _cf, _vp] + [_ci] * 6 + [_vp]),
@@ -682,3 +689,211 @@ def paged_attn(q, K, V, pages, past, scale: float, causal: bool = True, row_star
     if status:
         _check("da_paged_attn", status)
     return out
+
+
+# --- whole prompts ----------------------------------------------------------------
+
+# da_prompt: two pointers, ten ints.  da_rotary: two pointers, twelve ints.
+_pack_prompt = struct.Struct("=2Q10i").pack
+_pack_rotary = struct.Struct("=2Q12i").pack
+
+
+def _tokens(t, name, dtype, gpu, rows, heads, d):
+    """(address, token stride) of rows [rows, heads, d] of a token-major array."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 3:
+        raise ValueError(f"{name} must be [rows, heads, d]")
+    if t.dtype is not dtype or t.get_device() != gpu or gpu < 0:
+        _refuse(t, name, dtype, gpu)
+    shape = t.shape
+    if shape[0] != rows or shape[1] != heads or shape[2] != d:
+        raise ValueError(f"{name} must be [{rows},{heads},{d}], got {list(shape)}")
+    return t.data_ptr(), heads * d if t.is_contiguous() else _stride(t, name, shape)
+
+
+def _prompt(q, k, row_start, T, key_start, N, causal):
+    """(da_prompt as bytes, current device) of a call's batch."""
+    rows, h_q, d = _rows(q, "q")
+    keys, h_kv, _ = _rows(k, "k")
+    code = _DTYPES.get(q.dtype)
+    if code is None:
+        raise TypeError(f"q must be float32, bfloat16 or float16, got {q.dtype}")
+    gpu = q.get_device()
+    if gpu < 0 or gpu != torch._C._cuda_getDevice():
+        _refuse(q, "q", q.dtype, torch.cuda.current_device() if gpu >= 0 else 0)
+    if key_start is None and N == 0 and row_start is not None and keys == rows:
+        key_start, N = row_start, T
+    rs = ks = 0
+    B = None
+    if row_start is not None:
+        rs = _here(row_start, "row_start", _i32, gpu)
+        _need(row_start.dim() == 1 and row_start.numel() >= 2, "row_start must be [B+1]")
+        _need(T >= 1, "with row_start, T is the most rows of a sequence")
+        B = row_start.numel() - 1
+    if key_start is not None:
+        ks = _here(key_start, "key_start", _i32, gpu)
+        _need(key_start.dim() == 1 and key_start.numel() >= 2, "key_start must be [B+1]")
+        _need(N >= 1, "with key_start, N is the most keys of a sequence")
+        _need(B is None or B == key_start.numel() - 1, "row_start and key_start must be of one B")
+        B = key_start.numel() - 1
+    if row_start is None:
+        if B is None:
+            B = rows // T if T > 0 else 1
+        T = T or rows // max(B, 1)
+        _need(rows == B * T, "without row_start every sequence has T rows: rows must be B*T")
+    if key_start is None:
+        N = N or keys // max(B, 1)
+        _need(keys == B * N, "without key_start every sequence has N keys: keys must be B*N")
+    try:
+        return _pack_prompt(rs, ks, B, h_q, h_kv, d, rows, keys, T, N, code,
+                            1 if causal else 0), gpu
+    except struct.error as e:
+        raise ValueError(f"sizes, T and N must be integers of 32 bits: {e}") from None
+
+
+def _bytes(n, stream, gpu):
+    """n bytes in memory of the stream that will use them."""
+    with torch.cuda.stream(stream):            # (None: the current one)
+        return torch.empty(n, dtype=_u8, device=f"cuda:{gpu}")
+
+
+def prompt_workspace_bytes(q, k, row_start=None, T: int = 0, key_start=None, N: int = 0,
+                           grad: bool = False) -> int:
+    """Workspace bytes of prompt_attn (grad: of prompt_attn_grad) for these arrays (0:
+    invalid)."""
+    p, _ = _prompt(q, k, row_start, T, key_start, N, True)
+    return int((_lib.da_prompt_grad_workspace_bytes if grad
+                else _lib.da_prompt_workspace_bytes)(p))
+
+
+def prompt_workspace(q, k, row_start=None, T: int = 0, key_start=None, N: int = 0,
+                     grad: bool = False) -> torch.Tensor:
+    """A workspace for prompt_attn (grad: for prompt_attn_grad) with these arrays:
+    reusable call after call, by one call at a time."""
+    n = prompt_workspace_bytes(q, k, row_start, T, key_start, N, grad)
+    if n == 0:
+        _check("da_prompt_workspace_bytes", 2)
+    return torch.empty(n, dtype=_u8, device=q.device)
+
+
+def prompt_attn(q, k, v, scale: float, causal: bool = True, row_start=None, T: int = 0,
+                key_start=None, N: int = 0, out=None, lse=None, workspace=None,
+                stream=None) -> torch.Tensor:
+    """out[n,h,:] = softmax(scale * q[n,h] k) v over packed sequences: rows
+    row_start[b] .. row_start[b+1]-1 of q [rows,h_q,d], at most ``T``, attend to keys
+    key_start[b] .. of k and v [keys,h_kv,d], at most ``N``, all of them or (causal) up
+    to the row's own, the last row's being the last key.  Without ``row_start`` every
+    sequence has T rows (0: one sequence), without ``key_start`` N keys; where neither
+    is given and there are as many keys as rows, the keys are the rows' own.  ``lse``
+    [rows,h_q] float32 is written where given: what prompt_attn_grad needs.  Any stride
+    between tokens.  An ``out`` or ``workspace`` not given is allocated on ``stream``."""
+    p, gpu = _prompt(q, k, row_start, T, key_start, N, causal)
+    rows, h_q, d = q.shape
+    keys, h_kv = k.shape[:2]
+    dtype = q.dtype
+    qp, qs = _tokens(q, "q", dtype, gpu, rows, h_q, d)
+    kp, ks = _tokens(k, "k", dtype, gpu, keys, h_kv, d)
+    vp, vs = _tokens(v, "v", dtype, gpu, keys, h_kv, d)
+    if out is None:
+        out = _empty(q, "q", stream)
+    op = _here(out, "out", dtype, gpu)
+    _need(out.shape == q.shape, "out must have q's shape")
+    lp = None
+    if lse is not None:
+        lp = _here(lse, "lse", _f32, gpu)
+        _need(lse.shape == (rows, h_q), "lse must be [rows,h_q]")
+    if workspace is None:
+        n = _lib.da_prompt_workspace_bytes(p)
+        workspace = _bytes(max(int(n), 16), stream, gpu)
+    status = _lib.da_prompt_attn(p, qp, qs, kp, ks, vp, vs, scale, op, lp,
+                                 _here(workspace, "workspace", _u8, gpu), workspace.numel(),
+                                 _paged_stream(stream, gpu))
+    if status:
+        _check("da_prompt_attn", status)
+    return out
+
+
+def prompt_attn_grad(q, k, v, out, lse, d_out, scale: float, causal: bool = True, row_start=None,
+                     T: int = 0, key_start=None, N: int = 0, dq=None, dk=None, dv=None,
+                     workspace=None, stream=None):
+    """(dq, dk, dv): the gradient of prompt_attn's ``out`` with respect to q, k and v
+    for d_out [rows,h_q,d], out and lse being that call's.  dq, dk and dv may be given
+    with any stride between tokens (views into a fused projection's gradient); those
+    not given, and the workspace, are allocated on ``stream``."""
+    p, gpu = _prompt(q, k, row_start, T, key_start, N, causal)
+    rows, h_q, d = q.shape
+    keys, h_kv = k.shape[:2]
+    dtype = q.dtype
+    a = _tokens(q, "q", dtype, gpu, rows, h_q, d)
+    b = _tokens(k, "k", dtype, gpu, keys, h_kv, d)
+    c = _tokens(v, "v", dtype, gpu, keys, h_kv, d)
+    op = _here(out, "out", dtype, gpu)
+    _need(out.shape == q.shape, "out must have q's shape")
+    lp = _here(lse, "lse", _f32, gpu)
+    _need(lse.shape == (rows, h_q), "lse must be [rows,h_q]")
+    g = _tokens(d_out, "d_out", dtype, gpu, rows, h_q, d)
+    if dq is None:
+        dq = _empty(q, "q", stream)
+    if dk is None:
+        dk = _empty(k, "k", stream)
+    if dv is None:
+        dv = _empty(v, "v", stream)
+    results = (*_tokens(dq, "dq", dtype, gpu, rows, h_q, d),
+               *_tokens(dk, "dk", dtype, gpu, keys, h_kv, d),
+               *_tokens(dv, "dv", dtype, gpu, keys, h_kv, d))
+    if workspace is None:
+        n = _lib.da_prompt_grad_workspace_bytes(p)
+        workspace = _bytes(max(int(n), 16), stream, gpu)
+    status = _lib.da_prompt_attn_grad(p, *a, *b, *c, op, lp, *g, scale, *results,
+                                      _here(workspace, "workspace", _u8, gpu),
+                                      workspace.numel(), _paged_stream(stream, gpu))
+    if status:
+        _check("da_prompt_attn_grad", status)
+    return dq, dk, dv
+
+
+def rotary_axes(q, positions, table, sections, k=None, interleaved: bool = False,
+                inverse: bool = False, q_out=None, k_out=None, stream=None):
+    """(q_out, k_out): q [rows,h_q,d] and, where given, k [rows,h_kv,d] turned by
+    positions of several axes.  ``positions`` int32 [axes,rows]; ``table`` as of
+    rotary_table, [positions,rot_dim]; ``sections``: how many of the rot_dim/2 pairs
+    each axis turns.  ``inverse`` turns back, which is the gradient.  Any stride
+    between tokens; results not given are allocated on ``stream``, and may be the
+    inputs."""
+    rows, h_q, d = _rows(q, "q")
+    dtype = q.dtype
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise TypeError(f"q must be float32, bfloat16 or float16, got {dtype}")
+    gpu = q.get_device()
+    if gpu < 0 or gpu != torch._C._cuda_getDevice():
+        _refuse(q, "q", dtype, torch.cuda.current_device() if gpu >= 0 else 0)
+    pp = _here(positions, "positions", _i32, gpu)
+    axes = len(sections)
+    _need(1 <= axes <= 4, "there must be 1 to 4 sections")
+    _need(positions.shape == (axes, rows), "positions must be [axes,rows]")
+    tp = _here(table, "table", _f32, gpu)
+    _need(table.dim() == 2, "table must be [positions, rot_dim]")
+    n_table, rot_dim = table.shape
+    qp, qs = _tokens(q, "q", dtype, gpu, rows, h_q, d)
+    if q_out is None:
+        q_out = _empty(q, "q", stream)
+    qo, qos = _tokens(q_out, "q_out", dtype, gpu, rows, h_q, d)
+    h_kv = ks = kos = 0
+    kp = ko = None
+    if k is not None:
+        h_kv = _rows(k, "k")[1]
+        kp, ks = _tokens(k, "k", dtype, gpu, rows, h_kv, d)
+        if k_out is None:
+            k_out = _empty(k, "k", stream)
+        ko, kos = _tokens(k_out, "k_out", dtype, gpu, rows, h_kv, d)
+    try:
+        p = _pack_rotary(pp, tp, rows, d, code, n_table, rot_dim, axes,
+                         *sections, *(0,) * (4 - axes), 1 if interleaved else 0,
+                         1 if inverse else 0)
+    except struct.error as e:
+        raise ValueError(f"sizes and sections must be integers of 32 bits: {e}") from None
+    status = _lib.da_rotary_axes(p, qp, qs, h_q, qo, qos, kp, ks, h_kv, ko, kos,
+                                 _paged_stream(stream, gpu))
+    if status:
+        _check("da_rotary_axes", status)
+    return q_out, k_out

@@ -14,6 +14,10 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "decode_attn.hip")
 PAGED_SRC = os.path.join(PKG, "csrc", "paged_kv.hip")
+PROMPT_SRC = os.path.join(PKG, "csrc", "prompt_attn.hip")
+PROMPT_GRAD_SRC = os.path.join(PKG, "csrc", "prompt_grad.hip")
+ROTARY_SRC = os.path.join(PKG, "csrc", "rotary_axes.hip")
+SOURCES = (SRC, PAGED_SRC, PROMPT_SRC, PROMPT_GRAD_SRC, ROTARY_SRC)
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libdecode_attn.so")
 # The read-ceiling probe the benchmark reports beside the decode (not part of
@@ -36,12 +40,15 @@ FLAGS = [
     # rewrite reads the result at once, which stalls the load pipeline
     # behind the work counter of the decode kernel.
     "-mllvm", "-amdgpu-atomic-optimizer-strategy=None",
-    # Matrix-core results in VGPRs: the decode's accumulators then stay in
-    # the registers its softmax rescale works on, instead of being copied
-    # between AGPRs and VGPRs around every tile.
-    "-mllvm", "-amdgpu-mfma-vgpr-form",
     f"-I{INCLUDE}",
 ]
+# Matrix-core results in VGPRs: the decode's accumulators then stay in
+# the registers its softmax rescale works on, instead of being copied
+# between AGPRs and VGPRs around every tile.
+VGPR_RESULTS = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+# (The gradient's kernels hold more results than there are VGPRs: theirs are left
+# to the compiler.)
+SOURCE_FLAGS = {SRC: VGPR_RESULTS, PAGED_SRC: VGPR_RESULTS, PROMPT_SRC: VGPR_RESULTS}
 
 
 def _start(cmd: list, verbose: bool) -> subprocess.Popen:
@@ -75,12 +82,12 @@ def build(verbose: bool = False) -> str:
     argument handling (always; a stale build must never be used).  Returns the
     decode library's path."""
     tag = ".tmp%d" % os.getpid()
-    objects = [LIB + tag + ".%d.o" % i for i in range(2)]
+    objects = [LIB + tag + ".%d.o" % i for i in range(len(SOURCES))]
     compile_flags = [f for f in FLAGS if f != "-shared"]
     try:
-        _finish([_start([HIPCC, *compile_flags, "-c", "-o", obj, src], verbose)
-                 for obj, src in zip(objects, (SRC, PAGED_SRC))]
-                + [_start([HIPCC, *FLAGS, "-o", PROBE_LIB + tag, PROBE_SRC], verbose),
+        _finish([_start([HIPCC, *compile_flags, *SOURCE_FLAGS.get(src, []), "-c", "-o", obj, src], verbose)
+                 for obj, src in zip(objects, SOURCES)]
+                + [_start([HIPCC, *FLAGS, *VGPR_RESULTS, "-o", PROBE_LIB + tag, PROBE_SRC], verbose),
                    _start(_call_command(CALL_LIB + tag), verbose)])
         _finish([_start([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", LIB + tag,
                          *objects], verbose)])

@@ -1,0 +1,491 @@
+// prompt_attn.hip -- gfx950 kernels and C ABI of attention over whole prompts:
+// sequences of different lengths packed one after the other, as a projection
+// leaves them, without a cache.
+//
+// Kernels
+//   prompt_attn_kernel    softmax(scale q.K) V for a tile of query rows of one
+//                         (sequence, KV head), over all keys that they see or a
+//                         part of them.
+//   prompt_merge_kernel   combines the parts of each row.
+#include <algorithm>
+#include <cfloat>
+
+#include "prompt_common.h"
+
+namespace {
+
+using namespace prompt;
+
+struct AttnArgs {
+  const char *q, *k, *v;
+  char* out;
+  float* lse;
+  int64_t q_stride, k_stride, v_stride;       // bytes between tokens
+  // |scale| times log2(e), or 1 for a scale of 0; q's words are taken as
+  // (q & q_keep) ^ q_flip: negated for a negative scale, 0 for that of 0.
+  float scale;
+  uint32_t q_keep, q_flip;
+  int splits;
+  float* parts;         // splits > 1: [workgroup][R][D], then [workgroup][R][3]
+  int64_t stats;        // where the latter begin
+};
+
+// Beyond this distance the rounding of the reference would show: the product is
+// rounded first, so that the largest score's weight is 1.
+constexpr float kFar = 0x1p26f;
+
+template <class T, int D>
+constexpr int kKeys = is_f32<T> || D == 256 ? 32 : 64;     // keys of a tile
+
+// ---------------------------------------------------------------------------
+// Attention.  A workgroup's R = 128 NQ rows are (token, head of the group)
+// pairs of one KV head, 32 NQ to a wave, side by side as columns:
+//   S^T [keys x rows] = K . Q^T,   O^T [D x rows] += V^T . P^T
+// so a row's scores lie in two lanes and its statistics need no LDS.
+// ---------------------------------------------------------------------------
+template <class T, int D, int NQ, bool LSE>
+__global__ __launch_bounds__(kThreads, NQ == 1 && D <= 128 && !is_f32<T> ? 2 : 1)
+void prompt_attn_kernel(Batch bt, AttnArgs a) {
+  using L = Tile<T, D>;
+  constexpr int KT = kKeys<T, D>, R = 32 * NQ * kWaves;
+  constexpr int NS = KT / 32, ND = L::ND, NW = L::NW;
+  constexpr int kTile = KT * L::row_bytes;
+  constexpr int NP = is_f32<T> ? 1 : 2 * NS;
+
+  __shared__ __align__(16) char s_k[2][kTile];
+  __shared__ __align__(16) char s_v[2][kTile];
+  __shared__ int s_spoilt[2][kWaves];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int i = lane & 31, k = lane >> 5;
+
+  const int head = blockIdx.x % bt.h_kv;
+  const int split = (blockIdx.x / bt.h_kv) % a.splits;
+  Place at;
+  if (!find(bt.row_start, bt.B, bt.T, bt.rows, bt.G, R, blockIdx.x / bt.h_kv / a.splits, lane, &at))
+    return;
+  const Span rows = span(bt.row_start, at.b, bt.T, bt.rows);
+  const Span keys = span(bt.key_start, at.b, bt.N, bt.keys);
+  // (the longest first)
+  const int row0 = (bt.causal ? at.tiles - 1 - at.tile : at.tile) * R;
+  const int in_tile = min(rows.n * bt.G - row0, R);
+  const int min_seen = seen_by(bt, rows.n, keys.n, token_of(bt, row0));
+  const int max_seen = seen_by(bt, rows.n, keys.n, token_of(bt, row0 + in_tile - 1));
+  const int tiles = (max_seen + KT - 1) / KT;
+  const int t0 = (int)((int64_t)tiles * split / a.splits);
+  const int t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
+
+  // This wave's rows.
+  const int my_row0 = row0 + 32 * NQ * wave;
+  const int my_rows = min(max(in_tile - 32 * NQ * wave, 0), 32 * NQ);
+  const int my_min = my_rows ? seen_by(bt, rows.n, keys.n, token_of(bt, my_row0)) : 0;
+  int seen[NQ];
+  int64_t place[NQ];                         // row * h_q + head
+  u32x4 q[NQ][NW];
+#pragma unroll
+  for (int b = 0; b < NQ; ++b) {
+    const int x = my_row0 + min(32 * b + i, max(my_rows - 1, 0));
+    const int t = my_rows ? token_of(bt, x) : 0;
+    const int g = my_rows ? x - t * bt.G : 0;
+    seen[b] = 32 * b + i < my_rows ? seen_by(bt, rows.n, keys.n, t) : 0;
+    place[b] = (int64_t)(rows.start + t) * bt.h_q + head * bt.G + g;
+    const char* src = a.q + (int64_t)(rows.start + t) * a.q_stride +
+                      (int64_t)(head * bt.G + g) * L::row_bytes + 16 * k;
+#pragma unroll
+    for (int w = 0; w < NW; ++w)
+      q[b][w] = (*reinterpret_cast<const u32x4*>(src + 32 * w) & a.q_keep) ^ a.q_flip;
+  }
+
+  f32x16 acc[NQ][ND];
+  float limit[NQ], ref[NQ], sum[NQ], whole[NQ];
+#pragma unroll
+  for (int b = 0; b < NQ; ++b) {
+#pragma unroll
+    for (int c = 0; c < ND; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[b][c][r] = 0.f;
+    limit[b] = -INFINITY, ref[b] = 0.f, sum[b] = 0.f, whole[b] = 0.f;
+  }
+  float by = a.scale;
+
+  const char* k_base = a.k + (int64_t)keys.start * a.k_stride + (int64_t)head * L::row_bytes;
+  const char* v_base = a.v + (int64_t)keys.start * a.v_stride + (int64_t)head * L::row_bytes;
+  Stage<T, D, KT> k_next, v_next;
+  const RowReader<T, D> k_read(ordered_row(i), k);
+  const ColumnReader<T, D> v_read(lane);
+
+  auto load_k = [&](int t) { k_next.load(k_base, a.k_stride, t * KT, keys.n, tid); };
+  auto load_v = [&](int t) { v_next.load(v_base, a.v_stride, t * KT, keys.n, tid); };
+  // Where some rows see keys of a tile that others do not, values that are not
+  // finite must not meet the others' weights of 0.
+  auto store_v = [&](int t) {
+    v_next.store(s_v[t & 1], tid);
+    if ((t + 1) * KT > min_seen) {
+      const bool bad = __any(v_next.spoilt());
+      if (lane == 0) s_spoilt[t & 1][wave] = bad;
+    }
+  };
+
+  auto scores = [&](int t, f32x16 (&s)[NQ][NS]) {
+    const char* tile = s_k[t & 1];
+#pragma unroll
+    for (int b = 0; b < NQ; ++b)
+#pragma unroll
+      for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[b][n][r] = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w)
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        const u32x4 x = k_read.get(tile, n, w);
+#pragma unroll
+        for (int b = 0; b < NQ; ++b) s[b][n] = mma<T>(x, q[b][w], s[b][n]);
+      }
+  };
+  auto mask = [&](int t, f32x16 (&s)[NQ][NS]) {
+    if ((t + 1) * KT <= my_min) return;
+#pragma unroll
+    for (int b = 0; b < NQ; ++b)
+#pragma unroll
+      for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (t * KT + 32 * n + row_of(r, k) >= seen[b]) s[b][n][r] = -INFINITY;
+  };
+  // The reference is raised when a score lies 8 above it: weights stay below
+  // 2^8, and most tiles rescale nothing.
+  auto raise = [&](f32x16 (&s)[NQ][NS]) {
+    float top[NQ];
+    bool over = false;
+#pragma unroll
+    for (int b = 0; b < NQ; ++b) {
+      top[b] = s[b][0][0];
+#pragma unroll
+      for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top[b] = fmaxf(top[b], s[b][n][r]);
+      top[b] *= a.scale;
+      over |= !(top[b] <= limit[b]);
+    }
+    if (__any(over)) {
+      bool far = false;
+#pragma unroll
+      for (int b = 0; b < NQ; ++b) {
+        top[b] = fmaxf(top[b], __shfl_xor(top[b], 32));
+        far |= fabsf(top[b]) > kFar && top[b] != -INFINITY;
+        if (!(top[b] <= limit[b])) {
+          const float f = limit[b] == -INFINITY ? 0.f : exp2f(ref[b] - top[b]);
+          ref[b] = top[b];
+          limit[b] = top[b] + 8.f;
+          sum[b] *= f;
+          whole[b] *= f;
+#pragma unroll
+          for (int c = 0; c < ND; ++c) acc[b][c] *= f;
+        }
+      }
+      if (__any(far)) by = 1.f;
+    }
+    if (__builtin_expect(by != a.scale, 0)) {
+#pragma unroll
+      for (int b = 0; b < NQ; ++b)
+#pragma unroll
+        for (int n = 0; n < NS; ++n) s[b][n] *= a.scale;
+    }
+  };
+  // s becomes the weights; 16-bit ones are rounded into p.
+  auto weights = [&](f32x16 (&s)[NQ][NS], u32x4 (&p)[NQ][NP]) {
+#pragma unroll
+    for (int b = 0; b < NQ; ++b)
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          s[b][n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][n][r], by, -ref[b]));
+        if constexpr (is_f32<T>) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sum[b] += s[b][n][r];
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; r += 2) {
+            const uint32_t w = pack2<T>(s[b][n][r], s[b][n][r + 1]);
+            p[b][2 * n + r / 8][r % 8 / 2] = w;
+            sum[b] = add2<T>(w, sum[b]);
+            if constexpr (LSE) whole[b] += s[b][n][r] + s[b][n][r + 1];
+          }
+        }
+      }
+  };
+  auto values = [&](int t, f32x16 (&s)[NQ][NS], u32x4 (&p)[NQ][NP]) {
+    const char* tile = s_v[t & 1];
+    if ((t + 1) * KT > min_seen) {
+      int bad = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) bad |= s_spoilt[t & 1][w];
+      if (__builtin_expect(uniform(bad), 0)) {
+        // key by key, those alone that the row sees
+#pragma unroll 1
+        for (int e = 0; e < 16 * NS; ++e) {
+#pragma unroll
+          for (int b = 0; b < NQ; ++b) {
+            float mine = 0.f;
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) mine = 16 * n + r == e ? s[b][n][r] : mine;
+            if constexpr (!is_f32<T>) mine = (float)(T)mine;
+            const float other = __shfl_xor(mine, 32);
+#pragma unroll 1
+            for (int kk = 0; kk < 2; ++kk) {
+              const int key = 32 * (e / 16) + row_of(e % 16, kk);
+              if (t * KT + key >= seen[b]) continue;
+              const float w = kk == k ? mine : other;
+#pragma unroll
+              for (int c = 0; c < ND; ++c)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                  const int d = (32 * c + 8 * (r / 4) + 4 * k + r % 4) * (int)sizeof(T);
+                  acc[b][c][r] +=
+                      w * (float)*reinterpret_cast<const T*>(tile + L::at(key, d / 16) + d % 16);
+                }
+            }
+          }
+        }
+        return;
+      }
+    }
+    if constexpr (is_f32<T>) {
+#pragma unroll
+      for (int c = 0; c < ND; ++c)
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float x = v_read.get(tile, 2 * n + r / 8, r % 8, c);
+#pragma unroll
+            for (int b = 0; b < NQ; ++b)
+              acc[b][c] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[b][n][r], acc[b][c], 0, 0, 0);
+          }
+    } else {
+#pragma unroll
+      for (int c = 0; c < ND; ++c)
+#pragma unroll
+        for (int h = 0; h < 2 * NS; ++h) {
+          const u32x4 x = v_read.get(tile, h, c);
+#pragma unroll
+          for (int b = 0; b < NQ; ++b) acc[b][c] = mma<T>(x, p[b][h], acc[b][c]);
+        }
+    }
+  };
+
+  if (t0 < t1) {
+    load_k(t0);
+    load_v(t0);
+    k_next.store(s_k[t0 & 1], tid);
+    store_v(t0);
+    __syncthreads();
+    for (int t = t0; t < t1; ++t) {
+      const bool more = t + 1 < t1;
+      if (more) {
+        load_k(t + 1);
+        load_v(t + 1);
+      }
+      if (my_rows) {
+        f32x16 s[NQ][NS];
+        u32x4 p[NQ][NP];
+        scores(t, s);
+        mask(t, s);
+        raise(s);
+        weights(s, p);
+        values(t, s, p);
+      }
+      if (more) {
+        k_next.store(s_k[(t + 1) & 1], tid);
+        store_v(t + 1);
+      }
+      __syncthreads();
+    }
+  }
+
+#pragma unroll
+  for (int b = 0; b < NQ; ++b) {
+    float total = sum[b] + __shfl_xor(sum[b], 32);
+    const float all = LSE ? whole[b] + __shfl_xor(whole[b], 32) : total;
+    if (32 * b + i >= my_rows) continue;
+    // (a row whose scores are all -infinity counts as one that sees nothing)
+    const bool none = limit[b] == -INFINITY && total == 0.f;
+    if (a.splits == 1) {
+      const float inverse = 1.f / total;
+      auto mean = [&](float x) { return none ? 0.f : x * inverse; };
+      char* dst = a.out + place[b] * L::row_bytes;
+#pragma unroll
+      for (int c = 0; c < ND; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const f32x4 o{mean(acc[b][c][r]), mean(acc[b][c][r + 1]), mean(acc[b][c][r + 2]),
+                        mean(acc[b][c][r + 3])};
+          const int d = 32 * c + 2 * r + 4 * k;
+          if constexpr (is_f32<T>)
+            *reinterpret_cast<f32x4*>(dst + 4 * d) = o;
+          else
+            *reinterpret_cast<u32x2*>(dst + 2 * d) =
+                u32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
+        }
+      if (a.lse && k == 0)
+        a.lse[place[b]] = none ? -INFINITY : (ref[b] + log2f(is_f32<T> || !LSE ? total : all)) * kLn2;
+    } else {
+      const int64_t row = (int64_t)blockIdx.x * R + 32 * NQ * wave + 32 * b + i;
+      float* dst = a.parts + row * D + 4 * k;
+#pragma unroll
+      for (int c = 0; c < ND; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+          *reinterpret_cast<f32x4*>(dst + 32 * c + 2 * r) =
+              f32x4{acc[b][c][r], acc[b][c][r + 1], acc[b][c][r + 2], acc[b][c][r + 3]};
+      if (k == 0) {
+        float* st = a.parts + a.stats + row * 3;
+        st[0] = none ? -INFINITY : ref[b], st[1] = total, st[2] = is_f32<T> ? total : all;
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Puts the parts of each row together, D/4 lanes a row.
+// ---------------------------------------------------------------------------
+template <class T, int D>
+__global__ __launch_bounds__(kThreads) void prompt_merge_kernel(Batch bt, AttnArgs a, int R) {
+  constexpr int kPer = D / 4;                  // lanes of a row
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int head = blockIdx.x % bt.h_kv, item = blockIdx.x / bt.h_kv;
+  Place at;
+  if (!find(bt.row_start, bt.B, bt.T, bt.rows, bt.G, R, item, lane, &at)) return;
+  const Span rows = span(bt.row_start, at.b, bt.T, bt.rows);
+  const int row0 = (bt.causal ? at.tiles - 1 - at.tile : at.tile) * R;
+  const int in_tile = min(rows.n * bt.G - row0, R);
+  const int x = blockIdx.y * (kThreads / kPer) + tid / kPer, l = tid % kPer;
+  if (x >= in_tile) return;
+  const int t = token_of(bt, row0 + x), g = row0 + x - t * bt.G;
+  const int64_t place = (int64_t)(rows.start + t) * bt.h_q + head * bt.G + g;
+  auto part = [&](int s) {
+    return ((int64_t)(item * a.splits + s) * bt.h_kv + head) * R + x;
+  };
+  float ref = -INFINITY;
+  bool bad = false;                            // (a NaN is no maximum)
+  for (int s = 0; s < a.splits; ++s) {
+    const float m = a.parts[a.stats + part(s) * 3];
+    bad |= m != m;
+    ref = fmaxf(ref, m);
+  }
+  f32x4 o{0.f, 0.f, 0.f, 0.f};
+  float total = 0.f, all = 0.f;
+  for (int s = 0; s < a.splits; ++s) {
+    const float* st = a.parts + a.stats + part(s) * 3;
+    if (st[0] == -INFINITY) continue;
+    const float f = bad ? NAN : st[0] == ref ? 1.f : exp2f(st[0] - ref);
+    total += f * st[1], all += f * st[2];
+    o += f * *reinterpret_cast<const f32x4*>(a.parts + part(s) * D + 4 * l);
+  }
+  const bool none = ref == -INFINITY && !bad;
+  const float inverse = none ? 0.f : 1.f / total;
+  o *= inverse;
+  char* dst = a.out + place * D * (int)sizeof(T);
+  if constexpr (is_f32<T>)
+    *reinterpret_cast<f32x4*>(dst + 16 * l) = o;
+  else
+    *reinterpret_cast<u32x2*>(dst + 8 * l) = u32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
+  if (a.lse && l == 0) a.lse[place] = none ? -INFINITY : (ref + log2f(all)) * kLn2;
+}
+
+}  // namespace
+
+namespace {
+
+// How a call is divided: NQ blocks of 32 rows a wave, and the parts that the keys
+// of a tile of rows are read in.
+struct Plan {
+  int NQ, splits;
+  int64_t items;                // tiles of rows, over all sequences
+  size_t bytes;
+};
+
+Plan plan_attn(const da_prompt& p) {
+  Plan plan{1, 1, 0, 0};
+  const int64_t G = p.h_q / p.h_kv;
+  plan.items = most_tiles(p.row_start, p.B, p.T, p.rows, G, 128);
+  const int64_t groups = plan.items * p.h_kv;
+  if (groups < kCus) {
+    const int64_t most = std::max<int64_t>(ceil_div(p.N, 128), 1);
+    plan.splits = (int)std::min<int64_t>(2 * kCus / groups, most);
+  }
+  if (plan.splits > 1)
+    plan.bytes = (size_t)(groups * plan.splits * 128) * (p.d + 3) * sizeof(float);
+  return plan;
+}
+
+template <class T, int D>
+void launch_attn(const Plan& plan, const Batch& bt, const AttnArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)(plan.items * bt.h_kv * plan.splits)), block(kThreads);
+  if (a.lse && !is_f32<T>)
+    hipLaunchKernelGGL((prompt_attn_kernel<T, D, 1, !is_f32<T>>), grid, block, 0, s, bt, a);
+  else
+    hipLaunchKernelGGL((prompt_attn_kernel<T, D, 1, false>), grid, block, 0, s, bt, a);
+  if (plan.splits > 1) {
+    const int R = 128;
+    const int rows = (int)std::min<int64_t>((int64_t)bt.T * bt.G, R);
+    hipLaunchKernelGGL((prompt_merge_kernel<T, D>),
+                       dim3((unsigned)(plan.items * bt.h_kv),
+                            (unsigned)ceil_div(rows, kThreads / (D / 4))),
+                       block, 0, s, bt, a, R);
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t da_prompt_workspace_bytes(const da_prompt* p) {
+  if (!p || check_sizes(*p) != DA_OK) return 0;
+  return std::max<size_t>(plan_attn(*p).bytes, 16);
+}
+
+da_status da_prompt_attn(const da_prompt* prompt, const void* q, int64_t q_stride, const void* k,
+                         int64_t k_stride, const void* v, int64_t v_stride, float scale, void* out,
+                         float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!prompt || !q || !k || !v || !out) return DA_ERR_NULL;
+  const da_prompt& p = *prompt;
+  const da_status st = check_sizes(p);
+  if (st == DA_ERR_SHAPE || !stride_fits(q_stride, p.h_q, p.d) ||
+      !stride_fits(k_stride, p.h_kv, p.d) || !stride_fits(v_stride, p.h_kv, p.d))
+    return DA_ERR_SHAPE;
+  if (st != DA_OK) return st;
+  const Plan plan = plan_attn(p);
+  if (plan.items * p.h_kv * plan.splits > kMaxGroups) return DA_ERR_SHAPE;
+  if (!starts_aligned(p) || !aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) ||
+      !aligned(out, 16) || !aligned(lse, 4) || !stride_aligned(q_stride, p.dtype) ||
+      !stride_aligned(k_stride, p.dtype) || !stride_aligned(v_stride, p.dtype))
+    return DA_ERR_ALIGN;
+  if (!std::isfinite(scale)) return DA_ERR_SCALE;
+  if (plan.bytes && (!workspace || workspace_bytes < plan.bytes)) return DA_ERR_WORKSPACE;
+  if (plan.bytes && !aligned(workspace, 16)) return DA_ERR_ALIGN;
+  const int size = type_bytes(p.dtype);
+  AttnArgs a{};
+  a.q = static_cast<const char*>(q), a.k = static_cast<const char*>(k);
+  a.v = static_cast<const char*>(v), a.out = static_cast<char*>(out);
+  a.lse = lse;
+  a.q_stride = q_stride * size, a.k_stride = k_stride * size, a.v_stride = v_stride * size;
+  a.scale = scale == 0.f ? 1.f : std::min(std::fabs(scale) * kLog2e, FLT_MAX);
+  a.q_keep = scale == 0.f ? 0u : ~0u;
+  a.q_flip = scale < 0.f ? (p.dtype == DA_F32 ? 0x80000000u : 0x80008000u) : 0u;
+  a.splits = plan.splits;
+  a.parts = static_cast<float*>(workspace);
+  a.stats = plan.items * p.h_kv * plan.splits * 128 * p.d;
+  const Batch bt = device_batch(p);
+  (void)hipGetLastError();
+  with_type_and_dim(p.dtype, p.d, [&](auto t, auto d) {
+    launch_attn<typename decltype(t)::type, d.value>(plan, bt, a, static_cast<hipStream_t>(stream));
+  });
+  return launch_status();
+}
+
+}  // extern "C"

@@ -1,0 +1,399 @@
+// prompt_common.h -- what the kernels of prompt attention and of its gradient
+// share: the batch of packed sequences, the tiles of rows, the matrix
+// instructions and the layout of tiles in LDS.
+//
+// Register layouts of the 32 x 32 matrix instructions (lane = 0..63, i = lane % 32,
+// k = lane / 32):
+//   A operand: lane holds A[i][..], k's share of the summed index
+//   B operand: lane holds B[..][i], k's share of the summed index
+//   result:    component r of a lane is D[8*(r/4) + 4*k + r%4][i]
+// The summed index is shared out 8 to a lane (16-bit types, 16 in all) or 1
+// (float32, 2 in all).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+
+#include "decode_attn.h"
+
+namespace prompt {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kCus = 256;             // what grids and workspaces are planned for
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+template <class T>
+constexpr bool is_f32 = std::is_same<T, float>::value;
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// ---------------------------------------------------------------------------
+// The batch.
+// ---------------------------------------------------------------------------
+struct Batch {
+  const int32_t *row_start, *key_start;
+  int B, rows, keys, T, N;
+  int h_q, h_kv, G, causal;
+  uint32_t G_mul, G_shift;
+};
+
+// First row (or key) and number of them of sequence b, within the arrays
+// whatever the starts hold; b is the same for the whole wave.
+struct Span {
+  int start, n;
+};
+__device__ __forceinline__ Span span(const int32_t* start, int b, int most, int total) {
+  if (!start) return {b * most, most};
+  const int s = min(max(uniform(start[b]), 0), total);
+  const int e = min(max(uniform(start[b + 1]), s), total);
+  return {s, min(e - s, most)};
+}
+
+// x / G, 0 <= x < 2^31 (the host's multiplier: floor(2^shift / G) + 1).
+__device__ __forceinline__ int token_of(const Batch& bt, int x) {
+  return (int)((uint64_t)(uint32_t)x * bt.G_mul >> bt.G_shift);
+}
+
+// Keys that row t of a sequence of `rows` rows and `keys` keys sees.
+__device__ __forceinline__ int seen_by(const Batch& bt, int rows, int keys, int t) {
+  return bt.causal ? min(max(t + 1 + keys - rows, 0), keys) : keys;
+}
+
+// Item `item` of the batch, items being tiles of R of each sequence's n*per
+// rows: its sequence and its number there.  False beyond the last.
+struct Place {
+  int b, tile, tiles;
+};
+__device__ __forceinline__ bool find(const int32_t* start, int B, int most, int total, int per,
+                                     int R, int item, int lane, Place* at) {
+  if (!start) {
+    const int tiles = (int)(((int64_t)most * per + R - 1) / R);
+    *at = {item / tiles, item % tiles, tiles};
+    return at->b < B;
+  }
+  int left = item;
+  for (int b0 = 0; b0 < B; b0 += 64) {
+    int n = 0;
+    if (b0 + lane < B) {
+      const int s = min(max(start[b0 + lane], 0), total);
+      const int e = min(max(start[b0 + lane + 1], s), total);
+      n = (int)(((int64_t)min(e - s, most) * per + R - 1) / R);
+    }
+    int upto = n;
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) {
+      const int x = __shfl_up(upto, step);
+      if (lane >= step) upto += x;
+    }
+    const int all = __builtin_amdgcn_readlane(upto, 63);
+    if (left < all) {
+      const int l = __ffsll((unsigned long long)__ballot(upto > left)) - 1;
+      const int tiles = __builtin_amdgcn_readlane(n, l);
+      *at = {b0 + l, left - (__builtin_amdgcn_readlane(upto, l) - tiles), tiles};
+      return true;
+    }
+    left -= all;
+  }
+  return false;
+}
+
+// ---------------------------------------------------------------------------
+// Products.
+// ---------------------------------------------------------------------------
+template <class T>
+struct Vec8;
+template <>
+struct Vec8<__bf16> {
+  using type = bf16x8;
+};
+template <>
+struct Vec8<_Float16> {
+  using type = f16x8;
+};
+
+// c += a b over the 16 bytes of the summed index that each lane holds (two
+// lanes: 16 values of 16 bits, or 8 of 32).
+template <class T>
+__device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (std::is_same<T, __bf16>::value) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  } else if constexpr (std::is_same<T, _Float16>::value) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  } else {
+    const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], y[e], c, 0, 0, 0);
+    return c;
+  }
+}
+
+// Two values rounded to T, in a word; and both values of such a word added to x.
+template <class T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  typedef T t2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), t2));
+}
+template <class T>
+__device__ __forceinline__ float add2(uint32_t w, float x) {
+  if constexpr (std::is_same<T, __bf16>::value)
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w),
+                                           bf16x2{(__bf16)1.f, (__bf16)1.f}, x, false);
+  else
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, w), f16x2{(_Float16)1.f, (_Float16)1.f},
+                                  x, false);
+}
+
+template <class T>
+__device__ __forceinline__ bool not_finite(uint32_t w) {
+  if constexpr (is_f32<T>)
+    return (w & 0x7f800000u) == 0x7f800000u;
+  else if constexpr (std::is_same<T, __bf16>::value)
+    return (w & 0x7f800000u) == 0x7f800000u || (w & 0x7f80u) == 0x7f80u;
+  else
+    return (w & 0x7c000000u) == 0x7c000000u || (w & 0x7c00u) == 0x7c00u;
+}
+
+// ---------------------------------------------------------------------------
+// A tile in LDS: rows of D values, row-major, in chunks of 16 bytes that stand
+// at their index XOR turn(row).  The turn takes all values that it can over 16
+// rows, the low two bits of the row first: 16 rows read at one chunk, four
+// rows (aligned) read over 64 bytes by the transposing loads, and a row read or
+// written along itself then spread over all banks.
+// ---------------------------------------------------------------------------
+template <class T, int D>
+struct Tile {
+  static constexpr int row_bytes = D * (int)sizeof(T);
+  static constexpr int chunks = row_bytes / 16;
+  static constexpr int NW = chunks / 2;       // steps of a product over D
+  static constexpr int ND = D / 32;           // blocks of 32 dimensions
+
+  __device__ static __forceinline__ int turn(int row) {
+    return chunks == 8 ? (row >> 1 & 1) << 2 | (row >> 2 & 3) : (row & 3) << 2 | (row >> 2 & 3);
+  }
+  __device__ static __forceinline__ int at(int row, int chunk) {
+    return row * row_bytes + ((chunk ^ turn(row)) << 4);
+  }
+};
+
+// The order in which the rows of a block of 32 are given to the first product,
+// so that its result is the second one's operand as it lies: component r of a
+// lane is row 16*(r/8) + 8*k + r%8 of the block.
+__device__ __forceinline__ int ordered_row(int i) {
+  return 16 * (i >> 4) + 8 * (i >> 2 & 1) + 4 * (i >> 3 & 1) + (i & 3);
+}
+__device__ __forceinline__ int row_of(int r, int k) { return 16 * (r / 8) + 8 * k + r % 8; }
+
+// Reading a tile by rows (operand of a product over D): this lane's row of a
+// block of 32, chunk 2w + k.
+template <class T, int D>
+struct RowReader {
+  using L = Tile<T, D>;
+  static constexpr int N = L::NW < 8 ? L::NW : 8;
+  int off[N];
+  __device__ __forceinline__ RowReader(int row, int k) {
+#pragma unroll
+    for (int w = 0; w < N; ++w) off[w] = L::at(row, 2 * w + k);
+  }
+  __device__ __forceinline__ u32x4 get(const char* tile, int block, int w) const {
+    return *reinterpret_cast<const u32x4*>(tile + off[w % N] + (w / N) * 256 +
+                                           block * 32 * L::row_bytes);
+  }
+};
+
+// Reading a tile by columns (operand of a product over its rows): this lane's
+// dimension 32c + i, rows 16h + 8k + 0..7 of the tile, of a 16-bit type.
+template <class T, int D>
+struct ColumnReader {
+  using L = Tile<T, D>;
+  static constexpr int N = L::ND < 4 ? L::ND : 4;
+  int off[N][2];
+  __device__ __forceinline__ ColumnReader(int lane) {
+    const int i = lane & 31, k = lane >> 5;
+#pragma unroll
+    for (int c = 0; c < N; ++c)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        off[c][j] = L::at(8 * k + 4 * j + (lane >> 2 & 3), 4 * c + 2 * (i >> 4) + (lane >> 1 & 1)) +
+                    8 * (lane & 1);
+  }
+  __device__ __forceinline__ u32x4 get(const char* tile, int h, int c) const {
+    // (16 lanes at 8 bytes each hold a matrix of 4 rows by 16 columns; a lane
+    // gets one column of it)
+    typedef __attribute__((address_space(3))) s16x4* lds;
+    u32x2 x[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      x[j] = __builtin_bit_cast(
+          u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                     (lds)(const_cast<char*>(tile) + off[c % N][j] + (c / N) * 256 +
+                           h * 16 * L::row_bytes)));
+    return u32x4{x[0][0], x[0][1], x[1][0], x[1][1]};
+  }
+};
+template <int D>
+struct ColumnReader<float, D> {
+  using L = Tile<float, D>;
+  int base, in;
+  __device__ __forceinline__ ColumnReader(int lane) {
+    const int i = lane & 31, k = lane >> 5;
+    base = 8 * k * L::row_bytes + (i & 3) * 4;
+    in = (i >> 2) ^ (2 * k);
+  }
+  // row 16h + 8k + e
+  __device__ __forceinline__ float get(const char* tile, int h, int e, int c) const {
+    return *reinterpret_cast<const float*>(
+        tile + base + (16 * h + e) * L::row_bytes +
+        (((8 * c) ^ in ^ ((e & 3) << 2 | (e >> 2))) << 4));
+  }
+};
+
+// acc[c] += X^T p over the 16 rows h of a tile, p being eight of a lane's
+// weights of those rows (components 8*(h%2) .. +7 of a block).
+template <class T, int D>
+__device__ __forceinline__ f32x16 mma_columns(const ColumnReader<T, D>& rd, const char* tile,
+                                              int h, int c, u32x4 p, f32x16 acc) {
+  return mma<T>(rd.get(tile, h, c), p, acc);
+}
+
+// ---------------------------------------------------------------------------
+// Tiles on their way from memory to LDS, through registers: 16 bytes a unit.
+// ---------------------------------------------------------------------------
+template <class T, int D, int ROWS, int THREADS = kThreads>
+struct Stage {
+  using L = Tile<T, D>;
+  static constexpr int units = ROWS * L::chunks / THREADS;
+  static_assert(units >= 1 && ROWS * L::chunks % THREADS == 0, "whole units");
+  static constexpr int step = THREADS / L::chunks;      // rows between a thread's units
+  u32x4 x[units];
+
+  // Rows row0 .. row0 + ROWS - 1 of `base` (a row's own place, stride between
+  // rows in bytes); rows from `n` on are zeros.
+  __device__ __forceinline__ void load(const char* base, int64_t stride, int row0, int n, int tid) {
+    const int r = tid / L::chunks, c = tid % L::chunks;
+#pragma unroll
+    for (int u = 0; u < units; ++u) {
+      const int row = row0 + r + step * u;
+      const char* p = base + (int64_t)(row < n ? row : 0) * stride + 16 * c;
+      x[u] = *reinterpret_cast<const u32x4*>(p);
+      if (row >= n) x[u] = u32x4{0u, 0u, 0u, 0u};
+    }
+  }
+  __device__ __forceinline__ void store(char* tile, int tid) const {
+    const int r = tid / L::chunks, c = tid % L::chunks;
+#pragma unroll
+    for (int u = 0; u < units; ++u)
+      *reinterpret_cast<u32x4*>(tile + L::at(r + step * u, c)) = x[u];
+  }
+  __device__ __forceinline__ bool spoilt() const {
+    bool bad = false;
+#pragma unroll
+    for (int u = 0; u < units; ++u)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) bad |= not_finite<T>(x[u][w]);
+    return bad;
+  }
+};
+
+}  // namespace prompt
+
+// ---------------------------------------------------------------------------
+// Host side.
+// ---------------------------------------------------------------------------
+namespace prompt {
+
+inline bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int type_bytes(int dtype) { return dtype == DA_F32 ? 4 : 2; }
+
+constexpr int64_t kMaxPerSequence = int64_t(1) << 30;   // rows times the group, and keys
+constexpr int64_t kMaxHeads = int64_t(1) << 24;         // sequences x query heads
+constexpr int64_t kMaxGroups = (int64_t(1) << 24) - 1;  // of 256 threads: a grid has < 2^32
+
+// The sizes, then what is supported; pointers not looked at.
+inline da_status check_sizes(const da_prompt& p) {
+  if (p.B < 1 || p.h_q < 1 || p.h_kv < 1 || p.d < 1 || p.rows < 1 || p.keys < 1 || p.T < 1 ||
+      p.N < 1 || p.h_q % p.h_kv != 0)
+    return DA_ERR_SHAPE;
+  if ((int64_t)p.T * (p.h_q / p.h_kv) > kMaxPerSequence || p.N > kMaxPerSequence ||
+      (int64_t)p.B * p.h_q > kMaxHeads || (int64_t)p.h_q * p.d > (int64_t(1) << 30))
+    return DA_ERR_SHAPE;
+  if ((!p.row_start && (int64_t)p.B * p.T != p.rows) ||
+      (!p.key_start && (int64_t)p.B * p.N != p.keys))
+    return DA_ERR_SHAPE;
+  if ((p.d != 64 && p.d != 128 && p.d != 256) || p.dtype < DA_F32 || p.dtype > DA_F16)
+    return DA_ERR_UNSUPPORTED;
+  return DA_OK;
+}
+
+inline bool starts_aligned(const da_prompt& p) {
+  return aligned(p.row_start, 4) && aligned(p.key_start, 4);
+}
+
+// A token stride (elements) that rows of `heads` heads may have.
+inline bool stride_fits(int64_t stride, int heads, int d) { return stride >= (int64_t)heads * d; }
+inline bool stride_aligned(int64_t stride, int dtype) {
+  return stride % (16 / type_bytes(dtype)) == 0;
+}
+
+inline Batch device_batch(const da_prompt& p) {
+  const uint32_t G = p.h_q / p.h_kv;
+  uint32_t shift = 31;
+  while (G > 1u << (shift - 31)) ++shift;
+  const uint32_t mul = (uint32_t)((uint64_t(1) << shift) / G + 1);
+  return {p.row_start, p.key_start, p.B, p.rows, p.keys, p.T, p.N, p.h_q, p.h_kv, (int)G,
+          p.causal != 0, mul, shift};
+}
+
+// No fewer than the tiles of R that the sequences' n*per rows make.
+inline int64_t most_tiles(const int32_t* start, int64_t B, int64_t most, int64_t total,
+                          int64_t per, int64_t R) {
+  const int64_t even = B * ceil_div(most * per, R);
+  return start ? std::min(even, total * per / R + B) : even;
+}
+
+inline da_status launch_status() {
+  return hipGetLastError() == hipSuccess ? DA_OK : DA_ERR_HIP;
+}
+
+// Calls f(type tag, d) with these as compile-time constants.
+template <class T>
+struct Tag {
+  using type = T;
+};
+template <class F>
+void with_type_and_dim(int dtype, int d, F&& f) {
+  auto with_dim = [&](auto t) {
+    if (d == 64)
+      f(t, std::integral_constant<int, 64>{});
+    else if (d == 128)
+      f(t, std::integral_constant<int, 128>{});
+    else
+      f(t, std::integral_constant<int, 256>{});
+  };
+  if (dtype == DA_F32)
+    with_dim(Tag<float>{});
+  else if (dtype == DA_BF16)
+    with_dim(Tag<__bf16>{});
+  else
+    with_dim(Tag<_Float16>{});
+}
+
+}  // namespace prompt

@@ -1,0 +1,443 @@
+"""Attention over packed prompts and its gradient on the GPU against the plain
+64-bit forms of prompt_reference.py: every type, head size and group, lengths from
+none to several tiles, rows that no sequence has poisoned."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_19456_amd as lib
+import prompt_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def starts(counts):
+    return np.concatenate(([0], np.cumsum(counts))).astype(np.int32)
+
+
+class Case:
+    """Arrays of a call on the CPU, everything outside the sequences poisoned."""
+
+    def __init__(self, dtype="bf16", d=64, h_q=4, h_kv=2, t=(37,), n=None, causal=True, seed=0,
+                 behind=3, T=None, N=None, scale=None, q_scale=1.5):
+        self.t, self.n = list(t), list(t if n is None else n)
+        self.type, self.d, self.h_q, self.h_kv = ref.DTYPES[dtype], d, h_q, h_kv
+        self.rs, self.ks = starts(self.t), starts(self.n)
+        self.rows, self.keys = int(self.rs[-1]) + behind, int(self.ks[-1]) + behind
+        self.T, self.N = T or max(max(self.t), 1), N or max(max(self.n), 1)
+        self.scale = 1 / math.sqrt(d) if scale is None else scale
+        self.causal, self.seed = causal, seed
+        rng = np.random.default_rng(seed)
+
+        def normal(rows, heads, by=1.0):
+            return torch.from_numpy(rng.standard_normal((rows, heads, d)) * by).to(self.type)
+
+        self.q, self.k = normal(self.rows, h_q, q_scale), normal(self.keys, h_kv)
+        self.v, self.g = normal(self.keys, h_kv), normal(self.rows, h_q)
+        self.batch = ref.Batch(self.rows, self.keys, self.rs, self.ks, self.T, self.N,
+                               len(self.t), causal)
+        for x in (self.q, self.g):
+            x[torch.from_numpy(~self.batch.mine("q"))] = math.nan
+        for x in (self.k, self.v):
+            x[torch.from_numpy(~self.batch.mine("k"))] = math.nan
+        say(f"{dtype} d={d} h={h_q}/{h_kv} t={self.t[:6]} n={self.n[:6]} causal={causal} "
+            f"seed={seed}")
+
+    def packed(self, device):
+        return dict(causal=self.causal, row_start=torch.from_numpy(self.rs).to(device), T=self.T,
+                    key_start=torch.from_numpy(self.ks).to(device), N=self.N)
+
+    def forward(self, device, lse=True, **kw):
+        out = torch.full(self.q.shape, math.nan, dtype=self.type, device=device)
+        L = torch.full(self.q.shape[:2], math.nan, device=device) if lse else None
+        lib.prompt_attn(self.q.to(device), self.k.to(device), self.v.to(device), self.scale,
+                        out=out, lse=L, **{**self.packed(device), **kw})
+        torch.cuda.synchronize()
+        return out, L
+
+    def backward(self, device, out, lse, **kw):
+        nan = [torch.full(x.shape, math.nan, dtype=self.type, device=device)
+               for x in (self.q, self.k, self.v)]
+        lib.prompt_attn_grad(self.q.to(device), self.k.to(device), self.v.to(device), out, lse,
+                             self.g.to(device), self.scale, dq=nan[0], dk=nan[1], dv=nan[2],
+                             **{**self.packed(device), **kw})
+        torch.cuda.synchronize()
+        return nan
+
+
+def compare(name, got, want, tol, mine):
+    got = got.double().cpu().numpy()
+    assert np.isnan(got[~mine]).all(), f"{name}: places of no sequence were written"
+    got, want, tol = got[mine], want[mine], tol[mine]
+    assert np.array_equal(np.isnan(want), np.isnan(got)), f"{name}: NaN elsewhere"
+    odd = np.isinf(want)
+    assert np.array_equal(got[odd], want[odd]), f"{name}: infinities elsewhere"
+    ok = np.isfinite(want)
+    if not ok.any():
+        return
+    err = np.abs(got[ok] - want[ok])
+    worst = np.max(err / tol[ok])
+    say(f"  {name}: max error {err.max():.3e}, {worst:.3f} of the bound")
+    assert worst <= 1.0
+
+
+def check_forward(c, device, lse=True, **kw):
+    out, L = c.forward(device, lse, **kw)
+    want, want_L, mass, spread, seen, top_v = ref.attention(c.q, c.k, c.v, c.scale, c.batch)
+    mine = c.batch.mine("q")
+    compare("out", out, want, ref.tolerance(want, mass, spread, seen, top_v, c.type, c.d), mine)
+    if lse:
+        with np.errstate(invalid="ignore"):
+            compare("lse", L, want_L, ref.lse_tolerance(want_L, spread, seen, c.d), mine)
+    return out, L
+
+
+def check_gradient(c, device, **kw):
+    out, L = c.forward(device)
+    grads = c.backward(device, out, L, **kw)
+    want, tol = ref.gradient(c.q, c.k, c.v, out, L, c.g, c.scale, c.batch)
+    for name, x, w, b, which in zip(("dq", "dk", "dv"), grads, want, tol, "qkk"):
+        compare(name, x, w, b, c.batch.mine(which))
+    return grads
+
+
+DS = [64, 128, 256]
+TYPES = ["f32", "bf16", "f16"]
+LENGTHS = [1, 2, 31, 32, 33, 63, 64, 65, 127, 130]
+
+
+@pytest.mark.parametrize("d", DS)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("causal", [True, False])
+def test_lengths(cuda_device, dtype, d, causal):
+    """From one token on, around every tile's edges, and a sequence of none."""
+    check_forward(Case(dtype, d, t=LENGTHS + [0], causal=causal, seed=d), cuda_device)
+
+
+@pytest.mark.parametrize("d", DS)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("causal", [True, False])
+def test_gradient_lengths(cuda_device, dtype, d, causal):
+    check_gradient(Case(dtype, d, t=LENGTHS + [0], causal=causal, seed=d), cuda_device)
+
+
+@pytest.mark.parametrize("h_q,h_kv", [(1, 1), (3, 3), (5, 1), (8, 2), (7, 1), (16, 1), (40, 2),
+                                      (10, 5)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_head_groups(cuda_device, dtype, h_q, h_kv):
+    c = Case(dtype, 64, h_q, h_kv, t=[70, 9, 33], seed=h_q)
+    check_forward(c, cuda_device)
+    check_gradient(c, cuda_device)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64), ("f32", 128), ("bf16", 256)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_long_sequences(cuda_device, dtype, d, causal):
+    """Many tiles, of odd numbers; wider tiles of rows."""
+    c = Case(dtype, d, 8, 2, t=[517, 1030, 3], causal=causal, seed=1)
+    check_forward(c, cuda_device)
+    check_gradient(c, cuda_device)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("causal", [True, False])
+def test_other_keys(cuda_device, dtype, causal):
+    """Fewer keys than rows (causal: the first rows see nothing), more, and none."""
+    c = Case(dtype, 128, 4, 1, t=[5, 80, 100, 1, 7, 0, 64], n=[80, 5, 0, 300, 6, 9, 64],
+             causal=causal, seed=2)
+    check_forward(c, cuda_device)
+    check_gradient(c, cuda_device)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", DS)
+@pytest.mark.parametrize("t,n", [(1, 700), (1, 5000), (7, 3001), (40, 1500), (1, 1)])
+def test_few_rows_over_many_keys(cuda_device, dtype, d, t, n):
+    """The keys read in parts that are put together."""
+    check_forward(Case(dtype, d, 8, 2, t=[t], n=[n], seed=n), cuda_device)
+    check_forward(Case(dtype, d, 4, 2, t=[t, 3], n=[n, 64], causal=False, seed=n), cuda_device,
+                  lse=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_even_sequences_without_starts(cuda_device, dtype):
+    """T rows of every sequence, N keys; and one sequence, its own keys."""
+    c = Case(dtype, 64, 4, 2, t=[19] * 5, n=[45] * 5, behind=0, seed=3)
+    want = check_forward(c, cuda_device)
+    a = [x.to(cuda_device) for x in (c.q, c.k, c.v)]
+    lse = torch.empty(c.q.shape[:2], device=cuda_device)
+    out = lib.prompt_attn(*a, c.scale, T=19, N=45, lse=lse)
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    for other in (dict(T=19), dict(T=19, key_start=torch.from_numpy(c.ks).to(cuda_device), N=45),
+                  dict(row_start=torch.from_numpy(c.rs).to(cuda_device), T=19, N=45)):
+        assert torch.equal(lib.prompt_attn(*a, c.scale, **other), want[0])
+    grads = lib.prompt_attn_grad(*a, out, lse, c.g.to(cuda_device), c.scale, T=19, N=45)
+    for x, y in zip(grads, c.backward(cuda_device, *want)):
+        assert torch.equal(x, y)
+    c = Case(dtype, 64, 4, 2, t=[77], behind=0, seed=4)
+    want = check_forward(c, cuda_device)[0]
+    a = [x.to(cuda_device) for x in (c.q, c.k, c.v)]
+    assert torch.equal(lib.prompt_attn(*a, c.scale), want)
+    assert torch.equal(lib.prompt_attn(*a, c.scale, row_start=torch.tensor(
+        [0, 77], dtype=torch.int32, device=cuda_device), T=77), want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_views_into_fused_projections(cuda_device, dtype):
+    """Strided q, k, v, d_out, dq, dk and dv: the same bits as contiguous ones, and
+    nothing beside them written."""
+    c = Case(dtype, 64, 4, 2, t=[50, 81], behind=0, seed=5)
+    out, lse = check_forward(c, cuda_device)
+    want = c.backward(cuda_device, out, lse)
+    qkv = torch.cat((c.q, c.k, c.v), 1).to(cuda_device)
+    q, k, v = qkv.split((4, 2, 2), 1)
+    wide = torch.full((c.rows, 11, 64), math.nan, dtype=c.type, device=cuda_device)
+    g = torch.cat((c.g, c.g), 1).to(cuda_device)[:, 4:]
+    got, got_lse = torch.empty_like(out), torch.empty_like(lse)
+    lib.prompt_attn(q, k, v, c.scale, out=got, lse=got_lse, **c.packed(cuda_device))
+    assert torch.equal(got, out) and torch.equal(got_lse, lse)
+    lib.prompt_attn_grad(q, k, v, out, lse, g, c.scale, dq=wide[:, 1:5], dk=wide[:, 6:8],
+                         dv=wide[:, 8:10], **c.packed(cuda_device))
+    for x, y in zip((wide[:, 1:5], wide[:, 6:8], wide[:, 8:10]), want):
+        assert torch.equal(x, y)
+    assert torch.isnan(wide[:, [0, 5, 10]]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_starts_that_lie(cuda_device, dtype):
+    """Longer sequences than T and N, starts that fall, are negative or beyond the
+    arrays: what lies within is taken, the rest is not touched."""
+    c = Case(dtype, 64, 4, 2, t=[30, 30, 30], behind=0, seed=6)
+    for rs, ks, T, N in (([0, 40, 70, 90], [0, 35, 60, 90], 20, 25),
+                         ([-5, 10, 4, 200], [3, 50, 50, 1 << 30], 90, 90),
+                         ([50, 20, 90, 90], [90, 0, 60, 61], 64, 64)):
+        c.rs, c.ks, c.T, c.N = np.array(rs, np.int32), np.array(ks, np.int32), T, N
+        c.batch = ref.Batch(90, 90, c.rs, c.ks, T, N, 3, True)
+        if len(set(np.concatenate([np.arange(s, s + n) for s, n in c.batch.q]))) == \
+                sum(n for _, n in c.batch.q):
+            check_forward(c, cuda_device)
+        else:
+            c.forward(cuda_device)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("scale", [0.0, -0.125, 0.7, 1e-6])
+def test_scales(cuda_device, dtype, scale):
+    c = Case(dtype, 64, 4, 2, t=[40, 70], seed=7, scale=scale)
+    check_forward(c, cuda_device)
+    check_gradient(c, cuda_device)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_equal_calls_give_equal_bits(cuda_device, dtype):
+    c = Case(dtype, 128, 8, 2, t=[700, 45], seed=8)
+    out, lse = c.forward(cuda_device)
+    grads = c.backward(cuda_device, out, lse)
+    for _ in range(3):
+        again = c.forward(cuda_device)
+        assert torch.equal(again[0][:745], out[:745]) and torch.equal(again[1][:745], lse[:745])
+        for x, y in zip(c.backward(cuda_device, out, lse), grads):
+            assert torch.equal(x[:745], y[:745])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_without_lse_the_same_out(cuda_device, dtype):
+    c = Case(dtype, 64, 4, 2, t=[200, 33], behind=0, seed=9)
+    assert torch.equal(c.forward(cuda_device)[0], c.forward(cuda_device, lse=False)[0])
+
+
+# --- gradients against the function itself -------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("causal", [True, False])
+def test_gradient_of_the_function(cuda_device, dtype, causal):
+    """Forward and backward together against torch's gradient in 64 bits, and against
+    differences of the 64-bit function."""
+    c = Case(dtype, 64, 6, 2, t=[45, 70], n=[45, 90], causal=causal, behind=0, seed=10)
+    out, lse = c.forward(cuda_device)
+    grads = c.backward(cuda_device, out, lse)
+    x = [y.double().requires_grad_() for y in (c.q, c.k, c.v)]
+
+    def f(q, k, v):
+        total = 0.0
+        for rows, keys, seen in c.batch:
+            s = torch.einsum("thd,nhd->htn", q[rows], k[keys].repeat_interleave(3, 1)) * c.scale
+            s = s.masked_fill(~torch.from_numpy(seen), -math.inf)
+            o = torch.einsum("htn,nhd->thd", s.softmax(-1), v[keys].repeat_interleave(3, 1))
+            total = total + (o * c.g[rows].double()).sum()
+        return total
+
+    want = torch.autograd.grad(f(*x), x)
+    own, tol = ref.gradient(c.q, c.k, c.v, out, lse, c.g, c.scale, c.batch, exact=True)
+    rng = np.random.default_rng(11)
+    for i, name in enumerate(("dq", "dk", "dv")):
+        compare(name, grads[i], want[i].numpy(), tol[i], np.ones(len(tol[i]), bool))
+        way = torch.from_numpy(rng.standard_normal(x[i].shape))
+        step = 1e-5
+        with torch.no_grad():
+            ends = [f(*(y + sign * step * way if j == i else y for j, y in enumerate(x)))
+                    for sign in (1, -1)]
+        slope = float(ends[0] - ends[1]) / (2 * step)
+        got = float((grads[i].double().cpu() * way).sum())
+        # (64-bit differences: 1e-16 of f over the step, and the third derivative's
+        # share of its square)
+        room = float((tol[i] * way.abs().numpy()).sum()) + 1e-5 * (1 + abs(slope))
+        say(f"  {name} along a line: {got:.6f}, differences {slope:.6f}, room {room:.2e}")
+        assert abs(got - slope) <= room
+
+
+# --- values that are not finite -------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,d", [("f32", 64), ("bf16", 64), ("f16", 128), ("bf16", 256)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_keys_that_are_not_seen_stay_out(cuda_device, dtype, d, bad):
+    """v, k, q and d_out with a value that is not finite in places that some rows
+    (or keys) see and others of the same tile do not."""
+    for which in ("k", "v", "q", "g"):
+        c = Case(dtype, d, 4, 2, t=[100, 41], n=[130, 41], seed=12)
+        x = getattr(c, which)
+        x[60, 1, 3] = bad
+        x[90 if which in "qg" else 128, 0, d - 1] = bad
+        say(f"  {which}")
+        with np.errstate(invalid="ignore", over="ignore"):
+            if math.isnan(bad) or which == "v":
+                check_forward(c, cuda_device)
+            if math.isnan(bad) or which == "g":
+                check_gradient(c, cuda_device)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_scores_that_are_all_minus_infinity(cuda_device, dtype):
+    """Rows of them give 0, an lse of -infinity, and no gradient."""
+    c = Case(dtype, 64, 2, 1, t=[70], behind=0, seed=13)
+    c.q[20] = 0
+    c.q[20, :, 0] = 1.0
+    c.k[:, :, 0] = -math.inf
+    c.q[:20, :, 0] = c.q[21:, :, 0] = 1.0
+    out, lse = c.forward(cuda_device)
+    assert torch.equal(out, torch.zeros_like(out)) and (lse == -math.inf).all()
+    dq, dk, dv = c.backward(cuda_device, out, lse)
+    assert torch.equal(dv, torch.zeros_like(dv))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_scores_of_any_size(cuda_device, dtype):
+    """Far apart, and so large that a reference's rounding would show."""
+    top = {"f32": 3e12, "bf16": 3e12, "f16": 200.0}[dtype]
+    for by in (1.0, 40.0, top):
+        c = Case(dtype, 64, 4, 2, t=[150], seed=14, q_scale=by, behind=0)
+        out, lse = c.forward(cuda_device)
+        assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+        if by <= 40:
+            check_forward(c, cuda_device)
+            check_gradient(c, cuda_device)
+        else:                       # the largest score's value alone
+            s = np.stack([c.q[:, h].double().numpy() @ c.k[:, h // 2].double().numpy().T
+                          for h in range(4)])
+            s[:, ~np.tri(150, dtype=bool)] = -np.inf
+            best = s.argmax(-1)
+            two = np.sort(s, -1)[..., -2:]
+            clear = (two[..., 1] - two[..., 0]) * c.scale > 1e-4 * np.abs(two[..., 1]) + 40
+            for h in range(4):
+                rows = np.flatnonzero(clear[h])
+                assert len(rows) > 20
+                assert torch.equal(out[rows, h].cpu(), c.v[best[h, rows], h // 2])
+
+
+# --- streams, graphs, long arrays -----------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_captured_and_replayed(cuda_device, dtype):
+    """Forward (in parts, and whole) and backward in one graph, replayed over new
+    inputs, with eager work between."""
+    c = Case(dtype, 64, 4, 2, t=[90, 40], n=[90, 900], behind=0, seed=15)
+    dev = [x.to(cuda_device) for x in (c.q, c.k, c.v, c.g)]
+    p = c.packed(cuda_device)
+    out, lse = torch.empty_like(dev[0]), torch.empty(c.q.shape[:2], device=cuda_device)
+    grads = [torch.empty_like(x) for x in dev[:3]]
+    ws = [lib.prompt_workspace(*dev[:2], grad=g, **{k: v for k, v in p.items() if k != "causal"})
+          for g in (False, True)]
+
+    def step():
+        lib.prompt_attn(*dev[:3], c.scale, out=out, lse=lse, workspace=ws[0], **p)
+        lib.prompt_attn_grad(*dev[:3], out, lse, dev[3], c.scale, dq=grads[0], dk=grads[1],
+                             dv=grads[2], workspace=ws[1], **p)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for turn in range(4):
+        for x in dev:
+            x.copy_(torch.randn(x.shape, device=cuda_device))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (out, lse, *grads)]
+        step()
+        torch.cuda.synchronize()
+        for x, y in zip(got, (out, lse, *grads)):
+            assert torch.equal(x, y), turn
+
+
+def test_two_streams(cuda_device):
+    """Calls on two streams at once, each with what it allocates for itself."""
+    cases = [Case("bf16", 128, 8, 2, t=[900, 300], seed=16), Case("bf16", 128, 8, 2, t=[5], n=[4000],
+                                                                  seed=17)]
+    want = []
+    for c in cases:
+        out, lse = c.forward(cuda_device)
+        want.append((out, lse, *c.backward(cuda_device, out, lse)))
+    inputs = [[x.to(cuda_device) for x in (c.q, c.k, c.v, c.g)] for c in cases]
+    packed = [c.packed(cuda_device) for c in cases]
+    lse = [torch.full(c.q.shape[:2], math.nan, device=cuda_device) for c in cases]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for c, x, p, L, s in zip(cases, inputs, packed, lse, streams):
+            out = lib.prompt_attn(*x[:3], c.scale, lse=L, stream=s, **p)
+            got.append((out, L, *lib.prompt_attn_grad(*x[:3], out, L, x[3], c.scale, stream=s,
+                                                      **p)))
+        torch.cuda.synchronize()
+        for c, a, b in zip(cases, got, want):
+            rows, keys = c.rs[-1], c.ks[-1]
+            for x, y, n in zip(a, b, (rows, rows, rows, keys, keys)):
+                assert torch.equal(x[:n], y[:n])
+
+
+def test_offsets_beyond_32_bits(cuda_device):
+    """Sequences that begin more than 2^31 values into their arrays."""
+    d, h, far = 128, 8, (1 << 31) // (128 * 8) + 1000
+    c = Case("bf16", d, h, h, t=[150], behind=0, seed=18)
+    big = {}
+    for name in ("q", "k", "v", "g"):
+        big[name] = torch.zeros(far + 150, h, d, dtype=torch.bfloat16, device=cuda_device)
+        big[name][far:] = getattr(c, name).to(cuda_device)
+    start = torch.tensor([far, far + 150], dtype=torch.int32, device=cuda_device)
+    out, lse = c.forward(cuda_device)
+    want = c.backward(cuda_device, out, lse)
+    L = torch.zeros(far + 150, h, device=cuda_device)
+    p = dict(row_start=start, T=150, key_start=start, N=150)
+    got = lib.prompt_attn(big["q"], big["k"], big["v"], c.scale, lse=L, **p)
+    assert torch.equal(got[far:], out) and torch.equal(L[far:], lse)
+    grads = lib.prompt_attn_grad(big["q"], big["k"], big["v"], got, L, big["g"], c.scale, **p)
+    for x, y in zip(grads, want):
+        assert torch.equal(x[far:], y)
+
+
+def test_many_short_sequences(cuda_device):
+    """More sequences than a wave counts at once, some of none."""
+    rng = np.random.default_rng(19)
+    t = rng.integers(0, 12, 300).tolist()
+    c = Case("bf16", 64, 4, 1, t=t, seed=20)
+    check_forward(c, cuda_device)
+    check_gradient(c, cuda_device)
