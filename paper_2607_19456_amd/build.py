@@ -40,15 +40,12 @@ FLAGS = [
     # rewrite reads the result at once, which stalls the load pipeline
     # behind the work counter of the decode kernel.
     "-mllvm", "-amdgpu-atomic-optimizer-strategy=None",
+    # Matrix-core results in VGPRs: the decode's accumulators then stay in
+    # the registers its softmax rescale works on, instead of being copied
+    # between AGPRs and VGPRs around every tile.
+    "-mllvm", "-amdgpu-mfma-vgpr-form",
     f"-I{INCLUDE}",
 ]
-# Matrix-core results in VGPRs: the decode's accumulators then stay in
-# the registers its softmax rescale works on, instead of being copied
-# between AGPRs and VGPRs around every tile.
-VGPR_RESULTS = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
-# (The gradient's kernels hold more results than there are VGPRs: theirs are left
-# to the compiler.)
-SOURCE_FLAGS = {SRC: VGPR_RESULTS, PAGED_SRC: VGPR_RESULTS, PROMPT_SRC: VGPR_RESULTS}
 
 
 def _start(cmd: list, verbose: bool) -> subprocess.Popen:
@@ -85,9 +82,9 @@ def build(verbose: bool = False) -> str:
     objects = [LIB + tag + ".%d.o" % i for i in range(len(SOURCES))]
     compile_flags = [f for f in FLAGS if f != "-shared"]
     try:
-        _finish([_start([HIPCC, *compile_flags, *SOURCE_FLAGS.get(src, []), "-c", "-o", obj, src], verbose)
+        _finish([_start([HIPCC, *compile_flags, "-c", "-o", obj, src], verbose)
                  for obj, src in zip(objects, SOURCES)]
-                + [_start([HIPCC, *FLAGS, *VGPR_RESULTS, "-o", PROBE_LIB + tag, PROBE_SRC], verbose),
+                + [_start([HIPCC, *FLAGS, "-o", PROBE_LIB + tag, PROBE_SRC], verbose),
                    _start(_call_command(CALL_LIB + tag), verbose)])
         _finish([_start([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", LIB + tag,
                          *objects], verbose)])

@@ -145,6 +145,26 @@ __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
   }
 }
 
+// The same with the sum held in accumulation registers, of which a lane has 256
+// beside its 256 others: the compiler keeps results in one kind of the two, and
+// kernels with more than 256 of them need both.  (The no-op covers the two cycles
+// between a vector instruction's result and its use here, which the compiler counts
+// for instructions that it knows; settle() stands between the last product and the
+// first other use of a sum.)
+template <class T>
+__device__ __forceinline__ void mma_far(u32x4 a, u32x4 b, f32x16& c) {
+  if constexpr (std::is_same<T, __bf16>::value)
+    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  else
+    asm("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void mma_far(float a, float b, f32x16& c) {
+  asm("s_nop 1\n\tv_mfma_f32_32x32x2_f32 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void settle(f32x16& c) {
+  asm volatile("s_nop 15\n\ts_nop 7" : "+a"(c));
+}
+
 // Two values rounded to T, in a word; and both values of such a word added to x.
 template <class T>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
@@ -311,6 +331,44 @@ struct Stage {
     return bad;
   }
 };
+
+// The same without registers: each wave instruction brings 64 units of 16 bytes to
+// 1 KB of LDS in turn, so a lane fetches the chunk that belongs at its place.  The
+// data is there after the next barrier.
+template <class T, int D, int ROWS>
+struct Direct {
+  using L = Tile<T, D>;
+  static constexpr int units = ROWS * L::chunks / kThreads;
+  static_assert(units >= 1 && ROWS * L::chunks % kThreads == 0, "whole units");
+  static constexpr int step = kThreads / L::chunks;
+
+  // The row and chunk of this thread's unit u, and the unit's fetch from there.
+  __device__ static __forceinline__ int row(int tid, int u) { return tid / L::chunks + step * u; }
+  __device__ static __forceinline__ int chunk(int tid, int u) {
+    return (tid % L::chunks) ^ L::turn(row(tid, u));
+  }
+  // (In assembly: to the compiler a fetch may write what any later read of LDS
+  // reads, so that it would wait for it there.  arrived() stands before the barrier.)
+  __device__ static __forceinline__ void fetch(char* tile, int tid, int u, const char* from) {
+    typedef __attribute__((address_space(3))) char* lds;
+    const int to = uniform((int)(uintptr_t)(lds)tile + u * kThreads * 16 + (tid >> 6 << 10));
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"      // (m0 is the compiler's, between its uses)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :
+                 : "s"(to), "v"(from)
+                 : "m0");
+#pragma clang diagnostic pop
+  }
+};
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// A word (or several) of memory: not through the instructions that may be LDS too.
+template <class V, class P>
+__device__ __forceinline__ V far_load(const P* p) {
+  typedef const V __attribute__((address_space(1))) * global;
+  return *(global)p;
+}
 
 }  // namespace prompt
 

@@ -26,7 +26,6 @@ struct GradArgs {
   int64_t q_stride, k_stride, v_stride, d_out_stride;     // bytes between tokens
   int64_t dq_stride, dk_stride, dv_stride;
   float scale, scale2;          // and times log2(e)
-  uint32_t q_keep;              // 0 for a scale of 0, which takes q for 0
   f32x2* stats;                 // [rows][h_q]: lse times log2(e) (+infinity: no weights), delta
 };
 
@@ -164,7 +163,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
     float sum = 0.f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      q[b][w] = *reinterpret_cast<const u32x4*>(a.q + token * a.q_stride + in + 32 * w) & a.q_keep;
+      q[b][w] = *reinterpret_cast<const u32x4*>(a.q + token * a.q_stride + in + 32 * w);
       g[b][w] = *reinterpret_cast<const u32x4*>(a.d_out + token * a.d_out_stride + in + 32 * w);
       const u32x4 o = *reinterpret_cast<const u32x4*>(a.out + place * L::row_bytes + 16 * k + 32 * w);
       sum = dot16<T>(g[b][w], o, sum);
@@ -284,7 +283,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
 template <class T, int D>
 struct KeysForm {
   static constexpr bool wide = is_f32<T> && D == 256;
-  static constexpr int NK = 1;
+  static constexpr int NK = is_f32<T> || D == 256 ? 1 : 2;
   static constexpr int WK = wide ? 1 : 2, WR = wide ? 1 : 2, WD = wide ? 4 : 1;
   static constexpr int keys = 32 * NK * WK;
 };
@@ -298,13 +297,9 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
   constexpr int RT = 32 * WR;                 // rows of a step
   constexpr int NW = L::NW, ND = L::ND / WD;
   constexpr int kTile = RT * L::row_bytes;
-  constexpr int kUnits = RT * L::chunks / kThreads, kStep = kThreads / L::chunks;
-  static_assert(kUnits >= 1, "whole units");
 
-  __shared__ __align__(16) char s_q[2][kTile];
-  __shared__ __align__(16) char s_g[2][kTile];
+  __shared__ __align__(16) char s_rows[4][kTile];             // Q's two tiles, dO's two
   __shared__ __align__(16) float s_lse[2][RT], s_delta[2][RT];
-  __shared__ int s_spoilt[2][kWaves];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int i = lane & 31, k = lane >> 5;
@@ -346,169 +341,298 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
 #pragma unroll
       for (int r = 0; r < 16; ++r) dk[n][c][r] = 0.f, dv[n][c][r] = 0.f;
 
-  u32x4 q_next[kUnits], g_next[kUnits];
-  f32x2 stat_next{INFINITY, 0.f};
   const RowReader<T, D> read(ordered_row(i), k);
   const ColumnReader<T, D> read_columns(lane);
 
-  auto load = [&](int t) {
-    const int r = tid / L::chunks, c = tid % L::chunks;
-#pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      const int row = t * RT + r + kStep * u;
-      const int token = token_of(bt, min(row, end - 1));
-      const int64_t in = (int64_t)(head * bt.G + min(row, end - 1) - token * bt.G) * L::row_bytes +
-                         16 * c;
-      const int64_t tok = rows.start + token;
-      q_next[u] = *reinterpret_cast<const u32x4*>(a.q + tok * a.q_stride + in) & a.q_keep;
-      g_next[u] = *reinterpret_cast<const u32x4*>(a.d_out + tok * a.d_out_stride + in);
-      if (row >= end) q_next[u] = g_next[u] = u32x4{0u, 0u, 0u, 0u};
-    }
+  // Rows beyond the last are the last one again (their weights are taken as 0).
+  using Fetch = Direct<T, D, RT>;
+  auto load_unit = [&](int t, int u) {
+    const bool is_q = u < Fetch::units;
+    const int v = is_q ? u : u - Fetch::units;
+    const int x = min(t * RT + Fetch::row(tid, v), end - 1), tok = token_of(bt, x);
+    const int64_t token = rows.start + tok;
+    const int in = (head * bt.G + x - tok * bt.G) * L::row_bytes + 16 * Fetch::chunk(tid, v);
+    if (is_q)
+      Fetch::fetch(s_rows[t & 1], tid, v, a.q + token * a.q_stride + in);
+    else
+      Fetch::fetch(s_rows[2 + (t & 1)], tid, v, a.d_out + token * a.d_out_stride + in);
+  };
+  f32x2 stat{INFINITY, 0.f};
+  auto load_stats = [&](int t) {
     if (tid < RT) {
-      const int row = t * RT + tid;
-      const int token = token_of(bt, min(row, end - 1));
-      stat_next = a.stats[(int64_t)(rows.start + token) * bt.h_q + head * bt.G +
-                          min(row, end - 1) - token * bt.G];
-      if (row >= end) stat_next = f32x2{INFINITY, 0.f};
+      const int x = min(t * RT + tid, end - 1), tok = token_of(bt, x);
+      stat = far_load<f32x2>(a.stats + (int64_t)(rows.start + tok) * bt.h_q + head * bt.G + x -
+                             tok * bt.G);
     }
   };
-  auto store = [&](int t) {
-    const int buf = t & 1, r = tid / L::chunks, c = tid % L::chunks;
-    bool bad = false;
-#pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      *reinterpret_cast<u32x4*>(s_q[buf] + L::at(r + kStep * u, c)) = q_next[u];
-      *reinterpret_cast<u32x4*>(s_g[buf] + L::at(r + kStep * u, c)) = g_next[u];
-    }
-    if (tid < RT) s_lse[buf][tid] = stat_next[0], s_delta[buf][tid] = stat_next[1];
-    if (t * RT < all_from) {
-#pragma unroll
-      for (int u = 0; u < kUnits; ++u)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) bad |= not_finite<T>(q_next[u][w]) || not_finite<T>(g_next[u][w]);
-      bad = __any(bad);
-      if (lane == 0) s_spoilt[buf][wave] = bad;
-    }
+  auto store_stats = [&](int t) {
+    if (tid < RT) s_lse[t & 1][tid] = stat[0], s_delta[t & 1][tid] = stat[1];
   };
+  // Not all rows of a step see all keys, and what they do not see is masked.
+  auto partial = [&](int t) { return t * RT < all_from || (t + 1) * RT > end; };
+  bool skipped = false;
 
   if (r0 < r1) {
-    load(r0);
-    store(r0);
+#pragma unroll
+    for (int u = 0; u < 2 * Fetch::units; ++u) load_unit(r0, u);
+    load_stats(r0);
+    store_stats(r0);
+    arrived();
     __syncthreads();
+  }
+  // (waited for here, not at their first use in the loop, whose waits would count the
+  // fetches too)
+#pragma unroll
+  for (int n = 0; n < NK; ++n)
+#pragma unroll
+    for (int w = 0; w < NW; ++w) asm volatile("" : "+v"(kk[n][w]), "+v"(vv[n][w]));
+  {
     for (int t = r0; t < r1; ++t) {
-      const int buf = t & 1;
-      if (t + 1 < r1) load(t + 1);
-      const char *tile_q = s_q[buf] + 32 * wr * L::row_bytes;
-      const char *tile_g = s_g[buf] + 32 * wr * L::row_bytes;
+      const int buf = t & 1, next = min(t + 1, r1 - 1);
+      const char *tile_q = s_rows[buf] + 32 * wr * L::row_bytes;
+      const char *tile_g = s_rows[2 + buf] + 32 * wr * L::row_bytes;
+      const float *my_lse = &s_lse[buf][32 * wr], *my_delta = &s_delta[buf][32 * wr];
       const int row0 = t * RT + 32 * wr;
+      load_stats(next);
       f32x16 s[NK], dp[NK];
 #pragma unroll
       for (int n = 0; n < NK; ++n)
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[n][r] = 0.f, dp[n][r] = 0.f;
+      // S, and the next rows' fetches
+      {
+        u32x4 x = read.get(tile_q, 0, 0);
 #pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        const u32x4 x = read.get(tile_q, 0, w);
+        for (int w = 0; w < NW; ++w) {
+          const u32x4 y = read.get(w + 1 < NW ? tile_q : tile_g, 0, w + 1 < NW ? w + 1 : 0);
 #pragma unroll
-        for (int n = 0; n < NK; ++n) s[n] = mma<T>(x, kk[n][w], s[n]);
+          for (int n = 0; n < NK; ++n) s[n] = mma<T>(x, kk[n][w], s[n]);
+          if (w < 2 * Fetch::units) load_unit(next, w);
+          x = y;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        // dP, and P
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+          u32x4 y = x;
+          if (w + 1 < NW) y = read.get(tile_g, 0, w + 1);
+#pragma unroll
+          for (int n = 0; n < NK; ++n) dp[n] = mma<T>(x, vv[n][w], dp[n]);
+          if (4 * w % NW == 0) {
+            const int r = 16 * w / NW;
+            const f32x4 z = *reinterpret_cast<const f32x4*>(my_lse + row_of(r, k));
+#pragma unroll
+            for (int n = 0; n < NK; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                s[n][r + e] =
+                    __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r + e], a.scale2, -z[e]));
+          }
+          x = y;
+          if (4 * (w + 1) % NW == 0) __builtin_amdgcn_sched_barrier(0);
+        }
       }
+      if (__builtin_expect(partial(t), 0)) {
+        // What a row does not see must not meet its weight of 0 where it is not
+        // finite: such rows are left out here (zeros in their place) and added at the
+        // end.
+        bool bad = false;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        const u32x4 x = read.get(tile_g, 0, w);
+        for (int w = 0; w < NW; ++w) {
+          const u32x4 x = read.get(tile_q, 0, w), y = read.get(tile_g, 0, w);
 #pragma unroll
-        for (int n = 0; n < NK; ++n) dp[n] = mma<T>(x, vv[n][w], dp[n]);
-      }
-      float lse2[16], delta[16];
-#pragma unroll
-      for (int r = 0; r < 16; r += 4) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(&s_lse[buf][32 * wr + row_of(r, k)]);
-        const f32x4 y = *reinterpret_cast<const f32x4*>(&s_delta[buf][32 * wr + row_of(r, k)]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) lse2[r + e] = x[e], delta[r + e] = y[e];
-      }
-#pragma unroll
-      for (int n = 0; n < NK; ++n)
+          for (int e = 0; e < 4; ++e) bad = bad || not_finite<T>(x[e]) || not_finite<T>(y[e]);
+        }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], a.scale2, -lse2[r]));
-          dp[n][r] = s[n][r] * (dp[n][r] - delta[r]);
+          const float x = my_lse[row_of(r, k)];
+          bad = bad || x != x || !(fabsf(my_delta[row_of(r, k)]) < INFINITY);
         }
-      bool slow = false;
-      // (rows beyond the last are zeros, which K may turn into NaN)
-      if (t * RT < all_from || (t + 1) * RT > end) {
+        bad = __any(bad);
+        __syncthreads();
+        if (bad) {
+          skipped = true;
+          for (int x = lane; x < 32 * L::chunks; x += 64)
+            reinterpret_cast<u32x4*>(s_rows[buf] + 32 * wr * L::row_bytes)[x] =
+                reinterpret_cast<u32x4*>(s_rows[2 + buf] + 32 * wr * L::row_bytes)[x] =
+                    u32x4{0u, 0u, 0u, 0u};
+          s_delta[buf][32 * wr + i] = 0.f;
+        }
 #pragma unroll
         for (int n = 0; n < NK; ++n)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int row = row0 + row_of(r, k);
-            if (row < from[n] || row >= end) s[n][r] = 0.f, dp[n][r] = 0.f;
+            if (bad || row < from[n] || row >= end) s[n][r] = 0.f, dp[n][r] = 0.f;
           }
       }
-      if (t * RT < all_from) {
-        int bad = 0;
+      // dV, and dS
+      if constexpr (is_f32<T>) {
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) bad |= s_spoilt[buf][w];
-        slow = uniform(bad);
-      }
-      if (__builtin_expect(slow, 0)) {
+        for (int r = 0; r < 16; ++r) {
 #pragma unroll
-        for (int n = 0; n < NK; ++n) {
-          auto sees = [&](int row) { return row0 + row >= from[n] && row0 + row < end; };
-          add_seen<T, D>(tile_g, 0, 32 * ND * wd, s[n], k, dv[n], sees);
-          add_seen<T, D>(tile_q, 0, 32 * ND * wd, dp[n], k, dk[n], sees);
+          for (int c = 0; c < ND; ++c) {
+            const float x = read_columns.get(tile_g, r / 8, r % 8, ND * wd + c);
+#pragma unroll
+            for (int n = 0; n < NK; ++n) mma_far(x, s[n][r], dv[n][c]);
+          }
+          const float y = my_delta[row_of(r, k)];
+#pragma unroll
+          for (int n = 0; n < NK; ++n) dp[n][r] = s[n][r] * (dp[n][r] - y);
+#pragma unroll
+          for (int c = 0; c < ND; ++c) {
+            const float x = read_columns.get(tile_q, r / 8, r % 8, ND * wd + c);
+#pragma unroll
+            for (int n = 0; n < NK; ++n) mma_far(x, dp[n][r], dk[n][c]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
       } else {
-        add_columns<T, D, ND, NK>(read_columns, tile_g, 0, ND * wd, s, dv);
-        add_columns<T, D, ND, NK>(read_columns, tile_q, 0, ND * wd, dp, dk);
+        u32x4 p[NK], ds[2][NK];
+        u32x4 x = read_columns.get(tile_g, 0, 0);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int n = 0; n < NK; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              p[n][e] = pack2<T>(s[n][8 * h + 2 * e], s[n][8 * h + 2 * e + 1]);
+#pragma unroll
+          for (int c = 0; c < ND; ++c) {
+            const bool last = c + 1 == ND;
+            const u32x4 y = last ? read_columns.get(h == 0 ? tile_g : tile_q, h == 0 ? 1 : 0, 0)
+                                 : read_columns.get(tile_g, h, c + 1);
+#pragma unroll
+            for (int n = 0; n < NK; ++n) mma_far<T>(x, p[n], dv[n][c]);
+            if (2 * c % ND == 0) {
+              const int r = 8 * c / ND;
+              const f32x4 z = *reinterpret_cast<const f32x4*>(my_delta + row_of(8 * h + r, k));
+#pragma unroll
+              for (int n = 0; n < NK; ++n) {
+                float e4[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  e4[e] = s[n][8 * h + r + e] * (dp[n][8 * h + r + e] - z[e]);
+                ds[h][n][r / 2] = pack2<T>(e4[0], e4[1]);
+                ds[h][n][r / 2 + 1] = pack2<T>(e4[2], e4[3]);
+              }
+            }
+            x = y;
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        // dK
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int c = 0; c < ND; ++c) {
+            u32x4 y = x;
+            if (h == 0 || c + 1 < ND)
+              y = read_columns.get(tile_q, c + 1 < ND ? h : 1, c + 1 < ND ? c + 1 : 0);
+#pragma unroll
+            for (int n = 0; n < NK; ++n) mma_far<T>(x, ds[h][n], dk[n][c]);
+            x = y;
+            __builtin_amdgcn_sched_barrier(0);
+          }
       }
-      if (t + 1 < r1) store(t + 1);
+      store_stats(next);
+      arrived();
       __syncthreads();
     }
   }
 
-  // The row waves' sums: the others' to LDS, added in their order by the first.
-  if constexpr (WR > 1) {
-    static_assert(WR == 2 && WK * 64 * 16 * 4 * ND * NK <= 2 * kTile, "fits the rows' place");
-    auto exchange = [&](f32x16 (&x)[NK][ND], char* place) {
+  // The rows that were left out, pair by pair, those alone that see the key: what they
+  // add to block c of key n's dK or dV.
+  auto left_out = [&](int n, int c, bool is_dk, f32x16 x) {
+    const int64_t token = keys.start + min(key[n], keys.n - 1);
+    const T* k_row = reinterpret_cast<const T*>(a.k + token * a.k_stride) + head * D;
+    const T* v_row = reinterpret_cast<const T*>(a.v + token * a.v_stride) + head * D;
+    const T *q, *g;
+    f32x2 st;
+    auto at_row = [&](int row) {
+      const int tok = token_of(bt, row), h = head * bt.G + row - tok * bt.G;
+      const int64_t to = rows.start + tok;
+      q = reinterpret_cast<const T*>(a.q + to * a.q_stride) + h * D;
+      g = reinterpret_cast<const T*>(a.d_out + to * a.d_out_stride) + h * D;
+      st = a.stats[to * bt.h_q + h];
+    };
+#pragma unroll 1
+    for (int t = r0; t < r1; ++t) {
+      if (!partial(t)) continue;
+      const int row0 = t * RT + 32 * wr;
+      at_row(min(row0 + i, end - 1));
+      bool bad = st[0] != st[0] || !(fabsf(st[1]) < INFINITY);
+#pragma unroll 1
+      for (int d = k; d < D; d += 2)
+        bad = bad || !(fabsf((float)q[d]) < INFINITY) || !(fabsf((float)g[d]) < INFINITY);
+      if (!__any(bad)) continue;
+#pragma unroll 1
+      for (int row = max(row0, from[n]); row < min(row0 + 32, end); ++row) {
+        at_row(row);
+        float s = 0.f, dp = 0.f;
+#pragma unroll 1
+        for (int d = 0; d < D; ++d) {
+          s += (float)q[d] * (float)k_row[d];
+          dp += (float)g[d] * (float)v_row[d];
+        }
+        float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s, a.scale2, -st[0]));
+        if (is_dk) w *= dp - st[1];
+        if constexpr (!is_f32<T>) w = (float)(T)w;
+        const T* of = is_dk ? q : g;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r] += w * (float)of[32 * c + 8 * (r / 4) + 4 * k + r % 4];
+      }
+    }
+    return x;
+  };
+  // The row waves' sums: the others' to LDS, added by the first, which stores.
+  auto finish = [&](f32x16 (&acc)[NK][ND], bool is_dk) {
+    static_assert(WR == 1 || (WR == 2 && WK * 4096 * ND * NK <= 4 * kTile), "fits the rows' place");
+    const float by = is_dk ? a.scale : 1.f;
+    auto block = [&](int n, int c) {
+      settle(acc[n][c]);
+      f32x16 x = acc[n][c];
+      if (__builtin_expect(skipped, 0)) x = left_out(n, ND * wd + c, is_dk, x);
+      return x;
+    };
+    auto shared = [&](int n, int c) {
+      return reinterpret_cast<f32x4*>(s_rows[0]) + ((wk * NK + n) * ND + c) * 256 + lane;
+    };
+    if (wr == 1) {
 #pragma unroll
       for (int n = 0; n < NK; ++n)
 #pragma unroll
-        for (int c = 0; c < ND; ++c)
+        for (int c = 0; c < ND; ++c) {
+          const f32x16 x = block(n, c);
 #pragma unroll
-          for (int r = 0; r < 16; r += 4) {
-            f32x4* p = reinterpret_cast<f32x4*>(place) +
-                       (((wk * NK + n) * ND + c) * 4 + r / 4) * 64 + lane;
-            if (wr == 1) {
-              *p = f32x4{x[n][c][r], x[n][c][r + 1], x[n][c][r + 2], x[n][c][r + 3]};
-            } else {
-              const f32x4 y = *p;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) x[n][c][r + e] += y[e];
-            }
-          }
-    };
-    if (wr == 1) exchange(dk, s_q[0]), exchange(dv, s_g[0]);
-    __syncthreads();
-    if (wr == 0) exchange(dk, s_q[0]), exchange(dv, s_g[0]);
-  }
-  if (wr != 0) return;
-#pragma unroll
-  for (int n = 0; n < NK; ++n)
-    if (key[n] < keys.n) {
-      const int64_t token = keys.start + key[n], in = (int64_t)head * L::row_bytes;
-      char* dk_row = a.dk + token * a.dk_stride + in;
-      char* dv_row = a.dv + token * a.dv_stride + in;
-#pragma unroll
-      for (int c = 0; c < ND; ++c)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-          const int d = 32 * (ND * wd + c) + 2 * r + 4 * k;
-          store4<T>(dk_row, d, f32x4{dk[n][c][r], dk[n][c][r + 1], dk[n][c][r + 2],
-                                     dk[n][c][r + 3]} * a.scale);
-          store4<T>(dv_row, d, f32x4{dv[n][c][r], dv[n][c][r + 1], dv[n][c][r + 2],
-                                     dv[n][c][r + 3]});
+          for (int r = 0; r < 16; r += 4)
+            shared(n, c)[16 * r] = f32x4{x[r], x[r + 1], x[r + 2], x[r + 3]};
         }
     }
+    if (WR > 1) __syncthreads();
+    if (wr == 0) {
+#pragma unroll
+      for (int n = 0; n < NK; ++n) {
+        const int64_t token = keys.start + key[n];
+        char* dst = (is_dk ? a.dk + token * a.dk_stride : a.dv + token * a.dv_stride) +
+                    (int64_t)head * L::row_bytes;
+#pragma unroll
+        for (int c = 0; c < ND; ++c) {
+          f32x16 x = block(n, c);
+#pragma unroll
+          for (int r = 0; r < 16; r += 4) {
+            f32x4 y{x[r], x[r + 1], x[r + 2], x[r + 3]};
+            if (WR > 1) y += shared(n, c)[16 * r];
+            if (key[n] < keys.n)
+              store4<T>(dst, 32 * (ND * wd + c) + 2 * r + 4 * k, y * by);
+          }
+        }
+      }
+    }
+    if (WR > 1) __syncthreads();
+  };
+  finish(dk, true);
+  finish(dv, false);
 }
 
 }  // namespace
@@ -587,7 +711,6 @@ da_status da_prompt_attn_grad(const da_prompt* prompt, const void* q, int64_t q_
   a.d_out_stride = d_out_stride * size, a.dq_stride = dq_stride * size;
   a.dk_stride = dk_stride * size, a.dv_stride = dv_stride * size;
   a.scale = scale, a.scale2 = scale * kLog2e;
-  a.q_keep = scale == 0.f ? 0u : ~0u;
   a.stats = static_cast<f32x2*>(workspace);
   const Batch bt = device_batch(p);
   hipStream_t s = static_cast<hipStream_t>(stream);
