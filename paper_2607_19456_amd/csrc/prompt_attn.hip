@@ -51,10 +51,10 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   constexpr int NS = KT / 32, ND = L::ND, NW = L::NW;
   constexpr int kTile = KT * L::row_bytes;
   constexpr int NP = is_f32<T> ? 1 : 2 * NS;
+  using Fetch = Direct<T, D, KT>;
 
   __shared__ __align__(16) char s_k[2][kTile];
   __shared__ __align__(16) char s_v[2][kTile];
-  __shared__ int s_spoilt[2][kWaves];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int i = lane & 31, k = lane >> 5;
@@ -79,6 +79,8 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   const int my_row0 = row0 + 32 * NQ * wave;
   const int my_rows = min(max(in_tile - 32 * NQ * wave, 0), 32 * NQ);
   const int my_min = my_rows ? seen_by(bt, rows.n, keys.n, token_of(bt, my_row0)) : 0;
+  const int my_max =
+      my_rows ? seen_by(bt, rows.n, keys.n, token_of(bt, my_row0 + my_rows - 1)) : 0;
   int seen[NQ];
   int64_t place[NQ];                         // row * h_q + head
   u32x4 q[NQ][NW];
@@ -93,11 +95,11 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
                       (int64_t)(head * bt.G + g) * L::row_bytes + 16 * k;
 #pragma unroll
     for (int w = 0; w < NW; ++w)
-      q[b][w] = (*reinterpret_cast<const u32x4*>(src + 32 * w) & a.q_keep) ^ a.q_flip;
+      q[b][w] = (far_load<u32x4>(src + 32 * w) & a.q_keep) ^ a.q_flip;
   }
 
   f32x16 acc[NQ][ND];
-  float limit[NQ], ref[NQ], sum[NQ], whole[NQ];
+  float limit[NQ], ref[NQ], sum[NQ], whole[NQ], top[NQ];
 #pragma unroll
   for (int b = 0; b < NQ; ++b) {
 #pragma unroll
@@ -110,19 +112,23 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
 
   const char* k_base = a.k + (int64_t)keys.start * a.k_stride + (int64_t)head * L::row_bytes;
   const char* v_base = a.v + (int64_t)keys.start * a.v_stride + (int64_t)head * L::row_bytes;
-  Stage<T, D, KT> k_next, v_next;
   const RowReader<T, D> k_read(ordered_row(i), k);
   const ColumnReader<T, D> v_read(lane);
 
-  auto load_k = [&](int t) { k_next.load(k_base, a.k_stride, t * KT, keys.n, tid); };
-  auto load_v = [&](int t) { v_next.load(v_base, a.v_stride, t * KT, keys.n, tid); };
-  // Where some rows see keys of a tile that others do not, values that are not
-  // finite must not meet the others' weights of 0.
-  auto store_v = [&](int t) {
-    v_next.store(s_v[t & 1], tid);
-    if ((t + 1) * KT > min_seen) {
-      const bool bad = __any(v_next.spoilt());
-      if (lane == 0) s_spoilt[t & 1][wave] = bad;
+  // (Keys beyond the last are the last one again; no row sees them.)
+  auto load_k = [&](int t, int u) {
+    const int key = min(t * KT + Fetch::row(tid, u), keys.n - 1);
+    Fetch::fetch(s_k[t & 1], tid, u, k_base + key * a.k_stride + 16 * Fetch::chunk(tid, u));
+  };
+  auto load_v = [&](int t, int u) {
+    const int key = min(t * KT + Fetch::row(tid, u), keys.n - 1);
+    Fetch::fetch(s_v[t & 1], tid, u, v_base + key * a.v_stride + 16 * Fetch::chunk(tid, u));
+  };
+  auto load_all = [&](int t, bool want_k, bool want_v) {
+#pragma unroll
+    for (int u = 0; u < Fetch::units; ++u) {
+      if (want_k) load_k(t, u);
+      if (want_v) load_v(t, u);
     }
   };
 
@@ -146,18 +152,16 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   auto mask = [&](int t, f32x16 (&s)[NQ][NS]) {
     if ((t + 1) * KT <= my_min) return;
 #pragma unroll
-    for (int b = 0; b < NQ; ++b)
+    for (int b = 0; b < NQ; ++b) {
+      const int left = seen[b] - t * KT - 8 * k;
 #pragma unroll
       for (int n = 0; n < NS; ++n)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (t * KT + 32 * n + row_of(r, k) >= seen[b]) s[b][n][r] = -INFINITY;
+          if (32 * n + row_of(r, 0) >= left) s[b][n][r] = -INFINITY;
+    }
   };
-  // The reference is raised when a score lies 8 above it: weights stay below
-  // 2^8, and most tiles rescale nothing.
-  auto raise = [&](f32x16 (&s)[NQ][NS]) {
-    float top[NQ];
-    bool over = false;
+  auto find_top = [&](const f32x16 (&s)[NQ][NS]) {
 #pragma unroll
     for (int b = 0; b < NQ; ++b) {
       top[b] = s[b][0][0];
@@ -165,27 +169,38 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
       for (int n = 0; n < NS; ++n)
 #pragma unroll
         for (int r = 0; r < 16; ++r) top[b] = fmaxf(top[b], s[b][n][r]);
+    }
+  };
+  // The reference is raised when a score lies 8 above it: weights stay below
+  // 2^8, and most tiles rescale nothing.
+  auto over = [&]() {
+    bool x = false;
+#pragma unroll
+    for (int b = 0; b < NQ; ++b) {
       top[b] *= a.scale;
-      over |= !(top[b] <= limit[b]);
+      x |= !(top[b] <= limit[b]);
     }
-    if (__any(over)) {
-      bool far = false;
+    return __any(x);
+  };
+  auto raise = [&]() {
+    bool far = false;
 #pragma unroll
-      for (int b = 0; b < NQ; ++b) {
-        top[b] = fmaxf(top[b], __shfl_xor(top[b], 32));
-        far |= fabsf(top[b]) > kFar && top[b] != -INFINITY;
-        if (!(top[b] <= limit[b])) {
-          const float f = limit[b] == -INFINITY ? 0.f : exp2f(ref[b] - top[b]);
-          ref[b] = top[b];
-          limit[b] = top[b] + 8.f;
-          sum[b] *= f;
-          whole[b] *= f;
+    for (int b = 0; b < NQ; ++b) {
+      top[b] = fmaxf(top[b], __shfl_xor(top[b], 32));
+      far |= fabsf(top[b]) > kFar && top[b] != -INFINITY;
+      if (!(top[b] <= limit[b])) {
+        const float f = limit[b] == -INFINITY ? 0.f : exp2f(ref[b] - top[b]);
+        ref[b] = top[b];
+        limit[b] = top[b] + 8.f;
+        sum[b] *= f;
+        whole[b] *= f;
 #pragma unroll
-          for (int c = 0; c < ND; ++c) acc[b][c] *= f;
-        }
+        for (int c = 0; c < ND; ++c) acc[b][c] *= f;
       }
-      if (__any(far)) by = 1.f;
     }
+    if (__any(far)) by = 1.f;
+  };
+  auto rescore = [&](f32x16 (&s)[NQ][NS]) {
     if (__builtin_expect(by != a.scale, 0)) {
 #pragma unroll
       for (int b = 0; b < NQ; ++b)
@@ -193,66 +208,65 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
         for (int n = 0; n < NS; ++n) s[b][n] *= a.scale;
     }
   };
-  // s becomes the weights; 16-bit ones are rounded into p.
+  // Components 8h .. 8h+7 of a block become weights; 16-bit ones are rounded into p.
+  auto weigh = [&](int b, int h, f32x16& s, u32x4& p) {
+#pragma unroll
+    for (int r = 8 * h; r < 8 * h + 8; ++r)
+      s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], by, -ref[b]));
+    if constexpr (is_f32<T>) {
+#pragma unroll
+      for (int r = 8 * h; r < 8 * h + 8; ++r) sum[b] += s[r];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        p[e] = pack2<T>(s[8 * h + 2 * e], s[8 * h + 2 * e + 1]);
+        sum[b] = add2<T>(p[e], sum[b]);
+        if constexpr (LSE) whole[b] += s[8 * h + 2 * e] + s[8 * h + 2 * e + 1];
+      }
+    }
+  };
   auto weights = [&](f32x16 (&s)[NQ][NS], u32x4 (&p)[NQ][NP]) {
 #pragma unroll
     for (int b = 0; b < NQ; ++b)
 #pragma unroll
-      for (int n = 0; n < NS; ++n) {
+      for (int n = 0; n < NS; ++n)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          s[b][n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][n][r], by, -ref[b]));
-        if constexpr (is_f32<T>) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) sum[b] += s[b][n][r];
-        } else {
-#pragma unroll
-          for (int r = 0; r < 16; r += 2) {
-            const uint32_t w = pack2<T>(s[b][n][r], s[b][n][r + 1]);
-            p[b][2 * n + r / 8][r % 8 / 2] = w;
-            sum[b] = add2<T>(w, sum[b]);
-            if constexpr (LSE) whole[b] += s[b][n][r] + s[b][n][r + 1];
-          }
-        }
-      }
+        for (int h = 0; h < 2; ++h) weigh(b, h, s[b][n], p[b][is_f32<T> ? 0 : 2 * n + h]);
   };
   auto values = [&](int t, f32x16 (&s)[NQ][NS], u32x4 (&p)[NQ][NP]) {
     const char* tile = s_v[t & 1];
-    if ((t + 1) * KT > min_seen) {
-      int bad = 0;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) bad |= s_spoilt[t & 1][w];
-      if (__builtin_expect(uniform(bad), 0)) {
-        // key by key, those alone that the row sees
+    // Where some rows see keys of a tile that others do not, values that are not
+    // finite must not meet the others' weights of 0.
+    if ((t + 1) * KT > my_min && __builtin_expect(!tile_finite<T, D, KT>(tile, lane), 0)) {
+      // key by key, those alone that the row sees
 #pragma unroll 1
-        for (int e = 0; e < 16 * NS; ++e) {
+      for (int e = 0; e < 16 * NS; ++e) {
 #pragma unroll
-          for (int b = 0; b < NQ; ++b) {
-            float mine = 0.f;
+        for (int b = 0; b < NQ; ++b) {
+          float mine = 0.f;
 #pragma unroll
-            for (int n = 0; n < NS; ++n)
+          for (int n = 0; n < NS; ++n)
 #pragma unroll
-              for (int r = 0; r < 16; ++r) mine = 16 * n + r == e ? s[b][n][r] : mine;
-            if constexpr (!is_f32<T>) mine = (float)(T)mine;
-            const float other = __shfl_xor(mine, 32);
+            for (int r = 0; r < 16; ++r) mine = 16 * n + r == e ? s[b][n][r] : mine;
+          if constexpr (!is_f32<T>) mine = (float)(T)mine;
+          const float other = __shfl_xor(mine, 32);
 #pragma unroll 1
-            for (int kk = 0; kk < 2; ++kk) {
-              const int key = 32 * (e / 16) + row_of(e % 16, kk);
-              if (t * KT + key >= seen[b]) continue;
-              const float w = kk == k ? mine : other;
+          for (int kk = 0; kk < 2; ++kk) {
+            const int key = 32 * (e / 16) + row_of(e % 16, kk);
+            if (t * KT + key >= seen[b]) continue;
+            const float w = kk == k ? mine : other;
 #pragma unroll
-              for (int c = 0; c < ND; ++c)
+            for (int c = 0; c < ND; ++c)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                  const int d = (32 * c + 8 * (r / 4) + 4 * k + r % 4) * (int)sizeof(T);
-                  acc[b][c][r] +=
-                      w * (float)*reinterpret_cast<const T*>(tile + L::at(key, d / 16) + d % 16);
-                }
-            }
+              for (int r = 0; r < 16; ++r) {
+                const int d = (32 * c + 8 * (r / 4) + 4 * k + r % 4) * (int)sizeof(T);
+                acc[b][c][r] +=
+                    w * (float)*reinterpret_cast<const T*>(tile + L::at(key, d / 16) + d % 16);
+              }
           }
         }
-        return;
       }
+      return;
     }
     if constexpr (is_f32<T>) {
 #pragma unroll
@@ -278,31 +292,146 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
     }
   };
 
-  if (t0 < t1) {
-    load_k(t0);
-    load_v(t0);
-    k_next.store(s_k[t0 & 1], tid);
-    store_v(t0);
-    __syncthreads();
-    for (int t = t0; t < t1; ++t) {
-      const bool more = t + 1 < t1;
-      if (more) {
-        load_k(t + 1);
-        load_v(t + 1);
+  int t = t0;
+  // Tiles that all rows see whole, in a pipeline: a tile's scores are multiplied
+  // while those before become weights, and its largest score is found while those
+  // weights meet V.
+  if constexpr (NQ == 2) {
+    const int whole_tiles = min(min_seen / KT, t1);
+    if (t0 < whole_tiles) {
+      load_all(t0, true, true);
+      load_all(t0 + 1, true, false);
+      arrived();
+      __syncthreads();
+      f32x16 sa[NQ][NS], sb[NQ][NS];
+      u32x4 p[NQ][NP];
+      scores(t0, sa);
+      find_top(sa);
+      if (over()) raise();
+      rescore(sa);
+      __syncthreads();
+      auto step = [&](f32x16 (&s)[NQ][NS], f32x16 (&next)[NQ][NS]) {
+        const char *tile_k = s_k[(t + 1) & 1], *tile_v = s_v[t & 1];
+#pragma unroll
+        for (int b = 0; b < NQ; ++b)
+#pragma unroll
+          for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) next[b][n][r] = 0.f;
+        u32x4 x[NS];
+#pragma unroll
+        for (int n = 0; n < NS; ++n) x[n] = k_read.get(tile_k, n, 0);
+        constexpr int kPieces = NQ * NP / NW;           // of 8 weights, a step of the product
+        static_assert(NQ * NP % NW == 0, "whole pieces");
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+          u32x4 y[NS];
+#pragma unroll
+          for (int n = 0; n < NS; ++n) y[n] = w + 1 < NW ? k_read.get(tile_k, n, w + 1) : x[n];
+#pragma unroll
+          for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int b = 0; b < NQ; ++b) next[b][n] = mma<T>(x[n], q[b][w], next[b][n]);
+#pragma unroll
+          for (int e = w * kPieces; e < (w + 1) * kPieces; ++e) {
+            const int b = e / NP, n = e % NP / 2, h = e % 2;
+            weigh(b, h, s[b][n], p[b][2 * n + h]);
+          }
+          if (w < Fetch::units) load_k(t + 2, w);
+          else if (w < 2 * Fetch::units) load_v(t + 1, w - Fetch::units);
+#pragma unroll
+          for (int n = 0; n < NS; ++n) x[n] = y[n];
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        u32x4 v0 = v_read.get(tile_v, 0, 0), v1 = v_read.get(tile_v, 0, 1);
+#pragma unroll
+        for (int b = 0; b < NQ; ++b) top[b] = next[b][0][0];
+#pragma unroll
+        for (int e = 0; e < NP * ND; ++e) {
+          u32x4 v2 = v0;
+          if (e + 2 < NP * ND) v2 = v_read.get(tile_v, (e + 2) / ND, (e + 2) % ND);
+#pragma unroll
+          for (int b = 0; b < NQ; ++b) mma_far<T>(v0, p[b][e / ND], acc[b][e % ND]);
+          constexpr int kEach = 16 * NS / (NP * ND);    // scores of a row's lane, a step
+#pragma unroll
+          for (int b = 0; b < NQ; ++b)
+#pragma unroll
+            for (int r = e * kEach; r < (e + 1) * kEach; ++r)
+              top[b] = fmaxf(top[b], next[b][r / 16][r % 16]);
+          v0 = v1, v1 = v2;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        arrived();
+        __syncthreads();
+      };
+      bool again = true;
+      while (again) {
+        again = false;
+        while (t + 1 < whole_tiles) {
+          step(sa, sb);
+          ++t;
+          if (over()) {
+            again = true;
+#pragma unroll
+            for (int b = 0; b < NQ; ++b)
+#pragma unroll
+              for (int n = 0; n < NS; ++n) sa[b][n] = sb[b][n];
+            break;
+          }
+          rescore(sb);
+          if (t + 1 >= whole_tiles) {
+#pragma unroll
+            for (int b = 0; b < NQ; ++b)
+#pragma unroll
+              for (int n = 0; n < NS; ++n) sa[b][n] = sb[b][n];
+            break;
+          }
+          step(sb, sa);
+          ++t;
+          if (over()) {
+            again = true;
+            break;
+          }
+          rescore(sa);
+        }
+#pragma unroll
+        for (int b = 0; b < NQ; ++b)
+#pragma unroll
+          for (int c = 0; c < ND; ++c) settle(acc[b][c]);
+        if (again) {
+          raise();
+          rescore(sa);
+        }
       }
-      if (my_rows) {
+      load_all(t + 1, false, true);
+      weights(sa, p);
+      values(t, sa, p);
+      ++t;
+      arrived();
+      __syncthreads();
+    }
+  }
+  // Tiles that are masked for some rows, or all of them.
+  if (t < t1) {
+    if (t == t0) {
+      load_all(t, true, true);
+      arrived();
+      __syncthreads();
+    }
+    for (; t < t1; ++t) {
+      if (t + 1 < t1) load_all(t + 1, true, true);
+      if (t * KT < my_max) {
         f32x16 s[NQ][NS];
         u32x4 p[NQ][NP];
         scores(t, s);
         mask(t, s);
-        raise(s);
+        find_top(s);
+        if (over()) raise();
+        rescore(s);
         weights(s, p);
         values(t, s, p);
       }
-      if (more) {
-        k_next.store(s_k[(t + 1) & 1], tid);
-        store_v(t + 1);
-      }
+      arrived();
       __syncthreads();
     }
   }
@@ -412,6 +541,11 @@ struct Plan {
 Plan plan_attn(const da_prompt& p) {
   Plan plan{1, 1, 0, 0};
   const int64_t G = p.h_q / p.h_kv;
+  plan.items = most_tiles(p.row_start, p.B, p.T, p.rows, G, 256);
+  if (p.dtype != DA_F32 && p.d <= 128 && plan.items * p.h_kv >= kCus) {
+    plan.NQ = 2;
+    return plan;
+  }
   plan.items = most_tiles(p.row_start, p.B, p.T, p.rows, G, 128);
   const int64_t groups = plan.items * p.h_kv;
   if (groups < kCus) {
@@ -423,20 +557,28 @@ Plan plan_attn(const da_prompt& p) {
   return plan;
 }
 
-template <class T, int D>
-void launch_attn(const Plan& plan, const Batch& bt, const AttnArgs& a, hipStream_t s) {
+template <class T, int D, int NQ>
+void launch_rows(const Plan& plan, const Batch& bt, const AttnArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)(plan.items * bt.h_kv * plan.splits)), block(kThreads);
   if (a.lse && !is_f32<T>)
-    hipLaunchKernelGGL((prompt_attn_kernel<T, D, 1, !is_f32<T>>), grid, block, 0, s, bt, a);
+    hipLaunchKernelGGL((prompt_attn_kernel<T, D, NQ, !is_f32<T>>), grid, block, 0, s, bt, a);
   else
-    hipLaunchKernelGGL((prompt_attn_kernel<T, D, 1, false>), grid, block, 0, s, bt, a);
+    hipLaunchKernelGGL((prompt_attn_kernel<T, D, NQ, false>), grid, block, 0, s, bt, a);
+}
+
+template <class T, int D>
+void launch_attn(const Plan& plan, const Batch& bt, const AttnArgs& a, hipStream_t s) {
+  if constexpr (!is_f32<T> && D <= 128) {
+    if (plan.NQ == 2) return launch_rows<T, D, 2>(plan, bt, a, s);
+  }
+  launch_rows<T, D, 1>(plan, bt, a, s);
   if (plan.splits > 1) {
     const int R = 128;
     const int rows = (int)std::min<int64_t>((int64_t)bt.T * bt.G, R);
     hipLaunchKernelGGL((prompt_merge_kernel<T, D>),
                        dim3((unsigned)(plan.items * bt.h_kv),
                             (unsigned)ceil_div(rows, kThreads / (D / 4))),
-                       block, 0, s, bt, a, R);
+                       dim3(kThreads), 0, s, bt, a, R);
   }
 }
 

@@ -332,6 +332,39 @@ struct Stage {
   }
 };
 
+// Whether a value is not finite, of many: the largest magnitude, as bits.
+template <class T>
+struct Finite {
+  uint32_t top = 0;
+  __device__ __forceinline__ void take(u32x4 x) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if constexpr (is_f32<T>)
+        top = max(top, x[w] & 0x7fffffffu);
+      else
+        top = __builtin_bit_cast(
+            uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top),
+                                                __builtin_bit_cast(u16x2, x[w] & 0x7fff7fffu)));
+    }
+  }
+  __device__ __forceinline__ bool all() const {
+    if constexpr (is_f32<T>) return top < 0x7f800000u;
+    constexpr uint32_t inf = std::is_same<T, __bf16>::value ? 0x7f80u : 0x7c00u;
+    return (top >> 16) < inf && (top & 0xffffu) < inf;
+  }
+};
+
+// Whether all of a tile in LDS is finite (a wave looks at the whole of it).
+template <class T, int D, int ROWS>
+__device__ __forceinline__ bool tile_finite(const char* tile, int lane) {
+  Finite<T> f;
+#pragma unroll 4
+  for (int x = lane; x < ROWS * Tile<T, D>::chunks; x += 64)
+    f.take(*reinterpret_cast<const u32x4*>(tile + 16 * x));
+  return !__any(!f.all());
+}
+
 // The same without registers: each wave instruction brings 64 units of 16 bytes to
 // 1 KB of LDS in turn, so a lane fetches the chunk that belongs at its place.  The
 // data is there after the next barrier.
