@@ -115,24 +115,35 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   const RowReader<T, D> k_read(ordered_row(i), k);
   const ColumnReader<T, D> v_read(lane);
 
-  // (Keys beyond the last are the last one again; no row sees them.)
-  auto load_k = [&](int t, int u) {
-    const int key = min(t * KT + Fetch::row(tid, u), keys.n - 1);
-    Fetch::fetch(s_k[t & 1], tid, u, k_base + key * a.k_stride + 16 * Fetch::chunk(tid, u));
+  // Keys beyond the last are zeros, which no row sees.
+  int k_byte[Fetch::phases], v_byte[Fetch::phases];
+#pragma unroll
+  for (int u = 0; u < Fetch::phases; ++u) {
+    k_byte[u] = Fetch::row(tid, u) * (int)a.k_stride + Fetch::byte(tid, u);
+    v_byte[u] = Fetch::row(tid, u) * (int)a.v_stride + Fetch::byte(tid, u);
+  }
+  auto window_of = [&](const char* base, int64_t stride, int t) INLINE {
+    return window(base + (int64_t)t * KT * stride, ((int64_t)keys.n - (int64_t)t * KT) * stride);
   };
-  auto load_v = [&](int t, int u) {
-    const int key = min(t * KT + Fetch::row(tid, u), keys.n - 1);
-    Fetch::fetch(s_v[t & 1], tid, u, v_base + key * a.v_stride + 16 * Fetch::chunk(tid, u));
+  auto load_k = [&](const Window& from, int t, int u) INLINE {
+    fetch(Fetch::place(s_k[t & 1], wave, u), from, k_byte[u % Fetch::phases],
+          u / Fetch::phases * (Fetch::phases * Fetch::step) * (int)a.k_stride);
   };
-  auto load_all = [&](int t, bool want_k, bool want_v) {
+  auto load_v = [&](const Window& from, int t, int u) INLINE {
+    fetch(Fetch::place(s_v[t & 1], wave, u), from, v_byte[u % Fetch::phases],
+          u / Fetch::phases * (Fetch::phases * Fetch::step) * (int)a.v_stride);
+  };
+  auto load_all = [&](int t, bool want_k, bool want_v) INLINE {
+    const Window from_k = window_of(k_base, a.k_stride, t);
+    const Window from_v = window_of(v_base, a.v_stride, t);
 #pragma unroll
     for (int u = 0; u < Fetch::units; ++u) {
-      if (want_k) load_k(t, u);
-      if (want_v) load_v(t, u);
+      if (want_k) load_k(from_k, t, u);
+      if (want_v) load_v(from_v, t, u);
     }
   };
 
-  auto scores = [&](int t, f32x16 (&s)[NQ][NS]) {
+  auto scores = [&](int t, f32x16 (&s)[NQ][NS]) INLINE {
     const char* tile = s_k[t & 1];
 #pragma unroll
     for (int b = 0; b < NQ; ++b)
@@ -149,7 +160,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
         for (int b = 0; b < NQ; ++b) s[b][n] = mma<T>(x, q[b][w], s[b][n]);
       }
   };
-  auto mask = [&](int t, f32x16 (&s)[NQ][NS]) {
+  auto mask = [&](int t, f32x16 (&s)[NQ][NS]) INLINE {
     if ((t + 1) * KT <= my_min) return;
 #pragma unroll
     for (int b = 0; b < NQ; ++b) {
@@ -161,7 +172,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
           if (32 * n + row_of(r, 0) >= left) s[b][n][r] = -INFINITY;
     }
   };
-  auto find_top = [&](const f32x16 (&s)[NQ][NS]) {
+  auto find_top = [&](const f32x16 (&s)[NQ][NS]) INLINE {
 #pragma unroll
     for (int b = 0; b < NQ; ++b) {
       top[b] = s[b][0][0];
@@ -173,7 +184,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   };
   // The reference is raised when a score lies 8 above it: weights stay below
   // 2^8, and most tiles rescale nothing.
-  auto over = [&]() {
+  auto over = [&]() INLINE {
     bool x = false;
 #pragma unroll
     for (int b = 0; b < NQ; ++b) {
@@ -182,7 +193,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
     }
     return __any(x);
   };
-  auto raise = [&]() {
+  auto raise = [&]() INLINE {
     bool far = false;
 #pragma unroll
     for (int b = 0; b < NQ; ++b) {
@@ -200,7 +211,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
     }
     if (__any(far)) by = 1.f;
   };
-  auto rescore = [&](f32x16 (&s)[NQ][NS]) {
+  auto rescore = [&](f32x16 (&s)[NQ][NS]) INLINE {
     if (__builtin_expect(by != a.scale, 0)) {
 #pragma unroll
       for (int b = 0; b < NQ; ++b)
@@ -209,7 +220,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
     }
   };
   // Components 8h .. 8h+7 of a block become weights; 16-bit ones are rounded into p.
-  auto weigh = [&](int b, int h, f32x16& s, u32x4& p) {
+  auto weigh = [&](int b, int h, f32x16& s, u32x4& p) INLINE {
 #pragma unroll
     for (int r = 8 * h; r < 8 * h + 8; ++r)
       s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], by, -ref[b]));
@@ -225,7 +236,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
       }
     }
   };
-  auto weights = [&](f32x16 (&s)[NQ][NS], u32x4 (&p)[NQ][NP]) {
+  auto weights = [&](f32x16 (&s)[NQ][NS], u32x4 (&p)[NQ][NP]) INLINE {
 #pragma unroll
     for (int b = 0; b < NQ; ++b)
 #pragma unroll
@@ -233,7 +244,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) weigh(b, h, s[b][n], p[b][is_f32<T> ? 0 : 2 * n + h]);
   };
-  auto values = [&](int t, f32x16 (&s)[NQ][NS], u32x4 (&p)[NQ][NP]) {
+  auto values = [&](int t, f32x16 (&s)[NQ][NS], u32x4 (&p)[NQ][NP]) INLINE {
     const char* tile = s_v[t & 1];
     // Where some rows see keys of a tile that others do not, values that are not
     // finite must not meet the others' weights of 0.
@@ -310,7 +321,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
       if (over()) raise();
       rescore(sa);
       __syncthreads();
-      auto step = [&](f32x16 (&s)[NQ][NS], f32x16 (&next)[NQ][NS]) {
+      auto step = [&](f32x16 (&s)[NQ][NS], f32x16 (&next)[NQ][NS]) INLINE {
         const char *tile_k = s_k[(t + 1) & 1], *tile_v = s_v[t & 1];
 #pragma unroll
         for (int b = 0; b < NQ; ++b)
@@ -318,6 +329,8 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
           for (int n = 0; n < NS; ++n)
 #pragma unroll
             for (int r = 0; r < 16; ++r) next[b][n][r] = 0.f;
+        const Window from_k = window_of(k_base, a.k_stride, t + 2);
+        const Window from_v = window_of(v_base, a.v_stride, t + 1);
         u32x4 x[NS];
 #pragma unroll
         for (int n = 0; n < NS; ++n) x[n] = k_read.get(tile_k, n, 0);
@@ -337,8 +350,8 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
             const int b = e / NP, n = e % NP / 2, h = e % 2;
             weigh(b, h, s[b][n], p[b][2 * n + h]);
           }
-          if (w < Fetch::units) load_k(t + 2, w);
-          else if (w < 2 * Fetch::units) load_v(t + 1, w - Fetch::units);
+          if (w < Fetch::units) load_k(from_k, t + 2, w);
+          else if (w < 2 * Fetch::units) load_v(from_v, t + 1, w - Fetch::units);
 #pragma unroll
           for (int n = 0; n < NS; ++n) x[n] = y[n];
           __builtin_amdgcn_sched_barrier(0);
@@ -364,44 +377,41 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
         arrived();
         __syncthreads();
       };
-      bool again = true;
-      while (again) {
-        again = false;
-        while (t + 1 < whole_tiles) {
-          step(sa, sb);
-          ++t;
-          if (over()) {
-            again = true;
-#pragma unroll
-            for (int b = 0; b < NQ; ++b)
-#pragma unroll
-              for (int n = 0; n < NS; ++n) sa[b][n] = sb[b][n];
-            break;
-          }
-          rescore(sb);
-          if (t + 1 >= whole_tiles) {
-#pragma unroll
-            for (int b = 0; b < NQ; ++b)
-#pragma unroll
-              for (int n = 0; n < NS; ++n) sa[b][n] = sb[b][n];
-            break;
-          }
-          step(sb, sa);
-          ++t;
-          if (over()) {
-            again = true;
-            break;
-          }
-          rescore(sa);
-        }
+      auto settle_all = [&]() INLINE {
 #pragma unroll
         for (int b = 0; b < NQ; ++b)
 #pragma unroll
           for (int c = 0; c < ND; ++c) settle(acc[b][c]);
-        if (again) {
-          raise();
+      };
+      // (The sums are in accumulation registers within the inner loop: what changes
+      // them otherwise stands outside.  Which scores are next is hidden from the
+      // compiler, so that it copies them outside too.)
+      bool again = true;
+      while (again) {
+        again = false;
+        int second = 0;
+        while (t + 1 < whole_tiles) {
+          step(sa, sb);
+          ++t, second = 1;
+          again = over();
+          if (again || t + 1 >= whole_tiles) break;
+          rescore(sb);
+          step(sb, sa);
+          ++t, second = 0;
+          again = over();
+          if (again) break;
           rescore(sa);
         }
+        settle_all();
+        asm volatile("" : "+s"(second));
+        if (second) {
+#pragma unroll
+          for (int b = 0; b < NQ; ++b)
+#pragma unroll
+            for (int n = 0; n < NS; ++n) sa[b][n] = sb[b][n];
+        }
+        if (again) raise();
+        if (again || second) rescore(sa);
       }
       load_all(t + 1, false, true);
       weights(sa, p);
@@ -445,7 +455,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
     const bool none = limit[b] == -INFINITY && total == 0.f;
     if (a.splits == 1) {
       const float inverse = 1.f / total;
-      auto mean = [&](float x) { return none ? 0.f : x * inverse; };
+      auto mean = [&](float x) INLINE { return none ? 0.f : x * inverse; };
       char* dst = a.out + place[b] * L::row_bytes;
 #pragma unroll
       for (int c = 0; c < ND; ++c)
@@ -496,7 +506,7 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(Batch bt, AttnAr
   if (x >= in_tile) return;
   const int t = token_of(bt, row0 + x), g = row0 + x - t * bt.G;
   const int64_t place = (int64_t)(rows.start + t) * bt.h_q + head * bt.G + g;
-  auto part = [&](int s) {
+  auto part = [&](int s) INLINE {
     return ((int64_t)(item * a.splits + s) * bt.h_kv + head) * R + x;
   };
   float ref = -INFINITY;
@@ -597,8 +607,8 @@ da_status da_prompt_attn(const da_prompt* prompt, const void* q, int64_t q_strid
   if (!prompt || !q || !k || !v || !out) return DA_ERR_NULL;
   const da_prompt& p = *prompt;
   const da_status st = check_sizes(p);
-  if (st == DA_ERR_SHAPE || !stride_fits(q_stride, p.h_q, p.d) ||
-      !stride_fits(k_stride, p.h_kv, p.d) || !stride_fits(v_stride, p.h_kv, p.d))
+  if (st == DA_ERR_SHAPE || !stride_fits(q_stride, p.h_q, p.d, p.dtype) ||
+      !stride_fits(k_stride, p.h_kv, p.d, p.dtype) || !stride_fits(v_stride, p.h_kv, p.d, p.dtype))
     return DA_ERR_SHAPE;
   if (st != DA_OK) return st;
   const Plan plan = plan_attn(p);

@@ -19,6 +19,9 @@
 
 #include "decode_attn.h"
 
+// (Of parts of a kernel that hold its sums: called, they would have them in memory.)
+#define INLINE __attribute__((always_inline))
+
 namespace prompt {
 
 constexpr int kThreads = 256;
@@ -366,34 +369,50 @@ __device__ __forceinline__ bool tile_finite(const char* tile, int lane) {
 }
 
 // The same without registers: each wave instruction brings 64 units of 16 bytes to
-// 1 KB of LDS in turn, so a lane fetches the chunk that belongs at its place.  The
-// data is there after the next barrier.
+// 1 KB of LDS in turn, so a lane fetches the chunk that belongs at its place.  A
+// thread's units are `step` rows apart; the turn repeats every 16 rows, so unit u has
+// the chunk of unit u % phases.
 template <class T, int D, int ROWS>
 struct Direct {
   using L = Tile<T, D>;
   static constexpr int units = ROWS * L::chunks / kThreads;
   static_assert(units >= 1 && ROWS * L::chunks % kThreads == 0, "whole units");
   static constexpr int step = kThreads / L::chunks;
+  static constexpr int phases = step < 16 ? 16 / step : 1;
 
-  // The row and chunk of this thread's unit u, and the unit's fetch from there.
+  // The row and the byte in it of this thread's unit u.
   __device__ static __forceinline__ int row(int tid, int u) { return tid / L::chunks + step * u; }
-  __device__ static __forceinline__ int chunk(int tid, int u) {
-    return (tid % L::chunks) ^ L::turn(row(tid, u));
+  __device__ static __forceinline__ int byte(int tid, int u) {
+    return ((tid % L::chunks) ^ L::turn(row(tid, u))) << 4;
   }
-  // (In assembly: to the compiler a fetch may write what any later read of LDS
-  // reads, so that it would wait for it there.  arrived() stands before the barrier.)
-  __device__ static __forceinline__ void fetch(char* tile, int tid, int u, const char* from) {
-    typedef __attribute__((address_space(3))) char* lds;
-    const int to = uniform((int)(uintptr_t)(lds)tile + u * kThreads * 16 + (tid >> 6 << 10));
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"      // (m0 is the compiler's, between its uses)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-                 :
-                 : "s"(to), "v"(from)
-                 : "m0");
-#pragma clang diagnostic pop
+  // Where a wave's unit u goes: an address in LDS.
+  __device__ static __forceinline__ int place(const char* tile, int wave, int u) {
+    typedef __attribute__((address_space(3))) const char* lds;
+    return uniform((int)(uintptr_t)(lds)tile + u * kThreads * 16 + (wave << 10));
   }
 };
+
+// Memory as the fetches see it: `bytes` from `base` on (at most 2^31 - 1 count), beyond
+// which they bring zeros.
+struct Window {
+  u32x4 words;
+};
+__device__ __forceinline__ Window window(const char* base, int64_t bytes) {
+  const uint64_t at = reinterpret_cast<uint64_t>(base);
+  return {u32x4{(uint32_t)at, (uint32_t)(at >> 32),
+                (uint32_t)min(max(bytes, (int64_t)0), (int64_t)0x7fffffff), 0x00027000u}};
+}
+// (In assembly: to the compiler a fetch may write what any later read of LDS
+// reads, so that it would wait for it there.  arrived() stands before the barrier.)
+__device__ __forceinline__ void fetch(int place, const Window& from, int lane_byte, int byte) {
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"      // (m0 is the compiler's, between its uses)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               :
+               : "s"(place), "v"(lane_byte), "s"(from.words), "s"(byte)
+               : "m0");
+#pragma clang diagnostic pop
+}
 __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // A word (or several) of memory: not through the instructions that may be LDS too.
@@ -438,8 +457,12 @@ inline bool starts_aligned(const da_prompt& p) {
   return aligned(p.row_start, 4) && aligned(p.key_start, 4);
 }
 
-// A token stride (elements) that rows of `heads` heads may have.
-inline bool stride_fits(int64_t stride, int heads, int d) { return stride >= (int64_t)heads * d; }
+// A token stride (elements) that rows of `heads` heads may have: the kernels take
+// offsets within 64 tokens in 32 bits.
+constexpr int64_t kMaxStrideBytes = int64_t(1) << 24;
+inline bool stride_fits(int64_t stride, int heads, int d, int dtype) {
+  return stride >= (int64_t)heads * d && stride <= kMaxStrideBytes / type_bytes(dtype);
+}
 inline bool stride_aligned(int64_t stride, int dtype) {
   return stride % (16 / type_bytes(dtype)) == 0;
 }

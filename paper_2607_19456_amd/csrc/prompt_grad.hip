@@ -188,11 +188,11 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
   const RowReader<T, D> read(ordered_row(i), k);
   const ColumnReader<T, D> read_columns(lane);
 
-  auto load = [&](int t) {
+  auto load = [&](int t) INLINE {
     k_next.load(k_base, a.k_stride, t * KT, keys.n, tid);
     v_next.load(v_base, a.v_stride, t * KT, keys.n, tid);
   };
-  auto store = [&](int t) {
+  auto store = [&](int t) INLINE {
     k_next.store(s_k[t & 1], tid);
     v_next.store(s_v[t & 1], tid);
     if ((t + 1) * KT > min_seen) {
@@ -312,7 +312,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
   const int end = rows.n * bt.G;
   const int key0 = at.tile * F::keys;
   // the first row (token and head) that sees a key
-  auto first_row = [&](int key) {
+  auto first_row = [&](int key) INLINE {
     return bt.causal ? (int)min((int64_t)max(key - keys.n + rows.n, 0) * bt.G, (int64_t)end) : 0;
   };
   const int all_from = first_row(min(key0 + F::keys, keys.n) - 1);   // rows that see all of the keys
@@ -346,35 +346,41 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
 
   // Rows beyond the last are the last one again (their weights are taken as 0).
   using Fetch = Direct<T, D, RT>;
-  auto load_unit = [&](int t, int u) {
-    const bool is_q = u < Fetch::units;
-    const int v = is_q ? u : u - Fetch::units;
-    const int x = min(t * RT + Fetch::row(tid, v), end - 1), tok = token_of(bt, x);
-    const int64_t token = rows.start + tok;
-    const int in = (head * bt.G + x - tok * bt.G) * L::row_bytes + 16 * Fetch::chunk(tid, v);
-    if (is_q)
-      Fetch::fetch(s_rows[t & 1], tid, v, a.q + token * a.q_stride + in);
-    else
-      Fetch::fetch(s_rows[2 + (t & 1)], tid, v, a.d_out + token * a.d_out_stride + in);
+  auto window_of = [&](const char* base, int64_t stride, int t) INLINE {
+    const int64_t tok = token_of(bt, min(t * RT, end - 1));
+    return window(base + (rows.start + tok) * stride + (int64_t)head * bt.G * L::row_bytes,
+                  (rows.n - tok) * stride);
+  };
+  auto load_rows = [&](int t) INLINE {
+    const Window from_q = window_of(a.q, a.q_stride, t);
+    const Window from_g = window_of(a.d_out, a.d_out_stride, t);
+    const int tok0 = token_of(bt, min(t * RT, end - 1));
+#pragma unroll
+    for (int u = 0; u < Fetch::units; ++u) {
+      const int x = min(t * RT + Fetch::row(tid, u), end - 1), tok = token_of(bt, x);
+      const int in = (x - tok * bt.G) * L::row_bytes + Fetch::byte(tid, u);
+      fetch(Fetch::place(s_rows[t & 1], wave, u), from_q, (tok - tok0) * (int)a.q_stride + in, 0);
+      fetch(Fetch::place(s_rows[2 + (t & 1)], wave, u), from_g,
+            (tok - tok0) * (int)a.d_out_stride + in, 0);
+    }
   };
   f32x2 stat{INFINITY, 0.f};
-  auto load_stats = [&](int t) {
+  auto load_stats = [&](int t) INLINE {
     if (tid < RT) {
       const int x = min(t * RT + tid, end - 1), tok = token_of(bt, x);
       stat = far_load<f32x2>(a.stats + (int64_t)(rows.start + tok) * bt.h_q + head * bt.G + x -
                              tok * bt.G);
     }
   };
-  auto store_stats = [&](int t) {
+  auto store_stats = [&](int t) INLINE {
     if (tid < RT) s_lse[t & 1][tid] = stat[0], s_delta[t & 1][tid] = stat[1];
   };
   // Not all rows of a step see all keys, and what they do not see is masked.
-  auto partial = [&](int t) { return t * RT < all_from || (t + 1) * RT > end; };
+  auto partial = [&](int t) INLINE { return t * RT < all_from || (t + 1) * RT > end; };
   bool skipped = false;
 
   if (r0 < r1) {
-#pragma unroll
-    for (int u = 0; u < 2 * Fetch::units; ++u) load_unit(r0, u);
+    load_rows(r0);
     load_stats(r0);
     store_stats(r0);
     arrived();
@@ -407,7 +413,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
           const u32x4 y = read.get(w + 1 < NW ? tile_q : tile_g, 0, w + 1 < NW ? w + 1 : 0);
 #pragma unroll
           for (int n = 0; n < NK; ++n) s[n] = mma<T>(x, kk[n][w], s[n]);
-          if (w < 2 * Fetch::units) load_unit(next, w);
+          if (w == 0) load_rows(next);
           x = y;
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -543,13 +549,13 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
 
   // The rows that were left out, pair by pair, those alone that see the key: what they
   // add to block c of key n's dK or dV.
-  auto left_out = [&](int n, int c, bool is_dk, f32x16 x) {
+  auto left_out = [&](int n, int c, bool is_dk, f32x16 x) INLINE {
     const int64_t token = keys.start + min(key[n], keys.n - 1);
     const T* k_row = reinterpret_cast<const T*>(a.k + token * a.k_stride) + head * D;
     const T* v_row = reinterpret_cast<const T*>(a.v + token * a.v_stride) + head * D;
     const T *q, *g;
     f32x2 st;
-    auto at_row = [&](int row) {
+    auto at_row = [&](int row) INLINE {
       const int tok = token_of(bt, row), h = head * bt.G + row - tok * bt.G;
       const int64_t to = rows.start + tok;
       q = reinterpret_cast<const T*>(a.q + to * a.q_stride) + h * D;
@@ -586,16 +592,16 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
     return x;
   };
   // The row waves' sums: the others' to LDS, added by the first, which stores.
-  auto finish = [&](f32x16 (&acc)[NK][ND], bool is_dk) {
+  auto finish = [&](f32x16 (&acc)[NK][ND], bool is_dk) INLINE {
     static_assert(WR == 1 || (WR == 2 && WK * 4096 * ND * NK <= 4 * kTile), "fits the rows' place");
     const float by = is_dk ? a.scale : 1.f;
-    auto block = [&](int n, int c) {
+    auto block = [&](int n, int c) INLINE {
       settle(acc[n][c]);
       f32x16 x = acc[n][c];
       if (__builtin_expect(skipped, 0)) x = left_out(n, ND * wd + c, is_dk, x);
       return x;
     };
-    auto shared = [&](int n, int c) {
+    auto shared = [&](int n, int c) INLINE {
       return reinterpret_cast<f32x4*>(s_rows[0]) + ((wk * NK + n) * ND + c) * 256 + lane;
     };
     if (wr == 1) {
@@ -683,9 +689,9 @@ da_status da_prompt_attn_grad(const da_prompt* prompt, const void* q, int64_t q_
   const int64_t narrow[] = {k_stride, v_stride, dk_stride, dv_stride};
   if (st == DA_ERR_SHAPE) return st;
   for (int64_t x : wide)
-    if (!stride_fits(x, p.h_q, p.d)) return DA_ERR_SHAPE;
+    if (!stride_fits(x, p.h_q, p.d, p.dtype)) return DA_ERR_SHAPE;
   for (int64_t x : narrow)
-    if (!stride_fits(x, p.h_kv, p.d)) return DA_ERR_SHAPE;
+    if (!stride_fits(x, p.h_kv, p.d, p.dtype)) return DA_ERR_SHAPE;
   if (st != DA_OK) return st;
   const Plan plan = plan_grad(p);
   if (plan.row_items * p.h_kv > kMaxGroups || plan.key_items * p.h_kv > kMaxGroups)
