@@ -53,8 +53,9 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   constexpr int NP = is_f32<T> ? 1 : 2 * NS;
   using Fetch = Direct<T, D, KT>;
 
-  __shared__ __align__(16) char s_k[2][kTile];
-  __shared__ __align__(16) char s_v[2][kTile];
+  constexpr int NB = NQ == 2 ? 3 : 2;        // tiles in LDS
+  __shared__ __align__(16) char s_k[NB][kTile];
+  __shared__ __align__(16) char s_v[NB][kTile];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int i = lane & 31, k = lane >> 5;
@@ -126,11 +127,11 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
     return window(base + (int64_t)t * KT * stride, ((int64_t)keys.n - (int64_t)t * KT) * stride);
   };
   auto load_k = [&](const Window& from, int t, int u) INLINE {
-    fetch(Fetch::place(s_k[t & 1], wave, u), from, k_byte[u % Fetch::phases],
+    fetch(Fetch::place(s_k[t % NB], wave, u), from, k_byte[u % Fetch::phases],
           u / Fetch::phases * (Fetch::phases * Fetch::step) * (int)a.k_stride);
   };
   auto load_v = [&](const Window& from, int t, int u) INLINE {
-    fetch(Fetch::place(s_v[t & 1], wave, u), from, v_byte[u % Fetch::phases],
+    fetch(Fetch::place(s_v[t % NB], wave, u), from, v_byte[u % Fetch::phases],
           u / Fetch::phases * (Fetch::phases * Fetch::step) * (int)a.v_stride);
   };
   auto load_all = [&](int t, bool want_k, bool want_v) INLINE {
@@ -144,7 +145,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   };
 
   auto scores = [&](int t, f32x16 (&s)[NQ][NS]) INLINE {
-    const char* tile = s_k[t & 1];
+    const char* tile = s_k[t % NB];
 #pragma unroll
     for (int b = 0; b < NQ; ++b)
 #pragma unroll
@@ -245,7 +246,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
         for (int h = 0; h < 2; ++h) weigh(b, h, s[b][n], p[b][is_f32<T> ? 0 : 2 * n + h]);
   };
   auto values = [&](int t, f32x16 (&s)[NQ][NS], u32x4 (&p)[NQ][NP]) INLINE {
-    const char* tile = s_v[t & 1];
+    const char* tile = s_v[t % NB];
     // Where some rows see keys of a tile that others do not, values that are not
     // finite must not meet the others' weights of 0.
     if ((t + 1) * KT > my_min && __builtin_expect(!tile_finite<T, D, KT>(tile, lane), 0)) {
@@ -311,7 +312,8 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
     const int whole_tiles = min(min_seen / KT, t1);
     if (t0 < whole_tiles) {
       load_all(t0, true, true);
-      load_all(t0 + 1, true, false);
+      load_all(t0 + 1, true, true);
+      load_all(t0 + 2, true, false);
       arrived();
       __syncthreads();
       f32x16 sa[NQ][NS], sb[NQ][NS];
@@ -322,16 +324,16 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
       rescore(sa);
       __syncthreads();
       auto step = [&](f32x16 (&s)[NQ][NS], f32x16 (&next)[NQ][NS]) INLINE {
-        const char *tile_k = s_k[(t + 1) & 1], *tile_v = s_v[t & 1];
+        const char *tile_k = s_k[(t + 1) % NB], *tile_v = s_v[t % NB];
 #pragma unroll
         for (int b = 0; b < NQ; ++b)
 #pragma unroll
           for (int n = 0; n < NS; ++n)
 #pragma unroll
             for (int r = 0; r < 16; ++r) next[b][n][r] = 0.f;
-        const Window from_k = window_of(k_base, a.k_stride, t + 2);
-        const Window from_v = window_of(v_base, a.v_stride, t + 1);
-        u32x4 x[NS];
+        const Window from_k = window_of(k_base, a.k_stride, t + 3);
+        const Window from_v = window_of(v_base, a.v_stride, t + 2);
+        u32x4 v0, v1, x[NS];
 #pragma unroll
         for (int n = 0; n < NS; ++n) x[n] = k_read.get(tile_k, n, 0);
         constexpr int kPieces = NQ * NP / NW;           // of 8 weights, a step of the product
@@ -341,22 +343,23 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
           u32x4 y[NS];
 #pragma unroll
           for (int n = 0; n < NS; ++n) y[n] = w + 1 < NW ? k_read.get(tile_k, n, w + 1) : x[n];
-#pragma unroll
-          for (int n = 0; n < NS; ++n)
-#pragma unroll
-            for (int b = 0; b < NQ; ++b) next[b][n] = mma<T>(x[n], q[b][w], next[b][n]);
+          if (w + 1 == NW) v0 = v_read.get(tile_v, 0, 0), v1 = v_read.get(tile_v, 0, 1);
+          if (w == 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int e = w * kPieces; e < (w + 1) * kPieces; ++e) {
             const int b = e / NP, n = e % NP / 2, h = e % 2;
             weigh(b, h, s[b][n], p[b][2 * n + h]);
           }
-          if (w < Fetch::units) load_k(from_k, t + 2, w);
-          else if (w < 2 * Fetch::units) load_v(from_v, t + 1, w - Fetch::units);
+#pragma unroll
+          for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int b = 0; b < NQ; ++b) next[b][n] = mma<T>(x[n], q[b][w], next[b][n]);
+          if (w < Fetch::units) load_k(from_k, t + 3, w);
+          else if (w < 2 * Fetch::units) load_v(from_v, t + 2, w - Fetch::units);
 #pragma unroll
           for (int n = 0; n < NS; ++n) x[n] = y[n];
           __builtin_amdgcn_sched_barrier(0);
         }
-        u32x4 v0 = v_read.get(tile_v, 0, 0), v1 = v_read.get(tile_v, 0, 1);
 #pragma unroll
         for (int b = 0; b < NQ; ++b) top[b] = next[b][0][0];
 #pragma unroll
@@ -374,7 +377,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
           v0 = v1, v1 = v2;
           __builtin_amdgcn_sched_barrier(0);
         }
-        arrived();
+        arrived<2 * Fetch::units>();                    // but those of this step
         __syncthreads();
       };
       auto settle_all = [&]() INLINE {
@@ -413,7 +416,6 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
         if (again) raise();
         if (again || second) rescore(sa);
       }
-      load_all(t + 1, false, true);
       weights(sa, p);
       values(t, sa, p);
       ++t;

@@ -413,7 +413,11 @@ __device__ __forceinline__ void fetch(int place, const Window& from, int lane_by
                : "m0");
 #pragma clang diagnostic pop
 }
-__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// All fetches but the last `more` have arrived.
+template <int more = 0>
+__device__ __forceinline__ void arrived() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(more) : "memory");
+}
 
 // A word (or several) of memory: not through the instructions that may be LDS too.
 template <class V, class P>
