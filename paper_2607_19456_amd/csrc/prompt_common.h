@@ -184,16 +184,6 @@ __device__ __forceinline__ float add2(uint32_t w, float x) {
                                   x, false);
 }
 
-template <class T>
-__device__ __forceinline__ bool not_finite(uint32_t w) {
-  if constexpr (is_f32<T>)
-    return (w & 0x7f800000u) == 0x7f800000u;
-  else if constexpr (std::is_same<T, __bf16>::value)
-    return (w & 0x7f800000u) == 0x7f800000u || (w & 0x7f80u) == 0x7f80u;
-  else
-    return (w & 0x7c000000u) == 0x7c000000u || (w & 0x7c00u) == 0x7c00u;
-}
-
 // ---------------------------------------------------------------------------
 // A tile in LDS: rows of D values, row-major, in chunks of 16 bytes that stand
 // at their index XOR turn(row).  The turn takes all values that it can over 16
@@ -288,53 +278,9 @@ struct ColumnReader<float, D> {
   }
 };
 
-// acc[c] += X^T p over the 16 rows h of a tile, p being eight of a lane's
-// weights of those rows (components 8*(h%2) .. +7 of a block).
-template <class T, int D>
-__device__ __forceinline__ f32x16 mma_columns(const ColumnReader<T, D>& rd, const char* tile,
-                                              int h, int c, u32x4 p, f32x16 acc) {
-  return mma<T>(rd.get(tile, h, c), p, acc);
-}
-
 // ---------------------------------------------------------------------------
-// Tiles on their way from memory to LDS, through registers: 16 bytes a unit.
+// Tiles on their way from memory to LDS.
 // ---------------------------------------------------------------------------
-template <class T, int D, int ROWS, int THREADS = kThreads>
-struct Stage {
-  using L = Tile<T, D>;
-  static constexpr int units = ROWS * L::chunks / THREADS;
-  static_assert(units >= 1 && ROWS * L::chunks % THREADS == 0, "whole units");
-  static constexpr int step = THREADS / L::chunks;      // rows between a thread's units
-  u32x4 x[units];
-
-  // Rows row0 .. row0 + ROWS - 1 of `base` (a row's own place, stride between
-  // rows in bytes); rows from `n` on are zeros.
-  __device__ __forceinline__ void load(const char* base, int64_t stride, int row0, int n, int tid) {
-    const int r = tid / L::chunks, c = tid % L::chunks;
-#pragma unroll
-    for (int u = 0; u < units; ++u) {
-      const int row = row0 + r + step * u;
-      const char* p = base + (int64_t)(row < n ? row : 0) * stride + 16 * c;
-      x[u] = *reinterpret_cast<const u32x4*>(p);
-      if (row >= n) x[u] = u32x4{0u, 0u, 0u, 0u};
-    }
-  }
-  __device__ __forceinline__ void store(char* tile, int tid) const {
-    const int r = tid / L::chunks, c = tid % L::chunks;
-#pragma unroll
-    for (int u = 0; u < units; ++u)
-      *reinterpret_cast<u32x4*>(tile + L::at(r + step * u, c)) = x[u];
-  }
-  __device__ __forceinline__ bool spoilt() const {
-    bool bad = false;
-#pragma unroll
-    for (int u = 0; u < units; ++u)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) bad |= not_finite<T>(x[u][w]);
-    return bad;
-  }
-};
-
 // Whether a value is not finite, of many: the largest magnitude, as bits.
 template <class T>
 struct Finite {
@@ -368,7 +314,7 @@ __device__ __forceinline__ bool tile_finite(const char* tile, int lane) {
   return !__any(!f.all());
 }
 
-// The same without registers: each wave instruction brings 64 units of 16 bytes to
+// Without registers on the way: each wave instruction brings 64 units of 16 bytes to
 // 1 KB of LDS in turn, so a lane fetches the chunk that belongs at its place.  A
 // thread's units are `step` rows apart; the turn repeats every 16 rows, so unit u has
 // the chunk of unit u % phases.

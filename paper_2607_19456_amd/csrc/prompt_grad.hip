@@ -29,73 +29,6 @@ struct GradArgs {
   f32x2* stats;                 // [rows][h_q]: lse times log2(e) (+infinity: no weights), delta
 };
 
-// Element (row, d) of a tile in LDS.
-template <class T, int D>
-__device__ __forceinline__ float element(const char* tile, int row, int d) {
-  const int byte = d * (int)sizeof(T);
-  return (float)*reinterpret_cast<const T*>(tile + Tile<T, D>::at(row, byte / 16) + byte % 16);
-}
-
-// acc += X^T w where only the pairs that `sees` allows are multiplied: what the
-// others would multiply by 0 may be an infinity or a NaN.  w holds this lane's
-// half of the rows of a block of 32 of X.
-template <class T, int D, int ND, class F>
-__device__ __forceinline__ void add_seen(const char* tile, int row0, int d0, f32x16 w, int k,
-                                         f32x16 (&acc)[ND], F&& sees) {
-#pragma unroll 1
-  for (int e = 0; e < 16; ++e) {
-    float mine = 0.f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) mine = r == e ? w[r] : mine;
-    if constexpr (!is_f32<T>) mine = (float)(T)mine;
-    const float other = __shfl_xor(mine, 32);
-#pragma unroll 1
-    for (int kk = 0; kk < 2; ++kk) {
-      const int row = row0 + row_of(e, kk);
-      if (!sees(row)) continue;
-      const float x = kk == k ? mine : other;
-#pragma unroll
-      for (int c = 0; c < ND; ++c)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          acc[c][r] += x * element<T, D>(tile, row, d0 + 32 * c + 8 * (r / 4) + 4 * k + r % 4);
-    }
-  }
-}
-
-// acc[c] += X^T w over a block of 32 rows of X, from row 32 n of the tile on,
-// dimensions d0 + 32 c.
-template <class T, int D, int ND, int NB>
-__device__ __forceinline__ void add_columns(const ColumnReader<T, D>& rd, const char* tile, int n,
-                                            int c0, const f32x16 (&w)[NB],
-                                            f32x16 (&acc)[NB][ND]) {
-  if constexpr (is_f32<T>) {
-#pragma unroll
-    for (int c = 0; c < ND; ++c)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float x = rd.get(tile, 2 * n + r / 8, r % 8, c0 + c);
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-          acc[b][c] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w[b][r], acc[b][c], 0, 0, 0);
-      }
-  } else {
-    u32x4 p[NB][2];
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; r += 2) p[b][r / 8][r % 8 / 2] = pack2<T>(w[b][r], w[b][r + 1]);
-#pragma unroll
-    for (int c = 0; c < ND; ++c)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const u32x4 x = rd.get(tile, 2 * n + h, c0 + c);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) acc[b][c] = mma<T>(x, p[b][h], acc[b][c]);
-      }
-  }
-}
-
 // Four dimensions of a row.
 template <class T>
 __device__ __forceinline__ void store4(char* row, int d, f32x4 x) {
@@ -117,18 +50,28 @@ __device__ __forceinline__ float dot16(u32x4 a, u32x4 b, float sum) {
 
 // ---------------------------------------------------------------------------
 // dQ.  As the attention itself: 32 NQ rows of a KV head to a wave, as columns;
-//   S^T = K . Q^T, dP^T = V . dO^T, dQ^T += K^T . dS^T.
+//   S^T = K . Q^T, dP^T = V . dO^T, dQ^T += K^T . dS^T
+// for 32 keys at a time.
 // ---------------------------------------------------------------------------
-template <class T, int D, int NQ>
+template <class T, int D>
+struct RowsForm {
+  static constexpr int NQ = is_f32<T> || D == 256 ? 1 : 2;
+  static constexpr int rows = 32 * NQ * kWaves;
+  static constexpr int keys = is_f32<T> || D == 256 ? 32 : 64;      // of a tile
+  static constexpr int tiles = is_f32<T> && D == 256 ? 2 : 3;       // in LDS
+};
+
+template <class T, int D>
 __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt, GradArgs a) {
   using L = Tile<T, D>;
-  constexpr int KT = 32, R = 32 * NQ * kWaves;
+  using F = RowsForm<T, D>;
+  constexpr int NQ = F::NQ, KT = F::keys, R = F::rows, NB = F::tiles;
   constexpr int ND = L::ND, NW = L::NW;
   constexpr int kTile = KT * L::row_bytes;
+  using Fetch = Direct<T, D, KT>;
 
-  __shared__ __align__(16) char s_k[2][kTile];
-  __shared__ __align__(16) char s_v[2][kTile];
-  __shared__ int s_spoilt[2][kWaves];
+  __shared__ __align__(16) char s_k[NB][kTile];
+  __shared__ __align__(16) char s_v[NB][kTile];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int i = lane & 31, k = lane >> 5;
@@ -145,8 +88,8 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
 
   const int my_row0 = row0 + 32 * NQ * wave;
   const int my_rows = min(max(in_tile - 32 * NQ * wave, 0), 32 * NQ);
-  const int my_min = my_rows ? seen_by(bt, rows.n, keys.n, token_of(bt, my_row0)) : 0;
   int seen[NQ];
+  int64_t place[NQ];                         // row * h_q + head
   int64_t to[NQ];
   float lse2[NQ], delta[NQ];
   u32x4 q[NQ][NW], g[NQ][NW];
@@ -157,21 +100,21 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
     const int t = my_rows ? token_of(bt, x) : 0;
     const int h = head * bt.G + (my_rows ? x - t * bt.G : 0);
     seen[b] = mine ? seen_by(bt, rows.n, keys.n, t) : 0;
-    const int64_t token = rows.start + t, place = token * bt.h_q + h;
+    const int64_t token = rows.start + t;
+    place[b] = token * bt.h_q + h;
     to[b] = token * a.dq_stride + (int64_t)h * L::row_bytes;
     const int64_t in = (int64_t)h * L::row_bytes + 16 * k;
     float sum = 0.f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      q[b][w] = *reinterpret_cast<const u32x4*>(a.q + token * a.q_stride + in + 32 * w);
-      g[b][w] = *reinterpret_cast<const u32x4*>(a.d_out + token * a.d_out_stride + in + 32 * w);
-      const u32x4 o = *reinterpret_cast<const u32x4*>(a.out + place * L::row_bytes + 16 * k + 32 * w);
-      sum = dot16<T>(g[b][w], o, sum);
+      q[b][w] = far_load<u32x4>(a.q + token * a.q_stride + in + 32 * w);
+      g[b][w] = far_load<u32x4>(a.d_out + token * a.d_out_stride + in + 32 * w);
+      sum = dot16<T>(g[b][w], far_load<u32x4>(a.out + place[b] * L::row_bytes + 16 * k + 32 * w), sum);
     }
     delta[b] = sum + __shfl_xor(sum, 32);
-    const float lse = a.lse[place];
+    const float lse = far_load<float>(a.lse + place[b]);
     lse2[b] = lse == -INFINITY ? INFINITY : lse * kLog2e;
-    if (mine && k == 0) a.stats[place] = f32x2{lse2[b], delta[b]};
+    if (mine && k == 0) a.stats[place[b]] = f32x2{lse2[b], delta[b]};
   }
 
   f32x16 acc[NQ][ND];
@@ -184,91 +127,198 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
 
   const char* k_base = a.k + (int64_t)keys.start * a.k_stride + (int64_t)head * L::row_bytes;
   const char* v_base = a.v + (int64_t)keys.start * a.v_stride + (int64_t)head * L::row_bytes;
-  Stage<T, D, KT> k_next, v_next;
   const RowReader<T, D> read(ordered_row(i), k);
   const ColumnReader<T, D> read_columns(lane);
 
+  // Keys beyond the last are zeros, which no row sees.
+  int k_byte[Fetch::phases], v_byte[Fetch::phases];
+#pragma unroll
+  for (int u = 0; u < Fetch::phases; ++u) {
+    k_byte[u] = Fetch::row(tid, u) * (int)a.k_stride + Fetch::byte(tid, u);
+    v_byte[u] = Fetch::row(tid, u) * (int)a.v_stride + Fetch::byte(tid, u);
+  }
   auto load = [&](int t) INLINE {
-    k_next.load(k_base, a.k_stride, t * KT, keys.n, tid);
-    v_next.load(v_base, a.v_stride, t * KT, keys.n, tid);
-  };
-  auto store = [&](int t) INLINE {
-    k_next.store(s_k[t & 1], tid);
-    v_next.store(s_v[t & 1], tid);
-    if ((t + 1) * KT > min_seen) {
-      const bool bad = __any(k_next.spoilt());
-      if (lane == 0) s_spoilt[t & 1][wave] = bad;
+    const int64_t key0 = (int64_t)t * KT;
+    const Window from_k = window(k_base + key0 * a.k_stride, (keys.n - key0) * a.k_stride);
+    const Window from_v = window(v_base + key0 * a.v_stride, (keys.n - key0) * a.v_stride);
+#pragma unroll
+    for (int u = 0; u < Fetch::units; ++u) {
+      const int further = u / Fetch::phases * (Fetch::phases * Fetch::step);
+      fetch(Fetch::place(s_k[t % NB], wave, u), from_k, k_byte[u % Fetch::phases],
+            further * (int)a.k_stride);
+      fetch(Fetch::place(s_v[t % NB], wave, u), from_v, v_byte[u % Fetch::phases],
+            further * (int)a.v_stride);
     }
   };
+  bool skipped = false;
 
   if (t1 > 0) {
-    load(0);
-    store(0);
+#pragma unroll
+    for (int t = 0; t < NB - 1; ++t) load(t);
+    arrived();
     __syncthreads();
-    for (int t = 0; t < t1; ++t) {
-      if (t + 1 < t1) load(t + 1);
-      if (my_rows) {
-        const char *tile_k = s_k[t & 1], *tile_v = s_v[t & 1];
-        f32x16 s[NQ], dp[NQ];
-#pragma unroll
-        for (int b = 0; b < NQ; ++b)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[b][r] = 0.f, dp[b][r] = 0.f;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-          const u32x4 x = read.get(tile_k, 0, w);
-#pragma unroll
-          for (int b = 0; b < NQ; ++b) s[b] = mma<T>(x, q[b][w], s[b]);
-        }
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-          const u32x4 x = read.get(tile_v, 0, w);
-#pragma unroll
-          for (int b = 0; b < NQ; ++b) dp[b] = mma<T>(x, g[b][w], dp[b]);
-        }
-#pragma unroll
-        for (int b = 0; b < NQ; ++b)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], a.scale2, -lse2[b])) *
-                      (dp[b][r] - delta[b]);
-        bool slow = false;
-        if ((t + 1) * KT > my_min) {
-#pragma unroll
-          for (int b = 0; b < NQ; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              if (t * KT + row_of(r, k) >= seen[b]) s[b][r] = 0.f;
-          int bad = 0;
-#pragma unroll
-          for (int w = 0; w < kWaves; ++w) bad |= s_spoilt[t & 1][w];
-          slow = uniform(bad);
-        }
-        if (__builtin_expect(slow, 0)) {
-#pragma unroll
-          for (int b = 0; b < NQ; ++b)
-            add_seen<T, D>(tile_k, 0, 0, s[b], k, acc[b],
-                           [&](int key) { return t * KT + key < seen[b]; });
-        } else {
-          add_columns<T, D, ND, NQ>(read_columns, tile_k, 0, 0, s, acc);
-        }
-      }
-      if (t + 1 < t1) store(t + 1);
-      __syncthreads();
-    }
   }
-
 #pragma unroll
   for (int b = 0; b < NQ; ++b)
-    if (32 * b + i < my_rows) {
-      char* dst = a.dq + to[b];
 #pragma unroll
-      for (int c = 0; c < ND; ++c)
+    for (int w = 0; w < NW; ++w) asm volatile("" : "+v"(q[b][w]), "+v"(g[b][w]));
+  for (int t = 0; t < t1; ++t) {
+    char* tile_k = s_k[t % NB];
+    const char* tile_v = s_v[t % NB];
+#pragma unroll
+    for (int n = 0; n < KT / 32; ++n) {
+      f32x16 s[NQ], dp[NQ];
+      float less[NQ];                        // delta, till dS is made
+#pragma unroll
+      for (int b = 0; b < NQ; ++b) {
+        less[b] = delta[b];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[b][r] = 0.f, dp[b][r] = 0.f;
+      }
+      // S
+      u32x4 x0 = read.get(tile_k, n, 0), x1 = read.get(tile_k, n, 1);
+      if (n == 0) load(t + NB - 1);
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const u32x4 x2 = w + 2 < NW ? read.get(tile_k, n, w + 2) : read.get(tile_v, n, w + 2 - NW);
+#pragma unroll
+        for (int b = 0; b < NQ; ++b) s[b] = mma<T>(x0, q[b][w], s[b]);
+        x0 = x1, x1 = x2;
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      // dP, and P
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        u32x4 x2 = x0;
+        if (w + 2 < NW) x2 = read.get(tile_v, n, w + 2);
+#pragma unroll
+        for (int b = 0; b < NQ; ++b) dp[b] = mma<T>(x0, g[b][w], dp[b]);
+        if (4 * w % NW == 0) {
+#pragma unroll
+          for (int b = 0; b < NQ; ++b)
+#pragma unroll
+            for (int r = 16 * w / NW; r < 16 * w / NW + 4; ++r)
+              s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], a.scale2, -lse2[b]));
+        }
+        x0 = x1, x1 = x2;
+        if (4 * (w + 1) % NW == 0) __builtin_amdgcn_sched_barrier(0);
+      }
+      const int key0 = t * KT + 32 * n;
+      if (__builtin_expect(key0 + 32 > min_seen, 0)) {
+        // What a row does not see must not meet its weight of 0 where it is not
+        // finite: such keys are left out here (zeros in their place) and added at the
+        // end.
+        const bool bad = !tile_finite<T, D, 32>(tile_k + 32 * n * L::row_bytes, lane);
+        __syncthreads();
+        if (bad) {
+          skipped = true;
+          for (int x = lane; x < 32 * L::chunks; x += 64)
+            reinterpret_cast<u32x4*>(tile_k + 32 * n * L::row_bytes)[x] = u32x4{0u, 0u, 0u, 0u};
+        }
+#pragma unroll
+        for (int b = 0; b < NQ; ++b) {
+          const int left = bad ? -INT32_MAX : seen[b] - key0 - 8 * k;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            s[b][r] = row_of(r, 0) >= left ? 0.f : s[b][r] * (dp[b][r] - delta[b]);
+            dp[b][r] = 1.f;
+          }
+          less[b] = 0.f;
+        }
+      }
+      // dS, and dQ
+      if constexpr (is_f32<T>) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+#pragma unroll
+          for (int b = 0; b < NQ; ++b) s[b][r] *= dp[b][r] - less[b];
+#pragma unroll
+          for (int c = 0; c < ND; ++c) {
+            const float x = read_columns.get(tile_k, 2 * n + r / 8, r % 8, c);
+#pragma unroll
+            for (int b = 0; b < NQ; ++b) mma_far(x, s[b][r], acc[b][c]);
+          }
+        }
+      } else {
+        u32x4 y0 = read_columns.get(tile_k, 2 * n, 0), y1 = read_columns.get(tile_k, 2 * n, 1);
+        u32x4 ds[2][NQ];
+        auto piece = [&](int h, int b) INLINE {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 8 * h + 2 * e;
+            ds[h][b][e] = pack2<T>(s[b][r] * (dp[b][r] - less[b]),
+                                   s[b][r + 1] * (dp[b][r + 1] - less[b]));
+          }
+        };
+#pragma unroll
+        for (int b = 0; b < NQ; ++b) piece(0, b);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int e = 0; e < 2 * ND; ++e) {
+          u32x4 y2 = y0;
+          if (e + 2 < 2 * ND) y2 = read_columns.get(tile_k, 2 * n + (e + 2) / ND, (e + 2) % ND);
+#pragma unroll
+          for (int b = 0; b < NQ; ++b) mma_far<T>(y0, ds[e / ND][b], acc[b][e % ND]);
+          if (e < NQ) piece(1, e);
+          y0 = y1, y1 = y2;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    arrived<2 * Fetch::units*(NB - 2)>();
+    __syncthreads();
+  }
+
+  // The keys that were left out, those alone that the row sees: what they add to block
+  // c of row block b.
+  auto left_out = [&](int b, int c, f32x16 x) INLINE {
+    const T* q_row = reinterpret_cast<const T*>(
+                         a.q + (place[b] / bt.h_q) * a.q_stride) + place[b] % bt.h_q * D;
+    const T* g_row = reinterpret_cast<const T*>(
+                         a.d_out + (place[b] / bt.h_q) * a.d_out_stride) + place[b] % bt.h_q * D;
+#pragma unroll 1
+    for (int key0 = min_seen / 32 * 32; key0 < max_seen; key0 += 32) {
+      auto at_key = [&](const char* base, int64_t stride, int key) INLINE {
+        return reinterpret_cast<const T*>(base + key * stride);
+      };
+      bool bad = false;
+      if (key0 + i < keys.n) {
+        const T* row = at_key(k_base, a.k_stride, key0 + i);
+#pragma unroll 1
+        for (int d = k; d < D; d += 2) bad = bad || !(fabsf((float)row[d]) < INFINITY);
+      }
+      if (!__any(bad)) continue;
+#pragma unroll 1
+      for (int key = key0; key < min(key0 + 32, seen[b]); ++key) {
+        const T* k_row = at_key(k_base, a.k_stride, key);
+        const T* v_row = at_key(v_base, a.v_stride, key);
+        float s = 0.f, dp = 0.f;
+#pragma unroll 1
+        for (int d = 0; d < D; ++d) {
+          s += (float)q_row[d] * (float)k_row[d];
+          dp += (float)g_row[d] * (float)v_row[d];
+        }
+        float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s, a.scale2, -lse2[b])) * (dp - delta[b]);
+        if constexpr (!is_f32<T>) w = (float)(T)w;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r] += w * (float)k_row[32 * c + 8 * (r / 4) + 4 * k + r % 4];
+      }
+    }
+    return x;
+  };
+#pragma unroll
+  for (int b = 0; b < NQ; ++b)
+#pragma unroll
+    for (int c = 0; c < ND; ++c) {
+      settle(acc[b][c]);
+      f32x16 x = acc[b][c];
+      if (__builtin_expect(skipped, 0)) x = left_out(b, c, x);
+      if (32 * b + i < my_rows) {
 #pragma unroll
         for (int r = 0; r < 16; r += 4)
-          store4<T>(dst, 32 * c + 2 * r + 4 * k,
-                    f32x4{acc[b][c][r], acc[b][c][r + 1], acc[b][c][r + 2], acc[b][c][r + 3]} *
-                        a.scale);
+          store4<T>(a.dq + to[b], 32 * c + 2 * r + 4 * k,
+                    f32x4{x[r], x[r + 1], x[r + 2], x[r + 3]} * a.scale);
+      }
     }
 }
 
@@ -442,19 +492,9 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
         // What a row does not see must not meet its weight of 0 where it is not
         // finite: such rows are left out here (zeros in their place) and added at the
         // end.
-        bool bad = false;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-          const u32x4 x = read.get(tile_q, 0, w), y = read.get(tile_g, 0, w);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) bad = bad || not_finite<T>(x[e]) || not_finite<T>(y[e]);
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float x = my_lse[row_of(r, k)];
-          bad = bad || x != x || !(fabsf(my_delta[row_of(r, k)]) < INFINITY);
-        }
-        bad = __any(bad);
+        const float x = my_lse[i], y = my_delta[i];
+        const bool bad = !tile_finite<T, D, 32>(tile_q, lane) || !tile_finite<T, D, 32>(tile_g, lane) ||
+                         __any(x != x || !(fabsf(y) < INFINITY));
         __syncthreads();
         if (bad) {
           skipped = true;
@@ -465,12 +505,13 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
           s_delta[buf][32 * wr + i] = 0.f;
         }
 #pragma unroll
-        for (int n = 0; n < NK; ++n)
+        for (int n = 0; n < NK; ++n) {
+          const int first = from[n] - row0 - 8 * k;
+          const unsigned seeing = bad ? 0u : (unsigned)max(end - max(from[n], 0), 0);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int row = row0 + row_of(r, k);
-            if (bad || row < from[n] || row >= end) s[n][r] = 0.f, dp[n][r] = 0.f;
-          }
+          for (int r = 0; r < 16; ++r)
+            if ((unsigned)(row_of(r, 0) - first) >= seeing) s[n][r] = 0.f, dp[n][r] = 0.f;
+        }
       }
       // dV, and dS
       if constexpr (is_f32<T>) {
@@ -650,16 +691,12 @@ struct Plan {
   size_t bytes;
 };
 
-template <class T, int D>
-constexpr int kRowBlocks = is_f32<T> || D == 256 ? 1 : 2;      // NQ of the rows' kernel
-
 Plan plan_grad(const da_prompt& p) {
   Plan plan{};
   const int64_t G = p.h_q / p.h_kv;
   with_type_and_dim(p.dtype, p.d, [&](auto t, auto d) {
     using T = typename decltype(t)::type;
-    plan.row_items =
-        most_tiles(p.row_start, p.B, p.T, p.rows, G, 32 * kWaves * kRowBlocks<T, d.value>);
+    plan.row_items = most_tiles(p.row_start, p.B, p.T, p.rows, G, RowsForm<T, d.value>::rows);
     plan.key_items =
         most_tiles(p.key_start, p.B, p.N, p.keys, 1, KeysForm<T, d.value>::keys);
   });
@@ -723,7 +760,7 @@ da_status da_prompt_attn_grad(const da_prompt* prompt, const void* q, int64_t q_
   (void)hipGetLastError();
   with_type_and_dim(p.dtype, p.d, [&](auto t, auto d) {
     using T = typename decltype(t)::type;
-    hipLaunchKernelGGL((prompt_grad_rows_kernel<T, d.value, kRowBlocks<T, d.value>>),
+    hipLaunchKernelGGL((prompt_grad_rows_kernel<T, d.value>),
                        dim3((unsigned)(plan.row_items * p.h_kv)), dim3(kThreads), 0, s, bt, a);
     hipLaunchKernelGGL((prompt_grad_keys_kernel<T, d.value>),
                        dim3((unsigned)(plan.key_items * p.h_kv)), dim3(kThreads), 0, s, bt, a);

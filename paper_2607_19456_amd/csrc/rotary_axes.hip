@@ -37,64 +37,97 @@ struct Eight {
 };
 
 // ---------------------------------------------------------------------------
-// A thread turns 16 dimensions of one head of one row: eight pairs, (i, i + half)
-// or (2i, 2i + 1), or copies 16 that are not turned.  An axis may begin inside
-// the eight pairs, so each has a position of its own.
+// A thread turns the same 16 dimensions of up to kHeads heads of one row: eight
+// pairs, (i, i + half) or (2i, 2i + 1), or copies 16 that are not turned.  The angles
+// are read once for them, in four loads where one axis has all eight pairs.  An axis
+// may begin inside them: each pair then has a position of its own.
 // ---------------------------------------------------------------------------
+constexpr int kHeads = 4;
+
 template <class T, int D>
 __global__ __launch_bounds__(kThreads) void rotary_axes_kernel(RotaryArgs a) {
+  constexpr int kPieces = D / 16;
   const uint32_t id = blockIdx.x * kThreads + threadIdx.x;
   const uint32_t row = id / a.per_row;
   const int x = (int)(id - row * a.per_row);
   if (row >= (uint32_t)a.rows) return;
-  const int head = x / (D / 16), piece = x % (D / 16);
-  const bool is_q = head < a.h_q;
-  const int h = is_q ? head : head - a.h_q;
-  const T* src = reinterpret_cast<const T*>((is_q ? a.q : a.k) +
-                                            row * (is_q ? a.q_stride : a.k_stride)) + h * D;
-  T* dst = reinterpret_cast<T*>((is_q ? a.q_out : a.k_out) +
-                                row * (is_q ? a.q_out_stride : a.k_out_stride)) + h * D;
-  const int half = a.rot_dim / 2;
-  const bool turned = 16 * piece < a.rot_dim;
+  const int piece = x % kPieces, head0 = x / kPieces, head_step = (int)a.per_row / kPieces;
+  const int half = a.rot_dim / 2, pair0 = 8 * piece;
+  const bool turned = 2 * pair0 < a.rot_dim;
   const bool near = a.interleaved || !turned;
-  const int at0 = near ? 16 * piece : 8 * piece;
-  const int at1 = near ? 16 * piece + 8 : 8 * piece + half;
-  Eight<T> u, v;
-  u.load(src + at0);
-  v.load(src + at1);
-  if (turned) {
-    const int pair0 = 8 * piece;
-    float cosine[8], sine[8];
-    int axis = 0;
+  const int at0 = near ? 2 * pair0 : pair0;
+  const int at1 = near ? 2 * pair0 + 8 : pair0 + half;
+
+  Eight<T> u[kHeads], v[kHeads];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      while (axis + 1 < a.axes && pair0 + e >= a.ends[axis]) ++axis;
+  for (int j = 0; j < kHeads; ++j) {
+    const int head = head0 + j * head_step;
+    if (head >= a.heads) break;
+    const bool is_q = head < a.h_q;
+    const T* src = reinterpret_cast<const T*>(is_q ? a.q + row * a.q_stride
+                                                   : a.k + row * a.k_stride) +
+                   (is_q ? head : head - a.h_q) * D;
+    u[j].load(src + at0);
+    v[j].load(src + at1);
+  }
+  float cosine[8], sine[8];
+  if (turned) {
+    int axis = 0;
+    while (axis + 1 < a.axes && pair0 >= a.ends[axis]) ++axis;
+    if (pair0 + 8 <= a.ends[axis]) {
       const int pos = a.positions[(int64_t)axis * a.rows + row];
       const bool held = (unsigned)pos < (unsigned)a.n_table;
-      const float* angles = a.table + (int64_t)(held ? pos : 0) * a.rot_dim + pair0 + e;
-      cosine[e] = held ? angles[0] : 1.f;
-      sine[e] = held ? a.sign * angles[half] : 0.f;
-    }
-    Eight<T> y0, y1;
+      const f32x4* angles = reinterpret_cast<const f32x4*>(
+          a.table + (int64_t)(held ? pos : 0) * a.rot_dim + pair0);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float p = a.interleaved ? (float)(e < 4 ? u.x[2 * e % 8] : v.x[2 * e % 8]) : (float)u.x[e];
-      const float r =
-          a.interleaved ? (float)(e < 4 ? u.x[2 * e % 8 + 1] : v.x[2 * e % 8 + 1]) : (float)v.x[e];
-      const T lo = (T)(p * cosine[e] - r * sine[e]), hi = (T)(r * cosine[e] + p * sine[e]);
-      if (a.interleaved) {
-        if (e < 4)
-          y0.x[2 * e % 8] = lo, y0.x[2 * e % 8 + 1] = hi;
-        else
-          y1.x[2 * e % 8] = lo, y1.x[2 * e % 8 + 1] = hi;
-      } else {
-        y0.x[e] = lo, y1.x[e] = hi;
+      for (int e = 0; e < 8; e += 4) {
+        const f32x4 c = angles[e / 4], s = angles[half / 4 + e / 4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          cosine[e + w] = held ? c[w] : 1.f, sine[e + w] = held ? a.sign * s[w] : 0.f;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        while (axis + 1 < a.axes && pair0 + e >= a.ends[axis]) ++axis;
+        const int pos = a.positions[(int64_t)axis * a.rows + row];
+        const bool held = (unsigned)pos < (unsigned)a.n_table;
+        const float* angles = a.table + (int64_t)(held ? pos : 0) * a.rot_dim + pair0 + e;
+        cosine[e] = held ? angles[0] : 1.f;
+        sine[e] = held ? a.sign * angles[half] : 0.f;
       }
     }
-    u = y0, v = y1;
   }
-  u.store(dst + at0);
-  v.store(dst + at1);
+#pragma unroll
+  for (int j = 0; j < kHeads; ++j) {
+    const int head = head0 + j * head_step;
+    if (head >= a.heads) break;
+    Eight<T> y0 = u[j], y1 = v[j];
+    if (turned) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int w = 2 * e % 8;
+        const T first = a.interleaved ? (e < 4 ? u[j].x[w] : v[j].x[w]) : u[j].x[e];
+        const T second = a.interleaved ? (e < 4 ? u[j].x[w + 1] : v[j].x[w + 1]) : v[j].x[e];
+        const float p = (float)first, r = (float)second;
+        const T lo = (T)(p * cosine[e] - r * sine[e]), hi = (T)(r * cosine[e] + p * sine[e]);
+        if (a.interleaved) {
+          if (e < 4)
+            y0.x[w] = lo, y0.x[w + 1] = hi;
+          else
+            y1.x[w] = lo, y1.x[w + 1] = hi;
+        } else {
+          y0.x[e] = lo, y1.x[e] = hi;
+        }
+      }
+    }
+    const bool is_q = head < a.h_q;
+    T* dst = reinterpret_cast<T*>(is_q ? a.q_out + row * a.q_out_stride
+                                       : a.k_out + row * a.k_out_stride) +
+             (is_q ? head : head - a.h_q) * D;
+    y0.store(dst + at0);
+    y1.store(dst + at1);
+  }
 }
 
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
@@ -137,7 +170,8 @@ extern "C" da_status da_rotary_axes(const da_rotary* rotary, const void* q, int6
       p.rot_dim % 16 != 0)
     return DA_ERR_UNSUPPORTED;
   const int size = p.dtype == DA_F32 ? 4 : 2, per16 = 16 / size;
-  const int64_t threads = (int64_t)p.rows * (h_q + h_kv) * (p.d / 16);
+  const int64_t per_row = (int64_t)((h_q + h_kv + kHeads - 1) / kHeads) * (p.d / 16);
+  const int64_t threads = p.rows * per_row;
   const int64_t groups = (threads + kThreads - 1) / kThreads;
   if (groups >= (1 << 24)) return DA_ERR_SHAPE;
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(q_out, 16) || !aligned(k_out, 16) ||
@@ -152,7 +186,7 @@ extern "C" da_status da_rotary_axes(const da_rotary* rotary, const void* q, int6
   a.rows = p.rows, a.heads = h_q + h_kv, a.h_q = h_q, a.n_table = p.n_table;
   a.rot_dim = p.rot_dim, a.axes = p.axes, a.interleaved = p.interleaved != 0;
   a.sign = p.inverse ? -1.f : 1.f;
-  a.per_row = (uint32_t)((h_q + h_kv) * (p.d / 16));
+  a.per_row = (uint32_t)per_row;
   (void)hipGetLastError();
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (p.dtype == DA_F32)
