@@ -63,10 +63,8 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   const int head = blockIdx.x % bt.h_kv;
   const int split = (blockIdx.x / bt.h_kv) % a.splits;
   Place at;
-  if (!find(bt.row_start, bt.B, bt.T, bt.rows, bt.G, R, blockIdx.x / bt.h_kv / a.splits, lane, &at))
-    return;
-  const Span rows = span(bt.row_start, at.b, bt.T, bt.rows);
-  const Span keys = span(bt.key_start, at.b, bt.N, bt.keys);
+  if (!find(bt, true, R, blockIdx.x / bt.h_kv / a.splits, lane, &at)) return;
+  const Span rows = at.rows, keys = at.keys;
   // (the longest first)
   const int row0 = (bt.causal ? at.tiles - 1 - at.tile : at.tile) * R;
   const int in_tile = min(rows.n * bt.G - row0, R);
@@ -500,8 +498,8 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(Batch bt, AttnAr
   const int tid = threadIdx.x, lane = tid & 63;
   const int head = blockIdx.x % bt.h_kv, item = blockIdx.x / bt.h_kv;
   Place at;
-  if (!find(bt.row_start, bt.B, bt.T, bt.rows, bt.G, R, item, lane, &at)) return;
-  const Span rows = span(bt.row_start, at.b, bt.T, bt.rows);
+  if (!find(bt, true, R, item, lane, &at)) return;
+  const Span rows = at.rows;
   const int row0 = (bt.causal ? at.tiles - 1 - at.tile : at.tile) * R;
   const int in_tile = min(rows.n * bt.G - row0, R);
   const int x = blockIdx.y * (kThreads / kPer) + tid / kPer, l = tid % kPer;

@@ -57,14 +57,14 @@ struct Batch {
 };
 
 // First row (or key) and number of them of sequence b, within the arrays
-// whatever the starts hold; b is the same for the whole wave.
+// whatever the starts hold.
 struct Span {
   int start, n;
 };
 __device__ __forceinline__ Span span(const int32_t* start, int b, int most, int total) {
   if (!start) return {b * most, most};
-  const int s = min(max(uniform(start[b]), 0), total);
-  const int e = min(max(uniform(start[b + 1]), s), total);
+  const int s = min(max(start[b], 0), total);
+  const int e = min(max(start[b + 1], s), total);
   return {s, min(e - s, most)};
 }
 
@@ -78,26 +78,34 @@ __device__ __forceinline__ int seen_by(const Batch& bt, int rows, int keys, int 
   return bt.causal ? min(max(t + 1 + keys - rows, 0), keys) : keys;
 }
 
-// Item `item` of the batch, items being tiles of R of each sequence's n*per
-// rows: its sequence and its number there.  False beyond the last.
+// Item `item` of the batch, items being tiles of R of each sequence's rows (times
+// G), or of its keys: its sequence's rows and keys, and its number there.  False
+// beyond the last.  The sequences are counted 64 at a time, a lane each.
 struct Place {
-  int b, tile, tiles;
+  Span rows, keys;
+  int tile, tiles;
 };
-__device__ __forceinline__ bool find(const int32_t* start, int B, int most, int total, int per,
-                                     int R, int item, int lane, Place* at) {
-  if (!start) {
-    const int tiles = (int)(((int64_t)most * per + R - 1) / R);
-    *at = {item / tiles, item % tiles, tiles};
-    return at->b < B;
-  }
+__device__ __forceinline__ bool find(const Batch& bt, bool by_rows, int R, int item, int lane,
+                                     Place* at) {
+  const int64_t per = by_rows ? bt.G : 1;
   int left = item;
-  for (int b0 = 0; b0 < B; b0 += 64) {
-    int n = 0;
-    if (b0 + lane < B) {
-      const int s = min(max(start[b0 + lane], 0), total);
-      const int e = min(max(start[b0 + lane + 1], s), total);
-      n = (int)(((int64_t)min(e - s, most) * per + R - 1) / R);
+  for (int b0 = 0; b0 < bt.B; b0 += 64) {
+    if (!(by_rows ? bt.row_start : bt.key_start)) {
+      // as many of each: at once
+      const int tiles = (int)(((by_rows ? bt.T : bt.N) * per + R - 1) / R);
+      const int b = item / tiles;
+      if (b >= bt.B) return false;
+      const Span r = span(bt.row_start, b, bt.T, bt.rows), k = span(bt.key_start, b, bt.N, bt.keys);
+      *at = {{uniform(r.start), uniform(r.n)}, {uniform(k.start), uniform(k.n)}, item % tiles, tiles};
+      return true;
     }
+    const bool there = b0 + lane < bt.B;
+    Span r{0, 0}, k{0, 0};
+    if (there) {
+      r = span(bt.row_start, b0 + lane, bt.T, bt.rows);
+      k = span(bt.key_start, b0 + lane, bt.N, bt.keys);
+    }
+    const int n = (int)(((by_rows ? r.n : k.n) * per + R - 1) / R);
     int upto = n;
 #pragma unroll
     for (int step = 1; step < 64; step *= 2) {
@@ -108,7 +116,10 @@ __device__ __forceinline__ bool find(const int32_t* start, int B, int most, int 
     if (left < all) {
       const int l = __ffsll((unsigned long long)__ballot(upto > left)) - 1;
       const int tiles = __builtin_amdgcn_readlane(n, l);
-      *at = {b0 + l, left - (__builtin_amdgcn_readlane(upto, l) - tiles), tiles};
+      *at = {{__builtin_amdgcn_readlane(r.start, l), __builtin_amdgcn_readlane(r.n, l)},
+             {__builtin_amdgcn_readlane(k.start, l), __builtin_amdgcn_readlane(k.n, l)},
+             left - (__builtin_amdgcn_readlane(upto, l) - tiles),
+             tiles};
       return true;
     }
     left -= all;
@@ -308,7 +319,7 @@ struct Finite {
 template <class T, int D, int ROWS>
 __device__ __forceinline__ bool tile_finite(const char* tile, int lane) {
   Finite<T> f;
-#pragma unroll 4
+#pragma unroll 8
   for (int x = lane; x < ROWS * Tile<T, D>::chunks; x += 64)
     f.take(*reinterpret_cast<const u32x4*>(tile + 16 * x));
   return !__any(!f.all());

@@ -72,14 +72,16 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
 
   __shared__ __align__(16) char s_k[NB][kTile];
   __shared__ __align__(16) char s_v[NB][kTile];
+  // 32 rows of zeros, where there is room
+  constexpr bool kZeros = 2 * NB * kTile + 32 * L::row_bytes < 160 << 10;
+  __shared__ __align__(16) char s_zero[kZeros ? 32 * L::row_bytes : 16];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int i = lane & 31, k = lane >> 5;
   const int head = blockIdx.x % bt.h_kv;
   Place at;
-  if (!find(bt.row_start, bt.B, bt.T, bt.rows, bt.G, R, blockIdx.x / bt.h_kv, lane, &at)) return;
-  const Span rows = span(bt.row_start, at.b, bt.T, bt.rows);
-  const Span keys = span(bt.key_start, at.b, bt.N, bt.keys);
+  if (!find(bt, true, R, blockIdx.x / bt.h_kv, lane, &at)) return;
+  const Span rows = at.rows, keys = at.keys;
   const int row0 = (bt.causal ? at.tiles - 1 - at.tile : at.tile) * R;
   const int in_tile = min(rows.n * bt.G - row0, R);
   const int min_seen = seen_by(bt, rows.n, keys.n, token_of(bt, row0));
@@ -151,6 +153,9 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
     }
   };
   bool skipped = false;
+  if (kZeros)
+    for (int x = tid; x < 32 * L::chunks; x += kThreads)
+      reinterpret_cast<u32x4*>(s_zero)[x] = u32x4{0u, 0u, 0u, 0u};
 
   if (t1 > 0) {
 #pragma unroll
@@ -204,14 +209,17 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
         if (4 * (w + 1) % NW == 0) __builtin_amdgcn_sched_barrier(0);
       }
       const int key0 = t * KT + 32 * n;
+      const char* by_columns = tile_k + 32 * n * L::row_bytes;
       if (__builtin_expect(key0 + 32 > min_seen, 0)) {
         // What a row does not see must not meet its weight of 0 where it is not
         // finite: such keys are left out here (zeros in their place) and added at the
         // end.
         const bool bad = !tile_finite<T, D, 32>(tile_k + 32 * n * L::row_bytes, lane);
-        __syncthreads();
-        if (bad) {
-          skipped = true;
+        if (!kZeros) __syncthreads();
+        if (bad) skipped = true;
+        if (kZeros) {
+          if (bad) by_columns = s_zero;
+        } else if (bad) {
           for (int x = lane; x < 32 * L::chunks; x += 64)
             reinterpret_cast<u32x4*>(tile_k + 32 * n * L::row_bytes)[x] = u32x4{0u, 0u, 0u, 0u};
         }
@@ -234,13 +242,13 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
           for (int b = 0; b < NQ; ++b) s[b][r] *= dp[b][r] - less[b];
 #pragma unroll
           for (int c = 0; c < ND; ++c) {
-            const float x = read_columns.get(tile_k, 2 * n + r / 8, r % 8, c);
+            const float x = read_columns.get(by_columns, r / 8, r % 8, c);
 #pragma unroll
             for (int b = 0; b < NQ; ++b) mma_far(x, s[b][r], acc[b][c]);
           }
         }
       } else {
-        u32x4 y0 = read_columns.get(tile_k, 2 * n, 0), y1 = read_columns.get(tile_k, 2 * n, 1);
+        u32x4 y0 = read_columns.get(by_columns, 0, 0), y1 = read_columns.get(by_columns, 0, 1);
         u32x4 ds[2][NQ];
         auto piece = [&](int h, int b) INLINE {
 #pragma unroll
@@ -256,7 +264,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
 #pragma unroll
         for (int e = 0; e < 2 * ND; ++e) {
           u32x4 y2 = y0;
-          if (e + 2 < 2 * ND) y2 = read_columns.get(tile_k, 2 * n + (e + 2) / ND, (e + 2) % ND);
+          if (e + 2 < 2 * ND) y2 = read_columns.get(by_columns, (e + 2) / ND, (e + 2) % ND);
 #pragma unroll
           for (int b = 0; b < NQ; ++b) mma_far<T>(y0, ds[e / ND][b], acc[b][e % ND]);
           if (e < NQ) piece(1, e);
@@ -350,15 +358,17 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
 
   __shared__ __align__(16) char s_rows[4][kTile];             // Q's two tiles, dO's two
   __shared__ __align__(16) float s_lse[2][RT], s_delta[2][RT];
+  // 32 rows of zeros, where there is room
+  constexpr bool kZeros = 4 * kTile + 16 * RT + 32 * L::row_bytes < 160 << 10;
+  __shared__ __align__(16) char s_zero[kZeros ? 32 * L::row_bytes : 16];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int i = lane & 31, k = lane >> 5;
   const int wk = wave % WK, wr = wave / WK % WR, wd = wave / (WK * WR);
   const int head = blockIdx.x % bt.h_kv;
   Place at;
-  if (!find(bt.key_start, bt.B, bt.N, bt.keys, 1, F::keys, blockIdx.x / bt.h_kv, lane, &at)) return;
-  const Span rows = span(bt.row_start, at.b, bt.T, bt.rows);
-  const Span keys = span(bt.key_start, at.b, bt.N, bt.keys);
+  if (!find(bt, false, F::keys, blockIdx.x / bt.h_kv, lane, &at)) return;
+  const Span rows = at.rows, keys = at.keys;
   const int end = rows.n * bt.G;
   const int key0 = at.tile * F::keys;
   // the first row (token and head) that sees a key
@@ -368,13 +378,13 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
   const int all_from = first_row(min(key0 + F::keys, keys.n) - 1);   // rows that see all of the keys
   const int r0 = first_row(key0) / RT, r1 = (end + RT - 1) / RT;
 
-  int key[NK], from[NK];
+  auto key_of = [&](int n, int lane) INLINE {
+    return key0 + 32 * (NK * wk + n) + (lane & 31);
+  };
   u32x4 kk[NK][NW], vv[NK][NW];
 #pragma unroll
   for (int n = 0; n < NK; ++n) {
-    key[n] = key0 + 32 * (NK * wk + n) + i;
-    const int64_t token = keys.start + min(key[n], keys.n - 1);
-    from[n] = first_row(min(key[n], keys.n - 1));
+    const int64_t token = keys.start + min(key_of(n, lane), keys.n - 1);
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
       const int64_t in = (int64_t)head * L::row_bytes + 32 * w + 16 * k;
@@ -394,16 +404,35 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
   const RowReader<T, D> read(ordered_row(i), k);
   const ColumnReader<T, D> read_columns(lane);
 
-  // Rows beyond the last are the last one again (their weights are taken as 0).
+  // (The weights of rows beyond the last are taken as 0.)
   using Fetch = Direct<T, D, RT>;
   auto window_of = [&](const char* base, int64_t stride, int t) INLINE {
     const int64_t tok = token_of(bt, min(t * RT, end - 1));
     return window(base + (rows.start + tok) * stride + (int64_t)head * bt.G * L::row_bytes,
                   (rows.n - tok) * stride);
   };
+  // Where a group's heads divide the rows between a thread's units, its place among a
+  // step's tokens is the same every step, and further units are whole tokens on.
+  const bool even = Fetch::step % bt.G == 0 && Fetch::phases == 1;
+  int q_byte = 0, g_byte = 0;
+  if (even) {
+    const int tok = token_of(bt, Fetch::row(tid, 0));
+    const int in = (Fetch::row(tid, 0) - tok * bt.G) * L::row_bytes + Fetch::byte(tid, 0);
+    q_byte = tok * (int)a.q_stride + in, g_byte = tok * (int)a.d_out_stride + in;
+  }
   auto load_rows = [&](int t) INLINE {
     const Window from_q = window_of(a.q, a.q_stride, t);
     const Window from_g = window_of(a.d_out, a.d_out_stride, t);
+    if (even) {
+      const int tokens = token_of(bt, Fetch::step);
+#pragma unroll
+      for (int u = 0; u < Fetch::units; ++u) {
+        fetch(Fetch::place(s_rows[t & 1], wave, u), from_q, q_byte, u * tokens * (int)a.q_stride);
+        fetch(Fetch::place(s_rows[2 + (t & 1)], wave, u), from_g, g_byte,
+              u * tokens * (int)a.d_out_stride);
+      }
+      return;
+    }
     const int tok0 = token_of(bt, min(t * RT, end - 1));
 #pragma unroll
     for (int u = 0; u < Fetch::units; ++u) {
@@ -428,6 +457,9 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
   // Not all rows of a step see all keys, and what they do not see is masked.
   auto partial = [&](int t) INLINE { return t * RT < all_from || (t + 1) * RT > end; };
   bool skipped = false;
+  if (kZeros)
+    for (int x = tid; x < 32 * L::chunks; x += kThreads)
+      reinterpret_cast<u32x4*>(s_zero)[x] = u32x4{0u, 0u, 0u, 0u};
 
   if (r0 < r1) {
     load_rows(r0);
@@ -488,6 +520,8 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
           if (4 * (w + 1) % NW == 0) __builtin_amdgcn_sched_barrier(0);
         }
       }
+      const char *columns_q = tile_q, *columns_g = tile_g;
+      const float* deltas = my_delta;
       if (__builtin_expect(partial(t), 0)) {
         // What a row does not see must not meet its weight of 0 where it is not
         // finite: such rows are left out here (zeros in their place) and added at the
@@ -495,19 +529,29 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
         const float x = my_lse[i], y = my_delta[i];
         const bool bad = !tile_finite<T, D, 32>(tile_q, lane) || !tile_finite<T, D, 32>(tile_g, lane) ||
                          __any(x != x || !(fabsf(y) < INFINITY));
-        __syncthreads();
+        if (!kZeros) __syncthreads();
         if (bad) {
           skipped = true;
-          for (int x = lane; x < 32 * L::chunks; x += 64)
-            reinterpret_cast<u32x4*>(s_rows[buf] + 32 * wr * L::row_bytes)[x] =
-                reinterpret_cast<u32x4*>(s_rows[2 + buf] + 32 * wr * L::row_bytes)[x] =
-                    u32x4{0u, 0u, 0u, 0u};
-          s_delta[buf][32 * wr + i] = 0.f;
+          if (kZeros) {
+            columns_q = columns_g = s_zero;
+            deltas = reinterpret_cast<const float*>(s_zero);
+          } else {
+            for (int x = lane; x < 32 * L::chunks; x += 64)
+              reinterpret_cast<u32x4*>(s_rows[buf] + 32 * wr * L::row_bytes)[x] =
+                  reinterpret_cast<u32x4*>(s_rows[2 + buf] + 32 * wr * L::row_bytes)[x] =
+                      u32x4{0u, 0u, 0u, 0u};
+            s_delta[buf][32 * wr + i] = 0.f;
+          }
         }
+        // (the lane hidden from the compiler: what follows from it would otherwise be
+        // held through the loop, in registers that there are none of)
+        int now = lane;
+        asm volatile("" : "+v"(now));
 #pragma unroll
         for (int n = 0; n < NK; ++n) {
-          const int first = from[n] - row0 - 8 * k;
-          const unsigned seeing = bad ? 0u : (unsigned)max(end - max(from[n], 0), 0);
+          const int from = first_row(min(key_of(n, now), keys.n - 1));
+          const int first = from - row0 - 8 * (now >> 5);
+          const unsigned seeing = bad ? 0u : (unsigned)max(end - from, 0);
 #pragma unroll
           for (int r = 0; r < 16; ++r)
             if ((unsigned)(row_of(r, 0) - first) >= seeing) s[n][r] = 0.f, dp[n][r] = 0.f;
@@ -519,16 +563,16 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
         for (int r = 0; r < 16; ++r) {
 #pragma unroll
           for (int c = 0; c < ND; ++c) {
-            const float x = read_columns.get(tile_g, r / 8, r % 8, ND * wd + c);
+            const float x = read_columns.get(columns_g, r / 8, r % 8, ND * wd + c);
 #pragma unroll
             for (int n = 0; n < NK; ++n) mma_far(x, s[n][r], dv[n][c]);
           }
-          const float y = my_delta[row_of(r, k)];
+          const float y = deltas[row_of(r, k)];
 #pragma unroll
           for (int n = 0; n < NK; ++n) dp[n][r] = s[n][r] * (dp[n][r] - y);
 #pragma unroll
           for (int c = 0; c < ND; ++c) {
-            const float x = read_columns.get(tile_q, r / 8, r % 8, ND * wd + c);
+            const float x = read_columns.get(columns_q, r / 8, r % 8, ND * wd + c);
 #pragma unroll
             for (int n = 0; n < NK; ++n) mma_far(x, dp[n][r], dk[n][c]);
           }
@@ -536,7 +580,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
         }
       } else {
         u32x4 p[NK], ds[2][NK];
-        u32x4 x = read_columns.get(tile_g, 0, 0);
+        u32x4 x = read_columns.get(columns_g, 0, 0);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -547,13 +591,13 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
 #pragma unroll
           for (int c = 0; c < ND; ++c) {
             const bool last = c + 1 == ND;
-            const u32x4 y = last ? read_columns.get(h == 0 ? tile_g : tile_q, h == 0 ? 1 : 0, 0)
-                                 : read_columns.get(tile_g, h, c + 1);
+            const u32x4 y = last ? read_columns.get(h == 0 ? columns_g : columns_q, h == 0 ? 1 : 0, 0)
+                                 : read_columns.get(columns_g, h, c + 1);
 #pragma unroll
             for (int n = 0; n < NK; ++n) mma_far<T>(x, p[n], dv[n][c]);
             if (2 * c % ND == 0) {
               const int r = 8 * c / ND;
-              const f32x4 z = *reinterpret_cast<const f32x4*>(my_delta + row_of(8 * h + r, k));
+              const f32x4 z = *reinterpret_cast<const f32x4*>(deltas + row_of(8 * h + r, k));
 #pragma unroll
               for (int n = 0; n < NK; ++n) {
                 float e4[4];
@@ -575,7 +619,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
           for (int c = 0; c < ND; ++c) {
             u32x4 y = x;
             if (h == 0 || c + 1 < ND)
-              y = read_columns.get(tile_q, c + 1 < ND ? h : 1, c + 1 < ND ? c + 1 : 0);
+              y = read_columns.get(columns_q, c + 1 < ND ? h : 1, c + 1 < ND ? c + 1 : 0);
 #pragma unroll
             for (int n = 0; n < NK; ++n) mma_far<T>(x, ds[h][n], dk[n][c]);
             x = y;
@@ -591,7 +635,8 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
   // The rows that were left out, pair by pair, those alone that see the key: what they
   // add to block c of key n's dK or dV.
   auto left_out = [&](int n, int c, bool is_dk, f32x16 x) INLINE {
-    const int64_t token = keys.start + min(key[n], keys.n - 1);
+    const int64_t token = keys.start + min(key_of(n, lane), keys.n - 1);
+    const int from = first_row(min(key_of(n, lane), keys.n - 1));
     const T* k_row = reinterpret_cast<const T*>(a.k + token * a.k_stride) + head * D;
     const T* v_row = reinterpret_cast<const T*>(a.v + token * a.v_stride) + head * D;
     const T *q, *g;
@@ -614,7 +659,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
         bad = bad || !(fabsf((float)q[d]) < INFINITY) || !(fabsf((float)g[d]) < INFINITY);
       if (!__any(bad)) continue;
 #pragma unroll 1
-      for (int row = max(row0, from[n]); row < min(row0 + 32, end); ++row) {
+      for (int row = max(row0, from); row < min(row0 + 32, end); ++row) {
         at_row(row);
         float s = 0.f, dp = 0.f;
 #pragma unroll 1
@@ -660,7 +705,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
     if (wr == 0) {
 #pragma unroll
       for (int n = 0; n < NK; ++n) {
-        const int64_t token = keys.start + key[n];
+        const int64_t token = keys.start + key_of(n, lane);
         char* dst = (is_dk ? a.dk + token * a.dk_stride : a.dv + token * a.dv_stride) +
                     (int64_t)head * L::row_bytes;
 #pragma unroll
@@ -670,7 +715,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
           for (int r = 0; r < 16; r += 4) {
             f32x4 y{x[r], x[r + 1], x[r + 2], x[r + 3]};
             if (WR > 1) y += shared(n, c)[16 * r];
-            if (key[n] < keys.n)
+            if (key_of(n, lane) < keys.n)
               store4<T>(dst, 32 * (ND * wd + c) + 2 * r + 4 * k, y * by);
           }
         }
