@@ -54,8 +54,10 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   using Fetch = Direct<T, D, KT>;
 
   constexpr int NB = NQ == 2 ? 3 : 2;        // tiles in LDS
-  __shared__ __align__(16) char s_k[NB][kTile];
-  __shared__ __align__(16) char s_v[NB][kTile];
+  // K's tiles, then V's; q on its way in, and out on its way out
+  static_assert(2 * NB * kTile >= R * L::row_bytes, "room for the rows");
+  __shared__ __align__(16) char s_all[2 * NB][kTile];
+  char(*s_k)[kTile] = s_all, (*s_v)[kTile] = s_all + NB;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int i = lane & 31, k = lane >> 5;
@@ -81,21 +83,24 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   const int my_max =
       my_rows ? seen_by(bt, rows.n, keys.n, token_of(bt, my_row0 + my_rows - 1)) : 0;
   int seen[NQ];
-  int64_t place[NQ];                         // row * h_q + head
   u32x4 q[NQ][NW];
+  fetch_rows<T, D, R>(s_all[0], bt,
+                      a.q + rows.start * a.q_stride + (int64_t)head * bt.G * L::row_bytes,
+                      a.q_stride, row0, row0 + in_tile - 1, tid, wave);
+  arrived();
+  __syncthreads();
+  {
+    const RowReader<T, D> rd(i, k);
 #pragma unroll
-  for (int b = 0; b < NQ; ++b) {
-    const int x = my_row0 + min(32 * b + i, max(my_rows - 1, 0));
-    const int t = my_rows ? token_of(bt, x) : 0;
-    const int g = my_rows ? x - t * bt.G : 0;
-    seen[b] = 32 * b + i < my_rows ? seen_by(bt, rows.n, keys.n, t) : 0;
-    place[b] = (int64_t)(rows.start + t) * bt.h_q + head * bt.G + g;
-    const char* src = a.q + (int64_t)(rows.start + t) * a.q_stride +
-                      (int64_t)(head * bt.G + g) * L::row_bytes + 16 * k;
+    for (int b = 0; b < NQ; ++b) {
+      const int x = 32 * b + i;
+      seen[b] = x < my_rows ? seen_by(bt, rows.n, keys.n, token_of(bt, my_row0 + x)) : 0;
 #pragma unroll
-    for (int w = 0; w < NW; ++w)
-      q[b][w] = (far_load<u32x4>(src + 32 * w) & a.q_keep) ^ a.q_flip;
+      for (int w = 0; w < NW; ++w)
+        q[b][w] = (rd.get(s_all[0], NQ * wave + b, w) & a.q_keep) ^ a.q_flip;
+    }
   }
+  __syncthreads();
 
   f32x16 acc[NQ][ND];
   float limit[NQ], ref[NQ], sum[NQ], whole[NQ], top[NQ];
@@ -446,33 +451,31 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
     }
   }
 
+  char* mine = s_all[0] + 32 * NQ * wave * L::row_bytes;
+  auto place = [&](int x) INLINE {           // row * h_q + head of this wave's row x
+    const int tok = token_of(bt, my_row0 + x);
+    return (int64_t)(rows.start + tok) * bt.h_q + head * bt.G + my_row0 + x - tok * bt.G;
+  };
 #pragma unroll
   for (int b = 0; b < NQ; ++b) {
-    float total = sum[b] + __shfl_xor(sum[b], 32);
-    const float all = LSE ? whole[b] + __shfl_xor(whole[b], 32) : total;
-    if (32 * b + i >= my_rows) continue;
+    const float total = sum[b] + __shfl_xor(sum[b], 32);
+    const float all = LSE && !is_f32<T> ? whole[b] + __shfl_xor(whole[b], 32) : total;
     // (a row whose scores are all -infinity counts as one that sees nothing)
     const bool none = limit[b] == -INFINITY && total == 0.f;
+    const bool here = 32 * b + i < my_rows && k == 0;
     if (a.splits == 1) {
       const float inverse = 1.f / total;
       auto mean = [&](float x) INLINE { return none ? 0.f : x * inverse; };
-      char* dst = a.out + place[b] * L::row_bytes;
 #pragma unroll
       for (int c = 0; c < ND; ++c)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-          const f32x4 o{mean(acc[b][c][r]), mean(acc[b][c][r + 1]), mean(acc[b][c][r + 2]),
-                        mean(acc[b][c][r + 3])};
-          const int d = 32 * c + 2 * r + 4 * k;
-          if constexpr (is_f32<T>)
-            *reinterpret_cast<f32x4*>(dst + 4 * d) = o;
-          else
-            *reinterpret_cast<u32x2*>(dst + 2 * d) =
-                u32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
-        }
-      if (a.lse && k == 0)
-        a.lse[place[b]] = none ? -INFINITY : (ref[b] + log2f(is_f32<T> || !LSE ? total : all)) * kLn2;
-    } else {
+        for (int r = 0; r < 16; r += 4)
+          put4<T, D>(mine, 32 * b + i, 32 * c + 2 * r + 4 * k,
+                     f32x4{mean(acc[b][c][r]), mean(acc[b][c][r + 1]), mean(acc[b][c][r + 2]),
+                           mean(acc[b][c][r + 3])});
+      if (a.lse && here)
+        a.lse[place(32 * b + i)] = none ? -INFINITY : (ref[b] + log2f(all)) * kLn2;
+    } else if (32 * b + i < my_rows) {
       const int64_t row = (int64_t)blockIdx.x * R + 32 * NQ * wave + 32 * b + i;
       float* dst = a.parts + row * D + 4 * k;
 #pragma unroll
@@ -481,12 +484,16 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
         for (int r = 0; r < 16; r += 4)
           *reinterpret_cast<f32x4*>(dst + 32 * c + 2 * r) =
               f32x4{acc[b][c][r], acc[b][c][r + 1], acc[b][c][r + 2], acc[b][c][r + 3]};
-      if (k == 0) {
+      if (here) {
         float* st = a.parts + a.stats + row * 3;
-        st[0] = none ? -INFINITY : ref[b], st[1] = total, st[2] = is_f32<T> ? total : all;
+        st[0] = none ? -INFINITY : ref[b], st[1] = total, st[2] = all;
       }
     }
   }
+  if (a.splits == 1)
+    store_rows<T, D>(mine, 32 * NQ, lane, [&](int x) INLINE {
+      return x < my_rows ? a.out + place(x) * L::row_bytes : nullptr;
+    });
 }
 
 // ---------------------------------------------------------------------------

@@ -376,6 +376,48 @@ __device__ __forceinline__ void arrived() {
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(more) : "memory");
 }
 
+// ROWS rows of a KV head (x0 on; those beyond `last` are the last again) on their way
+// to a tile.  `base`: the sequence's first row, the KV head's first head.
+template <class T, int D, int ROWS>
+__device__ __forceinline__ void fetch_rows(char* tile, const Batch& bt, const char* base,
+                                           int64_t stride, int x0, int last, int tid, int wave) {
+  using F = Direct<T, D, ROWS>;
+  const int tok0 = token_of(bt, x0);
+  const Window from = window(base + tok0 * stride, 0x7fffffff);
+#pragma unroll
+  for (int u = 0; u < F::units; ++u) {
+    const int x = min(x0 + F::row(tid, u), last), tok = token_of(bt, x);
+    fetch(F::place(tile, wave, u), from,
+          (tok - tok0) * (int)stride + (x - tok * bt.G) * F::L::row_bytes + F::byte(tid, u), 0);
+  }
+}
+
+// Results of a wave on their way back: 32 rows (columns of a product) in LDS, then whole
+// rows to memory, 16 bytes a lane (four dimensions a lane as they lie would touch each
+// line eight times).  `to(row)` is a row's place, or NULL.
+template <class T, int D>
+__device__ __forceinline__ void put4(char* tile, int row, int d, f32x4 x) {
+  using L = Tile<T, D>;
+  if constexpr (is_f32<T>)
+    *reinterpret_cast<f32x4*>(tile + L::at(row, d / 4)) = x;
+  else
+    *reinterpret_cast<u32x2*>(tile + L::at(row, d / 8) + d % 8 * 2) =
+        u32x2{pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3])};
+}
+template <class T, int D, class F>
+__device__ __forceinline__ void store_rows(const char* tile, int rows, int lane, F&& to) {
+  using L = Tile<T, D>;
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll 4
+  for (int p = 0; p < rows * L::chunks / 64; ++p) {
+    const int row = (p * 64 + lane) / L::chunks, chunk = lane % L::chunks;
+    const u32x4 x = *reinterpret_cast<const u32x4*>(tile + L::at(row, chunk));
+    char* dst = to(row);
+    if (dst) *reinterpret_cast<u32x4*>(dst + 16 * chunk) = x;
+  }
+  __builtin_amdgcn_wave_barrier();
+}
+
 // A word (or several) of memory: not through the instructions that may be LDS too.
 template <class V, class P>
 __device__ __forceinline__ V far_load(const P* p) {
@@ -419,8 +461,8 @@ inline bool starts_aligned(const da_prompt& p) {
 }
 
 // A token stride (elements) that rows of `heads` heads may have: the kernels take
-// offsets within 64 tokens in 32 bits.
-constexpr int64_t kMaxStrideBytes = int64_t(1) << 24;
+// offsets within 256 tokens in 32 bits.
+constexpr int64_t kMaxStrideBytes = int64_t(1) << 22;
 inline bool stride_fits(int64_t stride, int heads, int d, int dtype) {
   return stride >= (int64_t)heads * d && stride <= kMaxStrideBytes / type_bytes(dtype);
 }

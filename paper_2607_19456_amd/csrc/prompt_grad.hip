@@ -29,15 +29,6 @@ struct GradArgs {
   f32x2* stats;                 // [rows][h_q]: lse times log2(e) (+infinity: no weights), delta
 };
 
-// Four dimensions of a row.
-template <class T>
-__device__ __forceinline__ void store4(char* row, int d, f32x4 x) {
-  if constexpr (is_f32<T>)
-    *reinterpret_cast<f32x4*>(row + 4 * d) = x;
-  else
-    *reinterpret_cast<u32x2*>(row + 2 * d) = u32x2{pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3])};
-}
-
 template <class T>
 __device__ __forceinline__ float dot16(u32x4 a, u32x4 b, float sum) {
   constexpr int n = 16 / sizeof(T);
@@ -70,8 +61,10 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
   constexpr int kTile = KT * L::row_bytes;
   using Fetch = Direct<T, D, KT>;
 
-  __shared__ __align__(16) char s_k[NB][kTile];
-  __shared__ __align__(16) char s_v[NB][kTile];
+  // K's tiles, then V's; Q and dO on their way in, and dQ on its way out
+  static_assert(2 * NB * kTile >= R * L::row_bytes, "room for the rows");
+  __shared__ __align__(16) char s_all[2 * NB][kTile];
+  char(*s_k)[kTile] = s_all, (*s_v)[kTile] = s_all + NB;
   // 32 rows of zeros, where there is room
   constexpr bool kZeros = 2 * NB * kTile + 32 * L::row_bytes < 160 << 10;
   __shared__ __align__(16) char s_zero[kZeros ? 32 * L::row_bytes : 16];
@@ -91,32 +84,50 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
   const int my_row0 = row0 + 32 * NQ * wave;
   const int my_rows = min(max(in_tile - 32 * NQ * wave, 0), 32 * NQ);
   int seen[NQ];
-  int64_t place[NQ];                         // row * h_q + head
-  int64_t to[NQ];
   float lse2[NQ], delta[NQ];
   u32x4 q[NQ][NW], g[NQ][NW];
+  auto place = [&](int x) INLINE {           // row * h_q + head of this wave's row x
+    const int tok = token_of(bt, my_row0 + x);
+    return (int64_t)(rows.start + tok) * bt.h_q + head * bt.G + my_row0 + x - tok * bt.G;
+  };
+  {
+    const RowReader<T, D> rd(i, k);
+    const int64_t in = (int64_t)head * bt.G * L::row_bytes;
+    auto bring = [&](const char* base, int64_t stride) INLINE {
+      fetch_rows<T, D, R>(s_all[0], bt, base + rows.start * stride + in, stride, row0,
+                          row0 + in_tile - 1, tid, wave);
+      arrived();
+      __syncthreads();
+    };
+    bring(a.q, a.q_stride);
 #pragma unroll
-  for (int b = 0; b < NQ; ++b) {
-    const bool mine = 32 * b + i < my_rows;
-    const int x = my_row0 + min(32 * b + i, max(my_rows - 1, 0));
-    const int t = my_rows ? token_of(bt, x) : 0;
-    const int h = head * bt.G + (my_rows ? x - t * bt.G : 0);
-    seen[b] = mine ? seen_by(bt, rows.n, keys.n, t) : 0;
-    const int64_t token = rows.start + t;
-    place[b] = token * bt.h_q + h;
-    to[b] = token * a.dq_stride + (int64_t)h * L::row_bytes;
-    const int64_t in = (int64_t)h * L::row_bytes + 16 * k;
-    float sum = 0.f;
+    for (int b = 0; b < NQ; ++b)
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      q[b][w] = far_load<u32x4>(a.q + token * a.q_stride + in + 32 * w);
-      g[b][w] = far_load<u32x4>(a.d_out + token * a.d_out_stride + in + 32 * w);
-      sum = dot16<T>(g[b][w], far_load<u32x4>(a.out + place[b] * L::row_bytes + 16 * k + 32 * w), sum);
+      for (int w = 0; w < NW; ++w) q[b][w] = rd.get(s_all[0], NQ * wave + b, w);
+    __syncthreads();
+    bring(a.d_out, a.d_out_stride);
+#pragma unroll
+    for (int b = 0; b < NQ; ++b)
+#pragma unroll
+      for (int w = 0; w < NW; ++w) g[b][w] = rd.get(s_all[0], NQ * wave + b, w);
+    __syncthreads();
+    bring(a.out, (int64_t)bt.h_q * L::row_bytes);
+#pragma unroll
+    for (int b = 0; b < NQ; ++b) {
+      const int x = 32 * b + i;
+      float sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) sum = dot16<T>(g[b][w], rd.get(s_all[0], NQ * wave + b, w), sum);
+      delta[b] = sum + __shfl_xor(sum, 32);
+      seen[b] = 0, lse2[b] = INFINITY;
+      if (x < my_rows) {
+        seen[b] = seen_by(bt, rows.n, keys.n, token_of(bt, my_row0 + x));
+        const float lse = far_load<float>(a.lse + place(x));
+        lse2[b] = lse == -INFINITY ? INFINITY : lse * kLog2e;
+        if (k == 0) a.stats[place(x)] = f32x2{lse2[b], delta[b]};
+      }
     }
-    delta[b] = sum + __shfl_xor(sum, 32);
-    const float lse = far_load<float>(a.lse + place[b]);
-    lse2[b] = lse == -INFINITY ? INFINITY : lse * kLog2e;
-    if (mine && k == 0) a.stats[place[b]] = f32x2{lse2[b], delta[b]};
+    __syncthreads();
   }
 
   f32x16 acc[NQ][ND];
@@ -280,10 +291,10 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
   // The keys that were left out, those alone that the row sees: what they add to block
   // c of row block b.
   auto left_out = [&](int b, int c, f32x16 x) INLINE {
-    const T* q_row = reinterpret_cast<const T*>(
-                         a.q + (place[b] / bt.h_q) * a.q_stride) + place[b] % bt.h_q * D;
-    const T* g_row = reinterpret_cast<const T*>(
-                         a.d_out + (place[b] / bt.h_q) * a.d_out_stride) + place[b] % bt.h_q * D;
+    const int64_t to = place(min(32 * b + i, max(my_rows - 1, 0)));
+    const T* q_row = reinterpret_cast<const T*>(a.q + to / bt.h_q * a.q_stride) + to % bt.h_q * D;
+    const T* g_row =
+        reinterpret_cast<const T*>(a.d_out + to / bt.h_q * a.d_out_stride) + to % bt.h_q * D;
 #pragma unroll 1
     for (int key0 = min_seen / 32 * 32; key0 < max_seen; key0 += 32) {
       auto at_key = [&](const char* base, int64_t stride, int key) INLINE {
@@ -314,6 +325,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
     }
     return x;
   };
+  char* mine = s_all[0] + 32 * NQ * wave * L::row_bytes;
 #pragma unroll
   for (int b = 0; b < NQ; ++b)
 #pragma unroll
@@ -321,13 +333,17 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
       settle(acc[b][c]);
       f32x16 x = acc[b][c];
       if (__builtin_expect(skipped, 0)) x = left_out(b, c, x);
-      if (32 * b + i < my_rows) {
 #pragma unroll
-        for (int r = 0; r < 16; r += 4)
-          store4<T>(a.dq + to[b], 32 * c + 2 * r + 4 * k,
-                    f32x4{x[r], x[r + 1], x[r + 2], x[r + 3]} * a.scale);
-      }
+      for (int r = 0; r < 16; r += 4)
+        put4<T, D>(mine, 32 * b + i, 32 * c + 2 * r + 4 * k,
+                   f32x4{x[r], x[r + 1], x[r + 2], x[r + 3]} * a.scale);
     }
+  store_rows<T, D>(mine, 32 * NQ, lane, [&](int x) INLINE {
+    if (x >= my_rows) return (char*)nullptr;
+    const int tok = token_of(bt, my_row0 + x);
+    return a.dq + (rows.start + tok) * a.dq_stride +
+           (int64_t)(head * bt.G + my_row0 + x - tok * bt.G) * L::row_bytes;
+  });
 }
 
 // ---------------------------------------------------------------------------
@@ -382,15 +398,30 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
     return key0 + 32 * (NK * wk + n) + (lane & 31);
   };
   u32x4 kk[NK][NW], vv[NK][NW];
+  {
+    using Keys = Direct<T, D, F::keys>;
+    static_assert(2 * F::keys <= 4 * RT, "room for K and V");
+    char *tile_k = s_rows[0], *tile_v = s_rows[0] + F::keys * L::row_bytes;
+    auto bring = [&](char* tile, const char* base, int64_t stride) INLINE {
+      const char* first = base + (keys.start + (int64_t)key0) * stride +
+                          (int64_t)head * L::row_bytes;
+      const Window from = window(first, (int64_t)(keys.n - key0) * stride);
 #pragma unroll
-  for (int n = 0; n < NK; ++n) {
-    const int64_t token = keys.start + min(key_of(n, lane), keys.n - 1);
+      for (int u = 0; u < Keys::units; ++u)
+        fetch(Keys::place(tile, wave, u), from,
+              Keys::row(tid, u) * (int)stride + Keys::byte(tid, u), 0);
+    };
+    bring(tile_k, a.k, a.k_stride);
+    bring(tile_v, a.v, a.v_stride);
+    arrived();
+    __syncthreads();
+    const RowReader<T, D> rd(i, k);
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const int64_t in = (int64_t)head * L::row_bytes + 32 * w + 16 * k;
-      kk[n][w] = *reinterpret_cast<const u32x4*>(a.k + token * a.k_stride + in);
-      vv[n][w] = *reinterpret_cast<const u32x4*>(a.v + token * a.v_stride + in);
-    }
+    for (int n = 0; n < NK; ++n)
+#pragma unroll
+      for (int w = 0; w < NW; ++w)
+        kk[n][w] = rd.get(tile_k, NK * wk + n, w), vv[n][w] = rd.get(tile_v, NK * wk + n, w);
+    __syncthreads();
   }
 
   f32x16 dk[NK][ND], dv[NK][ND];
@@ -468,12 +499,6 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
     arrived();
     __syncthreads();
   }
-  // (waited for here, not at their first use in the loop, whose waits would count the
-  // fetches too)
-#pragma unroll
-  for (int n = 0; n < NK; ++n)
-#pragma unroll
-    for (int w = 0; w < NW; ++w) asm volatile("" : "+v"(kk[n][w]), "+v"(vv[n][w]));
   {
     for (int t = r0; t < r1; ++t) {
       const int buf = t & 1, next = min(t + 1, r1 - 1);
@@ -677,54 +702,75 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
     }
     return x;
   };
-  // The row waves' sums: the others' to LDS, added by the first, which stores.
-  auto finish = [&](f32x16 (&acc)[NK][ND], bool is_dk) INLINE {
-    static_assert(WR == 1 || (WR == 2 && WK * 4096 * ND * NK <= 4 * kTile), "fits the rows' place");
-    const float by = is_dk ? a.scale : 1.f;
-    auto block = [&](int n, int c) INLINE {
-      settle(acc[n][c]);
-      f32x16 x = acc[n][c];
-      if (__builtin_expect(skipped, 0)) x = left_out(n, ND * wd + c, is_dk, x);
-      return x;
-    };
-    auto shared = [&](int n, int c) INLINE {
-      return reinterpret_cast<f32x4*>(s_rows[0]) + ((wk * NK + n) * ND + c) * 256 + lane;
-    };
-    if (wr == 1) {
+  // The row waves' sums, a block of keys at a time: the first is given the other's dK,
+  // the second the first's dV, each adds its own; then rows to memory.
+  constexpr int kBlock = ND * 4096;          // bytes of a block's sums
+  static_assert(WR == 1 || kWaves * kBlock <= 4 * kTile, "room for the sums");
+  static_assert(kWaves * 32 * NK * L::row_bytes <= 4 * kTile * WR * WD, "room for the results");
+  auto block = [&](f32x16& acc, int n, int c, bool is_dk) INLINE {
+    settle(acc);
+    f32x16 x = acc;
+    if (__builtin_expect(skipped, 0)) x = left_out(n, ND * wd + c, is_dk, x);
+    return x;
+  };
+  auto shared = [&](int to, int c) INLINE {
+    return reinterpret_cast<f32x4*>(s_rows[0] + (to * WK + wk) * kBlock + c * 4096) + lane;
+  };
+  auto finish = [&](int n, f32x16 (&mine)[ND], f32x16 (&theirs)[ND], bool is_dk) INLINE {
+    if constexpr (WR == 2) {
 #pragma unroll
-      for (int n = 0; n < NK; ++n)
+      for (int c = 0; c < ND; ++c) {
+        const f32x16 x = block(theirs[c], n, c, !is_dk);
 #pragma unroll
-        for (int c = 0; c < ND; ++c) {
-          const f32x16 x = block(n, c);
-#pragma unroll
-          for (int r = 0; r < 16; r += 4)
-            shared(n, c)[16 * r] = f32x4{x[r], x[r + 1], x[r + 2], x[r + 3]};
-        }
+        for (int r = 0; r < 16; r += 4)
+          shared(1 - wr, c)[16 * r] = f32x4{x[r], x[r + 1], x[r + 2], x[r + 3]};
+      }
+      __syncthreads();
     }
-    if (WR > 1) __syncthreads();
-    if (wr == 0) {
 #pragma unroll
-      for (int n = 0; n < NK; ++n) {
-        const int64_t token = keys.start + key_of(n, lane);
-        char* dst = (is_dk ? a.dk + token * a.dk_stride : a.dv + token * a.dv_stride) +
-                    (int64_t)head * L::row_bytes;
+    for (int c = 0; c < ND; ++c) {
+      mine[c] = block(mine[c], n, c, is_dk);
+      if constexpr (WR == 2) {
 #pragma unroll
-        for (int c = 0; c < ND; ++c) {
-          f32x16 x = block(n, c);
+        for (int r = 0; r < 16; r += 4) {
+          const f32x4 y = shared(wr, c)[16 * r];
 #pragma unroll
-          for (int r = 0; r < 16; r += 4) {
-            f32x4 y{x[r], x[r + 1], x[r + 2], x[r + 3]};
-            if (WR > 1) y += shared(n, c)[16 * r];
-            if (key_of(n, lane) < keys.n)
-              store4<T>(dst, 32 * (ND * wd + c) + 2 * r + 4 * k, y * by);
-          }
+          for (int e = 0; e < 4; ++e) mine[c][r + e] += y[e];
         }
       }
     }
-    if (WR > 1) __syncthreads();
+    if constexpr (WR == 2) __syncthreads();
+    // (waves that share keys have dimensions of their own, in one place)
+    char* tile = s_rows[0] + (WD > 1 ? 0 : wave) * 32 * L::row_bytes;
+#pragma unroll
+    for (int c = 0; c < ND; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        put4<T, D>(tile, i, 32 * (ND * wd + c) + 2 * r + 4 * k,
+                   f32x4{mine[c][r], mine[c][r + 1], mine[c][r + 2], mine[c][r + 3]} *
+                       (is_dk ? a.scale : 1.f));
+    if constexpr (WD > 1) __syncthreads();
+    if (wd == 0)
+      store_rows<T, D>(tile, 32, lane, [&](int x) INLINE {
+        const int key = key_of(n, x);
+        if (key >= keys.n) return (char*)nullptr;
+        const int64_t token = keys.start + key;
+        return (is_dk ? a.dk + token * a.dk_stride : a.dv + token * a.dv_stride) +
+               (int64_t)head * L::row_bytes;
+      });
+    __syncthreads();
   };
-  finish(dk, true);
-  finish(dv, false);
+#pragma unroll
+  for (int n = 0; n < NK; ++n) {
+    if constexpr (WR == 1) {
+      finish(n, dk[n], dv[n], true);
+      finish(n, dv[n], dk[n], false);
+    } else if (wr == 0) {
+      finish(n, dk[n], dv[n], true);
+    } else {
+      finish(n, dv[n], dk[n], false);
+    }
+  }
 }
 
 }  // namespace
