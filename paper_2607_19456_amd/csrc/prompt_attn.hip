@@ -56,7 +56,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   constexpr int NB = NQ == 2 ? 3 : 2;        // tiles in LDS
   // K's tiles, then V's; q on its way in, and out on its way out
   static_assert(2 * NB * kTile >= R * L::row_bytes, "room for the rows");
-  __shared__ __align__(16) char s_all[2 * NB][kTile];
+  __shared__ __align__(1024) char s_all[2 * NB][kTile];
   char(*s_k)[kTile] = s_all, (*s_v)[kTile] = s_all + NB;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -67,8 +67,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   Place at;
   if (!find(bt, true, R, blockIdx.x / bt.h_kv / a.splits, lane, &at)) return;
   const Span rows = at.rows, keys = at.keys;
-  // (the longest first)
-  const int row0 = (bt.causal ? at.tiles - 1 - at.tile : at.tile) * R;
+  const int row0 = at.after * R;             // the last rows, which see most, first
   const int in_tile = min(rows.n * bt.G - row0, R);
   const int min_seen = seen_by(bt, rows.n, keys.n, token_of(bt, row0));
   const int max_seen = seen_by(bt, rows.n, keys.n, token_of(bt, row0 + in_tile - 1));
@@ -507,7 +506,7 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(Batch bt, AttnAr
   Place at;
   if (!find(bt, true, R, item, lane, &at)) return;
   const Span rows = at.rows;
-  const int row0 = (bt.causal ? at.tiles - 1 - at.tile : at.tile) * R;
+  const int row0 = at.after * R;
   const int in_tile = min(rows.n * bt.G - row0, R);
   const int x = blockIdx.y * (kThreads / kPer) + tid / kPer, l = tid % kPer;
   if (x >= in_tile) return;

@@ -79,50 +79,80 @@ __device__ __forceinline__ int seen_by(const Batch& bt, int rows, int keys, int 
 }
 
 // Item `item` of the batch, items being tiles of R of each sequence's rows (times
-// G), or of its keys: its sequence's rows and keys, and its number there.  False
-// beyond the last.  The sequences are counted 64 at a time, a lane each.
+// G), or of its keys: its sequence's rows and keys, and how many more tiles follow it
+// there.  False beyond the last.  Items are in the order of that number, the largest
+// first: where a causal mask gives a tile work in proportion to it, the most work comes
+// first, whatever the sequences' lengths.  (Workgroups start in their order, each
+// shader engine's in turn: one that must wait for a busy engine holds up all behind
+// it, and with the sequences one after the other a batch of four ran 1.7 times as long
+// as its work.)  The sequences are counted 64 at a time, a lane each.
 struct Place {
   Span rows, keys;
-  int tile, tiles;
+  int after, tiles;
 };
+__device__ __forceinline__ int wave_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);   // row_shr:2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);   // row_shr:4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);   // row_shr:8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast:31
+  return __builtin_amdgcn_readlane(x, 63);
+}
 __device__ __forceinline__ bool find(const Batch& bt, bool by_rows, int R, int item, int lane,
                                      Place* at) {
   const int64_t per = by_rows ? bt.G : 1;
-  int left = item;
+  if (bt.B == 1) {
+    const Span r1 = span(bt.row_start, 0, bt.T, bt.rows), k1 = span(bt.key_start, 0, bt.N, bt.keys);
+    const int tiles = uniform((int)(((by_rows ? r1.n : k1.n) * per + R - 1) / R));
+    *at = {{uniform(r1.start), uniform(r1.n)}, {uniform(k1.start), uniform(k1.n)},
+           tiles - 1 - item, tiles};
+    return item < tiles;
+  }
+  auto look = [&](int b, Span* r, Span* k) INLINE {
+    *r = *k = {0, 0};
+    if (b < bt.B) {
+      *r = span(bt.row_start, b, bt.T, bt.rows);
+      *k = span(bt.key_start, b, bt.N, bt.keys);
+    }
+    return (int)(((by_rows ? r->n : k->n) * per + R - 1) / R);
+  };
+  Span r, k;
+  const int first = look(lane, &r, &k);      // tiles of the first 64 sequences
+  // items with more than m tiles after them
+  auto before = [&](int m) INLINE {
+    int x = max(first - 1 - m, 0);
+    for (int b = 64 + lane; b < bt.B; b += 64) {
+      Span r1, k1;
+      x += max(look(b, &r1, &k1) - 1 - m, 0);
+    }
+    return wave_sum(x);
+  };
+  // the least m for which no more than `item` items come before its own
+  int lo = 0, hi = (int)(((by_rows ? bt.T : bt.N) * per + R - 1) / R) - 1;
+  while (lo < hi) {
+    const int m = (lo + hi) >> 1;
+    if (before(m) <= item)
+      hi = m;
+    else
+      lo = m + 1;
+  }
+  int left = item - before(lo);
+  // the left-th of the sequences with more than m tiles
   for (int b0 = 0; b0 < bt.B; b0 += 64) {
-    if (!(by_rows ? bt.row_start : bt.key_start)) {
-      // as many of each: at once
-      const int tiles = (int)(((by_rows ? bt.T : bt.N) * per + R - 1) / R);
-      const int b = item / tiles;
-      if (b >= bt.B) return false;
-      const Span r = span(bt.row_start, b, bt.T, bt.rows), k = span(bt.key_start, b, bt.N, bt.keys);
-      *at = {{uniform(r.start), uniform(r.n)}, {uniform(k.start), uniform(k.n)}, item % tiles, tiles};
-      return true;
-    }
-    const bool there = b0 + lane < bt.B;
-    Span r{0, 0}, k{0, 0};
-    if (there) {
-      r = span(bt.row_start, b0 + lane, bt.T, bt.rows);
-      k = span(bt.key_start, b0 + lane, bt.N, bt.keys);
-    }
-    const int n = (int)(((by_rows ? r.n : k.n) * per + R - 1) / R);
-    int upto = n;
-#pragma unroll
-    for (int step = 1; step < 64; step *= 2) {
-      const int x = __shfl_up(upto, step);
-      if (lane >= step) upto += x;
-    }
-    const int all = __builtin_amdgcn_readlane(upto, 63);
-    if (left < all) {
-      const int l = __ffsll((unsigned long long)__ballot(upto > left)) - 1;
-      const int tiles = __builtin_amdgcn_readlane(n, l);
+    const int n = b0 ? look(b0 + lane, &r, &k) : first;
+    const uint64_t has = __ballot(n > lo);
+    const int here = (int)__popcll(has);
+    if (left < here) {
+      const bool me = n > lo && (int)__popcll(has & ((uint64_t(1) << lane) - 1)) == left;
+      const int l = __ffsll((unsigned long long)__ballot(me)) - 1;
       *at = {{__builtin_amdgcn_readlane(r.start, l), __builtin_amdgcn_readlane(r.n, l)},
              {__builtin_amdgcn_readlane(k.start, l), __builtin_amdgcn_readlane(k.n, l)},
-             left - (__builtin_amdgcn_readlane(upto, l) - tiles),
-             tiles};
+             lo,
+             __builtin_amdgcn_readlane(n, l)};
       return true;
     }
-    left -= all;
+    left -= here;
   }
   return false;
 }
@@ -226,19 +256,18 @@ __device__ __forceinline__ int ordered_row(int i) {
 __device__ __forceinline__ int row_of(int r, int k) { return 16 * (r / 8) + 8 * k + r % 8; }
 
 // Reading a tile by rows (operand of a product over D): this lane's row of a
-// block of 32, chunk 2w + k.
+// block of 32, chunk 2w + k.  The turn and the chunk's number meet in an XOR, so one
+// register holds all of a lane's addresses.  (Tiles begin at multiples of 1 KB.)
 template <class T, int D>
 struct RowReader {
   using L = Tile<T, D>;
-  static constexpr int N = L::NW < 8 ? L::NW : 8;
-  int off[N];
-  __device__ __forceinline__ RowReader(int row, int k) {
-#pragma unroll
-    for (int w = 0; w < N; ++w) off[w] = L::at(row, 2 * w + k);
-  }
+  int off;
+  __device__ __forceinline__ RowReader(int row, int k) : off(L::at(row, k)) {}
   __device__ __forceinline__ u32x4 get(const char* tile, int block, int w) const {
-    return *reinterpret_cast<const u32x4*>(tile + off[w % N] + (w / N) * 256 +
-                                           block * 32 * L::row_bytes);
+    typedef __attribute__((address_space(3))) const char* lds;
+    typedef __attribute__((address_space(3))) const u32x4* lds16;
+    return *(lds16)((lds)(uintptr_t)(((uint32_t)(uintptr_t)(lds)tile + off) ^ (w << 5)) +
+                    block * 32 * L::row_bytes);
   }
 };
 
@@ -247,28 +276,22 @@ struct RowReader {
 template <class T, int D>
 struct ColumnReader {
   using L = Tile<T, D>;
-  static constexpr int N = L::ND < 4 ? L::ND : 4;
-  int off[N][2];
-  __device__ __forceinline__ ColumnReader(int lane) {
-    const int i = lane & 31, k = lane >> 5;
-#pragma unroll
-    for (int c = 0; c < N; ++c)
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-        off[c][j] = L::at(8 * k + 4 * j + (lane >> 2 & 3), 4 * c + 2 * (i >> 4) + (lane >> 1 & 1)) +
-                    8 * (lane & 1);
-  }
+  int off;
+  __device__ __forceinline__ ColumnReader(int lane)
+      : off(L::at(8 * (lane >> 5) + (lane >> 2 & 3), 2 * (lane >> 4 & 1) + (lane >> 1 & 1)) +
+            8 * (lane & 1)) {}
   __device__ __forceinline__ u32x4 get(const char* tile, int h, int c) const {
     // (16 lanes at 8 bytes each hold a matrix of 4 rows by 16 columns; a lane
     // gets one column of it)
-    typedef __attribute__((address_space(3))) s16x4* lds;
+    typedef __attribute__((address_space(3))) const char* lds;
+    typedef __attribute__((address_space(3))) s16x4* lds8;
     u32x2 x[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j)
       x[j] = __builtin_bit_cast(
-          u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                     (lds)(const_cast<char*>(tile) + off[c % N][j] + (c / N) * 256 +
-                           h * 16 * L::row_bytes)));
+          u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds8)(
+                     (lds)(uintptr_t)(((uint32_t)(uintptr_t)(lds)tile + off) ^ (c << 6 | j << 4)) +
+                     (16 * h + 4 * j) * L::row_bytes)));
     return u32x4{x[0][0], x[0][1], x[1][0], x[1][1]};
   }
 };

@@ -63,11 +63,11 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
 
   // K's tiles, then V's; Q and dO on their way in, and dQ on its way out
   static_assert(2 * NB * kTile >= R * L::row_bytes, "room for the rows");
-  __shared__ __align__(16) char s_all[2 * NB][kTile];
+  __shared__ __align__(1024) char s_all[2 * NB][kTile];
   char(*s_k)[kTile] = s_all, (*s_v)[kTile] = s_all + NB;
   // 32 rows of zeros, where there is room
   constexpr bool kZeros = 2 * NB * kTile + 32 * L::row_bytes < 160 << 10;
-  __shared__ __align__(16) char s_zero[kZeros ? 32 * L::row_bytes : 16];
+  __shared__ __align__(1024) char s_zero[kZeros ? 32 * L::row_bytes : 16];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int i = lane & 31, k = lane >> 5;
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
   Place at;
   if (!find(bt, true, R, blockIdx.x / bt.h_kv, lane, &at)) return;
   const Span rows = at.rows, keys = at.keys;
-  const int row0 = (bt.causal ? at.tiles - 1 - at.tile : at.tile) * R;
+  const int row0 = at.after * R;             // the last rows, which see most, first
   const int in_tile = min(rows.n * bt.G - row0, R);
   const int min_seen = seen_by(bt, rows.n, keys.n, token_of(bt, row0));
   const int max_seen = seen_by(bt, rows.n, keys.n, token_of(bt, row0 + in_tile - 1));
@@ -288,61 +288,89 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
     __syncthreads();
   }
 
-  // The keys that were left out, those alone that the row sees: what they add to block
-  // c of row block b.
-  auto left_out = [&](int b, int c, f32x16 x) INLINE {
-    const int64_t to = place(min(32 * b + i, max(my_rows - 1, 0)));
-    const T* q_row = reinterpret_cast<const T*>(a.q + to / bt.h_q * a.q_stride) + to % bt.h_q * D;
-    const T* g_row =
-        reinterpret_cast<const T*>(a.d_out + to / bt.h_q * a.d_out_stride) + to % bt.h_q * D;
-#pragma unroll 1
-    for (int key0 = min_seen / 32 * 32; key0 < max_seen; key0 += 32) {
-      auto at_key = [&](const char* base, int64_t stride, int key) INLINE {
-        return reinterpret_cast<const T*>(base + key * stride);
-      };
-      bool bad = false;
-      if (key0 + i < keys.n) {
-        const T* row = at_key(k_base, a.k_stride, key0 + i);
-#pragma unroll 1
-        for (int d = k; d < D; d += 2) bad = bad || !(fabsf((float)row[d]) < INFINITY);
-      }
-      if (!__any(bad)) continue;
-#pragma unroll 1
-      for (int key = key0; key < min(key0 + 32, seen[b]); ++key) {
-        const T* k_row = at_key(k_base, a.k_stride, key);
-        const T* v_row = at_key(v_base, a.v_stride, key);
-        float s = 0.f, dp = 0.f;
-#pragma unroll 1
-        for (int d = 0; d < D; ++d) {
-          s += (float)q_row[d] * (float)k_row[d];
-          dp += (float)g_row[d] * (float)v_row[d];
-        }
-        float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s, a.scale2, -lse2[b])) * (dp - delta[b]);
-        if constexpr (!is_f32<T>) w = (float)(T)w;
+  char* mine = s_all[0] + 32 * NQ * wave * L::row_bytes;
+  auto to = [&](int x) INLINE {              // the place of this wave's row x
+    const int tok = token_of(bt, my_row0 + x);
+    return a.dq + (rows.start + tok) * a.dq_stride +
+           (int64_t)(head * bt.G + my_row0 + x - tok * bt.G) * L::row_bytes;
+  };
+  // The keys that were left out, those alone that the row sees: the sums pass through
+  // LDS in 32 bits, 32 rows of one wave at a time.
+  if (__builtin_expect(skipped, 0)) {
+    static_assert(2 * NB * kTile >= 32 * D * 4, "room for the sums");
+    float* sums = reinterpret_cast<float*>(s_all[0]) + i * D;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] += w * (float)k_row[32 * c + 8 * (r / 4) + 4 * k + r % 4];
+    for (int b = 0; b < NQ; ++b)
+#pragma unroll
+      for (int c = 0; c < ND; ++c) settle(acc[b][c]);
+    for (int w = 0; w < kWaves; ++w) {
+#pragma unroll
+      for (int b = 0; b < NQ; ++b) {
+        __syncthreads();
+        if (w != wave) continue;
+#pragma unroll
+        for (int c = 0; c < ND; ++c)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            sums[32 * c + 8 * (r / 4) + 4 * k + r % 4] = acc[b][c][r];
+        __builtin_amdgcn_wave_barrier();
+        const int64_t at_row = place(min(32 * b + i, max(my_rows - 1, 0)));
+        const T* q_row =
+            reinterpret_cast<const T*>(a.q + at_row / bt.h_q * a.q_stride) + at_row % bt.h_q * D;
+        const T* g_row = reinterpret_cast<const T*>(a.d_out + at_row / bt.h_q * a.d_out_stride) +
+                         at_row % bt.h_q * D;
+#pragma unroll 1
+        for (int key0 = min_seen / 32 * 32; key0 < max_seen; key0 += 32) {
+          auto row_at = [&](const char* base, int64_t stride, int key) INLINE {
+            return reinterpret_cast<const T*>(base + key * stride);
+          };
+          bool bad = false;
+          if (key0 + i < keys.n) {
+            const T* row = row_at(k_base, a.k_stride, key0 + i);
+#pragma unroll 1
+            for (int d = k; d < D; d += 2) bad = bad || !(fabsf((float)row[d]) < INFINITY);
+          }
+          if (!__any(bad)) continue;
+#pragma unroll 1
+          for (int key = key0; key < min(key0 + 32, seen[b]); ++key) {
+            const T* k_row = row_at(k_base, a.k_stride, key);
+            const T* v_row = row_at(v_base, a.v_stride, key);
+            float s = 0.f, dp = 0.f;
+#pragma unroll 1
+            for (int d = 0; d < D; ++d) {
+              s += (float)q_row[d] * (float)k_row[d];
+              dp += (float)g_row[d] * (float)v_row[d];
+            }
+            float x =
+                __builtin_amdgcn_exp2f(__builtin_fmaf(s, a.scale2, -lse2[b])) * (dp - delta[b]);
+            if constexpr (!is_f32<T>) x = (float)(T)x;
+#pragma unroll 1
+            for (int d = k; d < D; d += 2) sums[d] += x * (float)k_row[d];
+          }
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (32 * b + i < my_rows) {
+          T* dst = reinterpret_cast<T*>(to(32 * b + i));
+#pragma unroll 1
+          for (int d = k; d < D; d += 2) dst[d] = (T)(sums[d] * a.scale);
+        }
       }
     }
-    return x;
-  };
-  char* mine = s_all[0] + 32 * NQ * wave * L::row_bytes;
+    return;
+  }
 #pragma unroll
   for (int b = 0; b < NQ; ++b)
 #pragma unroll
     for (int c = 0; c < ND; ++c) {
       settle(acc[b][c]);
-      f32x16 x = acc[b][c];
-      if (__builtin_expect(skipped, 0)) x = left_out(b, c, x);
 #pragma unroll
       for (int r = 0; r < 16; r += 4)
         put4<T, D>(mine, 32 * b + i, 32 * c + 2 * r + 4 * k,
-                   f32x4{x[r], x[r + 1], x[r + 2], x[r + 3]} * a.scale);
+                   f32x4{acc[b][c][r], acc[b][c][r + 1], acc[b][c][r + 2], acc[b][c][r + 3]} *
+                       a.scale);
     }
   store_rows<T, D>(mine, 32 * NQ, lane, [&](int x) INLINE {
-    if (x >= my_rows) return (char*)nullptr;
-    const int tok = token_of(bt, my_row0 + x);
-    return a.dq + (rows.start + tok) * a.dq_stride +
-           (int64_t)(head * bt.G + my_row0 + x - tok * bt.G) * L::row_bytes;
+    return x < my_rows ? to(x) : nullptr;
   });
 }
 
@@ -372,11 +400,12 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
   constexpr int NW = L::NW, ND = L::ND / WD;
   constexpr int kTile = RT * L::row_bytes;
 
-  __shared__ __align__(16) char s_rows[4][kTile];             // Q's two tiles, dO's two
+  __shared__ __align__(1024) char s_rows[4][kTile];             // Q's two tiles, dO's two
   __shared__ __align__(16) float s_lse[2][RT], s_delta[2][RT];
   // 32 rows of zeros, where there is room
   constexpr bool kZeros = 4 * kTile + 16 * RT + 32 * L::row_bytes < 160 << 10;
-  __shared__ __align__(16) char s_zero[kZeros ? 32 * L::row_bytes : 16];
+  __shared__ int s_skipped;
+  __shared__ __align__(1024) char s_zero[kZeros ? 32 * L::row_bytes : 16];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int i = lane & 31, k = lane >> 5;
@@ -386,7 +415,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
   if (!find(bt, false, F::keys, blockIdx.x / bt.h_kv, lane, &at)) return;
   const Span rows = at.rows, keys = at.keys;
   const int end = rows.n * bt.G;
-  const int key0 = at.tile * F::keys;
+  const int key0 = (at.tiles - 1 - at.after) * F::keys;
   // the first row (token and head) that sees a key
   auto first_row = [&](int key) INLINE {
     return bt.causal ? (int)min((int64_t)max(key - keys.n + rows.n, 0) * bt.G, (int64_t)end) : 0;
@@ -488,6 +517,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
   // Not all rows of a step see all keys, and what they do not see is masked.
   auto partial = [&](int t) INLINE { return t * RT < all_from || (t + 1) * RT > end; };
   bool skipped = false;
+  if (tid == 0) s_skipped = 0;
   if (kZeros)
     for (int x = tid; x < 32 * L::chunks; x += kThreads)
       reinterpret_cast<u32x4*>(s_zero)[x] = u32x4{0u, 0u, 0u, 0u};
@@ -657,9 +687,16 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
     }
   }
 
-  // The rows that were left out, pair by pair, those alone that see the key: what they
-  // add to block c of key n's dK or dV.
-  auto left_out = [&](int n, int c, bool is_dk, f32x16 x) INLINE {
+  // The row waves' sums, a block of keys at a time: the first is given the other's dK,
+  // the second the first's dV, each adds its own; then rows to memory.
+  constexpr int kBlock = ND * 4096;          // bytes of a block's sums
+  static_assert(kWaves * 32 * D * 4 / WD <= 4 * kTile && kWaves * kBlock <= 4 * kTile * WD,
+                "room for the sums");
+  static_assert(kWaves * 32 * NK * L::row_bytes <= 4 * kTile * WR * WD, "room for the results");
+  if (skipped) s_skipped = 1;
+  // The rows that were left out, pair by pair, those alone that see the key: added to
+  // the sums [32 keys][D] that lie in LDS.
+  auto left_out = [&](int n, bool is_dk, float* sums) INLINE {
     const int64_t token = keys.start + min(key_of(n, lane), keys.n - 1);
     const int from = first_row(min(key_of(n, lane), keys.n - 1));
     const T* k_row = reinterpret_cast<const T*>(a.k + token * a.k_stride) + head * D;
@@ -674,9 +711,8 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
       st = a.stats[to * bt.h_q + h];
     };
 #pragma unroll 1
-    for (int t = r0; t < r1; ++t) {
-      if (!partial(t)) continue;
-      const int row0 = t * RT + 32 * wr;
+    for (int row0 = r0 * RT; row0 < end; row0 += 32) {
+      if (!partial(row0 / RT)) continue;
       at_row(min(row0 + i, end - 1));
       bool bad = st[0] != st[0] || !(fabsf(st[1]) < INFINITY);
 #pragma unroll 1
@@ -696,22 +732,10 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
         if (is_dk) w *= dp - st[1];
         if constexpr (!is_f32<T>) w = (float)(T)w;
         const T* of = is_dk ? q : g;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] += w * (float)of[32 * c + 8 * (r / 4) + 4 * k + r % 4];
+#pragma unroll 1
+        for (int d = k; d < D; d += 2) sums[i * D + d] += w * (float)of[d];
       }
     }
-    return x;
-  };
-  // The row waves' sums, a block of keys at a time: the first is given the other's dK,
-  // the second the first's dV, each adds its own; then rows to memory.
-  constexpr int kBlock = ND * 4096;          // bytes of a block's sums
-  static_assert(WR == 1 || kWaves * kBlock <= 4 * kTile, "room for the sums");
-  static_assert(kWaves * 32 * NK * L::row_bytes <= 4 * kTile * WR * WD, "room for the results");
-  auto block = [&](f32x16& acc, int n, int c, bool is_dk) INLINE {
-    settle(acc);
-    f32x16 x = acc;
-    if (__builtin_expect(skipped, 0)) x = left_out(n, ND * wd + c, is_dk, x);
-    return x;
   };
   auto shared = [&](int to, int c) INLINE {
     return reinterpret_cast<f32x4*>(s_rows[0] + (to * WK + wk) * kBlock + c * 4096) + lane;
@@ -720,7 +744,8 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
     if constexpr (WR == 2) {
 #pragma unroll
       for (int c = 0; c < ND; ++c) {
-        const f32x16 x = block(theirs[c], n, c, !is_dk);
+        settle(theirs[c]);
+        const f32x16 x = theirs[c];
 #pragma unroll
         for (int r = 0; r < 16; r += 4)
           shared(1 - wr, c)[16 * r] = f32x4{x[r], x[r + 1], x[r + 2], x[r + 3]};
@@ -729,7 +754,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
     }
 #pragma unroll
     for (int c = 0; c < ND; ++c) {
-      mine[c] = block(mine[c], n, c, is_dk);
+      settle(mine[c]);
       if constexpr (WR == 2) {
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
@@ -739,7 +764,29 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
         }
       }
     }
-    if constexpr (WR == 2) __syncthreads();
+    __syncthreads();
+    const float by = is_dk ? a.scale : 1.f;
+    if (__builtin_expect(uniform(s_skipped), 0)) {
+      float* sums = reinterpret_cast<float*>(s_rows[0]) + (WD > 1 ? 0 : wave) * 32 * D;
+#pragma unroll
+      for (int c = 0; c < ND; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          sums[i * D + 32 * (ND * wd + c) + 8 * (r / 4) + 4 * k + r % 4] = mine[c][r];
+      __syncthreads();
+      if (wd == 0) {
+        left_out(n, is_dk, sums);
+        const int64_t token = keys.start + key_of(n, lane);
+        if (key_of(n, lane) < keys.n) {
+          T* dst = reinterpret_cast<T*>(is_dk ? a.dk + token * a.dk_stride
+                                              : a.dv + token * a.dv_stride) + head * D;
+#pragma unroll 1
+          for (int d = k; d < D; d += 2) dst[d] = (T)(sums[i * D + d] * by);
+        }
+      }
+      __syncthreads();
+      return;
+    }
     // (waves that share keys have dimensions of their own, in one place)
     char* tile = s_rows[0] + (WD > 1 ? 0 : wave) * 32 * L::row_bytes;
 #pragma unroll
@@ -748,7 +795,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
       for (int r = 0; r < 16; r += 4)
         put4<T, D>(tile, i, 32 * (ND * wd + c) + 2 * r + 4 * k,
                    f32x4{mine[c][r], mine[c][r + 1], mine[c][r + 2], mine[c][r + 3]} *
-                       (is_dk ? a.scale : 1.f));
+                       by);
     if constexpr (WD > 1) __syncthreads();
     if (wd == 0)
       store_rows<T, D>(tile, 32, lane, [&](int x) INLINE {
