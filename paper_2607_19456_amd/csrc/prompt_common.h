@@ -393,6 +393,21 @@ __device__ __forceinline__ void fetch(int place, const Window& from, int lane_by
                : "m0");
 #pragma clang diagnostic pop
 }
+// The same of one word a lane: 256 bytes in turn.
+__device__ __forceinline__ void fetch_word(int place, const Window& from, int lane_byte) {
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+               :
+               : "s"(place), "v"(lane_byte), "s"(from.words)
+               : "m0");
+#pragma clang diagnostic pop
+}
+__device__ __forceinline__ int lds_place(const void* p) {
+  typedef __attribute__((address_space(3))) const char* lds;
+  return uniform((int)(uintptr_t)(lds)(const char*)p);
+}
+
 // All fetches but the last `more` have arrived.
 template <int more = 0>
 __device__ __forceinline__ void arrived() {

@@ -26,7 +26,8 @@ struct GradArgs {
   int64_t q_stride, k_stride, v_stride, d_out_stride;     // bytes between tokens
   int64_t dq_stride, dk_stride, dv_stride;
   float scale, scale2;          // and times log2(e)
-  f32x2* stats;                 // [rows][h_q]: lse times log2(e) (+infinity: no weights), delta
+  // [rows][h_q] each: lse times log2(e) (+infinity: no weights), and delta
+  float *lse2, *delta;
 };
 
 template <class T>
@@ -124,7 +125,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
         seen[b] = seen_by(bt, rows.n, keys.n, token_of(bt, my_row0 + x));
         const float lse = far_load<float>(a.lse + place(x));
         lse2[b] = lse == -INFINITY ? INFINITY : lse * kLog2e;
-        if (k == 0) a.stats[place(x)] = f32x2{lse2[b], delta[b]};
+        if (k == 0) a.lse2[place(x)] = lse2[b], a.delta[place(x)] = delta[b];
       }
     }
     __syncthreads();
@@ -400,10 +401,12 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
   constexpr int NW = L::NW, ND = L::ND / WD;
   constexpr int kTile = RT * L::row_bytes;
 
-  __shared__ __align__(1024) char s_rows[4][kTile];             // Q's two tiles, dO's two
-  __shared__ __align__(16) float s_lse[2][RT], s_delta[2][RT];
+  // Steps in LDS: two on their way where there is room for them.
+  constexpr int NB = 6 * kTile + 32 * L::row_bytes < 150 << 10 ? 3 : 2;
+  __shared__ __align__(1024) char s_rows[2 * NB][kTile];        // Q's tiles, dO's tiles
+  __shared__ __align__(16) float s_lse[NB][64], s_delta[NB][64];
   // 32 rows of zeros, where there is room
-  constexpr bool kZeros = 4 * kTile + 16 * RT + 32 * L::row_bytes < 160 << 10;
+  constexpr bool kZeros = 2 * NB * kTile + NB * 512 + 32 * L::row_bytes < 160 << 10;
   __shared__ int s_skipped;
   __shared__ __align__(1024) char s_zero[kZeros ? 32 * L::row_bytes : 16];
 
@@ -429,7 +432,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
   u32x4 kk[NK][NW], vv[NK][NW];
   {
     using Keys = Direct<T, D, F::keys>;
-    static_assert(2 * F::keys <= 4 * RT, "room for K and V");
+    static_assert(2 * F::keys <= 2 * NB * RT, "room for K and V");
     char *tile_k = s_rows[0], *tile_v = s_rows[0] + F::keys * L::row_bytes;
     auto bring = [&](char* tile, const char* base, int64_t stride) INLINE {
       const char* first = base + (keys.start + (int64_t)key0) * stride +
@@ -480,15 +483,25 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
     const int in = (Fetch::row(tid, 0) - tok * bt.G) * L::row_bytes + Fetch::byte(tid, 0);
     q_byte = tok * (int)a.q_stride + in, g_byte = tok * (int)a.d_out_stride + in;
   }
+  const float* stats = wave & 1 ? a.delta : a.lse2;          // (two waves bring each)
   auto load_rows = [&](int t) INLINE {
+    {
+      const int x0 = min(t * RT, end - 1), tok0 = token_of(bt, x0);
+      const int x = min(t * RT + lane, end - 1), tok = token_of(bt, x);
+      const Window from = window(reinterpret_cast<const char*>(
+                                     stats + (int64_t)(rows.start + tok0) * bt.h_q + head * bt.G),
+                                 0x7fffffff);
+      fetch_word(lds_place(wave & 1 ? s_delta[t % NB] : s_lse[t % NB]), from,
+                 4 * ((tok - tok0) * bt.h_q + x - tok * bt.G));
+    }
     const Window from_q = window_of(a.q, a.q_stride, t);
     const Window from_g = window_of(a.d_out, a.d_out_stride, t);
     if (even) {
       const int tokens = token_of(bt, Fetch::step);
 #pragma unroll
       for (int u = 0; u < Fetch::units; ++u) {
-        fetch(Fetch::place(s_rows[t & 1], wave, u), from_q, q_byte, u * tokens * (int)a.q_stride);
-        fetch(Fetch::place(s_rows[2 + (t & 1)], wave, u), from_g, g_byte,
+        fetch(Fetch::place(s_rows[t % NB], wave, u), from_q, q_byte, u * tokens * (int)a.q_stride);
+        fetch(Fetch::place(s_rows[NB + t % NB], wave, u), from_g, g_byte,
               u * tokens * (int)a.d_out_stride);
       }
       return;
@@ -498,21 +511,10 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
     for (int u = 0; u < Fetch::units; ++u) {
       const int x = min(t * RT + Fetch::row(tid, u), end - 1), tok = token_of(bt, x);
       const int in = (x - tok * bt.G) * L::row_bytes + Fetch::byte(tid, u);
-      fetch(Fetch::place(s_rows[t & 1], wave, u), from_q, (tok - tok0) * (int)a.q_stride + in, 0);
-      fetch(Fetch::place(s_rows[2 + (t & 1)], wave, u), from_g,
+      fetch(Fetch::place(s_rows[t % NB], wave, u), from_q, (tok - tok0) * (int)a.q_stride + in, 0);
+      fetch(Fetch::place(s_rows[NB + t % NB], wave, u), from_g,
             (tok - tok0) * (int)a.d_out_stride + in, 0);
     }
-  };
-  f32x2 stat{INFINITY, 0.f};
-  auto load_stats = [&](int t) INLINE {
-    if (tid < RT) {
-      const int x = min(t * RT + tid, end - 1), tok = token_of(bt, x);
-      stat = far_load<f32x2>(a.stats + (int64_t)(rows.start + tok) * bt.h_q + head * bt.G + x -
-                             tok * bt.G);
-    }
-  };
-  auto store_stats = [&](int t) INLINE {
-    if (tid < RT) s_lse[t & 1][tid] = stat[0], s_delta[t & 1][tid] = stat[1];
   };
   // Not all rows of a step see all keys, and what they do not see is masked.
   auto partial = [&](int t) INLINE { return t * RT < all_from || (t + 1) * RT > end; };
@@ -523,55 +525,61 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
       reinterpret_cast<u32x4*>(s_zero)[x] = u32x4{0u, 0u, 0u, 0u};
 
   if (r0 < r1) {
-    load_rows(r0);
-    load_stats(r0);
-    store_stats(r0);
+#pragma unroll
+    for (int t = 0; t < NB - 1; ++t) load_rows(min(r0 + t, r1 - 1 + NB));
     arrived();
     __syncthreads();
   }
   {
     for (int t = r0; t < r1; ++t) {
-      const int buf = t & 1, next = min(t + 1, r1 - 1);
+      const int buf = t % NB;
       const char *tile_q = s_rows[buf] + 32 * wr * L::row_bytes;
-      const char *tile_g = s_rows[2 + buf] + 32 * wr * L::row_bytes;
+      const char *tile_g = s_rows[NB + buf] + 32 * wr * L::row_bytes;
       const float *my_lse = &s_lse[buf][32 * wr], *my_delta = &s_delta[buf][32 * wr];
       const int row0 = t * RT + 32 * wr;
-      load_stats(next);
       f32x16 s[NK], dp[NK];
 #pragma unroll
       for (int n = 0; n < NK; ++n)
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[n][r] = 0.f, dp[n][r] = 0.f;
-      // S, and the next rows' fetches
       {
-        u32x4 x = read.get(tile_q, 0, 0);
+        // S, and the fetches of rows to come; operands are read two products ahead
+        auto by_rows = [&](int w) INLINE {
+          return w < NW ? read.get(tile_q, 0, w) : read.get(tile_g, 0, w - NW);
+        };
+        auto lse_of = [&](int r) INLINE {
+          return *reinterpret_cast<const f32x4*>(my_lse + row_of(r, k));
+        };
+        u32x4 x0 = by_rows(0), x1 = by_rows(1);
+        f32x4 z = lse_of(0);
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-          const u32x4 y = read.get(w + 1 < NW ? tile_q : tile_g, 0, w + 1 < NW ? w + 1 : 0);
+          const u32x4 x2 = by_rows(w + 2);
 #pragma unroll
-          for (int n = 0; n < NK; ++n) s[n] = mma<T>(x, kk[n][w], s[n]);
-          if (w == 0) load_rows(next);
-          x = y;
+          for (int n = 0; n < NK; ++n) s[n] = mma<T>(x0, kk[n][w], s[n]);
+          if (w == 0) load_rows(t + NB - 1);
+          x0 = x1, x1 = x2;
           __builtin_amdgcn_sched_barrier(0);
         }
         // dP, and P
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-          u32x4 y = x;
-          if (w + 1 < NW) y = read.get(tile_g, 0, w + 1);
+          u32x4 x2 = x0;
+          if (w + 2 < NW) x2 = by_rows(NW + w + 2);
 #pragma unroll
-          for (int n = 0; n < NK; ++n) dp[n] = mma<T>(x, vv[n][w], dp[n]);
+          for (int n = 0; n < NK; ++n) dp[n] = mma<T>(x0, vv[n][w], dp[n]);
           if (4 * w % NW == 0) {
             const int r = 16 * w / NW;
-            const f32x4 z = *reinterpret_cast<const f32x4*>(my_lse + row_of(r, k));
+            const f32x4 z1 = r + 4 < 16 ? lse_of(r + 4) : z;
 #pragma unroll
             for (int n = 0; n < NK; ++n)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
                 s[n][r + e] =
                     __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r + e], a.scale2, -z[e]));
+            z = z1;
           }
-          x = y;
+          x0 = x1, x1 = x2;
           if (4 * (w + 1) % NW == 0) __builtin_amdgcn_sched_barrier(0);
         }
       }
@@ -593,7 +601,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
           } else {
             for (int x = lane; x < 32 * L::chunks; x += 64)
               reinterpret_cast<u32x4*>(s_rows[buf] + 32 * wr * L::row_bytes)[x] =
-                  reinterpret_cast<u32x4*>(s_rows[2 + buf] + 32 * wr * L::row_bytes)[x] =
+                  reinterpret_cast<u32x4*>(s_rows[NB + buf] + 32 * wr * L::row_bytes)[x] =
                       u32x4{0u, 0u, 0u, 0u};
             s_delta[buf][32 * wr + i] = 0.f;
           }
@@ -635,54 +643,55 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
         }
       } else {
         u32x4 p[NK], ds[2][NK];
-        u32x4 x = read_columns.get(columns_g, 0, 0);
+        auto by_columns = [&](int e) INLINE {
+          return read_columns.get(e < 2 * ND ? columns_g : columns_q, e / ND % 2, e % ND);
+        };
+        auto delta_of = [&](int r) INLINE {
+          return *reinterpret_cast<const f32x4*>(deltas + row_of(r, k));
+        };
+        u32x4 x0 = by_columns(0), x1 = by_columns(1);
+        f32x4 z = delta_of(0);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int e = 0; e < 2 * ND; ++e) {
+          const int h = e / ND, c = e % ND;
+          if (c == 0) {
 #pragma unroll
-          for (int n = 0; n < NK; ++n)
+            for (int n = 0; n < NK; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              p[n][e] = pack2<T>(s[n][8 * h + 2 * e], s[n][8 * h + 2 * e + 1]);
-#pragma unroll
-          for (int c = 0; c < ND; ++c) {
-            const bool last = c + 1 == ND;
-            const u32x4 y = last ? read_columns.get(h == 0 ? columns_g : columns_q, h == 0 ? 1 : 0, 0)
-                                 : read_columns.get(columns_g, h, c + 1);
-#pragma unroll
-            for (int n = 0; n < NK; ++n) mma_far<T>(x, p[n], dv[n][c]);
-            if (2 * c % ND == 0) {
-              const int r = 8 * c / ND;
-              const f32x4 z = *reinterpret_cast<const f32x4*>(deltas + row_of(8 * h + r, k));
-#pragma unroll
-              for (int n = 0; n < NK; ++n) {
-                float e4[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  e4[e] = s[n][8 * h + r + e] * (dp[n][8 * h + r + e] - z[e]);
-                ds[h][n][r / 2] = pack2<T>(e4[0], e4[1]);
-                ds[h][n][r / 2 + 1] = pack2<T>(e4[2], e4[3]);
-              }
-            }
-            x = y;
-            __builtin_amdgcn_sched_barrier(0);
+              for (int w = 0; w < 4; ++w)
+                p[n][w] = pack2<T>(s[n][8 * h + 2 * w], s[n][8 * h + 2 * w + 1]);
           }
+          const u32x4 x2 = by_columns(e + 2);
+#pragma unroll
+          for (int n = 0; n < NK; ++n) mma_far<T>(x0, p[n], dv[n][c]);
+          if (2 * c % ND == 0) {
+            const int r = 8 * h + 8 * c / ND;
+            const f32x4 z1 = r + 4 < 16 ? delta_of(r + 4) : z;
+#pragma unroll
+            for (int n = 0; n < NK; ++n) {
+              float x[4];
+#pragma unroll
+              for (int w = 0; w < 4; ++w) x[w] = s[n][r + w] * (dp[n][r + w] - z[w]);
+              ds[h][n][r % 8 / 2] = pack2<T>(x[0], x[1]);
+              ds[h][n][r % 8 / 2 + 1] = pack2<T>(x[2], x[3]);
+            }
+            z = z1;
+          }
+          x0 = x1, x1 = x2;
+          __builtin_amdgcn_sched_barrier(0);
         }
         // dK
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int e = 0; e < 2 * ND; ++e) {
+          u32x4 x2 = x0;
+          if (e + 2 < 2 * ND) x2 = by_columns(2 * ND + e + 2);
 #pragma unroll
-          for (int c = 0; c < ND; ++c) {
-            u32x4 y = x;
-            if (h == 0 || c + 1 < ND)
-              y = read_columns.get(columns_q, c + 1 < ND ? h : 1, c + 1 < ND ? c + 1 : 0);
-#pragma unroll
-            for (int n = 0; n < NK; ++n) mma_far<T>(x, ds[h][n], dk[n][c]);
-            x = y;
-            __builtin_amdgcn_sched_barrier(0);
-          }
+          for (int n = 0; n < NK; ++n) mma_far<T>(x0, ds[e / ND][n], dk[n][e % ND]);
+          x0 = x1, x1 = x2;
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
-      store_stats(next);
-      arrived();
+      arrived<(2 * Fetch::units + 1) * (NB - 2)>();
       __syncthreads();
     }
   }
@@ -690,9 +699,9 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
   // The row waves' sums, a block of keys at a time: the first is given the other's dK,
   // the second the first's dV, each adds its own; then rows to memory.
   constexpr int kBlock = ND * 4096;          // bytes of a block's sums
-  static_assert(kWaves * 32 * D * 4 / WD <= 4 * kTile && kWaves * kBlock <= 4 * kTile * WD,
+  static_assert(kWaves * 32 * D * 4 / WD <= 2 * NB * kTile && kWaves * kBlock <= 2 * NB * kTile * WD,
                 "room for the sums");
-  static_assert(kWaves * 32 * NK * L::row_bytes <= 4 * kTile * WR * WD, "room for the results");
+  static_assert(kWaves * 32 * NK * L::row_bytes <= 2 * NB * kTile * WR * WD, "room for the results");
   if (skipped) s_skipped = 1;
   // The rows that were left out, pair by pair, those alone that see the key: added to
   // the sums [32 keys][D] that lie in LDS.
@@ -702,19 +711,19 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
     const T* k_row = reinterpret_cast<const T*>(a.k + token * a.k_stride) + head * D;
     const T* v_row = reinterpret_cast<const T*>(a.v + token * a.v_stride) + head * D;
     const T *q, *g;
-    f32x2 st;
+    float row_lse, row_delta;
     auto at_row = [&](int row) INLINE {
       const int tok = token_of(bt, row), h = head * bt.G + row - tok * bt.G;
       const int64_t to = rows.start + tok;
       q = reinterpret_cast<const T*>(a.q + to * a.q_stride) + h * D;
       g = reinterpret_cast<const T*>(a.d_out + to * a.d_out_stride) + h * D;
-      st = a.stats[to * bt.h_q + h];
+      row_lse = a.lse2[to * bt.h_q + h], row_delta = a.delta[to * bt.h_q + h];
     };
 #pragma unroll 1
     for (int row0 = r0 * RT; row0 < end; row0 += 32) {
       if (!partial(row0 / RT)) continue;
       at_row(min(row0 + i, end - 1));
-      bool bad = st[0] != st[0] || !(fabsf(st[1]) < INFINITY);
+      bool bad = row_lse != row_lse || !(fabsf(row_delta) < INFINITY);
 #pragma unroll 1
       for (int d = k; d < D; d += 2)
         bad = bad || !(fabsf((float)q[d]) < INFINITY) || !(fabsf((float)g[d]) < INFINITY);
@@ -728,8 +737,8 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
           s += (float)q[d] * (float)k_row[d];
           dp += (float)g[d] * (float)v_row[d];
         }
-        float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s, a.scale2, -st[0]));
-        if (is_dk) w *= dp - st[1];
+        float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s, a.scale2, -row_lse));
+        if (is_dk) w *= dp - row_delta;
         if constexpr (!is_f32<T>) w = (float)(T)w;
         const T* of = is_dk ? q : g;
 #pragma unroll 1
@@ -838,7 +847,7 @@ Plan plan_grad(const da_prompt& p) {
     plan.key_items =
         most_tiles(p.key_start, p.B, p.N, p.keys, 1, KeysForm<T, d.value>::keys);
   });
-  plan.bytes = (size_t)p.rows * p.h_q * sizeof(f32x2);
+  plan.bytes = (size_t)p.rows * p.h_q * 2 * sizeof(float);
   return plan;
 }
 
@@ -892,7 +901,8 @@ da_status da_prompt_attn_grad(const da_prompt* prompt, const void* q, int64_t q_
   a.d_out_stride = d_out_stride * size, a.dq_stride = dq_stride * size;
   a.dk_stride = dk_stride * size, a.dv_stride = dv_stride * size;
   a.scale = scale, a.scale2 = scale * kLog2e;
-  a.stats = static_cast<f32x2*>(workspace);
+  a.lse2 = static_cast<float*>(workspace);
+  a.delta = a.lse2 + (int64_t)p.rows * p.h_q;
   const Batch bt = device_batch(p);
   hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
