@@ -46,6 +46,7 @@ constexpr int kKeys = is_f32<T> || D == 256 ? 32 : 64;     // keys of a tile
 template <class T, int D, int NQ, bool LSE>
 __global__ __launch_bounds__(kThreads, NQ == 1 && D <= 128 && !is_f32<T> ? 2 : 1)
 void prompt_attn_kernel(Batch bt, AttnArgs a) {
+  constexpr bool kPipe = NQ == 2 || (D == 256 && !is_f32<T>);
   using L = Tile<T, D>;
   constexpr int KT = kKeys<T, D>, R = 32 * NQ * kWaves;
   constexpr int NS = KT / 32, ND = L::ND, NW = L::NW;
@@ -53,11 +54,12 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   constexpr int NP = is_f32<T> ? 1 : 2 * NS;
   using Fetch = Direct<T, D, KT>;
 
-  constexpr int NB = NQ == 2 ? 3 : 2;        // tiles in LDS
+  constexpr int NB = kPipe ? 3 : 2;          // tiles in LDS
   // K's tiles, then V's; q on its way in, and out on its way out
-  static_assert(2 * NB * kTile >= R * L::row_bytes, "room for the rows");
   __shared__ __align__(1024) char s_all[2 * NB][kTile];
   char(*s_k)[kTile] = s_all, (*s_v)[kTile] = s_all + NB;
+  __shared__ __align__(1024) char s_zero[kPipe ? kTile : 16];
+  __shared__ int s_bad[kWaves];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int i = lane & 31, k = lane >> 5;
@@ -81,38 +83,6 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   const int my_min = my_rows ? seen_by(bt, rows.n, keys.n, token_of(bt, my_row0)) : 0;
   const int my_max =
       my_rows ? seen_by(bt, rows.n, keys.n, token_of(bt, my_row0 + my_rows - 1)) : 0;
-  int seen[NQ];
-  u32x4 q[NQ][NW];
-  fetch_rows<T, D, R>(s_all[0], bt,
-                      a.q + rows.start * a.q_stride + (int64_t)head * bt.G * L::row_bytes,
-                      a.q_stride, row0, row0 + in_tile - 1, tid, wave);
-  arrived();
-  __syncthreads();
-  {
-    const RowReader<T, D> rd(i, k);
-#pragma unroll
-    for (int b = 0; b < NQ; ++b) {
-      const int x = 32 * b + i;
-      seen[b] = x < my_rows ? seen_by(bt, rows.n, keys.n, token_of(bt, my_row0 + x)) : 0;
-#pragma unroll
-      for (int w = 0; w < NW; ++w)
-        q[b][w] = (rd.get(s_all[0], NQ * wave + b, w) & a.q_keep) ^ a.q_flip;
-    }
-  }
-  __syncthreads();
-
-  f32x16 acc[NQ][ND];
-  float limit[NQ], ref[NQ], sum[NQ], whole[NQ], top[NQ];
-#pragma unroll
-  for (int b = 0; b < NQ; ++b) {
-#pragma unroll
-    for (int c = 0; c < ND; ++c)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[b][c][r] = 0.f;
-    limit[b] = -INFINITY, ref[b] = 0.f, sum[b] = 0.f, whole[b] = 0.f;
-  }
-  float by = a.scale;
-
   const char* k_base = a.k + (int64_t)keys.start * a.k_stride + (int64_t)head * L::row_bytes;
   const char* v_base = a.v + (int64_t)keys.start * a.v_stride + (int64_t)head * L::row_bytes;
   const RowReader<T, D> k_read(ordered_row(i), k);
@@ -129,11 +99,11 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
     return window(base + (int64_t)t * KT * stride, ((int64_t)keys.n - (int64_t)t * KT) * stride);
   };
   auto load_k = [&](const Window& from, int t, int u) INLINE {
-    fetch(Fetch::place(s_k[t % NB], wave, u), from, k_byte[u % Fetch::phases],
+    fetch(Fetch::place(s_k[(t - t0) % NB], wave, u), from, k_byte[u % Fetch::phases],
           u / Fetch::phases * (Fetch::phases * Fetch::step) * (int)a.k_stride);
   };
   auto load_v = [&](const Window& from, int t, int u) INLINE {
-    fetch(Fetch::place(s_v[t % NB], wave, u), from, v_byte[u % Fetch::phases],
+    fetch(Fetch::place(s_v[(t - t0) % NB], wave, u), from, v_byte[u % Fetch::phases],
           u / Fetch::phases * (Fetch::phases * Fetch::step) * (int)a.v_stride);
   };
   auto load_all = [&](int t, bool want_k, bool want_v) INLINE {
@@ -146,8 +116,44 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
     }
   };
 
+  int seen[NQ];
+  u32x4 q[NQ][NW];
+  // (in a pipeline beside the first keys)
+  char* q_rows = s_all[kPipe ? 1 : 0];
+  static_assert((2 * NB - (kPipe ? 2 : 0)) * kTile >= R * L::row_bytes, "room for the rows");
+  fetch_rows<T, D, R>(q_rows, bt,
+                      a.q + rows.start * a.q_stride + (int64_t)head * bt.G * L::row_bytes,
+                      a.q_stride, row0, row0 + in_tile - 1, tid, wave);
+  if (kPipe && t0 < t1) load_all(t0, true, false);
+  arrived();
+  __syncthreads();
+  {
+    const RowReader<T, D> rd(i, k);
+#pragma unroll
+    for (int b = 0; b < NQ; ++b) {
+      const int x = 32 * b + i;
+      seen[b] = x < my_rows ? seen_by(bt, rows.n, keys.n, token_of(bt, my_row0 + x)) : 0;
+#pragma unroll
+      for (int w = 0; w < NW; ++w)
+        q[b][w] = (rd.get(q_rows, NQ * wave + b, w) & a.q_keep) ^ a.q_flip;
+    }
+  }
+  __syncthreads();
+
+  f32x16 acc[NQ][ND];
+  float limit[NQ], ref[NQ], sum[NQ], whole[NQ], top[NQ];
+#pragma unroll
+  for (int b = 0; b < NQ; ++b) {
+#pragma unroll
+    for (int c = 0; c < ND; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[b][c][r] = 0.f;
+    limit[b] = -INFINITY, ref[b] = 0.f, sum[b] = 0.f, whole[b] = 0.f;
+  }
+  float by = a.scale;
+
   auto scores = [&](int t, f32x16 (&s)[NQ][NS]) INLINE {
-    const char* tile = s_k[t % NB];
+    const char* tile = s_k[(t - t0) % NB];
 #pragma unroll
     for (int b = 0; b < NQ; ++b)
 #pragma unroll
@@ -248,7 +254,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
         for (int h = 0; h < 2; ++h) weigh(b, h, s[b][n], p[b][is_f32<T> ? 0 : 2 * n + h]);
   };
   auto values = [&](int t, f32x16 (&s)[NQ][NS], u32x4 (&p)[NQ][NP]) INLINE {
-    const char* tile = s_v[t % NB];
+    const char* tile = s_v[(t - t0) % NB];
     // Where some rows see keys of a tile that others do not, values that are not
     // finite must not meet the others' weights of 0.
     if ((t + 1) * KT > my_min && __builtin_expect(!tile_finite<T, D, KT>(tile, lane), 0)) {
@@ -307,26 +313,44 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   };
 
   int t = t0;
-  // Tiles that all rows see whole, in a pipeline: a tile's scores are multiplied
-  // while those before become weights, and its largest score is found while those
-  // weights meet V.
-  if constexpr (NQ == 2) {
-    const int whole_tiles = min(min_seen / KT, t1);
-    if (t0 < whole_tiles) {
-      load_all(t0, true, true);
+  bool skipped = false;
+  // In a pipeline: a tile's scores are multiplied while those before become weights,
+  // and its largest score is found while those weights meet V.
+  if constexpr (kPipe) {
+    for (int x = tid; x < kTile / 16; x += kThreads)
+      reinterpret_cast<u32x4*>(s_zero)[x] = u32x4{0u, 0u, 0u, 0u};
+    if (t0 < t1) {
+      load_all(t0, false, true);
       load_all(t0 + 1, true, true);
       load_all(t0 + 2, true, false);
-      arrived();
-      __syncthreads();
       f32x16 sa[NQ][NS], sb[NQ][NS];
       u32x4 p[NQ][NP];
       scores(t0, sa);
+      mask(t0, sa);
       find_top(sa);
       if (over()) raise();
       rescore(sa);
+      arrived();
       __syncthreads();
       auto step = [&](f32x16 (&s)[NQ][NS], f32x16 (&next)[NQ][NS]) INLINE {
-        const char *tile_k = s_k[(t + 1) % NB], *tile_v = s_v[t % NB];
+        const char *tile_k = s_k[(t + 1 - t0) % NB], *tile_v = s_v[(t - t0) % NB];
+        // Where some rows see keys of a tile that others do not, values that are not
+        // finite must not meet the others' weights of 0: such a tile is left out here
+        // (zeros in its place) and added at the end.
+        if (__builtin_expect((t + 1) * KT > min_seen, 0)) {
+          constexpr int part = kTile / kWaves;
+          Finite<T> f;
+#pragma unroll
+          for (int x = 0; x < part / 1024; ++x)
+            f.take(*reinterpret_cast<const u32x4*>(tile_v + wave * part + x * 1024 + lane * 16));
+          const bool bad = __any(!f.all());
+          if (lane == 0) s_bad[wave] = bad;
+          __syncthreads();
+          int any = 0;
+#pragma unroll
+          for (int w = 0; w < kWaves; ++w) any |= s_bad[w];
+          if (uniform(any)) skipped = true, tile_v = s_zero;
+        }
 #pragma unroll
         for (int b = 0; b < NQ; ++b)
 #pragma unroll
@@ -338,8 +362,6 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
         u32x4 v0, v1, x[NS];
 #pragma unroll
         for (int n = 0; n < NS; ++n) x[n] = k_read.get(tile_k, n, 0);
-        constexpr int kPieces = NQ * NP / NW;           // of 8 weights, a step of the product
-        static_assert(NQ * NP % NW == 0, "whole pieces");
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
           u32x4 y[NS];
@@ -347,11 +369,14 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
           for (int n = 0; n < NS; ++n) y[n] = w + 1 < NW ? k_read.get(tile_k, n, w + 1) : x[n];
           if (w + 1 == NW) v0 = v_read.get(tile_v, 0, 0), v1 = v_read.get(tile_v, 0, 1);
           if (w == 0) __builtin_amdgcn_sched_barrier(0);
+          // weights in pieces of eight, spread over the steps of the product
 #pragma unroll
-          for (int e = w * kPieces; e < (w + 1) * kPieces; ++e) {
-            const int b = e / NP, n = e % NP / 2, h = e % 2;
-            weigh(b, h, s[b][n], p[b][2 * n + h]);
-          }
+          for (int e = 0; e < NQ * NP; ++e)
+            if (e * NW / (NQ * NP) == w) {
+              const int b = e / NP, n = e % NP / 2, h = e % 2;
+              weigh(b, h, s[b][n], p[b][2 * n + h]);
+              asm volatile("" : "+v"(p[b][2 * n + h]));  // (here, not where it is used)
+            }
 #pragma unroll
           for (int n = 0; n < NS; ++n)
 #pragma unroll
@@ -362,6 +387,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
           for (int n = 0; n < NS; ++n) x[n] = y[n];
           __builtin_amdgcn_sched_barrier(0);
         }
+        if (__builtin_expect((t + 2) * KT > my_min, 0)) mask(t + 1, next);
 #pragma unroll
         for (int b = 0; b < NQ; ++b) top[b] = next[b][0][0];
 #pragma unroll
@@ -382,12 +408,6 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
         arrived<2 * Fetch::units>();                    // but those of this step
         __syncthreads();
       };
-      auto settle_all = [&]() INLINE {
-#pragma unroll
-        for (int b = 0; b < NQ; ++b)
-#pragma unroll
-          for (int c = 0; c < ND; ++c) settle(acc[b][c]);
-      };
       // (The sums are in accumulation registers within the inner loop: what changes
       // them otherwise stands outside.  Which scores are next is hidden from the
       // compiler, so that it copies them outside too.)
@@ -395,11 +415,11 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
       while (again) {
         again = false;
         int second = 0;
-        while (t + 1 < whole_tiles) {
+        while (t < t1) {
           step(sa, sb);
           ++t, second = 1;
           again = over();
-          if (again || t + 1 >= whole_tiles) break;
+          if (again || t >= t1) break;
           rescore(sb);
           step(sb, sa);
           ++t, second = 0;
@@ -407,7 +427,10 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
           if (again) break;
           rescore(sa);
         }
-        settle_all();
+#pragma unroll
+        for (int b = 0; b < NQ; ++b)
+#pragma unroll
+          for (int c = 0; c < ND; ++c) settle(acc[b][c]);
         asm volatile("" : "+s"(second));
         if (second) {
 #pragma unroll
@@ -418,20 +441,14 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
         if (again) raise();
         if (again || second) rescore(sa);
       }
-      weights(sa, p);
-      values(t, sa, p);
-      ++t;
-      arrived();
+      arrived();                             // (what was fetched beyond the last)
       __syncthreads();
     }
   }
-  // Tiles that are masked for some rows, or all of them.
-  if (t < t1) {
-    if (t == t0) {
-      load_all(t, true, true);
-      arrived();
-      __syncthreads();
-    }
+  if (!kPipe && t < t1) {
+    load_all(t, true, true);
+    arrived();
+    __syncthreads();
     for (; t < t1; ++t) {
       if (t + 1 < t1) load_all(t + 1, true, true);
       if (t * KT < my_max) {
@@ -450,6 +467,56 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
     }
   }
 
+  // The keys that were left out, those alone that the row sees: the sums pass through
+  // LDS in 32 bits, 32 rows of one wave at a time.
+  if (kPipe && __builtin_expect(skipped, 0)) {
+    float* sums = reinterpret_cast<float*>(s_all[0]) + i * D;
+    for (int w = 0; w < kWaves; ++w) {
+#pragma unroll
+      for (int b = 0; b < NQ; ++b) {
+        __syncthreads();
+        if (w != wave) continue;
+#pragma unroll
+        for (int c = 0; c < ND; ++c)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sums[32 * c + 8 * (r / 4) + 4 * k + r % 4] = acc[b][c][r];
+        __builtin_amdgcn_wave_barrier();
+        const int x = my_row0 + min(32 * b + i, max(my_rows - 1, 0));
+        const int tok = my_rows ? token_of(bt, x) : 0, g = my_rows ? x - tok * bt.G : 0;
+        const T* q_row = reinterpret_cast<const T*>(a.q + (rows.start + tok) * a.q_stride) +
+                         (head * bt.G + g) * D;
+#pragma unroll 1
+        for (int key0 = max(min_seen / KT, t0) * KT; key0 < min(max_seen, t1 * KT); key0 += KT) {
+          bool bad = false;
+          for (int key = key0 + i; key < min(key0 + KT, keys.n); key += 32) {
+            const T* row = reinterpret_cast<const T*>(v_base + key * a.v_stride);
+#pragma unroll 1
+            for (int d = k; d < D; d += 2) bad = bad || !(fabsf((float)row[d]) < INFINITY);
+          }
+          if (!__any(bad)) continue;
+#pragma unroll 1
+          for (int key = key0; key < min(key0 + KT, seen[b]); ++key) {
+            const T* k_row = reinterpret_cast<const T*>(k_base + key * a.k_stride);
+            const T* v_row = reinterpret_cast<const T*>(v_base + key * a.v_stride);
+            float s = 0.f;
+#pragma unroll 1
+            for (int d = 0; d < D; ++d) s += (float)q_row[d] * (float)k_row[d];
+            s = a.q_keep ? a.q_flip ? -s : s : 0.f;
+            if (by != a.scale) s *= a.scale;
+            const float w = (float)(T)__builtin_amdgcn_exp2f(__builtin_fmaf(s, by, -ref[b]));
+#pragma unroll 1
+            for (int d = k; d < D; d += 2) sums[d] += w * (float)v_row[d];
+          }
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int c = 0; c < ND; ++c)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[b][c][r] = sums[32 * c + 8 * (r / 4) + 4 * k + r % 4];
+      }
+    }
+    __syncthreads();
+  }
   char* mine = s_all[0] + 32 * NQ * wave * L::row_bytes;
   auto place = [&](int x) INLINE {           // row * h_q + head of this wave's row x
     const int tok = token_of(bt, my_row0 + x);
