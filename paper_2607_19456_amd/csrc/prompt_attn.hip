@@ -43,8 +43,11 @@ constexpr int kKeys = is_f32<T> || D == 256 ? 32 : 64;     // keys of a tile
 //   S^T [keys x rows] = K . Q^T,   O^T [D x rows] += V^T . P^T
 // so a row's scores lie in two lanes and its statistics need no LDS.
 // ---------------------------------------------------------------------------
+template <int D, int NQ>
+constexpr int kGroupsPerCu = NQ == 2 || D == 256 ? 1 : D == 128 ? 2 : 3;
+
 template <class T, int D, int NQ, bool LSE>
-__global__ __launch_bounds__(kThreads, NQ == 1 && D <= 128 && !is_f32<T> ? 2 : 1)
+__global__ __launch_bounds__(kThreads, (kGroupsPerCu<D, NQ>))
 void prompt_attn_kernel(Batch bt, AttnArgs a) {
   constexpr bool kPipe = NQ == 2 || (D == 256 && !is_f32<T>);
   using L = Tile<T, D>;
@@ -55,9 +58,10 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   using Fetch = Direct<T, D, KT>;
 
   constexpr int NB = kPipe ? 3 : 2;          // tiles in LDS
-  // K's tiles, then V's; q on its way in, and out on its way out
+  // K's and V's tiles in turn; q on its way in, and out on its way out
   __shared__ __align__(1024) char s_all[2 * NB][kTile];
-  char(*s_k)[kTile] = s_all, (*s_v)[kTile] = s_all + NB;
+  auto s_k = [&](int t) INLINE { return s_all[2 * (t % NB)]; };
+  auto s_v = [&](int t) INLINE { return s_all[2 * (t % NB) + 1]; };
   __shared__ __align__(1024) char s_zero[kPipe ? kTile : 16];
   __shared__ int s_bad[kWaves];
 
@@ -80,7 +84,8 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   // This wave's rows.
   const int my_row0 = row0 + 32 * NQ * wave;
   const int my_rows = min(max(in_tile - 32 * NQ * wave, 0), 32 * NQ);
-  const int my_min = my_rows ? seen_by(bt, rows.n, keys.n, token_of(bt, my_row0)) : 0;
+  // (without rows there is nothing to mask)
+  const int my_min = my_rows ? seen_by(bt, rows.n, keys.n, token_of(bt, my_row0)) : INT32_MAX;
   const int my_max =
       my_rows ? seen_by(bt, rows.n, keys.n, token_of(bt, my_row0 + my_rows - 1)) : 0;
   const char* k_base = a.k + (int64_t)keys.start * a.k_stride + (int64_t)head * L::row_bytes;
@@ -99,11 +104,11 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
     return window(base + (int64_t)t * KT * stride, ((int64_t)keys.n - (int64_t)t * KT) * stride);
   };
   auto load_k = [&](const Window& from, int t, int u) INLINE {
-    fetch(Fetch::place(s_k[(t - t0) % NB], wave, u), from, k_byte[u % Fetch::phases],
+    fetch(Fetch::place(s_k(t - t0), wave, u), from, k_byte[u % Fetch::phases],
           u / Fetch::phases * (Fetch::phases * Fetch::step) * (int)a.k_stride);
   };
   auto load_v = [&](const Window& from, int t, int u) INLINE {
-    fetch(Fetch::place(s_v[(t - t0) % NB], wave, u), from, v_byte[u % Fetch::phases],
+    fetch(Fetch::place(s_v(t - t0), wave, u), from, v_byte[u % Fetch::phases],
           u / Fetch::phases * (Fetch::phases * Fetch::step) * (int)a.v_stride);
   };
   auto load_all = [&](int t, bool want_k, bool want_v) INLINE {
@@ -118,13 +123,14 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
 
   int seen[NQ];
   u32x4 q[NQ][NW];
-  // (in a pipeline beside the first keys)
-  char* q_rows = s_all[kPipe ? 1 : 0];
-  static_assert((2 * NB - (kPipe ? 2 : 0)) * kTile >= R * L::row_bytes, "room for the rows");
+  // (beside the first keys, where there is room)
+  constexpr bool kBeside = (2 * NB - 2) * kTile >= R * L::row_bytes;
+  static_assert(2 * NB * kTile >= R * L::row_bytes, "room for the rows");
+  char* q_rows = s_all[kBeside ? 2 : 0];
   fetch_rows<T, D, R>(q_rows, bt,
                       a.q + rows.start * a.q_stride + (int64_t)head * bt.G * L::row_bytes,
                       a.q_stride, row0, row0 + in_tile - 1, tid, wave);
-  if (kPipe && t0 < t1) load_all(t0, true, false);
+  if (kBeside && t0 < t1) load_all(t0, true, true);
   arrived();
   __syncthreads();
   {
@@ -153,7 +159,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   float by = a.scale;
 
   auto scores = [&](int t, f32x16 (&s)[NQ][NS]) INLINE {
-    const char* tile = s_k[(t - t0) % NB];
+    const char* tile = s_k(t - t0);
 #pragma unroll
     for (int b = 0; b < NQ; ++b)
 #pragma unroll
@@ -253,11 +259,26 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) weigh(b, h, s[b][n], p[b][is_f32<T> ? 0 : 2 * n + h]);
   };
-  auto values = [&](int t, f32x16 (&s)[NQ][NS], u32x4 (&p)[NQ][NP]) INLINE {
-    const char* tile = s_v[(t - t0) % NB];
-    // Where some rows see keys of a tile that others do not, values that are not
-    // finite must not meet the others' weights of 0.
-    if ((t + 1) * KT > my_min && __builtin_expect(!tile_finite<T, D, KT>(tile, lane), 0)) {
+  // Where some rows see keys of a tile that others do not, values that are not finite
+  // must not meet the others' weights of 0.  Each wave looks at a quarter of the tile.
+  auto spoilt = [&](int t) INLINE {
+    constexpr int part = kTile / kWaves;
+    const char* tile = s_v(t - t0) + wave * part;
+    Finite<T> f;
+#pragma unroll
+    for (int x = 0; x < part / 1024; ++x)
+      f.take(*reinterpret_cast<const u32x4*>(tile + x * 1024 + lane * 16));
+    const bool bad = __any(!f.all());
+    if (lane == 0) s_bad[wave] = bad;
+    __syncthreads();
+    int any = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) any |= s_bad[w];
+    return uniform(any) != 0;
+  };
+  auto values = [&](int t, bool bad, f32x16 (&s)[NQ][NS], u32x4 (&p)[NQ][NP]) INLINE {
+    const char* tile = s_v(t - t0);
+    if (__builtin_expect(bad, 0)) {
       // key by key, those alone that the row sees
 #pragma unroll 1
       for (int e = 0; e < 16 * NS; ++e) {
@@ -320,7 +341,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
     for (int x = tid; x < kTile / 16; x += kThreads)
       reinterpret_cast<u32x4*>(s_zero)[x] = u32x4{0u, 0u, 0u, 0u};
     if (t0 < t1) {
-      load_all(t0, false, true);
+      if (!kBeside) load_all(t0, true, true);
       load_all(t0 + 1, true, true);
       load_all(t0 + 2, true, false);
       f32x16 sa[NQ][NS], sb[NQ][NS];
@@ -333,24 +354,10 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
       arrived();
       __syncthreads();
       auto step = [&](f32x16 (&s)[NQ][NS], f32x16 (&next)[NQ][NS]) INLINE {
-        const char *tile_k = s_k[(t + 1 - t0) % NB], *tile_v = s_v[(t - t0) % NB];
-        // Where some rows see keys of a tile that others do not, values that are not
-        // finite must not meet the others' weights of 0: such a tile is left out here
-        // (zeros in its place) and added at the end.
-        if (__builtin_expect((t + 1) * KT > min_seen, 0)) {
-          constexpr int part = kTile / kWaves;
-          Finite<T> f;
-#pragma unroll
-          for (int x = 0; x < part / 1024; ++x)
-            f.take(*reinterpret_cast<const u32x4*>(tile_v + wave * part + x * 1024 + lane * 16));
-          const bool bad = __any(!f.all());
-          if (lane == 0) s_bad[wave] = bad;
-          __syncthreads();
-          int any = 0;
-#pragma unroll
-          for (int w = 0; w < kWaves; ++w) any |= s_bad[w];
-          if (uniform(any)) skipped = true, tile_v = s_zero;
-        }
+        const char *tile_k = s_k(t + 1 - t0), *tile_v = s_v(t - t0);
+        // (such a tile is left out here, zeros in its place, and added at the end)
+        if (__builtin_expect((t + 1) * KT > min_seen, 0) && spoilt(t))
+          skipped = true, tile_v = s_zero;
 #pragma unroll
         for (int b = 0; b < NQ; ++b)
 #pragma unroll
@@ -446,11 +453,14 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
     }
   }
   if (!kPipe && t < t1) {
-    load_all(t, true, true);
-    arrived();
-    __syncthreads();
+    if (!kBeside) {
+      load_all(t, true, true);
+      arrived();
+      __syncthreads();
+    }
     for (; t < t1; ++t) {
       if (t + 1 < t1) load_all(t + 1, true, true);
+      const bool bad = (t + 1) * KT > min_seen && spoilt(t);
       if (t * KT < my_max) {
         f32x16 s[NQ][NS];
         u32x4 p[NQ][NP];
@@ -460,7 +470,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
         if (over()) raise();
         rescore(s);
         weights(s, p);
-        values(t, s, p);
+        values(t, bad, s, p);
       }
       arrived();
       __syncthreads();
@@ -624,8 +634,14 @@ struct Plan {
 Plan plan_attn(const da_prompt& p) {
   Plan plan{1, 1, 0, 0};
   const int64_t G = p.h_q / p.h_kv;
+  // Two blocks of rows a wave halve what each product reads from LDS, but leave one
+  // workgroup a CU, which nothing covers while it starts and ends: worth it where a row
+  // tile has many key tiles.  d = 128, 32/8 heads, causal, us with two and with one:
+  // one sequence of 16384 rows 2099 and 2804, 4 of 2048 190 and 190, 16 of 512 95 and
+  // 74.  d = 64 (4 of 4096, 16 heads: 240 and 186) is bound by the softmax.
   plan.items = most_tiles(p.row_start, p.B, p.T, p.rows, G, 256);
-  if (p.dtype != DA_F32 && p.d <= 128 && plan.items * p.h_kv >= kCus) {
+  const int64_t seen = p.keys / p.B / (p.causal ? 2 : 1);
+  if (p.dtype != DA_F32 && p.d == 128 && seen >= 1024 && plan.items * p.h_kv >= kCus) {
     plan.NQ = 2;
     return plan;
   }
@@ -651,7 +667,7 @@ void launch_rows(const Plan& plan, const Batch& bt, const AttnArgs& a, hipStream
 
 template <class T, int D>
 void launch_attn(const Plan& plan, const Batch& bt, const AttnArgs& a, hipStream_t s) {
-  if constexpr (!is_f32<T> && D <= 128) {
+  if constexpr (!is_f32<T> && D == 128) {
     if (plan.NQ == 2) return launch_rows<T, D, 2>(plan, bt, a, s);
   }
   launch_rows<T, D, 1>(plan, bt, a, s);

@@ -441,3 +441,70 @@ def test_many_short_sequences(cuda_device):
     c = Case("bf16", 64, 4, 1, t=t, seed=20)
     check_forward(c, cuda_device)
     check_gradient(c, cuda_device)
+
+
+# --- the forms that large calls take ---------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("causal", [True, False])
+def test_long_keys_and_many_rows(cuda_device, dtype, causal):
+    """Rows enough to fill the card and keys enough for the form of two blocks of rows a
+    wave: a few rows of each head over long keys, and tiles that end anywhere."""
+    c = Case(dtype, 128, 64, 64, t=[4, 257, 1], n=[3100, 3000, 3000], causal=causal, seed=21)
+    out, L = c.forward(cuda_device)
+    rows = [0, 3, 4, 5, 67, 68, 130, 200, 260, 261]
+    heads = [0, 31, 63]
+    q, k, v = c.q[rows][:, heads], c.k[:, heads], c.v[:, heads]
+    for j, r in enumerate(rows):
+        b = next(i for i in range(3) if c.rs[i] <= r < c.rs[i + 1])
+        t, n = c.t[b], c.n[b]
+        seen = (r - c.rs[b]) + n - t + 1 if causal else n
+        at = slice(c.ks[b], c.ks[b] + seen)
+        sub = ref.Batch(1, seen, T=1, N=seen, B=1, causal=False)
+        o, lse, mass, spread, seen_n, top = ref.attention(q[j:j + 1], k[at], v[at], c.scale, sub)
+        tol = ref.tolerance(o, mass, spread, seen_n, top, c.type, 128)
+        err = np.abs(out[r, heads].double().cpu().numpy() - o[0])
+        assert (err <= tol[0]).all(), (r, float((err / tol[0]).max()))
+        err = np.abs(L[r, heads].double().cpu().numpy() - lse[0])
+        assert (err <= ref.lse_tolerance(lse, spread, seen_n, 128)[0]).all(), r
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_long_keys_that_are_not_seen_stay_out(cuda_device, bad):
+    """The same form: a value that is not finite in a tile that only some rows see."""
+    c = Case("bf16", 128, 64, 64, t=[300, 260], n=[2300, 2200], seed=22, behind=0)
+    clean, L = c.forward(cuda_device)
+    again, _ = c.forward(cuda_device, lse=False)
+    assert torch.equal(clean, again)
+    at = 2300 - 40                              # of the first sequence: rows from 260 on see it
+    c.v[at, 5, 7] = bad
+    out, L2 = c.forward(cuda_device)
+    assert torch.equal(L, L2)
+    keep = torch.ones_like(out, dtype=torch.bool)
+    keep[260:300, 5, 7] = False
+    assert not torch.isfinite(out[260:300, 5, 7]).any()
+    # rows of tiles that are left out are summed in another order
+    assert torch.isfinite(out[keep]).all()
+    room = 4 * ref.half_step(c.type) * float(c.v[torch.isfinite(c.v)].abs().max())
+    assert float((out - clean)[keep].abs().max()) <= room
+    assert torch.equal(out[300:], clean[300:]) and torch.equal(out[:, 6:], clean[:, 6:])
+
+
+@pytest.mark.parametrize("scale", [-0.3, 40.0])
+def test_long_keys_whose_scores_rise(cuda_device, scale):
+    """The same form where the largest score lies far behind: every tile's is higher than
+    the last one's by more than what is let pass."""
+    c = Case("bf16", 128, 64, 64, t=[256, 1, 1, 1], n=[2300] * 4, causal=False, seed=23, behind=0)
+    c.k[:2300, :, 0] = torch.linspace(-20, 20, 2300)[:, None] * (-1 if scale < 0 else 1)
+    c.q[:, :, 0] = 3.0
+    c.scale = scale / 11.3
+    out, L = c.forward(cuda_device)
+    heads, rows = [0, 40], [0, 100, 255]
+    sub = ref.Batch(3, 2300, T=3, N=2300, B=1, causal=False)
+    o, lse, mass, spread, seen_n, top = ref.attention(
+        c.q[rows][:, heads], c.k[:2300, heads], c.v[:2300, heads], c.scale, sub)
+    tol = ref.tolerance(o, mass, spread, seen_n, top, c.type, 128)
+    err = np.abs(out[rows][:, heads].double().cpu().numpy() - o)
+    assert (err <= tol).all(), float((err / tol).max())
+    err = np.abs(L[rows][:, heads].double().cpu().numpy() - lse)
+    assert (err <= ref.lse_tolerance(lse, spread, seen_n, 128)).all()
