@@ -173,6 +173,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
         const u32x4 x = k_read.get(tile, n, w);
 #pragma unroll
         for (int b = 0; b < NQ; ++b) s[b][n] = mma<T>(x, q[b][w], s[b][n]);
+        if (is_f32<T> && w % 4 == 3) __builtin_amdgcn_sched_barrier(0);
       }
   };
   auto mask = [&](int t, f32x16 (&s)[NQ][NS]) INLINE {
@@ -310,17 +311,22 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
       return;
     }
     if constexpr (is_f32<T>) {
+      // (eight reads at a time: more would not fit the registers)
 #pragma unroll
       for (int c = 0; c < ND; ++c)
 #pragma unroll
-        for (int n = 0; n < NS; ++n)
+        for (int h = 0; h < 2 * NS; ++h) {
+          float x[8];
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float x = v_read.get(tile, 2 * n + r / 8, r % 8, c);
+          for (int e = 0; e < 8; ++e) x[e] = v_read.get(tile, h, e, c);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
 #pragma unroll
             for (int b = 0; b < NQ; ++b)
-              acc[b][c] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[b][n][r], acc[b][c], 0, 0, 0);
-          }
+              acc[b][c] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], s[b][h / 2][8 * (h % 2) + e],
+                                                               acc[b][c], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
     } else {
 #pragma unroll
       for (int c = 0; c < ND; ++c)

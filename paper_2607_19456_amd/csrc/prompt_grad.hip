@@ -28,6 +28,11 @@ struct GradArgs {
   float scale, scale2;          // and times log2(e)
   // [rows][h_q] each: lse times log2(e) (+infinity: no weights), and delta
   float *lse2, *delta;
+  // Each tile's keys (or rows) are taken in so many parts, whose sums in 32 bits go to
+  // parts and are added by a kernel of their own where there is more than one:
+  // [workgroup][rows][D], for dK and dV [workgroup][dK, dV][keys][D].
+  int row_splits, key_splits;
+  float* parts;
 };
 
 template <class T>
@@ -72,15 +77,17 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int i = lane & 31, k = lane >> 5;
-  const int head = blockIdx.x % bt.h_kv;
+  const int head = blockIdx.x % bt.h_kv, split = blockIdx.x / bt.h_kv % a.row_splits;
   Place at;
-  if (!find(bt, true, R, blockIdx.x / bt.h_kv, lane, &at)) return;
+  if (!find(bt, true, R, blockIdx.x / bt.h_kv / a.row_splits, lane, &at)) return;
   const Span rows = at.rows, keys = at.keys;
   const int row0 = at.after * R;             // the last rows, which see most, first
   const int in_tile = min(rows.n * bt.G - row0, R);
   const int min_seen = seen_by(bt, rows.n, keys.n, token_of(bt, row0));
   const int max_seen = seen_by(bt, rows.n, keys.n, token_of(bt, row0 + in_tile - 1));
-  const int t1 = (max_seen + KT - 1) / KT;
+  const int tiles = (max_seen + KT - 1) / KT;
+  const int t0 = (int)((int64_t)tiles * split / a.row_splits);
+  const int t1 = (int)((int64_t)tiles * (split + 1) / a.row_splits);
 
   const int my_row0 = row0 + 32 * NQ * wave;
   const int my_rows = min(max(in_tile - 32 * NQ * wave, 0), 32 * NQ);
@@ -125,7 +132,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
         seen[b] = seen_by(bt, rows.n, keys.n, token_of(bt, my_row0 + x));
         const float lse = far_load<float>(a.lse + place(x));
         lse2[b] = lse == -INFINITY ? INFINITY : lse * kLog2e;
-        if (k == 0) a.lse2[place(x)] = lse2[b], a.delta[place(x)] = delta[b];
+        if (k == 0 && split == 0) a.lse2[place(x)] = lse2[b], a.delta[place(x)] = delta[b];
       }
     }
     __syncthreads();
@@ -158,9 +165,9 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
 #pragma unroll
     for (int u = 0; u < Fetch::units; ++u) {
       const int further = u / Fetch::phases * (Fetch::phases * Fetch::step);
-      fetch(Fetch::place(s_k[t % NB], wave, u), from_k, k_byte[u % Fetch::phases],
+      fetch(Fetch::place(s_k[(t - t0) % NB], wave, u), from_k, k_byte[u % Fetch::phases],
             further * (int)a.k_stride);
-      fetch(Fetch::place(s_v[t % NB], wave, u), from_v, v_byte[u % Fetch::phases],
+      fetch(Fetch::place(s_v[(t - t0) % NB], wave, u), from_v, v_byte[u % Fetch::phases],
             further * (int)a.v_stride);
     }
   };
@@ -169,9 +176,9 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
     for (int x = tid; x < 32 * L::chunks; x += kThreads)
       reinterpret_cast<u32x4*>(s_zero)[x] = u32x4{0u, 0u, 0u, 0u};
 
-  if (t1 > 0) {
+  if (t0 < t1) {
 #pragma unroll
-    for (int t = 0; t < NB - 1; ++t) load(t);
+    for (int t = 0; t < NB - 1; ++t) load(t0 + t);
     arrived();
     __syncthreads();
   }
@@ -179,9 +186,9 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
   for (int b = 0; b < NQ; ++b)
 #pragma unroll
     for (int w = 0; w < NW; ++w) asm volatile("" : "+v"(q[b][w]), "+v"(g[b][w]));
-  for (int t = 0; t < t1; ++t) {
-    char* tile_k = s_k[t % NB];
-    const char* tile_v = s_v[t % NB];
+  for (int t = t0; t < t1; ++t) {
+    char* tile_k = s_k[(t - t0) % NB];
+    const char* tile_v = s_v[(t - t0) % NB];
 #pragma unroll
     for (int n = 0; n < KT / 32; ++n) {
       f32x16 s[NQ], dp[NQ];
@@ -295,6 +302,9 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
     return a.dq + (rows.start + tok) * a.dq_stride +
            (int64_t)(head * bt.G + my_row0 + x - tok * bt.G) * L::row_bytes;
   };
+  auto part_of = [&](int x) INLINE {
+    return a.parts + ((int64_t)blockIdx.x * R + 32 * NQ * wave + x) * D;
+  };
   // The keys that were left out, those alone that the row sees: the sums pass through
   // LDS in 32 bits, 32 rows of one wave at a time.
   if (__builtin_expect(skipped, 0)) {
@@ -321,7 +331,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
         const T* g_row = reinterpret_cast<const T*>(a.d_out + at_row / bt.h_q * a.d_out_stride) +
                          at_row % bt.h_q * D;
 #pragma unroll 1
-        for (int key0 = min_seen / 32 * 32; key0 < max_seen; key0 += 32) {
+        for (int key0 = max(min_seen / 32 * 32, t0 * KT); key0 < min(max_seen, t1 * KT); key0 += 32) {
           auto row_at = [&](const char* base, int64_t stride, int key) INLINE {
             return reinterpret_cast<const T*>(base + key * stride);
           };
@@ -352,8 +362,14 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
         __builtin_amdgcn_wave_barrier();
         if (32 * b + i < my_rows) {
           T* dst = reinterpret_cast<T*>(to(32 * b + i));
+          float* part = part_of(32 * b + i);
 #pragma unroll 1
-          for (int d = k; d < D; d += 2) dst[d] = (T)(sums[d] * a.scale);
+          for (int d = k; d < D; d += 2) {
+            if (a.row_splits > 1)
+              part[d] = sums[d];
+            else
+              dst[d] = (T)(sums[d] * a.scale);
+          }
         }
       }
     }
@@ -365,11 +381,16 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
     for (int c = 0; c < ND; ++c) {
       settle(acc[b][c]);
 #pragma unroll
-      for (int r = 0; r < 16; r += 4)
-        put4<T, D>(mine, 32 * b + i, 32 * c + 2 * r + 4 * k,
-                   f32x4{acc[b][c][r], acc[b][c][r + 1], acc[b][c][r + 2], acc[b][c][r + 3]} *
-                       a.scale);
+      for (int r = 0; r < 16; r += 4) {
+        const f32x4 x{acc[b][c][r], acc[b][c][r + 1], acc[b][c][r + 2], acc[b][c][r + 3]};
+        const int d = 32 * c + 2 * r + 4 * k;
+        if (a.row_splits == 1)
+          put4<T, D>(mine, 32 * b + i, d, x * a.scale);
+        else if (32 * b + i < my_rows)
+          *reinterpret_cast<f32x4*>(part_of(32 * b + i) + d) = x;
+      }
     }
+  if (a.row_splits > 1) return;
   store_rows<T, D>(mine, 32 * NQ, lane, [&](int x) INLINE {
     return x < my_rows ? to(x) : nullptr;
   });
@@ -413,9 +434,9 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int i = lane & 31, k = lane >> 5;
   const int wk = wave % WK, wr = wave / WK % WR, wd = wave / (WK * WR);
-  const int head = blockIdx.x % bt.h_kv;
+  const int head = blockIdx.x % bt.h_kv, split = blockIdx.x / bt.h_kv % a.key_splits;
   Place at;
-  if (!find(bt, false, F::keys, blockIdx.x / bt.h_kv, lane, &at)) return;
+  if (!find(bt, false, F::keys, blockIdx.x / bt.h_kv / a.key_splits, lane, &at)) return;
   const Span rows = at.rows, keys = at.keys;
   const int end = rows.n * bt.G;
   const int key0 = (at.tiles - 1 - at.after) * F::keys;
@@ -424,7 +445,9 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
     return bt.causal ? (int)min((int64_t)max(key - keys.n + rows.n, 0) * bt.G, (int64_t)end) : 0;
   };
   const int all_from = first_row(min(key0 + F::keys, keys.n) - 1);   // rows that see all of the keys
-  const int r0 = first_row(key0) / RT, r1 = (end + RT - 1) / RT;
+  const int from = first_row(key0) / RT, steps = (end + RT - 1) / RT - from;
+  const int r0 = from + (int)((int64_t)steps * split / a.key_splits);
+  const int r1 = from + (int)((int64_t)steps * (split + 1) / a.key_splits);
 
   auto key_of = [&](int n, int lane) INLINE {
     return key0 + 32 * (NK * wk + n) + (lane & 31);
@@ -526,7 +549,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
 
   if (r0 < r1) {
 #pragma unroll
-    for (int t = 0; t < NB - 1; ++t) load_rows(min(r0 + t, r1 - 1 + NB));
+    for (int t = 0; t < NB - 1; ++t) load_rows(r0 + t);
     arrived();
     __syncthreads();
   }
@@ -720,7 +743,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
       row_lse = a.lse2[to * bt.h_q + h], row_delta = a.delta[to * bt.h_q + h];
     };
 #pragma unroll 1
-    for (int row0 = r0 * RT; row0 < end; row0 += 32) {
+    for (int row0 = r0 * RT; row0 < min(r1 * RT, end); row0 += 32) {
       if (!partial(row0 / RT)) continue;
       at_row(min(row0 + i, end - 1));
       bool bad = row_lse != row_lse || !(fabsf(row_delta) < INFINITY);
@@ -748,6 +771,10 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
   };
   auto shared = [&](int to, int c) INLINE {
     return reinterpret_cast<f32x4*>(s_rows[0] + (to * WK + wk) * kBlock + c * 4096) + lane;
+  };
+  auto part_of = [&](int n, bool is_dk, int x) INLINE {
+    return a.parts +
+           (((int64_t)blockIdx.x * 2 + !is_dk) * F::keys + 32 * (NK * wk + n) + x) * D;
   };
   auto finish = [&](int n, f32x16 (&mine)[ND], f32x16 (&theirs)[ND], bool is_dk) INLINE {
     if constexpr (WR == 2) {
@@ -786,7 +813,11 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
       if (wd == 0) {
         left_out(n, is_dk, sums);
         const int64_t token = keys.start + key_of(n, lane);
-        if (key_of(n, lane) < keys.n) {
+        if (a.key_splits > 1) {
+          float* part = part_of(n, is_dk, i);
+#pragma unroll 1
+          for (int d = k; d < D; d += 2) part[d] = sums[i * D + d];
+        } else if (key_of(n, lane) < keys.n) {
           T* dst = reinterpret_cast<T*>(is_dk ? a.dk + token * a.dk_stride
                                               : a.dv + token * a.dv_stride) + head * D;
 #pragma unroll 1
@@ -794,6 +825,15 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
         }
       }
       __syncthreads();
+      return;
+    }
+    if (a.key_splits > 1) {
+#pragma unroll
+      for (int c = 0; c < ND; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+          *reinterpret_cast<f32x4*>(part_of(n, is_dk, i) + 32 * (ND * wd + c) + 2 * r + 4 * k) =
+              f32x4{mine[c][r], mine[c][r + 1], mine[c][r + 2], mine[c][r + 3]};
       return;
     }
     // (waves that share keys have dimensions of their own, in one place)
@@ -829,13 +869,52 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
   }
 }
 
+// ---------------------------------------------------------------------------
+// Adds the parts of a tile's rows (is_rows: of dQ; else its keys', of dK and dV), in
+// their order, D/4 lanes a row.
+// ---------------------------------------------------------------------------
+template <class T, int D, bool is_rows>
+__global__ __launch_bounds__(kThreads) void prompt_grad_merge_kernel(Batch bt, GradArgs a) {
+  constexpr int R = is_rows ? RowsForm<T, D>::rows : KeysForm<T, D>::keys;
+  constexpr int kPer = D / 4;
+  const int tid = threadIdx.x, l = tid % kPer;
+  const int head = blockIdx.x % bt.h_kv, item = blockIdx.x / bt.h_kv;
+  const int splits = is_rows ? a.row_splits : a.key_splits;
+  Place at;
+  if (!find(bt, is_rows, R, item, tid & 63, &at)) return;
+  const int x = blockIdx.y * (kThreads / kPer) + tid / kPer;
+  const int row = (is_rows ? at.after : at.tiles - 1 - at.after) * R + x;
+  if (x >= R || row >= (is_rows ? at.rows.n * bt.G : at.keys.n)) return;
+  const int tok = is_rows ? token_of(bt, row) : row;
+  const int64_t token = (is_rows ? at.rows.start : at.keys.start) + (int64_t)tok;
+  const int64_t in = (int64_t)(is_rows ? head * bt.G + row - tok * bt.G : head) * D * sizeof(T);
+#pragma unroll
+  for (int which = 0; which < (is_rows ? 1 : 2); ++which) {
+    f32x4 sum{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < splits; ++s) {
+      const int64_t group = (int64_t)(item * splits + s) * bt.h_kv + head;
+      const int64_t first = is_rows ? group * R : (group * 2 + which) * R;
+      sum += far_load<f32x4>(a.parts + (first + x) * D + 4 * l);
+    }
+    char* dst = is_rows ? a.dq + token * a.dq_stride
+                        : which ? a.dv + token * a.dv_stride : a.dk + token * a.dk_stride;
+    if (is_rows || which == 0) sum *= a.scale;
+    if constexpr (is_f32<T>)
+      *reinterpret_cast<f32x4*>(dst + in + 16 * l) = sum;
+    else
+      *reinterpret_cast<u32x2*>(dst + in + 8 * l) =
+          u32x2{pack2<T>(sum[0], sum[1]), pack2<T>(sum[2], sum[3])};
+  }
+}
+
 }  // namespace
 
 namespace {
 
 struct Plan {
   int64_t row_items, key_items;
-  size_t bytes;
+  int row_splits, key_splits;
+  size_t stat_bytes, bytes;
 };
 
 Plan plan_grad(const da_prompt& p) {
@@ -847,7 +926,23 @@ Plan plan_grad(const da_prompt& p) {
     plan.key_items =
         most_tiles(p.key_start, p.B, p.N, p.keys, 1, KeysForm<T, d.value>::keys);
   });
-  plan.bytes = (size_t)p.rows * p.h_q * 2 * sizeof(float);
+  // Few tiles are divided, so that the card is busy (a sequence of 2048 rows, 32/8 heads
+  // of 128: dK and dV 234 us whole, 104 in four parts).
+  auto parts = [&](int64_t items, int64_t tile, int64_t most, size_t* bytes) {
+    const int64_t groups = items * p.h_kv;
+    const int splits = groups < kCus ? (int)std::min(2 * kCus / groups, std::max<int64_t>(most, 1)) : 1;
+    if (splits > 1) *bytes = std::max(*bytes, (size_t)(groups * splits * tile * p.d) * sizeof(float));
+    return splits;
+  };
+  size_t part_bytes = 0;
+  with_type_and_dim(p.dtype, p.d, [&](auto t, auto d) {
+    using T = typename decltype(t)::type;
+    plan.row_splits = parts(plan.row_items, RowsForm<T, d.value>::rows, p.N / 256, &part_bytes);
+    plan.key_splits =
+        parts(plan.key_items, 2 * KeysForm<T, d.value>::keys, p.T * G / 256, &part_bytes);
+  });
+  plan.stat_bytes = ((size_t)p.rows * p.h_q * 2 * sizeof(float) + 15) & ~(size_t)15;
+  plan.bytes = plan.stat_bytes + part_bytes;
   return plan;
 }
 
@@ -878,7 +973,8 @@ da_status da_prompt_attn_grad(const da_prompt* prompt, const void* q, int64_t q_
     if (!stride_fits(x, p.h_kv, p.d, p.dtype)) return DA_ERR_SHAPE;
   if (st != DA_OK) return st;
   const Plan plan = plan_grad(p);
-  if (plan.row_items * p.h_kv > kMaxGroups || plan.key_items * p.h_kv > kMaxGroups)
+  if (plan.row_items * p.h_kv * plan.row_splits > kMaxGroups ||
+      plan.key_items * p.h_kv * plan.key_splits > kMaxGroups)
     return DA_ERR_SHAPE;
   for (const void* x : {q, k, v, out, d_out, (const void*)dq, (const void*)dk, (const void*)dv})
     if (!aligned(x, 16)) return DA_ERR_ALIGN;
@@ -903,15 +999,26 @@ da_status da_prompt_attn_grad(const da_prompt* prompt, const void* q, int64_t q_
   a.scale = scale, a.scale2 = scale * kLog2e;
   a.lse2 = static_cast<float*>(workspace);
   a.delta = a.lse2 + (int64_t)p.rows * p.h_q;
+  a.row_splits = plan.row_splits, a.key_splits = plan.key_splits;
+  a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.stat_bytes);
   const Batch bt = device_batch(p);
   hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   with_type_and_dim(p.dtype, p.d, [&](auto t, auto d) {
     using T = typename decltype(t)::type;
-    hipLaunchKernelGGL((prompt_grad_rows_kernel<T, d.value>),
-                       dim3((unsigned)(plan.row_items * p.h_kv)), dim3(kThreads), 0, s, bt, a);
-    hipLaunchKernelGGL((prompt_grad_keys_kernel<T, d.value>),
-                       dim3((unsigned)(plan.key_items * p.h_kv)), dim3(kThreads), 0, s, bt, a);
+    constexpr int D = d.value, kPass = kThreads / (D / 4);     // rows of a merge's pass
+    const unsigned row_groups = (unsigned)(plan.row_items * p.h_kv);
+    const unsigned key_groups = (unsigned)(plan.key_items * p.h_kv);
+    hipLaunchKernelGGL((prompt_grad_rows_kernel<T, D>), dim3(row_groups * plan.row_splits),
+                       dim3(kThreads), 0, s, bt, a);
+    if (plan.row_splits > 1)
+      hipLaunchKernelGGL((prompt_grad_merge_kernel<T, D, true>),
+                         dim3(row_groups, RowsForm<T, D>::rows / kPass), dim3(kThreads), 0, s, bt, a);
+    hipLaunchKernelGGL((prompt_grad_keys_kernel<T, D>), dim3(key_groups * plan.key_splits),
+                       dim3(kThreads), 0, s, bt, a);
+    if (plan.key_splits > 1)
+      hipLaunchKernelGGL((prompt_grad_merge_kernel<T, D, false>),
+                         dim3(key_groups, KeysForm<T, D>::keys / kPass), dim3(kThreads), 0, s, bt, a);
   });
   return launch_status();
 }
