@@ -7,8 +7,9 @@ returns an error status, a Python exception is raised.
 
 Tensors must be contiguous, on the current HIP device, float32 (int32 for
 ``len``).  Calls are asynchronous on torch's current stream (or ``stream``).
-The ``paged_*`` calls also take bfloat16 and float16, and rows with a stride
-between tokens (views into a fused projection's output).
+The ``paged_*`` and ``prompt_*`` calls and ``rotary_axes`` also take bfloat16 and
+float16, and rows with a stride between tokens (views into a fused projection's
+output).
 """
 from __future__ import annotations
 
@@ -392,13 +393,14 @@ def kv_append_rows(K, V, k_new, v_new, lens, stream=None) -> None:
 
 # --- paged cache ----------------------------------------------------------------
 
-# The paged calls' arguments, taken apart in C++.  It is made for one Python and one
+# The arguments of the calls from here on, taken apart in C++.  It is made for one Python and one
 # torch; where it cannot be imported, the calls below do the same work in Python
 # (10 us more a call), and all others do not need it.
 try:
     from . import paged_call as _call
     _call.use(*(ctypes.cast(getattr(_lib, f), _vp).value
-                for f in ("da_paged_append", "da_paged_gather", "da_paged_attn")))
+                for f in ("da_paged_append", "da_paged_gather", "da_paged_attn",
+                          "da_prompt_attn", "da_prompt_attn_grad", "da_rotary_axes")))
 except ImportError as e:
     import warnings
 
@@ -786,6 +788,16 @@ def prompt_attn(q, k, v, scale: float, causal: bool = True, row_start=None, T: i
     is given and there are as many keys as rows, the keys are the rows' own.  ``lse``
     [rows,h_q] float32 is written where given: what prompt_attn_grad needs.  Any stride
     between tokens.  An ``out`` or ``workspace`` not given is allocated on ``stream``."""
+    if out is None:
+        out = _empty(q, "q", stream)
+    fast = _fast(q, stream) if workspace is not None else None
+    if fast is not None:
+        status = _call.prompt(q, k, v, scale, causal, row_start, T, key_start, N, out, lse,
+                              workspace, *fast)
+        if status == 0:
+            return out
+        if status > 0:
+            _check("da_prompt_attn", status)
     p, gpu = _prompt(q, k, row_start, T, key_start, N, causal)
     rows, h_q, d = q.shape
     keys, h_kv = k.shape[:2]
@@ -793,8 +805,6 @@ def prompt_attn(q, k, v, scale: float, causal: bool = True, row_start=None, T: i
     qp, qs = _tokens(q, "q", dtype, gpu, rows, h_q, d)
     kp, ks = _tokens(k, "k", dtype, gpu, keys, h_kv, d)
     vp, vs = _tokens(v, "v", dtype, gpu, keys, h_kv, d)
-    if out is None:
-        out = _empty(q, "q", stream)
     op = _here(out, "out", dtype, gpu)
     _need(out.shape == q.shape, "out must have q's shape")
     lp = None
@@ -819,6 +829,20 @@ def prompt_attn_grad(q, k, v, out, lse, d_out, scale: float, causal: bool = True
     for d_out [rows,h_q,d], out and lse being that call's.  dq, dk and dv may be given
     with any stride between tokens (views into a fused projection's gradient); those
     not given, and the workspace, are allocated on ``stream``."""
+    if dq is None:
+        dq = _empty(q, "q", stream)
+    if dk is None:
+        dk = _empty(k, "k", stream)
+    if dv is None:
+        dv = _empty(v, "v", stream)
+    fast = _fast(q, stream) if workspace is not None else None
+    if fast is not None:
+        status = _call.prompt_grad(q, k, v, out, lse, d_out, scale, causal, row_start, T,
+                                   key_start, N, dq, dk, dv, workspace, *fast)
+        if status == 0:
+            return dq, dk, dv
+        if status > 0:
+            _check("da_prompt_attn_grad", status)
     p, gpu = _prompt(q, k, row_start, T, key_start, N, causal)
     rows, h_q, d = q.shape
     keys, h_kv = k.shape[:2]
@@ -831,12 +855,6 @@ def prompt_attn_grad(q, k, v, out, lse, d_out, scale: float, causal: bool = True
     lp = _here(lse, "lse", _f32, gpu)
     _need(lse.shape == (rows, h_q), "lse must be [rows,h_q]")
     g = _tokens(d_out, "d_out", dtype, gpu, rows, h_q, d)
-    if dq is None:
-        dq = _empty(q, "q", stream)
-    if dk is None:
-        dk = _empty(k, "k", stream)
-    if dv is None:
-        dv = _empty(v, "v", stream)
     results = (*_tokens(dq, "dq", dtype, gpu, rows, h_q, d),
                *_tokens(dk, "dk", dtype, gpu, keys, h_kv, d),
                *_tokens(dv, "dv", dtype, gpu, keys, h_kv, d))
@@ -859,6 +877,18 @@ def rotary_axes(q, positions, table, sections, k=None, interleaved: bool = False
     each axis turns.  ``inverse`` turns back, which is the gradient.  Any stride
     between tokens; results not given are allocated on ``stream``, and may be the
     inputs."""
+    if q_out is None:
+        q_out = _empty(q, "q", stream)
+    if k is not None and k_out is None:
+        k_out = _empty(k, "k", stream)
+    fast = _fast(q, stream)
+    if fast is not None:
+        status = _call.rotary(q, positions, table, sections, k, interleaved, inverse, q_out,
+                              k_out, *fast)
+        if status == 0:
+            return q_out, k_out if k is not None else None
+        if status > 0:
+            _check("da_rotary_axes", status)
     rows, h_q, d = _rows(q, "q")
     dtype = q.dtype
     code = _DTYPES.get(dtype)
@@ -875,16 +905,12 @@ def rotary_axes(q, positions, table, sections, k=None, interleaved: bool = False
     _need(table.dim() == 2, "table must be [positions, rot_dim]")
     n_table, rot_dim = table.shape
     qp, qs = _tokens(q, "q", dtype, gpu, rows, h_q, d)
-    if q_out is None:
-        q_out = _empty(q, "q", stream)
     qo, qos = _tokens(q_out, "q_out", dtype, gpu, rows, h_q, d)
     h_kv = ks = kos = 0
     kp = ko = None
     if k is not None:
         h_kv = _rows(k, "k")[1]
         kp, ks = _tokens(k, "k", dtype, gpu, rows, h_kv, d)
-        if k_out is None:
-            k_out = _empty(k, "k", stream)
         ko, kos = _tokens(k_out, "k_out", dtype, gpu, rows, h_kv, d)
     try:
         p = _pack_rotary(pp, tp, rows, d, code, n_table, rot_dim, axes,
@@ -896,4 +922,4 @@ def rotary_axes(q, positions, table, sections, k=None, interleaved: bool = False
                                  _paged_stream(stream, gpu))
     if status:
         _check("da_rotary_axes", status)
-    return q_out, k_out
+    return q_out, k_out if k is not None else None

@@ -1,4 +1,5 @@
-// paged_call.cpp -- the paged calls' arguments, taken apart in C++.
+// paged_call.cpp -- the arguments of the paged calls, of prompt attention and of the
+// rotation by several axes, taken apart in C++.
 //
 // A decode step makes two calls a layer, whose kernels take 3 to 10 us on small
 // batches; looking at ten tensors from Python takes as long (0.1 us an
@@ -16,6 +17,9 @@ namespace {
 decltype(&da_paged_append) g_append;
 decltype(&da_paged_gather) g_gather;
 decltype(&da_paged_attn) g_attn;
+decltype(&da_prompt_attn) g_prompt;
+decltype(&da_prompt_attn_grad) g_prompt_grad;
+decltype(&da_rotary_axes) g_rotary;
 
 using at::Tensor;
 
@@ -173,6 +177,173 @@ PyObject* attn_call(PyObject* const* a, Py_ssize_t n) {
                                 (size_t)ws->numel(), stream));
 }
 
+int type_of(const Tensor& t) {
+  const at::ScalarType type = t.scalar_type();
+  return type == at::kFloat ? DA_F32 : type == at::kBFloat16 ? DA_BF16
+         : type == at::kHalf ? DA_F16 : -1;
+}
+
+// The starts of packed sequences, or NULL; *B: how many sequences, 0 if not known.
+bool starts(PyObject* o, long most, long gpu, const int32_t** p, int64_t* B) {
+  *p = nullptr;
+  if (o == Py_None) return true;
+  const Tensor* t = whole(o, at::kInt, gpu);
+  if (!t || t->dim() != 1 || t->size(0) < 2 || most < 1 || (*B && *B != t->size(0) - 1)) return false;
+  *p = static_cast<const int32_t*>(t->data_ptr());
+  *B = t->size(0) - 1;
+  return true;
+}
+
+// The packed sequences that q, k, the starts and T and N describe.
+bool prompt(PyObject* q_, PyObject* k_, PyObject* row_start, long T, PyObject* key_start, long N,
+            int causal, long gpu, da_prompt* p) {
+  if (!THPVariable_Check(q_) || !THPVariable_Check(k_)) return false;
+  const Tensor &q = THPVariable_Unpack(q_), &k = THPVariable_Unpack(k_);
+  if (q.dim() != 3 || k.dim() != 3 || type_of(q) < 0 || T < 0 || N < 0) return false;
+  const int64_t rows = q.size(0), keys = k.size(0);
+  if (key_start == Py_None && N == 0 && row_start != Py_None && keys == rows)
+    key_start = row_start, N = T;
+  const int32_t *rs, *ks;
+  int64_t B = 0;
+  if (!starts(row_start, T, gpu, &rs, &B) || !starts(key_start, N, gpu, &ks, &B)) return false;
+  if (!rs) {
+    if (!B) B = T > 0 ? rows / T : 1;
+    if (B < 1) return false;
+    if (!T) T = rows / B;
+    if (rows != B * T) return false;
+  }
+  if (!ks) {
+    if (!N) N = keys / B;
+    if (keys != B * N) return false;
+  }
+  for (int64_t x : {B, q.size(1), k.size(1), q.size(2), rows, keys, (int64_t)T, (int64_t)N})
+    if (!fits(x)) return false;
+  *p = {rs, ks, (int)B, (int)q.size(1), (int)k.size(1), (int)q.size(2),
+        (int)rows, (int)keys, (int)T, (int)N, type_of(q), causal};
+  return true;
+}
+
+// [rows][h_q] float, contiguous.
+const Tensor* statistics(PyObject* o, const da_prompt& p, long gpu) {
+  const Tensor* t = whole(o, at::kFloat, gpu);
+  return t && t->dim() == 2 && t->size(0) == p.rows && t->size(1) == p.h_q ? t : nullptr;
+}
+
+// prompt(q, k, v, scale, causal, row_start, T, key_start, N, out, lse, workspace, gpu, stream)
+PyObject* prompt_call(PyObject* const* a, Py_ssize_t n) {
+  if (n != 14) return not_here();
+  const double scale = PyFloat_AsDouble(a[3]);
+  const long T = PyLong_AsLong(a[6]), N = PyLong_AsLong(a[8]), gpu = PyLong_AsLong(a[12]);
+  void* stream = PyLong_AsVoidPtr(a[13]);
+  if (PyErr_Occurred()) {
+    PyErr_Clear();
+    return not_here();
+  }
+  const int causal = truth(a[4]);
+  da_prompt p;
+  if (causal < 0 || !prompt(a[0], a[1], a[5], T, a[7], N, causal, gpu, &p)) return not_here();
+  const at::ScalarType type = THPVariable_Unpack(a[0]).scalar_type();
+  int64_t qs, ks, vs;
+  const Tensor* q = tokens(a[0], type, gpu, p.rows, p.h_q, p.d, &qs);
+  const Tensor* k = tokens(a[1], type, gpu, p.keys, p.h_kv, p.d, &ks);
+  const Tensor* v = tokens(a[2], type, gpu, p.keys, p.h_kv, p.d, &vs);
+  const Tensor* out = whole(a[9], type, gpu);
+  const Tensor* lse = a[10] == Py_None ? nullptr : statistics(a[10], p, gpu);
+  const Tensor* ws = whole(a[11], at::kByte, gpu);
+  if (!q || !k || !v || !out || out->sizes() != q->sizes() || (a[10] != Py_None && !lse) || !ws)
+    return not_here();
+  return PyLong_FromLong(g_prompt(&p, q->data_ptr(), qs, k->data_ptr(), ks, v->data_ptr(), vs,
+                                  (float)scale, out->data_ptr(),
+                                  lse ? static_cast<float*>(lse->data_ptr()) : nullptr,
+                                  ws->data_ptr(), (size_t)ws->numel(), stream));
+}
+
+// prompt_grad(q, k, v, out, lse, d_out, scale, causal, row_start, T, key_start, N, dq, dk, dv,
+//             workspace, gpu, stream)
+PyObject* prompt_grad_call(PyObject* const* a, Py_ssize_t n) {
+  if (n != 18) return not_here();
+  const double scale = PyFloat_AsDouble(a[6]);
+  const long T = PyLong_AsLong(a[9]), N = PyLong_AsLong(a[11]), gpu = PyLong_AsLong(a[16]);
+  void* stream = PyLong_AsVoidPtr(a[17]);
+  if (PyErr_Occurred()) {
+    PyErr_Clear();
+    return not_here();
+  }
+  const int causal = truth(a[7]);
+  da_prompt p;
+  if (causal < 0 || !prompt(a[0], a[1], a[8], T, a[10], N, causal, gpu, &p)) return not_here();
+  const at::ScalarType type = THPVariable_Unpack(a[0]).scalar_type();
+  int64_t qs, ks, vs, gs, dqs, dks, dvs;
+  const Tensor* q = tokens(a[0], type, gpu, p.rows, p.h_q, p.d, &qs);
+  const Tensor* k = tokens(a[1], type, gpu, p.keys, p.h_kv, p.d, &ks);
+  const Tensor* v = tokens(a[2], type, gpu, p.keys, p.h_kv, p.d, &vs);
+  const Tensor* out = whole(a[3], type, gpu);
+  const Tensor* lse = statistics(a[4], p, gpu);
+  const Tensor* g = tokens(a[5], type, gpu, p.rows, p.h_q, p.d, &gs);
+  const Tensor* dq = tokens(a[12], type, gpu, p.rows, p.h_q, p.d, &dqs);
+  const Tensor* dk = tokens(a[13], type, gpu, p.keys, p.h_kv, p.d, &dks);
+  const Tensor* dv = tokens(a[14], type, gpu, p.keys, p.h_kv, p.d, &dvs);
+  const Tensor* ws = whole(a[15], at::kByte, gpu);
+  if (!q || !k || !v || !out || out->sizes() != q->sizes() || !lse || !g || !dq || !dk || !dv ||
+      !ws)
+    return not_here();
+  return PyLong_FromLong(g_prompt_grad(
+      &p, q->data_ptr(), qs, k->data_ptr(), ks, v->data_ptr(), vs, out->data_ptr(),
+      static_cast<const float*>(lse->data_ptr()), g->data_ptr(), gs, (float)scale, dq->data_ptr(),
+      dqs, dk->data_ptr(), dks, dv->data_ptr(), dvs, ws->data_ptr(), (size_t)ws->numel(), stream));
+}
+
+// rotary(q, positions, table, sections, k, interleaved, inverse, q_out, k_out, gpu, stream)
+PyObject* rotary_call(PyObject* const* a, Py_ssize_t n) {
+  if (n != 11 || !THPVariable_Check(a[0])) return not_here();
+  const long gpu = PyLong_AsLong(a[9]);
+  void* stream = PyLong_AsVoidPtr(a[10]);
+  const bool is_list = PyList_Check(a[3]);
+  if (PyErr_Occurred() || (!is_list && !PyTuple_Check(a[3]))) {
+    PyErr_Clear();
+    return not_here();
+  }
+  const Py_ssize_t axes = is_list ? PyList_GET_SIZE(a[3]) : PyTuple_GET_SIZE(a[3]);
+  const int interleaved = truth(a[5]), inverse = truth(a[6]);
+  const Tensor& like = THPVariable_Unpack(a[0]);
+  const Tensor *pos = whole(a[1], at::kInt, gpu), *table = whole(a[2], at::kFloat, gpu);
+  if (axes < 1 || axes > 4 || interleaved < 0 || inverse < 0 || like.dim() != 3 ||
+      type_of(like) < 0 || !pos || pos->dim() != 2 || !table || table->dim() != 2)
+    return not_here();
+  const at::ScalarType type = like.scalar_type();
+  const int64_t rows = like.size(0), h_q = like.size(1), d = like.size(2);
+  int64_t h_kv = 0, qs, qos, ks = 0, kos = 0;
+  const Tensor* q = tokens(a[0], type, gpu, rows, h_q, d, &qs);
+  const Tensor* q_out = tokens(a[7], type, gpu, rows, h_q, d, &qos);
+  const Tensor *k = nullptr, *k_out = nullptr;
+  if (a[4] != Py_None) {
+    if (!THPVariable_Check(a[4]) || THPVariable_Unpack(a[4]).dim() != 3) return not_here();
+    h_kv = THPVariable_Unpack(a[4]).size(1);
+    k = tokens(a[4], type, gpu, rows, h_kv, d, &ks);
+    k_out = tokens(a[8], type, gpu, rows, h_kv, d, &kos);
+    if (!k || !k_out) return not_here();
+  }
+  if (!q || !q_out || pos->size(0) != axes || pos->size(1) != rows) return not_here();
+  for (int64_t x : {rows, h_q, h_kv, d, table->size(0), table->size(1)})
+    if (!fits(x)) return not_here();
+  da_rotary p = {static_cast<const int32_t*>(pos->data_ptr()),
+                 static_cast<const float*>(table->data_ptr()), (int)rows, (int)d, type_of(like),
+                 (int)table->size(0), (int)table->size(1), (int)axes, {0, 0, 0, 0}, interleaved,
+                 inverse};
+  for (Py_ssize_t x = 0; x < axes; ++x) {
+    PyObject* o = is_list ? PyList_GET_ITEM(a[3], x) : PyTuple_GET_ITEM(a[3], x);
+    const long section = PyLong_Check(o) ? PyLong_AsLong(o) : -1;
+    if (!fits(section)) {
+      PyErr_Clear();
+      return not_here();
+    }
+    p.sections[x] = (int)section;
+  }
+  return PyLong_FromLong(g_rotary(&p, q->data_ptr(), qs, (int)h_q, q_out->data_ptr(), qos,
+                                  k ? k->data_ptr() : nullptr, ks, (int)h_kv,
+                                  k ? k_out->data_ptr() : nullptr, kos, stream));
+}
+
 // (What torch throws, say for a tensor without storage, is not for here either.)
 template <PyObject* (*call)(PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -183,15 +354,19 @@ PyObject* guarded(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
 }
 
-// use(append, gather, attn): the addresses of the C ABI's functions.
+// use(append, gather, attn, prompt, prompt_grad, rotary): the addresses of the C ABI's
+// functions.
 PyObject* use(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 3) {
-    PyErr_SetString(PyExc_TypeError, "use(append, gather, attn)");
+  if (n != 6) {
+    PyErr_SetString(PyExc_TypeError, "use(append, gather, attn, prompt, prompt_grad, rotary)");
     return nullptr;
   }
   g_append = reinterpret_cast<decltype(g_append)>(PyLong_AsVoidPtr(a[0]));
   g_gather = reinterpret_cast<decltype(g_gather)>(PyLong_AsVoidPtr(a[1]));
   g_attn = reinterpret_cast<decltype(g_attn)>(PyLong_AsVoidPtr(a[2]));
+  g_prompt = reinterpret_cast<decltype(g_prompt)>(PyLong_AsVoidPtr(a[3]));
+  g_prompt_grad = reinterpret_cast<decltype(g_prompt_grad)>(PyLong_AsVoidPtr(a[4]));
+  g_rotary = reinterpret_cast<decltype(g_rotary)>(PyLong_AsVoidPtr(a[5]));
   if (PyErr_Occurred()) return nullptr;
   Py_RETURN_NONE;
 }
@@ -202,6 +377,13 @@ PyMethodDef kMethods[] = {
     {"gather", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(guarded<gather_call>)),
      METH_FASTCALL, ""},
     {"attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(guarded<attn_call>)),
+     METH_FASTCALL, ""},
+    {"prompt", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(guarded<prompt_call>)),
+     METH_FASTCALL, ""},
+    {"prompt_grad",
+     reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(guarded<prompt_grad_call>)),
+     METH_FASTCALL, ""},
+    {"rotary", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(guarded<rotary_call>)),
      METH_FASTCALL, ""},
     {"use", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(use)), METH_FASTCALL, ""},
     {nullptr, nullptr, 0, nullptr}};

@@ -653,10 +653,14 @@ Plan plan_attn(const da_prompt& p) {
   }
   plan.items = most_tiles(p.row_start, p.B, p.T, p.rows, G, 128);
   const int64_t groups = plan.items * p.h_kv;
-  if (groups < kCus) {
-    const int64_t most = std::max<int64_t>(ceil_div(p.N, 128), 1);
-    plan.splits = (int)std::min<int64_t>(2 * kCus / groups, most);
-  }
+  // Few tiles are divided by their keys, so that every CU has work; more of float32,
+  // whose products take longer than the merge's launch (two sequences of 1500 rows, 16
+  // heads of 64: 149 us whole, 122 in two parts; bfloat16, 8 of 333 rows over 400 to
+  // 1500 keys, 39 and 45).
+  if (groups < kCus)
+    plan.splits = (int)std::min<int64_t>(2 * kCus / groups, ceil_div(p.N, 128));
+  else if (p.dtype == DA_F32 && p.d == 64 && groups < 3 * kCus)
+    plan.splits = (int)std::max<int64_t>(std::min<int64_t>(3 * kCus / groups, p.N / 512), 1);
   if (plan.splits > 1)
     plan.bytes = (size_t)(groups * plan.splits * 128) * (p.d + 3) * sizeof(float);
   return plan;

@@ -508,3 +508,94 @@ def test_long_keys_whose_scores_rise(cuda_device, scale):
     assert (err <= tol).all(), float((err / tol).max())
     err = np.abs(L[rows][:, heads].double().cpu().numpy() - lse)
     assert (err <= ref.lse_tolerance(lse, spread, seen_n, 128)).all()
+
+
+# --- the binding -------------------------------------------------------------------------
+
+def test_calls_give_the_same_bits_without_the_extension(cuda_device, monkeypatch):
+    from paper_2607_19456_amd import binding
+
+    c = Case("bf16", 64, 4, 2, t=[40, 33], behind=0, seed=24)
+    x = [y.to(cuda_device) for y in (c.q, c.k, c.v, c.g)]
+    start = torch.from_numpy(c.rs).to(cuda_device)
+    table = lib.rotary_table(100, 64)
+    pos = torch.randint(0, 100, (2, c.rows), dtype=torch.int32, device=cuda_device)
+
+    def steps():
+        got = []
+        for p in (dict(row_start=start, T=40), dict(row_start=start, T=40, key_start=start, N=40),
+                  dict(), dict(causal=False, key_start=start[[0, 2]].contiguous(), N=73)):
+            ws = [lib.prompt_workspace(*x[:2], grad=g,
+                                       **{k: v for k, v in p.items() if k != "causal"})
+                  for g in (False, True)]
+            lse = torch.empty(c.rows, 4, device=cuda_device)
+            out = lib.prompt_attn(*x[:3], c.scale, lse=lse, workspace=ws[0], **p)
+            got += [out, lse, *lib.prompt_attn_grad(*x[:3], out, lse, x[3], c.scale,
+                                                    workspace=ws[1], **p)]
+        got += lib.rotary_axes(x[0], pos, table, [16, 16], k=x[1])
+        got += lib.rotary_axes(x[0], pos, table, (0, 32), k=x[1], interleaved=True, inverse=True)
+        return got
+
+    assert binding._call is not None
+    first = steps()
+    monkeypatch.setattr(binding, "_call", None)
+    for a, b in zip(first, steps()):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("extension", [True, False])
+def test_tensors_that_are_refused(cuda_device, monkeypatch, extension):
+    from paper_2607_19456_amd import binding
+
+    if not extension:
+        monkeypatch.setattr(binding, "_call", None)
+    q = torch.randn(6, 4, 64, device=cuda_device)
+    k = torch.randn(6, 2, 64, device=cuda_device)
+    lse, ws = torch.empty(6, 4, device=cuda_device), None
+    start = torch.tensor([0, 6], dtype=torch.int32, device=cuda_device)
+    ws = lib.prompt_workspace(q, k)
+    wg = lib.prompt_workspace(q, k, grad=True)
+    heads = torch.randn(4, 6, 64, device=cuda_device).transpose(0, 1)
+
+    def attn(q=q, k=k, v=k, **kw):
+        return lib.prompt_attn(q, k, v, 0.1, **{"workspace": ws, **kw})
+
+    def grad(q=q, k=k, v=k, out=q, lse=lse, g=q, **kw):
+        return lib.prompt_attn_grad(q, k, v, out, lse, g, 0.1, **{"workspace": wg, **kw})
+
+    for call in (lambda: attn(v=k.bfloat16()), lambda: attn(v=k.cpu()), lambda: attn(lse=lse.half()),
+                 lambda: attn(row_start=start.long(), T=6), lambda: attn(workspace=ws.float()),
+                 lambda: grad(g=q.half()), lambda: grad(dk=k.cpu()), lambda: grad(lse=lse.double())):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: attn(q=heads), lambda: attn(v=k[:5]), lambda: attn(v=k[:, :1]),
+                 lambda: attn(out=q[:, :2].contiguous()), lambda: attn(out=heads),
+                 lambda: attn(lse=lse.t()), lambda: attn(lse=lse[:5]),
+                 lambda: attn(row_start=start), lambda: attn(row_start=start[:1], T=6),
+                 lambda: attn(T=4), lambda: attn(T=-1), lambda: attn(T=3, N=2),
+                 lambda: attn(row_start=start, T=6, key_start=start[[0, 0, 1]].contiguous(), N=6),
+                 lambda: grad(g=q[:, :2]), lambda: grad(dq=q[:, :2]), lambda: grad(dv=heads)):
+        with pytest.raises(ValueError):
+            call()
+    many = torch.randn(5000, 2, 64, device=cuda_device)     # read in parts
+    for call in (lambda: attn(k=many, v=many, workspace=ws[:3]), lambda: grad(workspace=wg[:40]),
+                 lambda: attn(q=torch.randn(6, 3, 64, device=cuda_device)),
+                 lambda: attn(q=torch.randn(6, 4, 80, device=cuda_device),
+                              k=torch.randn(6, 2, 80, device=cuda_device),
+                              v=torch.randn(6, 2, 80, device=cuda_device))):
+        with pytest.raises((lib.DecodeAttnError, ValueError)):
+            call()
+    table, pos = lib.rotary_table(9, 64), torch.zeros(2, 6, dtype=torch.int32, device=cuda_device)
+    for call in (lambda: lib.rotary_axes(q, pos.long(), table, (16, 16)),
+                 lambda: lib.rotary_axes(q, pos, table.half(), (16, 16)),
+                 lambda: lib.rotary_axes(q, pos, table, (16, 16), k=k.half())):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: lib.rotary_axes(q, pos, table, (32,)),
+                 lambda: lib.rotary_axes(q, pos, table, ()),
+                 lambda: lib.rotary_axes(heads, pos, table, (16, 16)),
+                 lambda: lib.rotary_axes(q, pos, table, (16, 16), k=k[:5])):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(lib.DecodeAttnError):
+        lib.rotary_axes(q, pos, table, (16, 17))
