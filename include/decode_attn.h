@@ -481,8 +481,8 @@ size_t da_paged_workspace_counter_bytes(int B, int h_q, int h_kv, int d, int T,
  * h_q; T*(h_q/h_kv) and N up to 2^30.  All sizes are at least 1: sequences may
  * have no rows or no keys, but arrays of none at all are DA_ERR_SHAPE.  Arrays are
  * 16-byte aligned (lse and the starts 4), strides between tokens multiples of 16
- * bytes and at least a token's own size.  Errors are checked in the order of the
- * enumeration (workspace last).
+ * bytes, at least a token's own size and at most 4 MiB.  Errors are checked in the
+ * order of the enumeration (workspace last).
  * ---------------------------------------------------------------------------
  */
 typedef struct da_prompt {
@@ -506,7 +506,8 @@ typedef struct da_prompt {
  * Scores, softmax and sums in 32 bits; 16-bit types multiply in their own type
  * (weights rounded to it, once, and divided by the sum of the rounded ones; lse
  * is that of the unrounded ones), float32 in float32.  Every sum has one order:
- * equal calls give equal bits.  One launch, or two where few rows see many keys.
+ * equal calls give equal bits.  One launch, or two where the rows' tiles are fewer
+ * than the card's compute units and their keys are read in parts.
  * workspace: da_prompt_workspace_bytes(...) bytes, 16-byte aligned, one call at
  * a time; it may hold anything.
  */
@@ -533,7 +534,9 @@ size_t da_prompt_workspace_bytes(const da_prompt *prompt);
  * and an infinity what the formulas give.  P carries the error of lse, 2^-23 of
  * its size.  Rows with an lse of -infinity have no weights.
  * Sums in 32 bits; 16-bit types multiply in their own type (P and dS rounded to
- * it, once), float32 in float32.  No atomics: equal calls give equal bits.
+ * it, once: float16 takes dS below 2^-24 for 0 and beyond 65504 for infinity), float32
+ * in float32.  With a scale of 0 the scores must be finite.  No atomics: equal calls
+ * give equal bits.  Two launches, four where tiles are few.
  * workspace: da_prompt_grad_workspace_bytes(...), as above.
  */
 da_status da_prompt_attn_grad(const da_prompt *prompt, const void *q,

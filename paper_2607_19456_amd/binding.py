@@ -404,7 +404,7 @@ try:
 except ImportError as e:
     import warnings
 
-    warnings.warn(f"paged_call cannot be imported ({e}); paged calls take their arguments apart "
+    warnings.warn(f"paged_call cannot be imported ({e}); calls take their arguments apart "
                   "in Python. Run __graft_entry__.build() to build it.", RuntimeWarning)
     _call = None
 
@@ -445,7 +445,7 @@ def rotary_table(n: int, rot_dim: int, base: float = 10000.0, device="cuda") -> 
 
 
 def _refuse(t, name, dtype, gpu):
-    """The error of a tensor that a paged call cannot take."""
+    """The error of a tensor that a call cannot take."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype != dtype:
@@ -787,7 +787,7 @@ def prompt_attn(q, k, v, scale: float, causal: bool = True, row_start=None, T: i
     sequence has T rows (0: one sequence), without ``key_start`` N keys; where neither
     is given and there are as many keys as rows, the keys are the rows' own.  ``lse``
     [rows,h_q] float32 is written where given: what prompt_attn_grad needs.  Any stride
-    between tokens.  An ``out`` or ``workspace`` not given is allocated on ``stream``."""
+    between tokens up to 4 MiB.  An ``out`` or ``workspace`` not given is allocated on ``stream``."""
     if out is None:
         out = _empty(q, "q", stream)
     fast = _fast(q, stream) if workspace is not None else None

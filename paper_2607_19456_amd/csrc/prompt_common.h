@@ -124,7 +124,7 @@ __device__ __forceinline__ bool find(const Batch& bt, bool by_rows, int R, int i
     int x = max(first - 1 - m, 0);
     for (int b = 64 + lane; b < bt.B; b += 64) {
       Span r1, k1;
-      x += max(look(b, &r1, &k1) - 1 - m, 0);
+      x = min(x + max(look(b, &r1, &k1) - 1 - m, 0), 1 << 24);    // (more than all items)
     }
     return wave_sum(x);
   };

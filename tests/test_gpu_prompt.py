@@ -210,6 +210,41 @@ def test_views_into_fused_projections(cuda_device, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+def test_out_in_the_place_of_q(cuda_device, dtype):
+    """Whole, and with the keys read in parts."""
+    for c in (Case(dtype, 64, 4, 2, t=[300, 33], behind=0, seed=25),
+              Case(dtype, 128, 8, 2, t=[9], n=[3000], behind=0, seed=26)):
+        want, _ = c.forward(cuda_device)
+        q = c.q.to(cuda_device)
+        lib.prompt_attn(q, c.k.to(cuda_device), c.v.to(cuda_device), c.scale, out=q,
+                        **c.packed(cuda_device))
+        assert torch.equal(q, want)
+
+
+def test_the_largest_strides(cuda_device):
+    """Tokens 4 MiB apart: offsets within a tile of rows near 2^30."""
+    c = Case("bf16", 64, 2, 1, t=[200], behind=0, seed=27)
+    out, lse = c.forward(cuda_device)
+    want = c.backward(cuda_device, out, lse)
+    wide = torch.empty(200, 1 << 21, dtype=torch.bfloat16, device=cuda_device)
+    parts, at = {}, 0
+    for name, x in (("q", c.q), ("k", c.k), ("v", c.v), ("g", c.g), ("dq", c.q), ("dk", c.k),
+                    ("dv", c.v)):
+        n = x.shape[1] * 64
+        parts[name] = wide[:, at:at + n].unflatten(1, (-1, 64))
+        parts[name].copy_(x)
+        at += n
+    p = c.packed(cuda_device)
+    got, L = torch.empty_like(out), torch.empty_like(lse)
+    lib.prompt_attn(parts["q"], parts["k"], parts["v"], c.scale, out=got, lse=L, **p)
+    assert torch.equal(got, out) and torch.equal(L, lse)
+    lib.prompt_attn_grad(parts["q"], parts["k"], parts["v"], out, lse, parts["g"], c.scale,
+                         dq=parts["dq"], dk=parts["dk"], dv=parts["dv"], **p)
+    for x, y in zip((parts["dq"], parts["dk"], parts["dv"]), want):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_starts_that_lie(cuda_device, dtype):
     """Longer sequences than T and N, starts that fall, are negative or beyond the
     arrays: what lies within is taken, the rest is not touched."""

@@ -74,6 +74,7 @@ def test_arguments_that_are_refused(call):
         assert call(**{name: least - 8}) == SHAPE, name
         assert call(**{name: least + 4}) == ALIGN, name
         assert call(**{name: -least}) == SHAPE, name
+        assert call(**{name: (1 << 21) + 8}) == SHAPE, name        # more than 4 MiB
     for bad in (math.nan, math.inf, -math.inf):
         assert call(scale=bad) == SCALE
     size = lib.da_prompt_workspace_bytes if call is attn else lib.da_prompt_grad_workspace_bytes
