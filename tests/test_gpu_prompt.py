@@ -480,6 +480,20 @@ def test_many_short_sequences(cuda_device):
 
 # --- the forms that large calls take ---------------------------------------------------
 
+@pytest.mark.parametrize("B,t_max,h_q,h_kv", [(65, 300, 4, 1), (128, 90, 8, 2), (200, 40, 12, 1),
+                                              (4096, 3, 4, 2), (4100, 2, 8, 1)])
+@pytest.mark.parametrize("even", [False, True])
+def test_many_sequences(cuda_device, B, t_max, h_q, h_kv, even):
+    """More sequences than a wave looks at in a step, and than it looks at in two: all their
+    items are found, once each, whether lengths differ (some are 0) or not."""
+    rng = np.random.default_rng(B + t_max)
+    t = [t_max] * B if even else [int(x) for x in rng.integers(0, t_max + 1, B)]
+    n = None if even else [int(x) for x in rng.integers(0, 2 * t_max + 1, B)]
+    c = Case("bf16", 64, h_q, h_kv, t=t, n=n, seed=B)
+    check_gradient(c, cuda_device)
+    check_forward(c, cuda_device)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("causal", [True, False])
 def test_long_keys_and_many_rows(cuda_device, dtype, causal):
