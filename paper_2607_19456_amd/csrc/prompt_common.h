@@ -89,7 +89,7 @@ __device__ __forceinline__ int seen_by(const Batch& bt, int rows, int keys, int 
 // So within each block of 64 sequences, a lane each.  The blocks' items begin at
 // start * G / R + b, which leaves room for all before (a sequence's last tile may be
 // partly empty), so no sequence is counted but the block's own: 4096 sequences of 64
-// rows took 5976 us when each workgroup counted them all.
+// rows: 1483 us (32/8 heads of 128), 5976 when each workgroup counted them all.
 struct Place {
   Span rows, keys;
   int after, tiles;

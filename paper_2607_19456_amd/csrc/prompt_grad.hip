@@ -65,24 +65,27 @@ __device__ __forceinline__ float dot16(u32x4 a, u32x4 b, float sum) {
 //   S^T = K . Q^T, dP^T = V . dO^T, dQ^T += K^T . dS^T
 // for 32 keys at a time: the exponentials between the products of dP, half of dS
 // between those of dQ, operands read two products ahead, K and V fetched two tiles
-// ahead.  Q and dO of 64 rows take 128 registers, the sums 128 accumulation registers.
-// Measured: one sequence of 8192 rows, 32/8 heads of 128, bfloat16, causal: 720 us, 1145
-// TFLOP/s of its three products (1250 for a library product; 509 with tiles on their way
-// through registers and the sums in whichever the compiler chose).
+// ahead.  32 rows a wave (d = 64 also 64): Q and dO of 128 dimensions take 64 registers, the
+// sums 64 accumulation registers, so two workgroups run on a CU, and one reads or writes
+// its rows (192 KB in, 64 out for 256 rows) while the other multiplies.  64 rows a wave
+// read half as much from LDS, but one workgroup has the CU to itself.
+// Measured, bfloat16, causal, 32/8 heads of 128, us (in brackets with 64 rows a wave, in
+// the same run): one sequence of 8192 rows 860 (907), 4 of 2048 230 (255), 16 of 1024
+// 284 (347), 32 of 512 212 (271), 64 of 256 180 (235).
 // ---------------------------------------------------------------------------
-template <class T, int D>
+template <class T, int D, int NQ>
 struct RowsForm {
-  static constexpr int NQ = is_f32<T> || D == 256 ? 1 : 2;
   static constexpr int rows = 32 * NQ * kWaves;
-  static constexpr int keys = is_f32<T> || D == 256 ? 32 : 64;      // of a tile
+  static constexpr int keys = NQ == 1 ? 32 : 64;                    // of a tile
   static constexpr int tiles = is_f32<T> && D == 256 ? 2 : 3;       // in LDS
+  static constexpr int groups = !is_f32<T> && D == 128 && NQ == 1 ? 2 : 1;     // a CU
 };
 
-template <class T, int D>
-__global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt, GradArgs a) {
+template <class T, int D, int NQ>
+__global__ __launch_bounds__(kThreads, (RowsForm<T, D, NQ>::groups)) void prompt_grad_rows_kernel(Batch bt, GradArgs a) {
   using L = Tile<T, D>;
-  using F = RowsForm<T, D>;
-  constexpr int NQ = F::NQ, KT = F::keys, R = F::rows, NB = F::tiles;
+  using F = RowsForm<T, D, NQ>;
+  constexpr int KT = F::keys, R = F::rows, NB = F::tiles;
   constexpr int ND = L::ND, NW = L::NW;
   constexpr int kTile = KT * L::row_bytes;
   using Fetch = Direct<T, D, KT>;
@@ -424,26 +427,31 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_rows_kernel(Batch bt,
 // and WD of dimensions (each computes the scores, and its dimensions of the
 // results).
 //
-// 64 keys a wave (d = 64 and 128): an operand read from LDS serves two products.  dK and
-// dV of d = 128 take all 256 accumulation registers and K and V 128 of the others, so
-// the rest is kept small: one register of addresses a reader, rows fetched straight to
-// LDS, P packed half a block at a time.  The exponentials stand between the products of
-// dP, dS between those of dV.  Two row waves instead of four key waves: tiles of 128 keys
-// divide a causal batch more evenly than 256.
-// Measured, as above: 1034 us, 1063 TFLOP/s of its four products (446 with 32 keys a wave
-// and the tiles through registers).  A step of 64 rows takes 2.0 us, 46 % of it products
-// at full rate; a masked one 3.4.  A workgroup's start and end take 11 us.
+// d = 128: 64 keys a wave, so an operand read from LDS serves two products.  dK and dV take
+// all 256 accumulation registers and K and V 128 of the others, so the rest is kept small:
+// one register of addresses a reader, rows fetched straight to LDS, P packed half a block at
+// a time.  The exponentials stand between the products of dP, dS between those of dV.  Two
+// row waves instead of four key waves: tiles of 128 keys divide a causal batch more evenly
+// than 256.  Measured, as above: 1025 to 1034 us, 1063 TFLOP/s of its four products (446
+// with 32 keys a wave and the tiles through registers; with 32 and two workgroups a CU, of
+// 256 registers and some in memory, 1.5 times as long).  A step of 64 rows takes 2.0 us, 46 %
+// of it products at full rate; a masked one 3.4.  A workgroup's start and end take 11 us.
+//
+// d = 64: four waves of 32 keys, two workgroups a CU, and no sums of row waves to add.
+// bfloat16, 16 heads, causal, us (in brackets with 64 keys and two row waves): 4 sequences
+// of 4096 rows 341 (404), 16 of 512 48 (68), 32 of 300 52 (87).
 // ---------------------------------------------------------------------------
 template <class T, int D>
 struct KeysForm {
   static constexpr bool wide = is_f32<T> && D == 256;
-  static constexpr int NK = is_f32<T> || D == 256 ? 1 : 2;
-  static constexpr int WK = wide ? 1 : 2, WR = wide ? 1 : 2, WD = wide ? 4 : 1;
+  static constexpr bool slim = !is_f32<T> && D == 64;
+  static constexpr int NK = !is_f32<T> && D == 128 ? 2 : 1;
+  static constexpr int WK = slim ? 4 : wide ? 1 : 2, WR = slim || wide ? 1 : 2, WD = wide ? 4 : 1;
   static constexpr int keys = 32 * NK * WK;
 };
 
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt, GradArgs a) {
+__global__ __launch_bounds__(kThreads, (KeysForm<T, D>::slim ? 2 : 1)) void prompt_grad_keys_kernel(Batch bt, GradArgs a) {
   using L = Tile<T, D>;
   using F = KeysForm<T, D>;
   constexpr int NK = F::NK, WK = F::WK, WR = F::WR, WD = F::WD;
@@ -454,7 +462,8 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
 
   // Steps in LDS: two on their way where there is room for them.
   constexpr int NB = 6 * kTile + 32 * L::row_bytes < 150 << 10 ? 3 : 2;
-  __shared__ __align__(1024) char s_rows[2 * NB][kTile];        // Q's tiles, dO's tiles
+  constexpr int kTiles = std::max(2 * NB, 2 * F::keys / RT);    // (K and V on their way in)
+  __shared__ __align__(1024) char s_rows[kTiles][kTile];        // Q's tiles, dO's tiles
   __shared__ __align__(16) float s_lse[NB][64], s_delta[NB][64];
   // 32 rows of zeros, where there is room
   constexpr bool kZeros = 2 * NB * kTile + NB * 512 + 32 * L::row_bytes < 160 << 10;
@@ -485,7 +494,6 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
   u32x4 kk[NK][NW], vv[NK][NW];
   {
     using Keys = Direct<T, D, F::keys>;
-    static_assert(2 * F::keys <= 2 * NB * RT, "room for K and V");
     char *tile_k = s_rows[0], *tile_v = s_rows[0] + F::keys * L::row_bytes;
     auto bring = [&](char* tile, const char* base, int64_t stride) INLINE {
       const char* first = base + (keys.start + (int64_t)key0) * stride +
@@ -752,9 +760,9 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
   // The row waves' sums, a block of keys at a time: the first is given the other's dK,
   // the second the first's dV, each adds its own; then rows to memory.
   constexpr int kBlock = ND * 4096;          // bytes of a block's sums
-  static_assert(kWaves * 32 * D * 4 / WD <= 2 * NB * kTile && kWaves * kBlock <= 2 * NB * kTile * WD,
+  static_assert(kWaves * 32 * D * 4 / WD <= kTiles * kTile && kWaves * kBlock <= kTiles * kTile * WD,
                 "room for the sums");
-  static_assert(kWaves * 32 * NK * L::row_bytes <= 2 * NB * kTile * WR * WD, "room for the results");
+  static_assert(kWaves * 32 * NK * L::row_bytes <= kTiles * kTile * WR * WD, "room for the results");
   if (skipped) s_skipped = 1;
   // The rows that were left out, pair by pair, those alone that see the key: added to
   // the sums [32 keys][D] that lie in LDS.
@@ -904,8 +912,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_grad_keys_kernel(Batch bt,
 // their order, D/4 lanes a row.
 // ---------------------------------------------------------------------------
 template <class T, int D, bool is_rows>
-__global__ __launch_bounds__(kThreads) void prompt_grad_merge_kernel(Batch bt, GradArgs a) {
-  constexpr int R = is_rows ? RowsForm<T, D>::rows : KeysForm<T, D>::keys;
+__global__ __launch_bounds__(kThreads) void prompt_grad_merge_kernel(Batch bt, GradArgs a, int R) {
   constexpr int kPer = D / 4;
   const int tid = threadIdx.x, l = tid % kPer;
   const int head = blockIdx.x % bt.h_kv, item = blockIdx.x / bt.h_kv;
@@ -942,6 +949,7 @@ __global__ __launch_bounds__(kThreads) void prompt_grad_merge_kernel(Batch bt, G
 namespace {
 
 struct Plan {
+  int NQ;                       // blocks of 32 rows a wave
   int64_t row_items, key_items;
   int row_splits, key_splits;
   size_t stat_bytes, bytes;
@@ -950,9 +958,13 @@ struct Plan {
 Plan plan_grad(const da_prompt& p) {
   Plan plan{};
   const int64_t G = p.h_q / p.h_kv;
+  // d = 64: two blocks of rows a wave for long sequences (16 heads, us with two and with one:
+  // 4 sequences of 4096 rows 235 and 243, 16 of 512 38 and 35, 32 of 300 54 and 40).
+  const int64_t seen = p.keys / p.B / (p.causal ? 2 : 1);
+  plan.NQ = p.dtype != DA_F32 && p.d == 64 && seen >= 1024 ? 2 : 1;
   with_type_and_dim(p.dtype, p.d, [&](auto t, auto d) {
     using T = typename decltype(t)::type;
-    plan.row_items = most_tiles(p.row_start, p.B, p.T, p.rows, G, RowsForm<T, d.value>::rows);
+    plan.row_items = most_tiles(p.row_start, p.B, p.T, p.rows, G, 128 * plan.NQ);
     plan.key_items =
         most_tiles(p.key_start, p.B, p.N, p.keys, 1, KeysForm<T, d.value>::keys);
   });
@@ -967,7 +979,7 @@ Plan plan_grad(const da_prompt& p) {
   size_t part_bytes = 0;
   with_type_and_dim(p.dtype, p.d, [&](auto t, auto d) {
     using T = typename decltype(t)::type;
-    plan.row_splits = parts(plan.row_items, RowsForm<T, d.value>::rows, p.N / 256, &part_bytes);
+    plan.row_splits = parts(plan.row_items, 128 * plan.NQ, p.N / 256, &part_bytes);
     plan.key_splits =
         parts(plan.key_items, 2 * KeysForm<T, d.value>::keys, p.T * G / 256, &part_bytes);
   });
@@ -1039,16 +1051,24 @@ da_status da_prompt_attn_grad(const da_prompt* prompt, const void* q, int64_t q_
     constexpr int D = d.value, kPass = kThreads / (D / 4);     // rows of a merge's pass
     const unsigned row_groups = (unsigned)(plan.row_items * p.h_kv);
     const unsigned key_groups = (unsigned)(plan.key_items * p.h_kv);
-    hipLaunchKernelGGL((prompt_grad_rows_kernel<T, D>), dim3(row_groups * plan.row_splits),
-                       dim3(kThreads), 0, s, bt, a);
+    const dim3 grid(row_groups * plan.row_splits);
+    const auto rows = [&](auto nq) {
+      hipLaunchKernelGGL((prompt_grad_rows_kernel<T, D, nq.value>), grid, dim3(kThreads), 0, s, bt, a);
+    };
+    bool done = false;
+    if constexpr (!is_f32<T> && D == 64)
+      if ((done = plan.NQ == 2)) rows(std::integral_constant<int, 2>{});
+    if (!done) rows(std::integral_constant<int, 1>{});
     if (plan.row_splits > 1)
       hipLaunchKernelGGL((prompt_grad_merge_kernel<T, D, true>),
-                         dim3(row_groups, RowsForm<T, D>::rows / kPass), dim3(kThreads), 0, s, bt, a);
+                         dim3(row_groups, 128 * plan.NQ / kPass), dim3(kThreads), 0, s, bt, a,
+                         128 * plan.NQ);
     hipLaunchKernelGGL((prompt_grad_keys_kernel<T, D>), dim3(key_groups * plan.key_splits),
                        dim3(kThreads), 0, s, bt, a);
     if (plan.key_splits > 1)
       hipLaunchKernelGGL((prompt_grad_merge_kernel<T, D, false>),
-                         dim3(key_groups, KeysForm<T, D>::keys / kPass), dim3(kThreads), 0, s, bt, a);
+                         dim3(key_groups, KeysForm<T, D>::keys / kPass), dim3(kThreads), 0, s, bt, a,
+                         KeysForm<T, D>::keys);
   });
   return launch_status();
 }
