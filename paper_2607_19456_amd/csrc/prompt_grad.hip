@@ -318,6 +318,8 @@ __global__ __launch_bounds__(kThreads, (RowsForm<T, D, NQ>::groups)) void prompt
     arrived<2 * Fetch::units*(NB - 2)>();
     __syncthreads();
   }
+  arrived();                                 // (what was fetched beyond the last)
+  __syncthreads();
 
   char* mine = s_all[0] + 32 * NQ * wave * L::row_bytes;
   auto to = [&](int x) INLINE {              // the place of this wave's row x
@@ -756,6 +758,8 @@ __global__ __launch_bounds__(kThreads, (KeysForm<T, D>::slim ? 2 : 1)) void prom
       __syncthreads();
     }
   }
+  arrived();                                 // (what was fetched beyond the last)
+  __syncthreads();
 
   // The row waves' sums, a block of keys at a time: the first is given the other's dK,
   // the second the first's dV, each adds its own; then rows to memory.
@@ -959,9 +963,9 @@ Plan plan_grad(const da_prompt& p) {
   Plan plan{};
   const int64_t G = p.h_q / p.h_kv;
   // d = 64: two blocks of rows a wave for long sequences (16 heads, us with two and with one:
-  // 4 sequences of 4096 rows 235 and 243, 16 of 512 38 and 35, 32 of 300 54 and 40).
-  const int64_t seen = p.keys / p.B / (p.causal ? 2 : 1);
-  plan.NQ = p.dtype != DA_F32 && p.d == 64 && seen >= 1024 ? 2 : 1;
+  // 4 sequences of 4096 rows 235 and 243, 8 of 1500 that see all 132 and 135, 16 of 512 38
+  // and 35, 32 of 300 54 and 40).  The workspace is the same whether causal or not.
+  plan.NQ = p.dtype != DA_F32 && p.d == 64 && p.keys / p.B >= 1500 ? 2 : 1;
   with_type_and_dim(p.dtype, p.d, [&](auto t, auto d) {
     using T = typename decltype(t)::type;
     plan.row_items = most_tiles(p.row_start, p.B, p.T, p.rows, G, 128 * plan.NQ);

@@ -494,6 +494,41 @@ def test_many_sequences(cuda_device, B, t_max, h_q, h_kv, even):
     check_forward(c, cuda_device)
 
 
+@pytest.mark.parametrize("dtype,d,h_q,h_kv,B,t,n", [
+    ("bf16", 128, 32, 2, 51, (194, 201), None), ("f16", 64, 64, 16, 37, (26, 85), None),
+    ("bf16", 128, 8, 8, 35, (515, 719), (1, 4)), ("bf16", 64, 16, 4, 40, (170, 330), (1, 90)),
+    ("bf16", 256, 16, 2, 24, (60, 130), None), ("f32", 64, 16, 4, 40, (60, 130), None)])
+def test_gradient_of_many_workgroups(cuda_device, dtype, d, h_q, h_kv, B, t, n):
+    """Rows and keys are fetched ahead, beyond the last too: while many workgroups share the
+    memory, such a fetch may arrive when the results already pass through LDS."""
+    rng = np.random.default_rng(B + d)
+    counts = rng.integers(t[0], t[1] + 1, B).tolist()
+    keys = None if n is None else rng.integers(n[0], n[1] + 1, B).tolist()
+    c = Case(dtype, d, h_q, h_kv, t=counts, n=keys, causal=n is None, seed=B)
+    out, L = c.forward(cuda_device)
+    first = c.backward(cuda_device, out, L)
+    for again in range(5):
+        for x, y in zip(first, c.backward(cuda_device, out, L)):
+            assert torch.equal(x.nan_to_num(nan=7.0), y.nan_to_num(nan=7.0)), f"call {again}"
+    check_gradient(c, cuda_device)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", DS)
+@pytest.mark.parametrize("rows,keys", [(600, 1600), (600, 2500), (100, 1100), (3000, 3000)])
+def test_a_workspace_serves_masked_calls_and_others(cuda_device, dtype, d, rows, keys):
+    """The workspace's size goes by the arrays, not by what their rows see."""
+    q = torch.randn(rows, 4, d, device=cuda_device).to(ref.DTYPES[dtype])
+    k = torch.randn(keys, 2, d, device=cuda_device).to(ref.DTYPES[dtype])
+    lse = torch.empty(rows, 4, device=cuda_device)
+    ws = lib.prompt_workspace(q, k)
+    back = lib.prompt_workspace(q, k, grad=True)
+    for causal in (True, False):
+        out = lib.prompt_attn(q, k, k, 0.1, causal, lse=lse, workspace=ws)
+        grads = lib.prompt_attn_grad(q, k, k, out, lse, q, 0.1, causal, workspace=back)
+        assert all(torch.isfinite(x).all() for x in (out, *grads))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("causal", [True, False])
 def test_long_keys_and_many_rows(cuda_device, dtype, causal):
