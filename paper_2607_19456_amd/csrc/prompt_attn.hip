@@ -59,7 +59,7 @@ constexpr int kKeys = is_f32<T> || D == 256 ? 32 : 64;     // keys of a tile
 //
 // Measured, bfloat16, causal.  One sequence of 16384 rows, 32/8 heads of 128, 2.2
 // TFLOP: 2093 us, 1050 TFLOP/s (an 8192^3 library product 1247; the form in turn 784);
-// matrix pipes busy for 46 % of the cycles, vector instructions for 41 %, waits 24 %.
+// matrix pipes busy for 49 % of the cycles, vector instructions for 44 %, waits 24 %.
 // Without the fetches and the barrier a tile's step is 11 % shorter, without the
 // exponentials 8 %, without the sums or the maximum 4 %: no one of them bounds it.
 // 4 sequences of 4096, 16 heads of 64: 189 us, 728 TFLOP/s, the softmax (14
