@@ -392,11 +392,14 @@ __device__ __forceinline__ Window window(const char* base, int64_t bytes) {
                 (uint32_t)min(max(bytes, (int64_t)0), (int64_t)0x7fffffff), 0x00027000u}};
 }
 // (In assembly: to the compiler a fetch may write what any later read of LDS
-// reads, so that it would wait for it there.  arrived() stands before the barrier.)
+// reads, so that it would wait for it there.  arrived() stands before the barrier.
+// A scalar register that a vector instruction wrote, as one that is reloaded from a
+// lane, may be read here five wait states later at the earliest: the compiler, which
+// counts them for instructions that it knows, may put such a one right before.)
 __device__ __forceinline__ void fetch(int place, const Window& from, int lane_byte, int byte) {
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"      // (m0 is the compiler's, between its uses)
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                :
                : "s"(place), "v"(lane_byte), "s"(from.words), "s"(byte)
                : "m0");
@@ -406,7 +409,7 @@ __device__ __forceinline__ void fetch(int place, const Window& from, int lane_by
 __device__ __forceinline__ void fetch_word(int place, const Window& from, int lane_byte) {
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds"
                :
                : "s"(place), "v"(lane_byte), "s"(from.words)
                : "m0");
