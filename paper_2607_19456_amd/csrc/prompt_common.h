@@ -203,7 +203,8 @@ __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
 // kernels with more than 256 of them need both.  (The no-op covers the two cycles
 // between a vector instruction's result and its use here, which the compiler counts
 // for instructions that it knows; settle() stands between the last product and the
-// first other use of a sum.)
+// first other use of a sum.  The compiler may copy a sum to other registers before that,
+// where the loop ends: finished() stands there.)
 template <class T>
 __device__ __forceinline__ void mma_far(u32x4 a, u32x4 b, f32x16& c) {
   if constexpr (std::is_same<T, __bf16>::value)
@@ -424,6 +425,11 @@ __device__ __forceinline__ int lds_place(const void* p) {
 template <int more = 0>
 __device__ __forceinline__ void arrived() {
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(more) : "memory");
+}
+
+// All fetches have arrived, and the sums of mma_far() before are there to be copied.
+__device__ __forceinline__ void finished() {
+  asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 7" : : : "memory");
 }
 
 // ROWS rows of a KV head (x0 on; those beyond `last` are the last again) on their way

@@ -318,7 +318,7 @@ __global__ __launch_bounds__(kThreads, (RowsForm<T, D, NQ>::groups)) void prompt
     arrived<2 * Fetch::units*(NB - 2)>();
     __syncthreads();
   }
-  arrived();                                 // (what was fetched beyond the last)
+  finished();                                // (what was fetched beyond the last, too)
   __syncthreads();
 
   char* mine = s_all[0] + 32 * NQ * wave * L::row_bytes;
@@ -758,7 +758,7 @@ __global__ __launch_bounds__(kThreads, (KeysForm<T, D>::slim ? 2 : 1)) void prom
       __syncthreads();
     }
   }
-  arrived();                                 // (what was fetched beyond the last)
+  finished();                                // (what was fetched beyond the last, too)
   __syncthreads();
 
   // The row waves' sums, a block of keys at a time: the first is given the other's dK,

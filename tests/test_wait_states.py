@@ -2,7 +2,9 @@
 for instructions that it knows, not for those inside assembly in the source.
 
 A vector instruction's scalar result may be read by a memory instruction five wait states
-later at the earliest.  A wait state is an instruction, or n + 1 of them with
+later at the earliest, and the sums of a 32 x 32 matrix instruction by one that is none after
+its passes (four cycles each: 8 for 16 products of 16 bits, 16 for 2 of float32) and four, or
+two, more.  A wait state is an instruction, or n + 1 of them with
 ``s_nop n``; every way to an instruction is followed back, over branches too.
 """
 import collections
@@ -112,6 +114,28 @@ def scalars_too_early(code):
     return out
 
 
+SUMS = {"v_mfma_f32_32x32x16_bf16": 12, "v_mfma_f32_32x32x16_f16": 12, "v_mfma_f32_32x32x2_f32": 18}
+
+
+def sums_too_early(code):
+    """Instructions other than products that read, or write over, a product's sums too early."""
+    ways, out = before(code), []
+    for i, x in enumerate(code):
+        if x.name.startswith("v_mfma") or not x.name.startswith(("v_", "ds_") + MEMORY):
+            continue
+        uses = set().union(*(registers(y, "va") for y in x.operands)) if x.operands else set()
+        out += [(x, w, y) for w, y in
+                search(code, ways, i, max(SUMS.values()),
+                       lambda y: y.name in SUMS and registers(y.operands[0], "va") & uses)
+                if w < SUMS[y.name]]
+    return out
+
+
+def said(bad):
+    return "\n".join(f"{name}: {x.name} {x.operands} at {x.at:#x}, {w} wait states after {y.name} "
+                     f"{y.operands}" for name, b in bad.items() for x, w, y in b[:5])
+
+
 @pytest.fixture(scope="module")
 def kernels(tmp_path_factory):
     """All kernels of the library."""
@@ -132,8 +156,14 @@ def kernels(tmp_path_factory):
 def test_scalar_registers_are_written_in_time(kernels):
     bad = {name: scalars_too_early(code) for name, code in kernels.items()}
     bad = {name: x for name, x in bad.items() if x}
-    assert not bad, "\n".join(f"{name}: {x.name} {x.operands} at {x.at:#x}, {w} wait states after "
-                              f"{y.name} {y.operands}" for name, b in bad.items() for x, w, y in b)
+    assert not bad, said(bad)
+
+
+def test_sums_are_there_when_they_are_read(kernels):
+    """Of the kernels whose products are in assembly."""
+    bad = {name: sums_too_early(code) for name, code in kernels.items() if "prompt_" in name}
+    bad = {name: x for name, x in bad.items() if x}
+    assert not bad, said(bad)
 
 
 EARLY = """
@@ -159,3 +189,14 @@ def test_what_the_search_finds():
     code[-2:] = [code[-1]._replace(at=0x101c), Instruction(0x1020, "s_branch", [], 0x8)]
     ((x, w, y),) = scalars_too_early(code)          # the branch alone lies between
     assert (x.at, w) == (0x1010, 1)
+    sums = """
+0000000000001000 <kernel>:
+\tv_mfma_f32_32x32x2_f32 a[0:15], v5, v2, a[0:15]            // 000000001000: D3C48000 04020505
+\ts_nop {nop}                                                   // 000000001008: BF80000F
+\tv_accvgpr_read_b32 v22, a15                                // 00000000100C: D3D84016 1800010F
+\ts_endpgm                                                   // 000000001014: BF810000
+"""
+    (code,) = parse(sums.format(nop=16)).values()
+    assert [(x.at, w) for x, w, _ in sums_too_early(code)] == [(0x100c, 17)]
+    (code,) = parse(sums.format(nop=17)).values()
+    assert not sums_too_early(code)
