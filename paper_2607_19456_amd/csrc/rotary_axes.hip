@@ -75,12 +75,16 @@ __global__ __launch_bounds__(kThreads) void rotary_axes_kernel(RotaryArgs a) {
     v[j].load(src + at1);
   }
   float cosine[8], sine[8];
+  // A bit for each pair but those whose position is outside the table, which are copied
+  // (multiplied by 1 and 0, an infinity's partner would become NaN).
+  unsigned here = 0xffu;
   if (turned) {
     int axis = 0;
     while (axis + 1 < a.axes && pair0 >= a.ends[axis]) ++axis;
     if (pair0 + 8 <= a.ends[axis]) {
       const int pos = a.positions[(int64_t)axis * a.rows + row];
       const bool held = (unsigned)pos < (unsigned)a.n_table;
+      here = held ? 0xffu : 0u;
       const f32x4* angles = reinterpret_cast<const f32x4*>(
           a.table + (int64_t)(held ? pos : 0) * a.rot_dim + pair0);
 #pragma unroll
@@ -88,17 +92,18 @@ __global__ __launch_bounds__(kThreads) void rotary_axes_kernel(RotaryArgs a) {
         const f32x4 c = angles[e / 4], s = angles[half / 4 + e / 4];
 #pragma unroll
         for (int w = 0; w < 4; ++w)
-          cosine[e + w] = held ? c[w] : 1.f, sine[e + w] = held ? a.sign * s[w] : 0.f;
+          cosine[e + w] = c[w], sine[e + w] = a.sign * s[w];
       }
     } else {
+      here = 0u;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         while (axis + 1 < a.axes && pair0 + e >= a.ends[axis]) ++axis;
         const int pos = a.positions[(int64_t)axis * a.rows + row];
         const bool held = (unsigned)pos < (unsigned)a.n_table;
         const float* angles = a.table + (int64_t)(held ? pos : 0) * a.rot_dim + pair0 + e;
-        cosine[e] = held ? angles[0] : 1.f;
-        sine[e] = held ? a.sign * angles[half] : 0.f;
+        here |= held ? 1u << e : 0u;
+        cosine[e] = angles[0], sine[e] = a.sign * angles[half];
       }
     }
   }
@@ -123,6 +128,13 @@ __global__ __launch_bounds__(kThreads) void rotary_axes_kernel(RotaryArgs a) {
         } else {
           y0.x[e] = lo, y1.x[e] = hi;
         }
+      }
+    }
+    if (__builtin_expect(here != 0xffu, 0)) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {          // (pairs of the values e of y0 and of y1)
+        if (!(here >> (a.interleaved ? e / 2 : e) & 1)) y0.x[e] = u[j].x[e];
+        if (!(here >> (a.interleaved ? 4 + e / 2 : e) & 1)) y1.x[e] = v[j].x[e];
       }
     }
     const bool is_q = head < a.h_q;

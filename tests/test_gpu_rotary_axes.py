@@ -61,6 +61,38 @@ def test_positions_outside_the_table_turn_nothing(cuda_device, dtype):
     assert torch.equal(qo[7].cpu(), q[7]) and torch.equal(ko[7].cpu(), k[7])
 
 
+@pytest.mark.parametrize("interleaved,inverse", [(False, False), (True, False), (False, True),
+                                                 (True, True)])
+@pytest.mark.parametrize("sections", [(16, 16), (32,), (10, 12, 10), (3, 2, 0, 27)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_pairs_outside_the_table_are_copied(cuda_device, dtype, sections, interleaved, inverse):
+    """To the bit, whatever the pair's other value is: infinities, NaN, zeros of either
+    sign, the smallest numbers.  The other axes' pairs are turned as ever."""
+    q, k, pos, table = make(cuda_device, dtype, 33, 4, 2, 64, 64, sections, n=20)
+    odd = torch.tensor([math.inf, -math.inf, math.nan, -0.0, 0.0, 3.0, -5.0,
+                        2.0 ** -24 if dtype == "f16" else 2.0 ** -133]).to(q.dtype)
+    bits = torch.int32 if dtype == "f32" else torch.int16
+    rng = np.random.default_rng(4)
+    for axis in range(len(sections)):
+        first = sum(sections[:axis])
+        pairs = torch.arange(first, first + sections[axis])
+        dims = torch.cat((2 * pairs, 2 * pairs + 1) if interleaved else (pairs, pairs + 32))
+        there = pos.clone()
+        there[axis] = torch.tensor([-1, 20, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32).repeat(9)[:33]
+        a = (there.to(cuda_device), table.to(cuda_device), sections)
+        kw = dict(interleaved=interleaved, inverse=inverse)
+        clean = lib.rotary_axes(q.to(cuda_device), *a, k=k.to(cuda_device), **kw)
+        x = [y.clone() for y in (q, k)]
+        for y in x:
+            y[..., dims] = odd[torch.from_numpy(rng.integers(0, len(odd), (*y.shape[:2],
+                                                                           len(dims))))]
+        got = lib.rotary_axes(x[0].to(cuda_device), *a, k=x[1].to(cuda_device), **kw)
+        for y, z, w in zip(got, x, clean):
+            want = w.cpu().clone()
+            want[..., dims] = z[..., dims]
+            assert torch.equal(y.cpu().view(bits), want.view(bits)), axis
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_views_in_place_and_back(cuda_device, dtype):
     """q and k as views into a projection's output, turned in place, the rest left
