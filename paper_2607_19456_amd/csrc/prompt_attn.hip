@@ -635,15 +635,15 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(Batch bt, AttnAr
   f32x4 o{0.f, 0.f, 0.f, 0.f};
   float total = 0.f, all = 0.f;
   for (int s = 0; s < a.splits; ++s) {
+    // (a part with no score above -infinity counts too: its weights of 0 may have met a
+    // value that is not finite)
     const float* st = a.parts + a.stats + part(s) * 3;
-    if (st[0] == -INFINITY) continue;
     const float f = bad ? NAN : st[0] == ref ? 1.f : exp2f(st[0] - ref);
     total += f * st[1], all += f * st[2];
     o += f * *reinterpret_cast<const f32x4*>(a.parts + part(s) * D + 4 * l);
   }
   const bool none = ref == -INFINITY && !bad;
-  const float inverse = none ? 0.f : 1.f / total;
-  o *= inverse;
+  o = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o * (1.f / total);
   char* dst = a.out + place * D * (int)sizeof(T);
   if constexpr (is_f32<T>)
     *reinterpret_cast<f32x4*>(dst + 16 * l) = o;

@@ -362,6 +362,39 @@ def test_scores_that_are_all_minus_infinity(cuda_device, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("h_q,h_kv,B", [(4, 2, 1), (64, 64, 4)])
+def test_weights_of_0_meet_infinities(cuda_device, dtype, h_q, h_kv, B):
+    """A row sees a thousand keys whose scores are -infinity, one of them with an infinity in
+    V, before others: 0 times that is NaN, in its dimension alone, whether the keys are read
+    whole (four sequences of 64 heads) or in parts, one of which has no other scores.  Rows of
+    such scores alone still give 0."""
+    c = Case(dtype, 128, h_q, h_kv, t=[3] * B, n=[3000] * B, causal=False, behind=0, seed=28)
+    c.q[:, :, 0] = 1.0
+    for b in range(B):
+        c.k[3000 * b:3000 * b + 1000, :, 0] = -math.inf
+        c.k[3000 * b + 1000:3000 * (b + 1), :, 0] = 0.0
+    c.v[100, 0, 3], c.v[777, 1, 5] = math.inf, -math.inf
+    out, lse = c.forward(cuda_device)
+    G = h_q // h_kv
+    want = torch.zeros(c.rows, h_q, 128, dtype=torch.bool)
+    want[:3, :G, 3] = want[:3, G:2 * G, 5] = True
+    assert torch.equal(torch.isnan(out).cpu(), want)
+    for head in (0, G, h_q - 1):
+        last = slice(c.keys - 2000, c.keys)
+        q, k, v = c.q[-3:, head:head + 1], c.k[last, [head // G]], c.v[last, [head // G]]
+        o, L, mass, spread, seen, top = ref.attention(q, k, v, c.scale,
+                                                      ref.Batch(3, 2000, T=3, N=2000, causal=False))
+        fine = ~want[-3:, head:head + 1].numpy()
+        err = np.abs(out[-3:, head:head + 1].double().cpu().numpy() - o)[fine]
+        assert (err <= ref.tolerance(o, mass, spread, seen, top, c.type, 128)[fine]).all()
+        err = np.abs(lse[-3:, head:head + 1].double().cpu().numpy() - L)
+        assert (err <= ref.lse_tolerance(L, spread, seen, 128)).all()
+    c.k[:, :, 0] = -math.inf
+    out, lse = c.forward(cuda_device)
+    assert torch.equal(out, torch.zeros_like(out)) and (lse == -math.inf).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_scores_of_any_size(cuda_device, dtype):
     """Far apart, and so large that a reference's rounding would show."""
     top = {"f32": 3e12, "bf16": 3e12, "f16": 200.0}[dtype]
