@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 import torch
 
+import paper_2607_19456_amd as lib
 import prompt_reference as ref
 from test_gpu_prompt import Case, check_forward, check_gradient, compare, say
 
@@ -242,3 +243,94 @@ def test_infinities_reach_what_sees_them(cuda_device, dtype, d, bad, which, t, n
         compare("dk", dk, want[1], tol[1], mine_k)
         compare("dv", dv, want[2], tol[2], mine_k)
         say(f"  {int(skip.sum())} rows, {int(seen_by_them.sum())} keys reached")
+
+
+# --- the operators as a program uses them ---------------------------------------------
+
+def turned_bound(bound, pos, table, sections):
+    """What a bound of the values before a rotation back is after it: each of a pair's
+    values is a sum of both, times a cosine and a sine."""
+    half = table.shape[1] // 2
+    axis = np.repeat(np.arange(len(sections)), sections)
+    at = pos.numpy().astype(np.int64)[axis].T               # [row][pair]
+    pair = np.arange(half)
+    c, s = (np.abs(table.double().numpy()[at, x])[:, None] for x in (pair, half + pair))
+    a, b = bound[..., :half], bound[..., half:]
+    return np.concatenate((a * c + b * s, b * c + a * s), -1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("h_q,h_kv,d,t", [(4, 2, 64, [40, 23]), (8, 2, 128, [130])])
+def test_a_training_step_value_by_value(cuda_device, dtype, h_q, h_kv, d, t):
+    """Turn q and k, attend, the gradient, turned back, each step against its 64-bit form of
+    what the step before gave: dq and dk within the gradient's bound as the rotation passes it
+    on, and the rotation's own.  A twentieth more of either would be found in most values."""
+    c = Case(dtype, d, h_q, h_kv, t=t, behind=0, seed=36)
+    sec, rows = (d // 8, d // 8 + 3, d // 4 - 3), sum(t)
+    rng = np.random.default_rng(37)
+    pos = torch.from_numpy(rng.integers(0, 300, (3, rows)).astype(np.int32))
+    table = lib.rotary_table(300, d, device="cpu")
+    a = (pos.to(cuda_device), table.to(cuda_device), sec)
+    qt, kt = lib.rotary_axes(c.q.to(cuda_device), *a, k=c.k.to(cuda_device))
+    for got, x in ((qt, c.q), (kt, c.k)):
+        want, tol = ref.rotate(x, pos, table, sec, False, False)
+        assert (np.abs(got.double().cpu().numpy() - want) <= tol).all()
+    c.q, c.k = qt.cpu(), kt.cpu()
+    out, lse = check_forward(c, cuda_device)
+    dqt, dkt, dv = c.backward(cuda_device, out, lse)
+    dq, dk = lib.rotary_axes(dqt, *a, k=dkt, inverse=True)
+    want, tol = ref.gradient(c.q, c.k, c.v, out, lse, c.g, c.scale, c.batch)
+    compare("dv", dv, want[2], tol[2], np.ones(rows, bool))
+    for name, got, before, w, b in (("dq", dq, dqt, want[0], tol[0]),
+                                    ("dk", dk, dkt, want[1], tol[1])):
+        # the rotation back of the 64-bit gradient, and the bound of rotating what was there
+        back, _ = ref.rotate(torch.from_numpy(w), pos, table, sec, False, True)
+        _, own = ref.rotate(before.cpu(), pos, table, sec, False, True)
+        bound = turned_bound(b, pos, table, sec) + own
+        compare(name, got, back, bound, np.ones(rows, bool))
+        assert (np.abs(0.05 * back) > bound).mean() > 0.5
+
+
+class Attention(torch.autograd.Function):
+    """How a program that uses autograd has both calls."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, scale, start, longest):
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        out = lib.prompt_attn(q, k, v, scale, row_start=start, T=longest, lse=lse)
+        ctx.save_for_backward(q, k, v, out, lse, start)
+        ctx.scale, ctx.longest = scale, longest
+        return out
+
+    @staticmethod
+    def backward(ctx, d_out):
+        q, k, v, out, lse, start = ctx.saved_tensors
+        return (*lib.prompt_attn_grad(q, k, v, out, lse, d_out.contiguous(), ctx.scale,
+                                      row_start=start, T=ctx.longest), None, None, None)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_in_a_program_that_uses_autograd(cuda_device, dtype):
+    """The calls alone are not recorded; inside a function of autograd their gradient is, and
+    reaches the projection's weights."""
+    c = Case(dtype, 64, 4, 2, t=[50, 33], behind=0, seed=38)
+    start = torch.from_numpy(c.rs).to(cuda_device)
+    x = torch.randn(83, 64, device=cuda_device).to(c.type)
+    w = (torch.randn(64, 8 * 64, device=cuda_device) / 8).to(c.type).requires_grad_()
+    qkv = (x @ w).unflatten(1, (8, 64))
+    q, k, v = qkv.split((4, 2, 2), 1)
+    assert not lib.prompt_attn(q, k, v, c.scale, row_start=start, T=50).requires_grad
+    out = Attention.apply(q, k, v, c.scale, start, 50)
+    g = c.g.to(cuda_device)
+    out.backward(g)
+    with torch.no_grad():
+        lse = torch.empty(83, 4, device=cuda_device)
+        again = lib.prompt_attn(q, k, v, c.scale, row_start=start, T=50, lse=lse)
+        d = lib.prompt_attn_grad(q, k, v, again, lse, g, c.scale, row_start=start, T=50)
+        want = x.t() @ torch.cat(d, 1).flatten(1)
+    assert torch.equal(out, again)
+    # (the same product of the same numbers, which the library may add in another order:
+    # 83 terms, and a rounding on either side)
+    size = x.float().abs().t() @ torch.cat(d, 1).flatten(1).float().abs()
+    assert ((w.grad.float() - want.float()).abs()
+            <= 83 * 2 * ref.E32 * size + 2 * ref.half_step(c.type) * (want.float().abs() + 1e-6)).all()
