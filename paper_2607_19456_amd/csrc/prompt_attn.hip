@@ -150,6 +150,7 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
   // (beside the first keys, where there is room)
   constexpr bool kBeside = (2 * NB - 2) * kTile >= R * L::row_bytes;
   static_assert(2 * NB * kTile >= R * L::row_bytes, "room for the rows");
+  static_assert(!kPipe || kBeside, "a pipeline's first keys come with the rows");
   char* q_rows = s_all[kBeside ? 2 : 0];
   fetch_rows<T, D, R>(q_rows, bt,
                       a.q + rows.start * a.q_stride + (int64_t)head * bt.G * L::row_bytes,
@@ -373,7 +374,6 @@ void prompt_attn_kernel(Batch bt, AttnArgs a) {
     for (int x = tid; x < kTile / 16; x += kThreads)
       reinterpret_cast<u32x4*>(s_zero)[x] = u32x4{0u, 0u, 0u, 0u};
     if (t0 < t1) {
-      if (!kBeside) load_all(t0, true, true);
       load_all(t0 + 1, true, true);
       load_all(t0 + 2, true, false);
       f32x16 sa[NQ][NS], sb[NQ][NS];
