@@ -478,8 +478,10 @@ size_t da_paged_workspace_counter_bytes(int B, int h_q, int h_kv, int d, int T,
  * causal (the last row sees all), else all n.  Head map as above.
  *
  * Supported: d in {64, 128, 256}; types DA_F32, DA_BF16, DA_F16; h_kv dividing
- * h_q; T*(h_q/h_kv) and N up to 2^30.  All sizes are at least 1: sequences may
- * have no rows or no keys, but arrays of none at all are DA_ERR_SHAPE.  Arrays are
+ * h_q; T*(h_q/h_kv), N and h_q*d up to 2^30, B*h_q up to 2^24, and no more than
+ * 2^24-1 workgroups (a KV head's 128 rows of a sequence, or its 32 to 128 keys in the
+ * gradient, are one): more is DA_ERR_SHAPE.  All sizes are at least 1: sequences may
+ * have no rows or no keys, but arrays of none at all are DA_ERR_SHAPE too.  Arrays are
  * 16-byte aligned (lse and the starts 4), strides between tokens multiples of 16
  * bytes, at least a token's own size and at most 4 MiB.  Errors are checked in the
  * order of the enumeration (workspace last).
@@ -566,10 +568,13 @@ size_t da_prompt_grad_workspace_bytes(const da_prompt *prompt);
  *     x1*cos - x2*sin,  x2*cos + x1*sin,
  * with inverse the sines negated: the rotation back, and the gradient.  Other
  * dimensions are copied.  A position outside [0, n_table) turns nothing: its
- * axis's pairs are copied.  Products and sums in 32 bits, one rounding.
+ * axis's pairs are copied to the bit, whatever they hold.  Products and sums in
+ * 32 bits, one rounding.
  *
  * Supported: d in {64, 128, 256}, rot_dim a multiple of 16 up to d, 1 to 4 axes
- * whose sections add up to rot_dim/2 (a section may be 0).
+ * whose sections add up to rot_dim/2 (a section may be 0), (h_q+h_kv)*d up to 2^30,
+ * fewer than 2^24 workgroups of 256 threads, each of which has 16 dimensions of up to
+ * four heads of a row.
  * ---------------------------------------------------------------------------
  */
 typedef struct da_rotary {

@@ -787,7 +787,14 @@ def prompt_attn(q, k, v, scale: float, causal: bool = True, row_start=None, T: i
     sequence has T rows (0: one sequence), without ``key_start`` N keys; where neither
     is given and there are as many keys as rows, the keys are the rows' own.  ``lse``
     [rows,h_q] float32 is written where given: what prompt_attn_grad needs.  Any stride
-    between tokens up to 4 MiB.  An ``out`` or ``workspace`` not given is allocated on ``stream``."""
+    between tokens up to 4 MiB.  An ``out`` or ``workspace`` not given is allocated on ``stream``.
+
+    Keys of other lengths than the rows' (cross attention) need ``key_start``, or ``N`` where
+    all have as many: without both, as many keys as rows in all are taken for the rows' own.
+
+    No call of this library is recorded by autograd: ``out`` does not require a gradient,
+    whatever q, k and v do.  A program that uses autograd calls this in the forward of a
+    torch.autograd.Function, with ``lse``, and prompt_attn_grad in its backward."""
     if out is None:
         out = _empty(q, "q", stream)
     fast = _fast(q, stream) if workspace is not None else None
@@ -876,7 +883,8 @@ def rotary_axes(q, positions, table, sections, k=None, interleaved: bool = False
     rotary_table, [positions,rot_dim]; ``sections``: how many of the rot_dim/2 pairs
     each axis turns.  ``inverse`` turns back, which is the gradient.  Any stride
     between tokens; results not given are allocated on ``stream``, and may be the
-    inputs."""
+    inputs.  Not recorded by autograd: in a torch.autograd.Function, the backward is the
+    call with ``inverse`` turned over."""
     if q_out is None:
         q_out = _empty(q, "q", stream)
     if k is not None and k_out is None:

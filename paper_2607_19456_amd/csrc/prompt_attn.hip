@@ -680,10 +680,12 @@ Plan plan_attn(const da_prompt& p) {
   }
   plan.items = most_tiles(p.row_start, p.B, p.T, p.rows, G, 128);
   const int64_t groups = plan.items * p.h_kv;
-  // Few tiles are divided by their keys, so that every CU has work; more of float32,
-  // whose products take longer than the merge's launch (two sequences of 1500 rows, 16
-  // heads of 64: 149 us whole, 122 in two parts; bfloat16, 8 of 333 rows over 400 to
-  // 1500 keys, 39 and 45).
+  // Few tiles are divided by their keys, so that every CU has work; more of float32 with
+  // heads of 64, whose products take longer than the merge's launch, in parts of 512 keys
+  // and more (us whole, in two and in three parts, causal: 384 tiles of 2 sequences of 1500
+  // rows 151, 114, 114; 320 of one of 4000 346, 247, 209; 256 of 4 of 1024 84, 68, 65; 360
+  // of 6 of 520 59, 62, 62; 280 of 5 of 400 41, 41, 42; 312 of 3 of 1600 that see all 220,
+  // 173, 161).  bfloat16, 8 of 333 rows over 400 to 1500 keys: 39 and 45.
   if (groups < kCus)
     plan.splits = (int)std::min<int64_t>(2 * kCus / groups, ceil_div(p.N, 128));
   else if (p.dtype == DA_F32 && p.d == 64 && groups < 3 * kCus)

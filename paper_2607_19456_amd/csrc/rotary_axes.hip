@@ -42,7 +42,7 @@ struct Eight {
 // pairs, (i, i + half) or (2i, 2i + 1), or copies 16 that are not turned.  The angles
 // are read once for them, in four loads where one axis has all eight pairs.  An axis
 // may begin inside them: each pair then has a position of its own.
-// Memory-bound: 16001 rows of 40 heads of 128 on three axes, 328 MB, 62 us (5.3 TB/s; a
+// Memory-bound: 16001 rows of 40 heads of 128 on three axes, 328 MB, 63 us (5.2 TB/s; a
 // copy too large for the caches 4.8).  With one head a thread, whose pairs each loaded
 // their own angles, 148 us.  16 rows: 4.8 us, a launch and loads that wait for each other.
 // ---------------------------------------------------------------------------
